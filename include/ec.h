@@ -24,7 +24,7 @@
  *    policy (all heads of a layer share anchor positions, Sec. 3.3), G = H the
  *    head-wise variant of the ablation (Table 3c).
  *  - Supported: D in {64,128}; dt in {EC_F32, EC_BF16}; multi-head attention
- *    with as many key/value heads as query heads.
+ *    with as many key/value heads as query heads; the calls on paged caches also take fewer key/value heads.
  */
 #ifndef EC_H_
 #define EC_H_
@@ -52,7 +52,11 @@ typedef enum {
     EC_FN_MERGE_COMPACT = 2,
     EC_FN_DECODE_STEP = 3,
     EC_FN_DECODE_SCORE_STEP = 4,
-    EC_FN_EVICT_MIN = 5
+    EC_FN_EVICT_MIN = 5,
+    EC_FN_PAGED_STORE = 6,
+    EC_FN_PAGED_DECODE_STEP = 7,
+    EC_FN_PAGED_DECODE_SCORE_STEP = 8,
+    EC_FN_PAGED_EVICT_MIN = 9
 } ec_fn;
 
 /* Budget rule of the retention test (Sec. 3.3 Output Generation; Alg. 1). */
@@ -78,7 +82,9 @@ const char* ec_status_string(int status);
 
 /*
  * Bytes of workspace the given entry point needs for these shapes.  Host, pure.
- * For EC_FN_DECODE_STEP and EC_FN_DECODE_SCORE_STEP pass T = cap.  Returns 0 for entry points that need none
+ * For EC_FN_DECODE_STEP and EC_FN_DECODE_SCORE_STEP pass T = cap; for EC_FN_PAGED_DECODE_STEP and
+ * EC_FN_PAGED_DECODE_SCORE_STEP H query heads and T = max_pages * page; for EC_FN_PAGED_EVICT_MIN H = G and
+ * T = max_evict.  Returns 0 for entry points that need none
  * and (size_t)-1 for unsupported shapes.
  */
 size_t ec_workspace_bytes(int fn, int B, int H, int T, int D, int dt);
@@ -373,6 +379,87 @@ int ec_decode_score_step_static(const void* q, const void* k_new, const void* v_
 int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B, int H, int G, int D,
                  int cap, int len, int protect_first, int protect_recent, int dt, int32_t* victim,
                  void* stream);
+
+/*
+ * Paged caches: rows of sequences that grow, shrink and end at different times, in pages of one pool, so that what the
+ * compression frees can hold other sequences.  For every layer
+ *   k_pages,v_pages  DEVICE [n_pages,Hkv,page,D] dt       pos_pages   DEVICE [n_pages,G,page] int32, original positions
+ *   page_table       DEVICE [B,max_pages] int32           mass_pages  DEVICE [n_pages,G,page] float, accumulated attention
+ * and slot s of sequence b (0 <= s < max_pages * page) is row s % page of page page_table[b][s / page].  A cache is a SET of
+ * rows in slots 0 .. len-1: attention does not see their order, positions go with them.  Common to the calls:
+ *  - page is a power of two from 8 to 256.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
+ *    h reads key/value head h / (H / Hkv).
+ *  - Everything that changes from token to token is read on the device, so the calls can be captured and replayed.
+ *  - A table entry outside 0 .. n_pages-1 names no page (entries behind a sequence's last page are not read at all): rows there are
+ *    not read, not written and weigh nothing.  Pages that a call only reads may be shared by sequences (a common prefix); a
+ *    page that it writes (the new row's; for ec_paged_evict_min all pages of a sequence) must be one sequence's alone, else that
+ *    page's contents are unspecified.  Nothing outside the pools is touched in any case.
+ *  - k, v, q, out and the pools start on 16-byte boundaries (else EC_EUNSUPPORTED), ws on one too.
+ */
+
+/*
+ * Rows 0 .. n-1 of dense buffers into slots start .. start + n - 1 of every sequence: a prompt's merged rows, a chunk's rows behind
+ * the cached ones, or, without k and v, new masses or positions for rows that are there.
+ *   k,v        DEVICE [B,Hkv,src_rows,D] dt, read only; NULL both or none
+ *   pos,mass   DEVICE [B,G,src_rows] int32, float, read only; either may be NULL
+ *   start_b    DEVICE [B] int32, first slot of each sequence; NULL: 0
+ *   n_rows_b   DEVICE [B] int32, rows of each sequence (clamped into 0 .. T); NULL: T
+ * Requires 1 <= T <= src_rows.  Of what is NULL the pool may be NULL too.  Rows whose slot lies outside 0 .. max_pages * page - 1 are left out.
+ */
+int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float* mass, const int32_t* page_table,
+                   const int32_t* start_b, const int32_t* n_rows_b, int B, int Hkv, int G, int T, int src_rows, int D, int page,
+                   int n_pages, int max_pages, int dt, void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages,
+                   void* stream);
+
+/*
+ * One output-generation step of one layer over paged caches.  For every sequence b, L = cache_len_b[b]:
+ *   1. slot L <- k_new, v_new (pos <- new_pos_b[b])
+ *   2. out = softmax_j(scale * <q, k_j>) . v_j over rows 0 .. L of the query head's key/value head
+ * Where L is outside 0 .. max_pages * page - 1 the place b of the batch holds no sequence: its out is zeros and nothing is stored.  The
+ * new row always counts, also where the table names no page for it.  cache_len_b is read only (all layers share it).
+ *   q,out          DEVICE [B,H,D] dt           k_new,v_new    DEVICE [B,Hkv,D] dt
+ *   pos_pages      may be NULL, new_pos_b then too
+ *   cache_len_b,new_pos_b  DEVICE [B] int32
+ *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_STEP, B,H, max_pages * page, D,dt)
+ * Products, sums and the softmax are formed in fp32.  Results are deterministic.
+ */
+int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
+                         const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv,
+                         int G, int D, int page, int n_pages, int max_pages, float scale, int dt, void* out, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * ec_paged_decode_step that also accumulates the attention which every row receives (the "Frequency" policy, as
+ * ec_decode_score_step):
+ *     mass_j += p_j for rows j < L,   mass_L = p_L
+ * where p is the mean of the step's softmax rows over all query heads (G == 1) or over the query heads of the key/value head
+ * (G == Hkv), added in ascending head order.
+ *   mass_pages     updated
+ *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_SCORE_STEP, B,H, max_pages * page, D,dt)
+ */
+int ec_paged_decode_score_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
+                               float* mass_pages, const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b,
+                               int B, int H, int Hkv, int G, int D, int page, int n_pages, int max_pages, float scale, int dt,
+                               void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention: of the n = len_b[b] rows of sequence b (clamped into 0 .. max_pages * page)
+ *     gone = min(max(n - max(keep_b[b], 0), 0), max_evict)
+ * rows go from every score group, those of least mass first, the lower slot among equals (masses compared as fp32 values, -0 ==
+ * +0; NaN counts as more than +inf).  Rows at positions below protect_first or at and above seen_b[b] - protect_recent
+ * (seen_b: tokens seen so far) and rows on no page are protected: they go only when no others are left, lower slots first.
+ * The m = n - gone rows that stay end up in slots 0 .. m-1: rows there stay where they are, and the i-th slot that a victim leaves
+ * below m takes the i-th of the rows that stay behind m, with its position and mass (both counted upwards).  Slots m .. n-1 keep what
+ * they held.  len_b and keep_b are not changed; pages behind slot m - 1 are the caller's to give away.
+ *   pos_pages      may be NULL; protect_first and protect_recent must be 0 then
+ *   seen_b         may be NULL when protect_recent is 0
+ *   max_evict      1 .. max_pages * page: what no sequence loses more than; sizes the scratch
+ *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_EVICT_MIN, B,G, max_evict, D,dt)
+ */
+int ec_paged_evict_min(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const int32_t* page_table,
+                       const int32_t* len_b, const int32_t* keep_b, const int32_t* seen_b, int B, int Hkv, int G, int D, int page,
+                       int n_pages, int max_pages, int max_evict, int protect_first, int protect_recent, int dt, void* ws,
+                       size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ LIB_PATH = os.environ.get("EC_LIB_PATH", os.path.join(_HERE, "libelastic_cache.s
 EC_OK, EC_EINVAL, EC_EUNSUPPORTED, EC_EWORKSPACE, EC_EDEVICE = range(5)
 EC_F32, EC_BF16 = 0, 1
 (EC_FN_PREFILL_SCORE, EC_FN_SELECT_ANCHORS, EC_FN_MERGE_COMPACT, EC_FN_DECODE_STEP, EC_FN_DECODE_SCORE_STEP,
- EC_FN_EVICT_MIN) = range(6)
+ EC_FN_EVICT_MIN, EC_FN_PAGED_STORE, EC_FN_PAGED_DECODE_STEP, EC_FN_PAGED_DECODE_SCORE_STEP, EC_FN_PAGED_EVICT_MIN) = range(10)
 EC_BUDGET_RATIO, EC_BUDGET_FIXED = 0, 1
 EC_TRUNC_RECENT, EC_TRUNC_ABS = 0, 1
 EC_MERGE_MEAN, EC_MERGE_EVICT = 0, 1
@@ -28,7 +28,7 @@ SYMBOLS = ("ec_status_string", "ec_workspace_bytes", "ec_prefill_score", "ec_chu
            "ec_merge_compact", "ec_remerge_compact", "ec_evict_index", "ec_decode_step", "ec_decode_score_step",
            "ec_evict_min", "ec_prefill_score_varlen", "ec_select_anchors_varlen", "ec_merge_compact_varlen",
            "ec_decode_step_varlen", "ec_importance_mean", "ec_retention_step_varlen", "ec_decode_step_shaped",
-           "ec_decode_score_step_static")
+           "ec_decode_score_step_static", "ec_paged_store", "ec_paged_decode_step", "ec_paged_decode_score_step", "ec_paged_evict_min")
 
 _lib = None
 _fast = None  # the usual calls in native code (csrc/fastcall.cpp); None in an answer of theirs: not a usual call
@@ -92,6 +92,14 @@ def load():
     lib.ec_importance_mean.restype = c_int
     lib.ec_retention_step_varlen.argtypes = [c_vp] * 5 + [c_int] * 10 + [c_vp]
     lib.ec_retention_step_varlen.restype = c_int
+    lib.ec_paged_store.argtypes = [c_vp] * 7 + [c_int] * 10 + [c_vp] * 5
+    lib.ec_paged_store.restype = c_int
+    lib.ec_paged_decode_step.argtypes = [c_vp] * 9 + [c_int] * 8 + [c_f, c_int, c_vp, c_vp, c_sz, c_vp]
+    lib.ec_paged_decode_step.restype = c_int
+    lib.ec_paged_decode_score_step.argtypes = [c_vp] * 10 + [c_int] * 8 + [c_f, c_int, c_vp, c_vp, c_sz, c_vp]
+    lib.ec_paged_decode_score_step.restype = c_int
+    lib.ec_paged_evict_min.argtypes = [c_vp] * 8 + [c_int] * 11 + [c_vp, c_sz, c_vp]
+    lib.ec_paged_evict_min.restype = c_int
     _fast = _load_fast(lib)
     _lib = lib
     return lib
@@ -413,7 +421,7 @@ def ec_decode_score_step_static(q, k_new, v_new, k_cache, v_cache, pos, freq, ca
     if freq.dim() != 3:
         raise ValueError("ec_decode_score_step_static: freq must be [B,G,cap]")
     ptrs, po, (B, H, G, D, cap) = _decode_args(q, k_new, v_new, k_cache, v_cache, pos, out, freq.shape[1],
-                                               "ec_decode_score_step_static")
+                                               "ec_decode_score_step_static", "ec_paged_store", "ec_paged_decode_step", "ec_paged_decode_score_step", "ec_paged_evict_min")
     rc = _call(load().ec_decode_score_step_static, *ptrs, _chk(freq, "freq", torch.float32, (B, G, cap)), B, H, G, D,
                cap, cache_len, new_pos, scale, dtype_code(k_cache), po, _stream())
     if check and rc != EC_OK:
@@ -554,3 +562,106 @@ def ec_retention_step_varlen(n_seen_b, cache_len_b, evict_idx_b, new_pos_b, pend
     if check and rc != EC_OK:
         raise EcError("ec_retention_step_varlen", rc)
     return rc
+
+
+# ------------------------------------------------------------------ paged caches
+def _same_device(*tensors):
+    """The library runs on the current device: a tensor of another one would be read through an address that means nothing there."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"all tensors must live on the current device, got one on {t.device}")
+
+
+def _paged_table(page_table, what):
+    if page_table.dim() != 2:
+        raise ValueError(f"{what}: page_table must be [B,max_pages]")
+    return page_table.shape
+
+
+def ec_paged_store(k, v, pos, mass, page_table, k_pages, v_pages, pos_pages, mass_pages, start_b=None, n_rows_b=None,
+                   T: int | None = None, check=True) -> int:
+    """k,v [B,Hkv,src_rows,D], pos [B,G,src_rows] int32, mass [B,G,src_rows] f32, each or None -> rows 0..T-1 (n_rows_b of them) to the slots
+    from start_b on; k_pages,v_pages [N,Hkv,page,D], pos_pages, mass_pages [N,G,page], page_table int32 [B,max_pages]."""
+    B, max_pages = _paged_table(page_table, "ec_paged_store")
+    i32, f32 = torch.int32, torch.float32
+    if (k is None) != (v is None):
+        raise ValueError("ec_paged_store: k and v go together")
+    meta = pos if pos is not None else mass
+    if k is None and meta is None:
+        raise ValueError("ec_paged_store: nothing to store")
+    if (k is not None and k.dim() != 4) or (meta is not None and meta.dim() != 3):
+        raise ValueError("ec_paged_store: k must be [B,Hkv,src_rows,D], pos and mass [B,G,src_rows]")
+    src_rows = k.shape[2] if k is not None else meta.shape[2]
+    pool = k_pages if k is not None else pos_pages if pos is not None else mass_pages
+    if pool is None or pool.dim() != (4 if k is not None else 3):
+        raise ValueError("ec_paged_store: what is stored needs its pool, k_pages [N,Hkv,page,D] or pos_pages, mass_pages [N,G,page]")
+    N, page = pool.shape[0], pool.shape[2]
+    G = meta.shape[1] if meta is not None else 1
+    Hkv, D, dt = (k.shape[1], k.shape[3], k.dtype) if k is not None else (G, 64, f32)
+    _groups(G, Hkv, "ec_paged_store")
+    _same_device(k, v, pos, mass, page_table, k_pages, v_pages, pos_pages, mass_pages, start_b, n_rows_b)
+    rows, store = (B, Hkv, src_rows, D), (N, Hkv, page, D)
+    rc = _call(load().ec_paged_store, _chk(k, "k", dt, rows, True), _chk(v, "v", dt, rows, True), _chk(pos, "pos", i32, (B, G, src_rows), True),
+               _chk(mass, "mass", f32, (B, G, src_rows), True), _chk(page_table, "page_table", i32, (B, max_pages)), _i32(start_b, "start_b", B, True),
+               _i32(n_rows_b, "n_rows_b", B, True), B, Hkv, G, src_rows if T is None else T, src_rows, D, page, N, max_pages,
+               EC_F32 if k is None else dtype_code(k), _chk(k_pages, "k_pages", dt, store, k is None) if k is not None else None,
+               _chk(v_pages, "v_pages", dt, store) if k is not None else None, _chk(pos_pages, "pos_pages", i32, (N, G, page)) if pos is not None else None,
+               _chk(mass_pages, "mass_pages", f32, (N, G, page)) if mass is not None else None, _stream())
+    return _status("ec_paged_store", rc, check)
+
+
+def _paged_step(fn, q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale, out, ws, check):
+    B, max_pages = _paged_table(page_table, fn)
+    if q.dim() != 3 or k_pages.dim() != 4:
+        raise ValueError(f"{fn}: q must be [B,H,D] and k_pages [N,Hkv,page,D]")
+    H = q.shape[1]
+    N, Hkv, page, D = k_pages.shape
+    dt, i32 = k_pages.dtype, torch.int32
+    scored = fn == "ec_paged_decode_score_step"
+    groups = mass_pages if scored else pos_pages
+    if groups is not None and groups.dim() != 3:
+        raise ValueError(f"{fn}: pos_pages and mass_pages must be [N,G,page]")
+    G = _groups(groups.shape[1] if groups is not None else 1, Hkv, fn)
+    _same_device(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, out, ws)
+    wp, wb = _ws(ws)
+    mass = (_chk(mass_pages, "mass_pages", torch.float32, (N, G, page)),) if scored else ()
+    rc = _call(getattr(load(), fn), _chk(q, "q", dt, (B, H, D)), _chk(k_new, "k_new", dt, (B, Hkv, D)), _chk(v_new, "v_new", dt, (B, Hkv, D)),
+               _chk(k_pages, "k_pages", dt, (N, Hkv, page, D)), _chk(v_pages, "v_pages", dt, (N, Hkv, page, D)),
+               _chk(pos_pages, "pos_pages", i32, (N, G, page), True), *mass, _chk(page_table, "page_table", i32, (B, max_pages)),
+               _i32(cache_len_b, "cache_len_b", B), _i32(new_pos_b, "new_pos_b", B, pos_pages is None), B, H, Hkv, G, D, page, N, max_pages, scale,
+               dtype_code(k_pages), _chk(out, "out", dt, (B, H, D)), wp, wb, _stream())
+    return _status(fn, rc, check)
+
+
+def ec_paged_decode_step(q, k_new, v_new, k_pages, v_pages, pos_pages, page_table, cache_len_b, new_pos_b, scale: float, out, ws,
+                         check=True) -> int:
+    """q,out [B,H,D]; k_new,v_new [B,Hkv,D]; pools as in ec_paged_store (pos_pages or None); cache_len_b, new_pos_b int32 [B] on the device."""
+    return _paged_step("ec_paged_decode_step", q, k_new, v_new, k_pages, v_pages, pos_pages, None, page_table, cache_len_b, new_pos_b, scale, out, ws,
+                       check)
+
+
+def ec_paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale: float, out,
+                               ws, check=True) -> int:
+    """ec_paged_decode_step that also adds the attention every row receives to mass_pages [N,G,page] f32."""
+    if mass_pages is None:
+        raise ValueError("mass_pages is required")
+    return _paged_step("ec_paged_decode_score_step", q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b,
+                       scale, out, ws, check)
+
+
+def ec_paged_evict_min(k_pages, v_pages, pos_pages, mass_pages, page_table, len_b, keep_b, seen_b, max_evict: int, protect_first: int,
+                       protect_recent: int, ws, check=True) -> int:
+    """Rows of least mass go until keep_b are left of the len_b (no more than max_evict); the holes are filled from behind."""
+    B, max_pages = _paged_table(page_table, "ec_paged_evict_min")
+    if k_pages.dim() != 4 or mass_pages.dim() != 3:
+        raise ValueError("ec_paged_evict_min: k_pages must be [N,Hkv,page,D] and mass_pages [N,G,page]")
+    N, Hkv, page, D = k_pages.shape
+    G = _groups(mass_pages.shape[1], Hkv, "ec_paged_evict_min")
+    dt, i32 = k_pages.dtype, torch.int32
+    _same_device(k_pages, v_pages, pos_pages, mass_pages, page_table, len_b, keep_b, seen_b, ws)
+    wp, wb = _ws(ws)
+    rc = _call(load().ec_paged_evict_min, _chk(k_pages, "k_pages", dt, (N, Hkv, page, D)), _chk(v_pages, "v_pages", dt, (N, Hkv, page, D)),
+               _chk(pos_pages, "pos_pages", i32, (N, G, page), True), _chk(mass_pages, "mass_pages", torch.float32, (N, G, page)),
+               _chk(page_table, "page_table", i32, (B, max_pages)), _i32(len_b, "len_b", B), _i32(keep_b, "keep_b", B), _i32(seen_b, "seen_b", B, True),
+               B, Hkv, G, D, page, N, max_pages, max_evict, protect_first, protect_recent, dtype_code(k_pages), wp, wb, _stream())
+    return _status("ec_paged_evict_min", rc, check)

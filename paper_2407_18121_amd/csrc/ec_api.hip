@@ -2,9 +2,11 @@
 // No allocation; every launch goes to the caller's stream.  The only state is the per-device address of
 // the built-in scratch array of ec_decode_score_step_static, looked up once.
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 
 #include "ec_common.h"
+#include "paged.h"
 #include "score_route.h"
 
 namespace ec {
@@ -38,6 +40,17 @@ int retention_step_launch(int32_t* n_seen_b, int32_t* cache_len_b, int32_t* evic
                           int32_t* pending_b, int B, int gamma_num, int gamma_den, int budget_mode, int fixed_len,
                           int trunc_mode, int recent, int n_tl, int protect_first, int flush_only, hipStream_t stream);
 int importance_mean_launch(float* score, int B, int G, int Tq, int P, hipStream_t stream);
+size_t paged_step_ws(int B, int H, int slots, bool emit);
+size_t paged_evict_ws(int B, int G, int max_evict);
+int paged_store_dispatch(const void* k, const void* v, const int32_t* pos, const float* mass, const Pages& pages, const int32_t* start_b,
+                         const int32_t* n_rows_b, int B, int Hkv, int G, int T, int src_rows, int row_bytes, void* k_pages, void* v_pages,
+                         int32_t* pos_pages, float* mass_pages, hipStream_t stream);
+int paged_step_dispatch(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages,
+                        const Pages& pages, const int32_t* len_b, const int32_t* new_pos_b, int B, int H, int Hkv, int G, int D, float scale, int dt,
+                        void* out, void* ws, hipStream_t stream);
+int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const Pages& pages, const int32_t* len_b,
+                         const int32_t* keep_b, const int32_t* seen_b, int B, int Hkv, int G, int row_bytes, int max_evict, int protect_first,
+                         int protect_recent, void* ws, hipStream_t stream);
 int head_mean_launch(const float* head_imp, float* score, int B, int H, int T, hipStream_t stream);
 }  // namespace ec
 
@@ -150,6 +163,12 @@ size_t ec_workspace_bytes(int fn, int B, int H, int T, int D, int dt)
             // every row's scaled score [B,H,T] + softmax maximum and denominator [B,H,2], fp32
             return align256((size_t)B * H * T * sizeof(float)) + align256((size_t)B * H * 2 * sizeof(float));
         case EC_FN_EVICT_MIN: return 0;
+        case EC_FN_PAGED_STORE: return 0;
+        case EC_FN_PAGED_DECODE_STEP:
+        case EC_FN_PAGED_DECODE_SCORE_STEP:
+            if (!shape_supported(D, dt)) return (size_t)-1;
+            return ec::paged_step_ws(B, H, T, fn == EC_FN_PAGED_DECODE_SCORE_STEP);
+        case EC_FN_PAGED_EVICT_MIN: return ec::paged_evict_ws(B, H, T);
         default: return (size_t)-1;
     }
 }
@@ -407,6 +426,93 @@ int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B,
     if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
     return ec::evict_min_dispatch(k_cache, v_cache, pos, freq, B, H, G, D, cap, len, protect_first, protect_recent, dt,
                                   victim, reinterpret_cast<hipStream_t>(stream));
+}
+
+namespace {
+bool aligned16(std::initializer_list<const void*> ptrs)
+{
+    uintptr_t all = 0;
+    for (const void* p : ptrs) all |= (uintptr_t)p;
+    return all % 16 == 0;
+}
+
+// What every call on paged caches is checked for; EC_OK, and the pages then.
+int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int page, int n_pages, int max_pages, int dt, ec::Pages& pages)
+{
+    if (!page_table || B < 1 || Hkv < 1 || D < 1 || page < 1 || n_pages < 1 || max_pages < 1) return EC_EINVAL;
+    if (G != 1 && G != Hkv) return EC_EINVAL;
+    if ((page & (page - 1)) || page < 8 || page > 256 || (long long)max_pages * page > 1 << 30) return EC_EUNSUPPORTED;
+    if ((long long)B * Hkv > 65535) return EC_EUNSUPPORTED;
+    if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
+    pages = {page_table, n_pages, max_pages, __builtin_ctz((unsigned)page)};
+    return EC_OK;
+}
+
+int row_bytes(int D, int dt) { return D * (dt == EC_BF16 ? 2 : 4); }
+
+int paged_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages,
+               const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv, int G, int D, int page,
+               int n_pages, int max_pages, float scale, int dt, void* out, int fn, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!q || !k_new || !v_new || !k_pages || !v_pages || !cache_len_b || !out) return EC_EINVAL;
+    if (pos_pages && !new_pos_b) return EC_EINVAL;
+    if (H < 1 || Hkv < 1 || H % Hkv) return EC_EINVAL;
+    if (!scale_ok(scale)) return EC_EINVAL;
+    ec::Pages pages;
+    if (const int rc = paged_shape(page_table, B, Hkv, G, D, page, n_pages, max_pages, dt, pages)) return rc;
+    if ((long long)B * H > 65535 || !aligned16({q, k_new, v_new, k_pages, v_pages, out})) return EC_EUNSUPPORTED;
+    if (!ws || ws_bytes < ec_workspace_bytes(fn, B, H, pages.slots(), D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
+    return ec::paged_step_dispatch(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, pages, cache_len_b, new_pos_b, B, H, Hkv, G, D, scale, dt,
+                                   out, ws, reinterpret_cast<hipStream_t>(stream));
+}
+}  // namespace
+
+int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float* mass, const int32_t* page_table, const int32_t* start_b,
+                   const int32_t* n_rows_b, int B, int Hkv, int G, int T, int src_rows, int D, int page, int n_pages, int max_pages, int dt,
+                   void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, void* stream)
+{
+    if (!k != !v || (!k && !pos && !mass) || (k && (!k_pages || !v_pages)) || (pos && !pos_pages) || (mass && !mass_pages)) return EC_EINVAL;
+    if (T < 1 || src_rows < T) return EC_EINVAL;
+    ec::Pages pages;
+    if (const int rc = paged_shape(page_table, B, Hkv, G, D, page, n_pages, max_pages, dt, pages)) return rc;
+    if (k && !aligned16({k, v, k_pages, v_pages})) return EC_EUNSUPPORTED;
+    return ec::paged_store_dispatch(k, v, pos, mass, pages, start_b, n_rows_b, B, Hkv, G, T, src_rows, row_bytes(D, dt), k_pages, v_pages, pos_pages,
+                                    mass_pages, reinterpret_cast<hipStream_t>(stream));
+}
+
+int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
+                         const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv, int G, int D,
+                         int page, int n_pages, int max_pages, float scale, int dt, void* out, void* ws, size_t ws_bytes, void* stream)
+{
+    return paged_step(q, k_new, v_new, k_pages, v_pages, pos_pages, nullptr, page_table, cache_len_b, new_pos_b, B, H, Hkv, G, D, page, n_pages,
+                      max_pages, scale, dt, out, EC_FN_PAGED_DECODE_STEP, ws, ws_bytes, stream);
+}
+
+int ec_paged_decode_score_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
+                               float* mass_pages, const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H,
+                               int Hkv, int G, int D, int page, int n_pages, int max_pages, float scale, int dt, void* out, void* ws,
+                               size_t ws_bytes, void* stream)
+{
+    if (!mass_pages) return EC_EINVAL;
+    return paged_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, B, H, Hkv, G, D, page, n_pages,
+                      max_pages, scale, dt, out, EC_FN_PAGED_DECODE_SCORE_STEP, ws, ws_bytes, stream);
+}
+
+int ec_paged_evict_min(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const int32_t* page_table, const int32_t* len_b,
+                       const int32_t* keep_b, const int32_t* seen_b, int B, int Hkv, int G, int D, int page, int n_pages, int max_pages,
+                       int max_evict, int protect_first, int protect_recent, int dt, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!k_pages || !v_pages || !mass_pages || !len_b || !keep_b) return EC_EINVAL;
+    if (max_evict < 1 || protect_first < 0 || protect_recent < 0) return EC_EINVAL;
+    if ((protect_first || protect_recent) && !pos_pages) return EC_EINVAL;
+    if (protect_recent && !seen_b) return EC_EINVAL;
+    ec::Pages pages;
+    if (const int rc = paged_shape(page_table, B, Hkv, G, D, page, n_pages, max_pages, dt, pages)) return rc;
+    if (max_evict > pages.slots()) return EC_EINVAL;
+    if (!aligned16({k_pages, v_pages})) return EC_EUNSUPPORTED;
+    if (!ws || ws_bytes < ec_workspace_bytes(EC_FN_PAGED_EVICT_MIN, B, G, max_evict, D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
+    return ec::paged_evict_dispatch(k_pages, v_pages, pos_pages, mass_pages, pages, len_b, keep_b, seen_b, B, Hkv, G, row_bytes(D, dt), max_evict,
+                                    protect_first, protect_recent, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
