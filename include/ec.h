@@ -387,7 +387,7 @@ int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B,
  *   page_table       DEVICE [B,max_pages] int32           mass_pages  DEVICE [n_pages,G,page] float, accumulated attention
  * and slot s of sequence b (0 <= s < max_pages * page) is row s % page of page page_table[b][s / page].  A cache is a SET of
  * rows in slots 0 .. len-1: attention does not see their order, positions go with them.  Common to the calls:
- *  - page is a power of two from 8 to 256.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
+ *  - page is a power of two from 8 to 256, max_pages * page at most 2^28.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
  *    h reads key/value head h / (H / Hkv).
  *  - Everything that changes from token to token is read on the device, so the calls can be captured and replayed.
  *  - A table entry outside 0 .. n_pages-1 names no page (entries behind a sequence's last page are not read at all): rows there are
@@ -420,8 +420,11 @@ int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float
  *   q,out          DEVICE [B,H,D] dt           k_new,v_new    DEVICE [B,Hkv,D] dt
  *   pos_pages      may be NULL, new_pos_b then too
  *   cache_len_b,new_pos_b  DEVICE [B] int32
- *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_STEP, B,H, max_pages * page, D,dt)
- * Products, sums and the softmax are formed in fp32.  Results are deterministic.
+ *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_STEP, B,H, max_pages * page, D,dt); all zeros before its first
+ *                  use (calls leave at zero what has to be), this call's and ec_paged_decode_score_step's alone, of one call at a
+ *                  time: calls that may overlap, on two streams or in two graphs, need one each
+ * Products are formed on the matrix cores with fp32 accumulation, sums and the softmax in fp32 (bf16: a weight enters its product with V
+ * as the sum of two bf16 numbers, 2^-16 of it off).  Results are deterministic.
  */
 int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
                          const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv,

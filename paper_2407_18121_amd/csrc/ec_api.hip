@@ -40,7 +40,7 @@ int retention_step_launch(int32_t* n_seen_b, int32_t* cache_len_b, int32_t* evic
                           int32_t* pending_b, int B, int gamma_num, int gamma_den, int budget_mode, int fixed_len,
                           int trunc_mode, int recent, int n_tl, int protect_first, int flush_only, hipStream_t stream);
 int importance_mean_launch(float* score, int B, int G, int Tq, int P, hipStream_t stream);
-size_t paged_step_ws(int B, int H, int slots, bool emit);
+size_t paged_step_ws(int B, int H, int slots, int D, bool emit);
 size_t paged_evict_ws(int B, int G, int max_evict);
 int paged_store_dispatch(const void* k, const void* v, const int32_t* pos, const float* mass, const Pages& pages, const int32_t* start_b,
                          const int32_t* n_rows_b, int B, int Hkv, int G, int T, int src_rows, int row_bytes, void* k_pages, void* v_pages,
@@ -167,7 +167,7 @@ size_t ec_workspace_bytes(int fn, int B, int H, int T, int D, int dt)
         case EC_FN_PAGED_DECODE_STEP:
         case EC_FN_PAGED_DECODE_SCORE_STEP:
             if (!shape_supported(D, dt)) return (size_t)-1;
-            return ec::paged_step_ws(B, H, T, fn == EC_FN_PAGED_DECODE_SCORE_STEP);
+            return ec::paged_step_ws(B, H, T, D, fn == EC_FN_PAGED_DECODE_SCORE_STEP);
         case EC_FN_PAGED_EVICT_MIN: return ec::paged_evict_ws(B, H, T);
         default: return (size_t)-1;
     }
@@ -441,7 +441,7 @@ int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int pag
 {
     if (!page_table || B < 1 || Hkv < 1 || D < 1 || page < 1 || n_pages < 1 || max_pages < 1) return EC_EINVAL;
     if (G != 1 && G != Hkv) return EC_EINVAL;
-    if ((page & (page - 1)) || page < 8 || page > 256 || (long long)max_pages * page > 1 << 30) return EC_EUNSUPPORTED;
+    if ((page & (page - 1)) || page < 8 || page > 256 || (long long)max_pages * page > 1 << 28) return EC_EUNSUPPORTED;
     if ((long long)B * Hkv > 65535) return EC_EUNSUPPORTED;
     if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
     pages = {page_table, n_pages, max_pages, __builtin_ctz((unsigned)page)};

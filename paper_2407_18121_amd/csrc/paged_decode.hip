@@ -1,7 +1,46 @@
 // ec_paged_decode_step, ec_paged_decode_score_step: attention of one new token per sequence over a cache in pages.
+//
+// The rows of one (sequence, key/value head, up to 16 of its query heads), a pair, are cut into segments, one workgroup each.  A wave takes every
+// WAVES-th tile of a segment's rows and keeps a running (maximum, sum, weighted V) for its 16 query heads:
+//   S^T = K . Q^T      matrix instructions, so that a lane owns one query head and 4 consecutive rows of a block of 16
+//   O^T += V^T . P^T   the probabilities are the second operand as they stand; V is transposed on its way out of LDS (bf16)
+// Every row of K and V is read once for all query heads of its head, straight from its page into LDS; a tile is in flight while the
+// one before it is used.  The new row takes part as the last row of the last tile and is stored by that tile's workgroup.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "paged.h"
+#include "tile_lds.h"
 
 namespace ec {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(4))) const int32_t const_i32;  // read through the scalar cache: nothing that a launch writes
+
+constexpr int kPagedWaves = 2;
+constexpr int kPagedSegments = 512;  // workgroups that a launch aims at
+constexpr int kHeadBlock = 16;       // query heads of a pair, at most
+constexpr float kSmall = 0x1p-100f;  // bf16: probabilities below it are multiplied apart
+
+// The scale in base-2 units, log2(e) * scale, as a factor of q and one of the differences of scores.  fp32: q takes all of it.  bf16: q
+// takes the power of two that leaves 1 .. 2, so that no sum leaves the range that the score itself stays in.
+struct PagedScale {
+    float of_q, of_diff, whole;
+};
+static PagedScale paged_scale(float scale, int dt)
+{
+    const float log2 = scale * kLog2e;
+    if (dt == EC_F32) return {log2, 1.f, log2};
+    int n;
+    const float rest = std::frexp(log2, &n);  // 0.5 .. 1
+    return {std::ldexp(1.f, n - 1), 2.f * rest, log2};
+}
 
 struct PagedStep {
     const void *q, *k_new, *v_new;
@@ -10,86 +49,511 @@ struct PagedStep {
     const int32_t *len_b, *new_pos_b;
     Pages pages;
     int B, H, Hkv, G;
-    float scale;
-    float *raw, *lse;  // EMIT: [B,H,slots] scaled scores, [B,H] log of the softmax denominators
+    PagedScale scale;
+    float *raw, *stats;            // EMIT: [B,H,slots] scores in base-2 units, [B,H,2] softmax maximum and denominator
+    unsigned int* tickets;         // of the pairs with several segments, by their first one's number; zeros before and after
+    unsigned long long* partials;  // of the segments of such pairs
 };
 
-template <int DT> __device__ __forceinline__ float load_elem(const void* p, size_t i)
+template <int DT, int D> struct PagedTile {
+    static constexpr bool kHalf = DT == EC_BF16;
+    static constexpr int kRowBytes = D * Elem<DT>::kBytes;
+    static constexpr int CH = kRowBytes / 16;      // 16-byte chunks of a row
+    static constexpr int RPI = kWave / CH;         // rows of a load instruction
+    static constexpr int TR = kHalf ? 32 : 16;     // rows of a tile
+    static constexpr int GROUPS = TR / 8;          // runs of 8 rows, which lie in one page
+    static constexpr int IPG = 8 / RPI;            // load instructions of a run
+    static constexpr int NI = GROUPS * IPG;        // of a tile of K or V
+    static constexpr int BYTES = TR * kRowBytes;
+    // chunk c of row r lies at place c ^ swizzle(r): reads of 16 rows at one chunk number (K), of two chunks of 16 rows (V, bf16) and of
+    // whole rows (V, fp32) meet all banks alike
+    static __device__ __forceinline__ int swz_k(int r) { return CH >= 16 ? r & 15 : r >> 1 & 7; }
+    static __device__ __forceinline__ int swz_v(int r) { return !kHalf ? 0 : CH >= 16 ? (r & 7) << 1 : (r >> 1 & 3) << 1; }
+};
+
+__device__ __forceinline__ int scan_wave(int x)  // sum over the lanes up to this one
 {
-    if constexpr (DT == EC_F32) return static_cast<const float*>(p)[i];
-    else return bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next one (rows 1, 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
+    return x;
 }
-template <int DT> __device__ __forceinline__ void store_elem(void* p, size_t i, float x)
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+
+// The maximum, the sum over the lanes that share a query head (l % 16); all four get it.
+__device__ __forceinline__ float head_max(float x)
 {
-    if constexpr (DT == EC_F32) static_cast<float*>(p)[i] = x;
-    else static_cast<uint16_t*>(p)[i] = f32_to_bf16(x);
+    auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float head_sum(float x)
+{
+    auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
-// One workgroup per (sequence, query head); a wave takes every fourth row, a lane D / 64 features of it.
-template <int DT, int D, bool EMIT> __global__ __launch_bounds__(256) void paged_step_kernel(PagedStep a)
+// Which segment a workgroup takes.  A sequence of N rows (the new one included) has rounds of ROUND rows; a segment is at most `most` rounds
+// of a pair, with `most` such that the batch has about kPagedSegments of them: long sequences are cut, short ones are not.  Every wave
+// finds it for itself, a lane per sequence: no exchange between waves.
+struct Segment {
+    int b, n, pair, first, last, count;  // rounds first .. last-1 of the pair, which has `count` segments; b < 0: none
+    int split;                           // number of the segment among those of cut pairs
+    int split0;                          // and of its pair's first one
+};
+template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32_t* __restrict__ len_b, int B, int pairs, int slots, int id)
 {
-    constexpr int E = D / kWave, WAVES = 4;
-    __shared__ float sh_m[WAVES], sh_l[WAVES], sh_o[WAVES][D];
-    const int b = blockIdx.x / a.H, h = blockIdx.x % a.H, g = a.H / a.Hkv, hk = h / g;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const size_t out_at = ((size_t)b * a.H + h) * D;
-    const int n = a.len_b[b];
-    if (n < 0 || n >= a.pages.slots()) {  // no sequence in this place
-        if (threadIdx.x < D) store_elem<DT>(a.out, out_at + threadIdx.x, 0.f);
+    const int lane = threadIdx.x % kWave;
+    // rows before the step, or -1 for a place without a sequence, which has one round all the same (somebody has to write its zeros)
+    auto rows = [&](int b) {
+        const int n = b < B ? len_b[b] : -1;
+        return n >= 0 && n < slots ? n : -1;
+    };
+    // (loops over scalars, so that all lanes are there for what passes between lanes)
+    int n = -1;
+    long long all = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        n = rows(b0 + lane);
+        all += last_lane(scan_wave(b0 + lane >= B ? 0 : n < 0 ? 1 : n / ROUND + 1));
+    }
+    const int most = (int)((all * pairs + kPagedSegments - 1) / kPagedSegments);
+    int before = 0, cut = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        const int b = b0 + lane;
+        if (B > kWave) n = rows(b);
+        const int rounds = n < 0 ? 1 : n / ROUND + 1, count = b < B ? (rounds + most - 1) / most : 0;
+        const int upto = scan_wave(count), cut_upto = scan_wave(count > 1 ? count : 0);
+        const unsigned long long beyond = __ballot(b < B && id < before + upto * pairs);
+        if (beyond) {
+            const int at = __ffsll(beyond) - 1;
+            const int c = __builtin_amdgcn_readlane(count, at), r = __builtin_amdgcn_readlane(rounds, at);
+            const int in = id - before - (__builtin_amdgcn_readlane(upto, at) - c) * pairs;  // number among the sequence's segments
+            const int pair = in / c, seg = in - pair * c;
+            const int split0 = cut + (c > 1 ? (__builtin_amdgcn_readlane(cut_upto, at) - c) * pairs + pair * c : 0);
+            const int each = r / c, more = r - each * c;  // the first `more` segments have a round more
+            const int first = seg * each + min(seg, more);
+            return {b0 + at, __builtin_amdgcn_readlane(n, at), pair, first, first + each + (seg < more), c, split0 + seg, split0};
+        }
+        before += last_lane(upto) * pairs, cut += last_lane(cut_upto) * pairs;
+    }
+    return {-1, 0, 0, 0, 0, 0, 0, 0};
+}
+
+// Partial results pass between workgroups at device scope: written through and read past the caches, no fence.
+__device__ __forceinline__ void put(unsigned long long* p, float x, float y)
+{
+    __hip_atomic_store(p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get(const unsigned long long* p)
+{
+    const unsigned long long x = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+}
+
+template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kWave) void paged_step_kernel(PagedStep a)
+{
+    using T = PagedTile<DT, D>;
+    constexpr int WAVES = kPagedWaves, TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
+    constexpr int KB = ROW / 64;      // 64-byte blocks of a row: what the four quarters of a wave contract together
+    constexpr int OB = D / 16;        // 16-feature blocks of the output
+    constexpr int PART = D / 2 + 1;   // 8-byte words of a head's partial result
+    constexpr int OROW = D + 4;       // floats of a head's sums in LDS, padded
+    static_assert(kHeadBlock * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
+    __shared__ __align__(256) unsigned char tiles[WAVES][4 * T::BYTES];  // of every wave: two tiles of K, two of V
+    __shared__ float sh_m[WAVES][kHeadBlock], sh_l[WAVES][kHeadBlock];
+    __shared__ unsigned int sh_ticket;
+
+    const int g = a.H / a.Hkv, blocks = (g + kHeadBlock - 1) / kHeadBlock, slots = a.pages.slots();
+    const Segment at = find_segment<ROUND>(a.len_b, a.B, a.Hkv * blocks, slots, blockIdx.x);
+    if (at.b < 0) return;
+    const int hk = at.pair / blocks, block = at.pair - hk * blocks, heads = min(g - block * kHeadBlock, kHeadBlock);
+    const int head0 = hk * g + block * kHeadBlock;  // first query head
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int c16 = lane % 16, quarter = lane / 16;
+    const size_t out_at = ((size_t)at.b * a.H + head0) * D;  // element
+    if (at.n < 0) {  // no sequence in this place
+        for (int i = tid; i < heads * D; i += WAVES * kWave) {
+            if constexpr (T::kHalf) static_cast<uint16_t*>(a.out)[out_at + i] = 0;
+            else static_cast<float*>(a.out)[out_at + i] = 0.f;
+        }
         return;
     }
-    const size_t new_at = ((size_t)b * a.Hkv + hk) * D;
-    float q[E], o[E] = {}, m = kLowest, l = 0.f;
+    const int n = at.n;  // the new row's number
+    const char* k_new = static_cast<const char*>(a.k_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
+    const char* v_new = static_cast<const char*>(a.v_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
+
+    // queries: lane's head, chunks 4 kb + quarter; zeros for heads that do not exist
+    u32x4 qf[KB];
+    float of_diff = a.scale.of_diff;
+    {
+        const u32x4* q = static_cast<const u32x4*>(a.q) + (out_at / Elem<DT>::kPerChunk) + (size_t)min(c16, heads - 1) * CH;
 #pragma unroll
-    for (int e = 0; e < E; ++e) q[e] = load_elem<DT>(a.q, out_at + lane + e * kWave);
-    for (int j = wave; j <= n; j += WAVES) {
-        const void *k = a.k_new, *v = a.v_new;
-        size_t at = new_at;
-        if (j < n) {
-            const int id = a.pages.page_of(b, j);
-            if (id < 0) {
-                if (EMIT && lane == 0) a.raw[((size_t)b * a.H + h) * a.pages.slots() + j] = -INFINITY;
-                continue;
+        for (int kb = 0; kb < KB; ++kb) qf[kb] = q[kb * 4 + quarter];
+        bool fits = true;
+        if constexpr (T::kHalf) {  // a power of two, unless it takes an element out of bf16's range
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const float x = __uint_as_float(half ? qf[kb][e] & 0xffff0000u : qf[kb][e] << 16), y = fabsf(x * a.scale.of_q);
+                        fits = fits & ((x == 0.f) | !((y < 1.1754944e-38f) | (y > 3.3e38f)));
+                    }
+        }
+        if (!T::kHalf || __all(fits)) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (T::kHalf)
+                        qf[kb][e] = __float_as_uint(__uint_as_float(qf[kb][e] & 0xffff0000u) * a.scale.of_q) |
+                                    __float_as_uint(__uint_as_float(qf[kb][e] << 16) * a.scale.of_q) >> 16;
+                    else qf[kb][e] = __float_as_uint(__uint_as_float(qf[kb][e]) * a.scale.of_q);
+                }
+        } else {
+            of_diff = a.scale.whole;
+        }
+        if (c16 >= heads)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) qf[kb] = u32x4{0, 0, 0, 0};
+    }
+
+    // the new row's chunk of this lane (the first CH lanes have one)
+    u32x4 new_k = reinterpret_cast<const u32x4*>(k_new)[lane % CH], new_v = reinterpret_cast<const u32x4*>(v_new)[lane % CH];
+    // taken as arrived here: the compiler would otherwise wait for them inside the loop, and with them for every tile in flight
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qf[kb]));
+    asm volatile("" : "+v"(new_k), "+v"(new_v));
+
+    // ------------------------------------------------------------------ rows into LDS
+    const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles[wave]));
+    const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
+    const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(n, at.last * ROUND);  // rows of the cache in the segment end there
+    uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in a run of 8 rows, K: of even and odd runs
+#pragma unroll
+    for (int i = 0; i < T::IPG; ++i) {
+        const int r = i * RPI + lane / CH;
+        k_part[0][i] = r * ROW + (lane % CH ^ T::swz_k(r)) * 16;
+        k_part[1][i] = r * ROW + (lane % CH ^ T::swz_k(r + 8)) * 16;
+        v_part[i] = r * ROW + (lane % CH ^ T::swz_v(r)) * 16;
+    }
+    struct Ids {
+        int id[T::GROUPS];
+    };
+    auto pages_of = [&](int row) __attribute__((always_inline)) {
+        Ids ids;
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u) ids.id[u] = table[min((row + u * 8) >> shift, a.pages.max_pages - 1)];
+        return ids;
+    };
+    // Where the runs of a tile lie in the pools, and how many bytes of them are there: none behind the segment or on no page, and what is not
+    // there becomes zeros in LDS.
+    struct Places {
+        size_t from[T::GROUPS];
+        int bytes[T::GROUPS], bad;  // bit u: run u has rows, but no page
+    };
+    auto places_of = [&](int row, const Ids& ids) __attribute__((always_inline)) {
+        Places pl;
+        pl.bad = 0;
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u) {
+            const int r = row + u * 8, left = end - r;
+            const bool page = (unsigned)ids.id[u] < (unsigned)a.pages.n_pages;
+            pl.from[u] = ((((size_t)(unsigned)(page ? ids.id[u] : 0) * (unsigned)a.Hkv + (unsigned)hk) << shift) + (r & mask)) * ROW;
+            pl.bytes[u] = page ? max(min(left, 8), 0) * ROW : 0;
+            pl.bad |= page || left <= 0 ? 0 : 1 << u;
+        }
+        return pl;
+    };
+    auto issue_k = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u)
+#pragma unroll
+            for (int i = 0; i < T::IPG; ++i)
+                load_lds_16(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
+    };
+    auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u)
+#pragma unroll
+            for (int i = 0; i < T::IPG; ++i)
+                load_lds_16(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, v_part[i]);
+    };
+    // the new row, where the tile has it: into the place that its loads left at zero
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    auto add_new = [&](uint32_t lds, int row, const u32x4& chunk, int swizzle) __attribute__((always_inline)) {
+        const int r = n - row;
+        if (r >= 0 && r < TR) {
+            if (lane < CH) *(lds_u32x4*)(uintptr_t)(lds + r * ROW + (lane ^ swizzle) * 16) = chunk;
+            wait_lds();
+        }
+    };
+    // loads of the wave but the newest three tiles' have landed
+    auto wait_tile = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory"); };
+
+    // ------------------------------------------------------------------ one tile after the other
+    f32x4 o[OB];
+#pragma unroll
+    for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kLowest, l = 0.f;  // l: of this lane's rows
+    uint32_t k_at[KB], v_at[OB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) k_at[kb] = mine + c16 * ROW + ((kb * 4 + quarter) ^ T::swz_k(c16)) * 16;
+#pragma unroll
+    for (int i = 0; i < OB; ++i) {
+        if constexpr (T::kHalf) {  // 4 features of row 4 quarter + (lane % 16) / 4: the transposing read's share
+            const int r = quarter * 4 + c16 / 4;
+            v_at[i] = mine + 2 * T::BYTES + r * ROW + ((i * 2 + c16 % 4 / 2) ^ T::swz_v(r)) * 16 + c16 % 2 * 8;
+        } else {  // row 4 quarter + i % 4, features 64 (i / 4) + 4 c16 .. + 3
+            v_at[i] = mine + 2 * T::BYTES + (quarter * 4 + i % 4) * ROW + (c16 + i / 4 * 16) * 16;
+        }
+    }
+    constexpr int BLOCKS = TR / 16;  // of 16 rows
+
+    // off: which of the two places; later: the tile after the next, whose loads are issued as this one's place becomes free
+    auto tile = [&](uint32_t off, int row, int bad, const Places& later) __attribute__((always_inline)) {
+        f32x4 s[BLOCKS];
+#pragma unroll
+        for (int t = 0; t < BLOCKS; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        wait_tile();
+        add_new(mine + off, row, new_k, T::swz_k(n - row));
+        if constexpr (T::kHalf) {
+            bf16x8 kf[KB][BLOCKS];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) kf[kb][t] = *(lds_bf16x8*)(uintptr_t)(k_at[kb] + off + t * 16 * ROW);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t)
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][t], __builtin_bit_cast(bf16x8, qf[kb]), s[t], 0, 0, 0);
+        } else {
+            f32x4 kf[KB], part[4];  // four chains, so that every partial sum is short
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) kf[kb] = *(lds_f32x4*)(uintptr_t)(k_at[kb] + off);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][e], __uint_as_float(qf[kb][e]), part[e], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[0][r] = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
+        }
+        wait_lds();
+        issue_k(mine + off, later);
+
+        if (bad || row + TR > n + 1) {
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = row + t * 16 + quarter * 4 + r;
+                    if (j > n || (j < n && (bad >> (t * 2 + quarter / 2) & 1))) s[t][r] = -INFINITY;
+                }
+        }
+        if constexpr (EMIT) {
+            if (c16 < heads) {
+                float* raw = a.raw + ((size_t)at.b * a.H + head0 + c16) * slots;
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) {
+                    const int j = row + t * 16 + quarter * 4;
+                    f32x4 x;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = s[t][r] * of_diff;
+                    if (j <= n) *reinterpret_cast<f32x4*>(raw + j) = x;
+                }
             }
-            k = a.k_pages, v = a.v_pages, at = a.pages.row(id, a.Hkv, hk, j) * D;
         }
-        float s = 0.f;
+        float top = s[0][0];
 #pragma unroll
-        for (int e = 0; e < E; ++e) s = fmaf(q[e], load_elem<DT>(k, at + lane + e * kWave), s);
-        s = group_sum<kWave>(s) * a.scale;
-        if (EMIT && lane == 0) a.raw[((size_t)b * a.H + h) * a.pages.slots() + j] = s;
-        const float m_new = fmaxf(m, s), c = expf(m - m_new), p = expf(s - m_new);
-        m = m_new, l = l * c + p;
+        for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * c + p * load_elem<DT>(v, at + lane + e * kWave);
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
+        const float m_new = fmaxf(m, head_max(top));
+        if (__any(m_new > m)) {
+            const float c = exp2f((m - m_new) * of_diff);
+            l *= c;
+#pragma unroll
+            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= c;
+        }
+        m = m_new;
+        float p[BLOCKS][4], sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[t][r] = exp2f((s[t][r] - m) * of_diff);
+                sum += p[t][r];
+            }
+        l += sum;
+
+        wait_tile();
+        add_new(mine + 2 * T::BYTES + off, row, new_v, T::swz_v(n - row));
+        if constexpr (T::kHalf) {
+            // a probability is the sum of two bf16 numbers, its upper half (cut, so that the rest is not negative) and the rest, together
+            // 2^-16 of it off; the rest of one that is not 0 is not 0 either, so that an infinite V stays infinite
+            auto halves = [](float x, int e, bf16x8& hi, bf16x8& lo) __attribute__((always_inline)) {
+                const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+                hi[e] = (__bf16)h;
+                lo[e] = (__bf16)fmaxf(x - h, x * 0x1p-20f);
+            };
+            auto v_frag = [&](int i) __attribute__((always_inline)) {
+                const uint32_t src = v_at[i] + off;
+                const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)src);
+                const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(src + 16 * ROW));
+                return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64
+            bool small = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) small = small | ((p[e / 4][e % 4] < kSmall) & (p[e / 4][e % 4] > 0.f));
+            bf16x8 hi, lo;
+            if (__builtin_expect(__any(small), 0)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float& x = p[e / 4][e % 4];
+                    halves(x < kSmall ? x * 0x1p64f : 0.f, e, hi, lo);
+                    x = x < kSmall ? 0.f : x;
+                }
+#pragma unroll
+                for (int i = 0; i < OB; ++i) {
+                    const bf16x8 vf = v_frag(i);
+                    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi, x, 0, 0, 0);
+                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, x, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[i][r] = fmaf(x[r], 0x1p-64f, o[i][r]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) halves(p[e / 4][e % 4], e, hi, lo);
+#pragma unroll
+            for (int i = 0; i < OB; ++i) {
+                const bf16x8 vf = v_frag(i);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi, o[i], 0, 0, 0);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, o[i], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4
+                const f32x4 vf = *(lds_f32x4*)(uintptr_t)(v_at[i] + off);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e], p[0][i % 4], o[i / 4 * 4 + e], 0, 0, 0);
+            }
+        }
+        wait_lds();
+        issue_v(mine + 2 * T::BYTES + off, later);
+    };
+    {
+        int row = (at.first * WAVES + wave) * TR;
+        const Places first = places_of(row, pages_of(row)), second = places_of(row + ROUND, pages_of(row + ROUND));
+        issue_k(mine, first);
+        issue_v(mine + 2 * T::BYTES, first);
+        issue_k(mine + T::BYTES, second);
+        issue_v(mine + 3 * T::BYTES, second);
+        Places later = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+        uint32_t off = 0;
+        for (int left = at.last - at.first, bad = first.bad, next_bad = second.bad; left > 0; --left) {
+            const Ids ids = pages_of(row + 3 * ROUND);
+            tile(off, row, bad, later);
+            bad = next_bad, next_bad = later.bad;
+            row += ROUND, off ^= T::BYTES;
+            later = places_of(row + 2 * ROUND, ids);
+        }
     }
-    if (lane == 0) sh_m[wave] = m, sh_l[wave] = l;
+
+    // ------------------------------------------------------------------ the waves' results together
+    l = head_sum(l);
+    wait_loads();  // nothing more arrives in the tiles, whose place the sums take
+    if (quarter == 0) sh_m[wave][c16] = m, sh_l[wave][c16] = l;
 #pragma unroll
-    for (int e = 0; e < E; ++e) sh_o[wave][lane + e * kWave] = o[e];
+    for (int i = 0; i < OB; ++i) {
+        if constexpr (T::kHalf) {
+            *(lds_f32x4*)(uintptr_t)(mine + (c16 * OROW + i * 16 + quarter * 4) * 4) = o[i];
+        } else {  // features 64 (i / 4) + 4 (4 quarter + r) + i % 4
+            typedef __attribute__((address_space(3))) float lds_float;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) *(lds_float*)(uintptr_t)(mine + (c16 * OROW + i / 4 * 64 + (quarter * 4 + r) * 4 + i % 4) * 4) = o[i][r];
+        }
+    }
     __syncthreads();
-    if (threadIdx.x < D) {
-        float top = sh_m[0], sum = 0.f, x = 0.f;
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_m[w]);
+    auto write = [&](int h, int d, float x, float y) {
+        if constexpr (T::kHalf)
+            static_cast<uint32_t*>(a.out)[(out_at + h * D + d) / 2] = (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16;
+        else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + out_at + h * D + d) = make_float2(x, y);
+    };
+    auto statistics = [&](int h, float top, float sum) {
+        if constexpr (EMIT) *reinterpret_cast<float2*>(a.stats + ((size_t)at.b * a.H + head0 + h) * 2) = make_float2(top * of_diff, sum);
+    };
+    unsigned long long* part = a.partials + (size_t)at.split * (kHeadBlock * PART);
+    for (int i = tid; i < heads * (D / 2); i += WAVES * kWave) {
+        const int h = i / (D / 2), d = i % (D / 2) * 2;
+        float top = sh_m[0][h], sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_m[w][h]);
+#pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float c = expf(sh_m[w] - top);
-            sum += sh_l[w] * c, x += sh_o[w][threadIdx.x] * c;
+            const float c = exp2f((sh_m[w][h] - top) * of_diff);
+            const float2 v = *reinterpret_cast<const float2*>(tiles[w] + (h * OROW + d) * 4);
+            sum += sh_l[w][h] * c, x += v.x * c, y += v.y * c;
         }
-        store_elem<DT>(a.out, out_at + threadIdx.x, x / sum);
-        if (EMIT && threadIdx.x == 0) a.lse[(size_t)b * a.H + h] = top + logf(sum);
+        if (at.count == 1) {
+            write(h, d, x / sum, y / sum);
+            if (d == 0) statistics(h, top, sum);
+        } else {
+            put(part + h * PART + 1 + d / 2, x, y);
+            if (d == 0) put(part + h * PART, top, sum);
+        }
     }
-    if (h % g == 0) {  // the new row; nobody reads it in this launch
-        const int id = a.pages.page_of(b, n);
-        if (id >= 0 && threadIdx.x < D) {
-            const size_t at = a.pages.row(id, a.Hkv, hk, n) * D + threadIdx.x;
-            store_elem<DT>(a.k_pages, at, load_elem<DT>(a.k_new, new_at + threadIdx.x));
-            store_elem<DT>(a.v_pages, at, load_elem<DT>(a.v_new, new_at + threadIdx.x));
+    if (at.last * ROUND > n && block == 0) {  // the new row; nobody reads its slot in this launch
+        const int id = a.pages.page_of(at.b, n);
+        if (id >= 0) {
+            const size_t to = a.pages.row(id, a.Hkv, hk, n) * CH;
+            if (tid < 2 * CH) {
+                const u32x4 x = reinterpret_cast<const u32x4*>(tid < CH ? k_new : v_new)[tid % CH];
+                (static_cast<u32x4*>(tid < CH ? a.k_pages : a.v_pages))[to + tid % CH] = x;
+            }
+            if (tid == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(id, a.G, a.G > 1 ? hk : 0, n)] = a.new_pos_b[at.b];
         }
-        if (id >= 0 && threadIdx.x == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(id, a.G, a.G > 1 ? hk : 0, n)] = a.new_pos_b[b];
+    }
+    if (at.count == 1) return;
+
+    // ------------------------------------------------------------------ the segments' results together, by the last to arrive
+    wait_loads();  // (stores count too) this wave's partial results are where every workgroup sees them
+    __syncthreads();
+    if (tid == 0) sh_ticket = atomicInc(a.tickets + at.split0, at.count - 1);  // back at 0 with the last
+    __syncthreads();
+    if (sh_ticket != (unsigned)at.count - 1) return;
+    const unsigned long long* parts = a.partials + (size_t)at.split0 * (kHeadBlock * PART);
+    for (int i = tid; i < heads * (D / 2); i += WAVES * kWave) {
+        const int h = i / (D / 2), d = i % (D / 2) * 2;
+        float top = kLowest, sum = 0.f, x = 0.f, y = 0.f;
+        for (int s = 0; s < at.count; ++s) top = fmaxf(top, get(parts + (size_t)s * (kHeadBlock * PART) + h * PART).x);
+        for (int s = 0; s < at.count; ++s) {
+            const unsigned long long* from = parts + (size_t)s * (kHeadBlock * PART) + h * PART;
+            const float2 ml = get(from), v = get(from + 1 + d / 2);
+            const float c = exp2f((ml.x - top) * of_diff);
+            sum += ml.y * c, x += v.x * c, y += v.y * c;
+        }
+        write(h, d, x / sum, y / sum);
+        if (d == 0) statistics(h, top, sum);
     }
 }
 
 // mass of every row += the mean of its group's probabilities; a thread a row, heads in ascending order.
-__global__ __launch_bounds__(256) void paged_mass_kernel(const float* __restrict__ raw, const float* __restrict__ lse, float* mass_pages,
+__global__ __launch_bounds__(256) void paged_mass_kernel(const float* __restrict__ raw, const float* __restrict__ stats, float* mass_pages,
                                                          const int32_t* __restrict__ len_b, Pages pages, int H, int G)
 {
     const int b = blockIdx.y / G, g = blockIdx.y % G, n = len_b[b];
@@ -99,26 +563,37 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const float* __restrict
     if (id < 0) return;
     const int heads = H / G;
     float sum = 0.f;
-    for (int h = g * heads; h < (g + 1) * heads; ++h) sum += expf(raw[((size_t)b * H + h) * pages.slots() + j] - lse[(size_t)b * H + h]);
+    for (int h = g * heads; h < (g + 1) * heads; ++h) {
+        const size_t bh = (size_t)b * H + h;
+        sum += exp2f(raw[bh * pages.slots() + j] - stats[bh * 2]) / stats[bh * 2 + 1];
+    }
     float* m = mass_pages + pages.row(id, G, g, j);
     *m = (j == n ? 0.f : *m) + sum / (float)heads;
 }
 
-size_t paged_step_ws(int B, int H, int slots, bool emit)
+// Workspace: tickets, partial results of cut pairs (a pair of r rounds is cut into less than 2 r / most segments, so there are less than twice
+// kPagedSegments of them), and for EMIT scores and statistics.
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+constexpr size_t kTicketBytes = 2 * kPagedSegments * sizeof(unsigned int);
+static size_t partial_bytes(int D) { return up256((size_t)2 * kPagedSegments * kHeadBlock * (D / 2 + 1) * 8); }
+size_t paged_step_ws(int B, int H, int slots, int D, bool emit)
 {
-    if (!emit) return 256;
-    return (((size_t)B * H * slots * 4 + 255) & ~(size_t)255) + (((size_t)B * H * 4 + 255) & ~(size_t)255);
+    return kTicketBytes + partial_bytes(D) + (emit ? up256((size_t)B * H * slots * 4) + up256((size_t)B * H * 8) : 0);
 }
 
 template <int DT, int D> static int launch(const PagedStep& a, float* mass_pages, hipStream_t stream)
 {
+    constexpr int ROUND = kPagedWaves * PagedTile<DT, D>::TR;
+    const int g = a.H / a.Hkv;
+    const long long pairs = (long long)a.B * a.Hkv * ((g + kHeadBlock - 1) / kHeadBlock), rounds = (a.pages.slots() + ROUND - 1) / ROUND;
+    const dim3 grid((unsigned)std::min(kPagedSegments + pairs, rounds * pairs));
     if (!mass_pages) {
-        hipLaunchKernelGGL((paged_step_kernel<DT, D, false>), dim3(a.B * a.H), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_step_kernel<DT, D, false>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
         return status_from_hip(hipGetLastError());
     }
-    hipLaunchKernelGGL((paged_step_kernel<DT, D, true>), dim3(a.B * a.H), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((paged_step_kernel<DT, D, true>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
-    hipLaunchKernelGGL(paged_mass_kernel, dim3((a.pages.slots() + 255) / 256, a.B * a.G), dim3(256), 0, stream, a.raw, a.lse, mass_pages, a.len_b,
+    hipLaunchKernelGGL(paged_mass_kernel, dim3((a.pages.slots() + 255) / 256, a.B * a.G), dim3(256), 0, stream, a.raw, a.stats, mass_pages, a.len_b,
                        a.pages, a.H, a.G);
     return status_from_hip(hipGetLastError());
 }
@@ -127,9 +602,11 @@ int paged_step_dispatch(const void* q, const void* k_new, const void* v_new, voi
                         const Pages& pages, const int32_t* len_b, const int32_t* new_pos_b, int B, int H, int Hkv, int G, int D, float scale, int dt,
                         void* out, void* ws, hipStream_t stream)
 {
-    float* raw = static_cast<float*>(ws);
-    float* lse = reinterpret_cast<float*>(static_cast<char*>(ws) + (((size_t)B * H * pages.slots() * 4 + 255) & ~(size_t)255));
-    const PagedStep a{q, k_new, v_new, k_pages, v_pages, out, pos_pages, len_b, new_pos_b, pages, B, H, Hkv, G, scale, raw, lse};
+    char* at = static_cast<char*>(ws);
+    const PagedStep a{q, k_new, v_new, k_pages, v_pages, out, pos_pages, len_b, new_pos_b, pages, B, H, Hkv, G, paged_scale(scale, dt),
+                      reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D)),
+                      reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D) + up256((size_t)B * H * pages.slots() * 4)),
+                      reinterpret_cast<unsigned int*>(at), reinterpret_cast<unsigned long long*>(at + kTicketBytes)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, mass_pages, stream) : launch<EC_BF16, 64>(a, mass_pages, stream);
     return D == 128 ? launch<EC_F32, 128>(a, mass_pages, stream) : launch<EC_F32, 64>(a, mass_pages, stream);
 }

@@ -56,7 +56,7 @@ class Dev:
         assert (np.isnan(want) | (got == want) | (err <= (0 if mass_tol is None else mass_tol))).all(), np.nanmax(err)
 
 
-def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=None, vn=None, with_pos=True):
+def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=None, vn=None, with_pos=True, more=0.0):
     rng = np.random.default_rng(seed)
     B, D = pool.table.shape[0], pool.k.shape[3]
     scale = D ** -0.5 if scale is None else scale
@@ -79,7 +79,7 @@ def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=No
     old = pool.mass.copy()
     want, A, big = ref.step(pool, q.astype(np.float64), kn, vn, lens, new_pos if with_pos else None, scale, scored)
     n = max(max(lens), 0) + 1
-    tol = ref.attention_tolerance(dtype, want, A, big, n, D)
+    tol = ref.attention_tolerance(dtype, want, A, big, n, D) + more
     got = to_host(out)
     with np.errstate(invalid="ignore"):
         err = np.abs(got - want)
@@ -181,6 +181,46 @@ def test_values_at_the_ends_of_the_range(dtype, what):
     elif what == "plus_inf":
         pool.k[p, 0, o, 3] = np.inf
     run_step(pool, dtype, 4, lens, 13, scale=scale, q=q, kn=kn)
+
+
+RANGES = {  # exponents of keys and of queries, scale
+    "keys below the normal range": (-130, 123, 1.0),
+    "queries below the normal range": (125, -130, 0.0884),
+    "queries that scaling takes below it": (124, -124, 0.0884),
+    "large queries": (-128, 127, 1.0),
+    "large keys": (127, -128, 1.0),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", RANGES)
+def test_queries_and_keys_at_the_ends_of_the_range(dtype, what):
+    """The scores are of size one; neither their products nor their sums leave the range that q * scale stays in."""
+    at_k, at_q, scale = RANGES[what]
+    rng = np.random.default_rng(14)
+    lens, D = [40, 300], 64
+    pool = make(rng, dtype, 2, 2, 1, D, 16, 20, lens, junk=0.0)
+    cut = lambda x, e: quantize(np.clip(x, -1.3, 1.3) * 2.0 ** e, dtype)  # noqa: E731
+    pool.k = cut(pool.k, at_k)
+    run_step(pool, dtype, 4, lens, 13, scale=scale, q=cut(rng.standard_normal((2, 4, D)), at_q), kn=cut(rng.standard_normal((2, 2, D)), at_k))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("below", [60, 110, 120, 130, 140])
+def test_small_weights_of_large_rows(dtype, below):
+    """A weight far below the normal range counts where its V decides the output: the other rows' V are zeros. A subnormal weight is off by 2^-150 at
+    most, here of four rows of 2^120 times at most 5, divided by a sum of at least 1."""
+    rng = np.random.default_rng(15)
+    lens, D = [50, 10], 64
+    pool = make(rng, dtype, 2, 2, 1, D, 16, 6, lens, junk=0.0)
+    pool.k[:], pool.v[:] = 0, 0
+    q, kn = np.zeros((2, 4, D), np.float32), np.zeros((2, 2, D), np.float32)
+    q[:, :, 0] = 1
+    for s in range(20, 24):
+        p, o = pool.at(0, s)
+        pool.k[p, :, o, 0] = -below * 0.5
+        pool.v[p, :, o] = quantize(rng.standard_normal((2, D)) * 2.0 ** 120, dtype)
+    run_step(pool, dtype, 4, lens, 13, scale=2 * float(np.log(2)), q=q, kn=kn, vn=np.zeros((2, 2, D), np.float32), more=4 * 5 * 2.0 ** (120 - 150))
 
 
 def test_rows_beyond_four_gibibytes():
