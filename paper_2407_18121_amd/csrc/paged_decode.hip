@@ -18,28 +18,33 @@ namespace ec {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 typedef __attribute__((address_space(4))) const int32_t const_i32;  // read through the scalar cache: nothing that a launch writes
 
-constexpr int kPagedWaves = 2;
-constexpr int kPagedSegments = 512;  // workgroups that a launch aims at
+constexpr int kPagedWaves = 4;
+constexpr int kPagedSegments = 256;  // workgroups that a launch of few pairs aims at: one a compute unit
+constexpr int kMostSegments = 256;   // of a pair, whose weights have to fit into LDS when they are joined
 constexpr int kHeadBlock = 16;       // query heads of a pair, at most
-constexpr float kSmall = 0x1p-100f;  // bf16: probabilities below it are multiplied apart
+constexpr float kSmallExponent = -100.f, kSmall = 0x1p-100f;  // probabilities below it are looked at apart
 
-// The scale in base-2 units, log2(e) * scale, as a factor of q and one of the differences of scores.  fp32: q takes all of it.  bf16: q
-// takes the power of two that leaves 1 .. 2, so that no sum leaves the range that the score itself stays in.
+// The scale in base-2 units, log2(e) * scale. fp32: q takes all of it. bf16: q takes the power of two, 2^exponent, that leaves 1 .. 2 for the
+// differences of scores, so that no sum leaves the range that the score itself stays in.
 struct PagedScale {
-    float of_q, of_diff, whole;
+    float whole, of_diff;
+    int exponent;
 };
 static PagedScale paged_scale(float scale, int dt)
 {
     const float log2 = scale * kLog2e;
-    if (dt == EC_F32) return {log2, 1.f, log2};
+    if (dt == EC_F32) return {log2, 1.f, 0};
     int n;
     const float rest = std::frexp(log2, &n);  // 0.5 .. 1
-    return {std::ldexp(1.f, n - 1), 2.f * rest, log2};
+    return {log2, 2.f * rest, n - 1};
 }
 
 struct PagedStep {
@@ -49,18 +54,26 @@ struct PagedStep {
     const int32_t *len_b, *new_pos_b;
     Pages pages;
     int B, H, Hkv, G;
+    int group, blocks;             // query heads of a key/value head, and pairs that they make
     PagedScale scale;
     float *raw, *stats;            // EMIT: [B,H,slots] scores in base-2 units, [B,H,2] softmax maximum and denominator
     unsigned int* tickets;         // of the pairs with several segments, by their first one's number; zeros before and after
     unsigned long long* partials;  // of the segments of such pairs
 };
 
+// load_lds_16 of data that is read once: the non-temporal hint keeps it from displacing cache lines (B16 H32 870 rows 46.8 -> 42.3 us a step, one
+// cache of 131071 rows 105 -> 91)
+__device__ __forceinline__ void load_once_lds_16(u32x4 rsrc, uint32_t lds, uint32_t byte_offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(byte_offset), "s"(rsrc) : "memory");
+}
+
 template <int DT, int D> struct PagedTile {
     static constexpr bool kHalf = DT == EC_BF16;
     static constexpr int kRowBytes = D * Elem<DT>::kBytes;
     static constexpr int CH = kRowBytes / 16;      // 16-byte chunks of a row
     static constexpr int RPI = kWave / CH;         // rows of a load instruction
-    static constexpr int TR = kHalf ? 32 : 16;     // rows of a tile
+    static constexpr int TR = kHalf && D < 128 ? 32 : 16;  // rows of a tile
     static constexpr int GROUPS = TR / 8;          // runs of 8 rows, which lie in one page
     static constexpr int IPG = 8 / RPI;            // load instructions of a run
     static constexpr int NI = GROUPS * IPG;        // of a tile of K or V
@@ -99,81 +112,96 @@ __device__ __forceinline__ float head_sum(float x)
     return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
-// Which segment a workgroup takes.  A sequence of N rows (the new one included) has rounds of ROUND rows; a segment is at most `most` rounds
-// of a pair, with `most` such that the batch has about kPagedSegments of them: long sequences are cut, short ones are not.  Every wave
-// finds it for itself, a lane per sequence: no exchange between waves.
+// Which segment a workgroup takes. A sequence of N rows (the new one included) has rounds of ROUND rows; a segment is at most `most` rounds
+// of a pair, `most` such that a batch of few pairs has kPagedSegments segments: long sequences are cut, short ones are not. Every wave finds its
+// segment for itself, a lane per sequence: no exchange between waves.
 struct Segment {
     int b, n, pair, first, last, count;  // rounds first .. last-1 of the pair, which has `count` segments; b < 0: none
     int split;                           // number of the segment among those of cut pairs
     int split0;                          // and of its pair's first one
 };
+__device__ __forceinline__ int divided(int x, int by)  // 0 <= x < 2^24, by > 0
+{
+    const int q = (int)((float)x * __builtin_amdgcn_rcpf((float)by)), r = x - q * by;
+    return q + (r >= by) - (r < 0);
+}
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Segment segment_of(int b, int n, int pair, int seg, int rounds, int count, int split0)
+{
+    const int each = scalar(divided(rounds, count)), more = rounds - each * count;  // the first `more` segments have a round more
+    const int first = seg * each + min(seg, more);
+    return {b, n, pair, first, first + each + (seg < more), count, split0 + seg, split0};
+}
 template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32_t* __restrict__ len_b, int B, int pairs, int slots, int id)
 {
     const int lane = threadIdx.x % kWave;
+    if (B == 1) {  // nothing to look through
+        const int n = ((const const_i32*)(uintptr_t)len_b)[0];
+        const bool live = n >= 0 && n < slots;
+        const int rounds = live ? n / ROUND + 1 : 1, count = min(min(rounds, kMostSegments), max(scalar(divided(kPagedSegments, pairs)), 1));
+        const int seg = scalar(divided(id, pairs));
+        if (seg >= count) return {-1, 0, 0, 0, 0, 0, 0, 0};
+        const int pair = id - seg * pairs;
+        return segment_of(0, live ? n : -1, pair, seg, rounds, count, pair * count);
+    }
     // rows before the step, or -1 for a place without a sequence, which has one round all the same (somebody has to write its zeros)
     auto rows = [&](int b) {
         const int n = b < B ? len_b[b] : -1;
         return n >= 0 && n < slots ? n : -1;
     };
+    auto rounds_of = [&](int b, int n) { return b >= B ? 0 : n < 0 ? 1 : n / ROUND + 1; };
     // (loops over scalars, so that all lanes are there for what passes between lanes)
     int n = -1;
     long long all = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
         n = rows(b0 + lane);
-        all += last_lane(scan_wave(b0 + lane >= B ? 0 : n < 0 ? 1 : n / ROUND + 1));
+        all += last_lane(scan_wave(rounds_of(b0 + lane, n)));
     }
-    const int most = (int)((all * pairs + kPagedSegments - 1) / kPagedSegments);
+    int most = (int)((all * pairs + kPagedSegments - 1) / kPagedSegments);
     int before = 0, cut = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
-        const int b = b0 + lane;
-        if (B > kWave) n = rows(b);
-        const int rounds = n < 0 ? 1 : n / ROUND + 1, count = b < B ? (rounds + most - 1) / most : 0;
+        if (B > kWave) n = rows(b0 + lane);
+        const int rounds = rounds_of(b0 + lane, n), count = min(divided(rounds + most - 1, most), kMostSegments);
         const int upto = scan_wave(count), cut_upto = scan_wave(count > 1 ? count : 0);
-        const unsigned long long beyond = __ballot(b < B && id < before + upto * pairs);
+        const unsigned long long beyond = __ballot(id < before + upto * pairs);
         if (beyond) {
             const int at = __ffsll(beyond) - 1;
-            const int c = __builtin_amdgcn_readlane(count, at), r = __builtin_amdgcn_readlane(rounds, at);
+            const int c = __builtin_amdgcn_readlane(count, at);
             const int in = id - before - (__builtin_amdgcn_readlane(upto, at) - c) * pairs;  // number among the sequence's segments
-            const int pair = in / c, seg = in - pair * c;
+            const int pair = scalar(divided(in, c));
             const int split0 = cut + (c > 1 ? (__builtin_amdgcn_readlane(cut_upto, at) - c) * pairs + pair * c : 0);
-            const int each = r / c, more = r - each * c;  // the first `more` segments have a round more
-            const int first = seg * each + min(seg, more);
-            return {b0 + at, __builtin_amdgcn_readlane(n, at), pair, first, first + each + (seg < more), c, split0 + seg, split0};
+            return segment_of(b0 + at, __builtin_amdgcn_readlane(n, at), pair, in - pair * c, __builtin_amdgcn_readlane(rounds, at), c, split0);
         }
         before += last_lane(upto) * pairs, cut += last_lane(cut_upto) * pairs;
     }
     return {-1, 0, 0, 0, 0, 0, 0, 0};
 }
 
+constexpr int kDeviceScope = 16;  // of a buffer load
 // Partial results pass between workgroups at device scope: written through and read past the caches, no fence.
 __device__ __forceinline__ void put(unsigned long long* p, float x, float y)
 {
     __hip_atomic_store(p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ float2 get(const unsigned long long* p)
-{
-    const unsigned long long x = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
-}
-
 template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kWave) void paged_step_kernel(PagedStep a)
 {
     using T = PagedTile<DT, D>;
     constexpr int WAVES = kPagedWaves, TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
     constexpr int KB = ROW / 64;      // 64-byte blocks of a row: what the four quarters of a wave contract together
     constexpr int OB = D / 16;        // 16-feature blocks of the output
-    constexpr int PART = D / 2 + 1;   // 8-byte words of a head's partial result
+    constexpr int PART = kHeadBlock * (D / 2 + 1);  // 8-byte words of a segment's result: (maximum, sum) of every head, then the sums
     constexpr int OROW = D + 4;       // floats of a head's sums in LDS, padded
     static_assert(kHeadBlock * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
+    static_assert(T::TR == 16 || T::TR == 32);
     __shared__ __align__(256) unsigned char tiles[WAVES][4 * T::BYTES];  // of every wave: two tiles of K, two of V
     __shared__ float sh_m[WAVES][kHeadBlock], sh_l[WAVES][kHeadBlock];
     __shared__ unsigned int sh_ticket;
 
-    const int g = a.H / a.Hkv, blocks = (g + kHeadBlock - 1) / kHeadBlock, slots = a.pages.slots();
-    const Segment at = find_segment<ROUND>(a.len_b, a.B, a.Hkv * blocks, slots, blockIdx.x);
+    const int slots = a.pages.slots();
+    const Segment at = find_segment<ROUND>(a.len_b, a.B, a.Hkv * a.blocks, slots, blockIdx.x);
     if (at.b < 0) return;
-    const int hk = at.pair / blocks, block = at.pair - hk * blocks, heads = min(g - block * kHeadBlock, kHeadBlock);
-    const int head0 = hk * g + block * kHeadBlock;  // first query head
+    const int hk = a.blocks == 1 ? at.pair : at.pair / a.blocks, block = at.pair - hk * a.blocks, heads = min(a.group - block * kHeadBlock, kHeadBlock);
+    const int head0 = hk * a.group + block * kHeadBlock;  // first query head
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c16 = lane % 16, quarter = lane / 16;
     const size_t out_at = ((size_t)at.b * a.H + head0) * D;  // element
@@ -188,49 +216,8 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     const char* k_new = static_cast<const char*>(a.k_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
     const char* v_new = static_cast<const char*>(a.v_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
 
-    // queries: lane's head, chunks 4 kb + quarter; zeros for heads that do not exist
-    u32x4 qf[KB];
-    float of_diff = a.scale.of_diff;
-    {
-        const u32x4* q = static_cast<const u32x4*>(a.q) + (out_at / Elem<DT>::kPerChunk) + (size_t)min(c16, heads - 1) * CH;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) qf[kb] = q[kb * 4 + quarter];
-        bool fits = true;
-        if constexpr (T::kHalf) {  // a power of two, unless it takes an element out of bf16's range
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const float x = __uint_as_float(half ? qf[kb][e] & 0xffff0000u : qf[kb][e] << 16), y = fabsf(x * a.scale.of_q);
-                        fits = fits & ((x == 0.f) | !((y < 1.1754944e-38f) | (y > 3.3e38f)));
-                    }
-        }
-        if (!T::kHalf || __all(fits)) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (T::kHalf)
-                        qf[kb][e] = __float_as_uint(__uint_as_float(qf[kb][e] & 0xffff0000u) * a.scale.of_q) |
-                                    __float_as_uint(__uint_as_float(qf[kb][e] << 16) * a.scale.of_q) >> 16;
-                    else qf[kb][e] = __float_as_uint(__uint_as_float(qf[kb][e]) * a.scale.of_q);
-                }
-        } else {
-            of_diff = a.scale.whole;
-        }
-        if (c16 >= heads)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) qf[kb] = u32x4{0, 0, 0, 0};
-    }
-
     // the new row's chunk of this lane (the first CH lanes have one)
-    u32x4 new_k = reinterpret_cast<const u32x4*>(k_new)[lane % CH], new_v = reinterpret_cast<const u32x4*>(v_new)[lane % CH];
-    // taken as arrived here: the compiler would otherwise wait for them inside the loop, and with them for every tile in flight
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qf[kb]));
-    asm volatile("" : "+v"(new_k), "+v"(new_v));
+    const u32x4 new_k = reinterpret_cast<const u32x4*>(k_new)[lane % CH], new_v = reinterpret_cast<const u32x4*>(v_new)[lane % CH];
 
     // ------------------------------------------------------------------ rows into LDS
     const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles[wave]));
@@ -277,14 +264,22 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
         for (int u = 0; u < T::GROUPS; ++u)
 #pragma unroll
             for (int i = 0; i < T::IPG; ++i)
-                load_lds_16(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
+                load_once_lds_16(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
+    };
+    auto issue_q = [&](uint32_t lds) __attribute__((always_inline)) {  // rows of queries like rows of K; zeros for heads that do not exist
+        const char* q = static_cast<const char*>(a.q) + out_at * Elem<DT>::kBytes;
+#pragma unroll
+        for (int u = 0; u < kHeadBlock / 8; ++u)
+#pragma unroll
+            for (int i = 0; i < T::IPG; ++i)
+                load_lds_16(tile_rsrc(q + u * 8 * ROW, max(heads - u * 8, 0) * ROW), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
     };
     auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::GROUPS; ++u)
 #pragma unroll
             for (int i = 0; i < T::IPG; ++i)
-                load_lds_16(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, v_part[i]);
+                load_once_lds_16(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, v_part[i]);
     };
     // the new row, where the tile has it: into the place that its loads left at zero
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -295,14 +290,19 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
             wait_lds();
         }
     };
-    // loads of the wave but the newest three tiles' have landed
-    auto wait_tile = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory"); };
+    // loads of the wave but the newest three tiles' have landed; or all of them, where no tile is issued any more
+    auto wait_tile = [&](bool more) __attribute__((always_inline)) {
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory");
+        else wait_loads();
+    };
 
     // ------------------------------------------------------------------ one tile after the other
     f32x4 o[OB];
 #pragma unroll
     for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kLowest, l = 0.f;  // l: of this lane's rows
+    u32x4 qf[KB];                // this lane's head, chunks 4 kb + quarter of its query
+    float of_diff = a.scale.of_diff;
     uint32_t k_at[KB], v_at[OB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) k_at[kb] = mine + c16 * ROW + ((kb * 4 + quarter) ^ T::swz_k(c16)) * 16;
@@ -318,11 +318,11 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     constexpr int BLOCKS = TR / 16;  // of 16 rows
 
     // off: which of the two places; later: the tile after the next, whose loads are issued as this one's place becomes free
-    auto tile = [&](uint32_t off, int row, int bad, const Places& later) __attribute__((always_inline)) {
+    auto tile = [&](uint32_t off, int row, int bad, bool more, const Places& later) __attribute__((always_inline)) {
         f32x4 s[BLOCKS];
 #pragma unroll
         for (int t = 0; t < BLOCKS; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        wait_tile();
+        wait_tile(more);
         add_new(mine + off, row, new_k, T::swz_k(n - row));
         if constexpr (T::kHalf) {
             bf16x8 kf[KB][BLOCKS];
@@ -350,7 +350,7 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
             for (int r = 0; r < 4; ++r) s[0][r] = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
         }
         wait_lds();
-        issue_k(mine + off, later);
+        if (more) issue_k(mine + off, later);
 
         if (bad || row + TR > n + 1) {
 #pragma unroll
@@ -389,62 +389,76 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
                 for (int r = 0; r < 4; ++r) o[i][r] *= c;
         }
         m = m_new;
-        float p[BLOCKS][4], sum = 0.f;
+        // 2^x; the exponential instruction gives zero where the result is subnormal, exp2f does not
+        float p[BLOCKS][4], sum = 0.f, least = 0.f;
 #pragma unroll
         for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                p[t][r] = exp2f((s[t][r] - m) * of_diff);
-                sum += p[t][r];
+                const float x = (s[t][r] - m) * of_diff;
+                least = fminf(least, x);
+                p[t][r] = __builtin_amdgcn_exp2f(x);
             }
+        const bool small = __any(least < kSmallExponent && c16 < heads);
+        if (__builtin_expect(small, 0)) {
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[t][r] = exp2f((s[t][r] - m) * of_diff);
+        }
+#pragma unroll
+        for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += p[t][r];
         l += sum;
 
-        wait_tile();
+        wait_tile(more);
         add_new(mine + 2 * T::BYTES + off, row, new_v, T::swz_v(n - row));
         if constexpr (T::kHalf) {
             // a probability is the sum of two bf16 numbers, its upper half (cut, so that the rest is not negative) and the rest, together
             // 2^-16 of it off; the rest of one that is not 0 is not 0 either, so that an infinite V stays infinite
-            auto halves = [](float x, int e, bf16x8& hi, bf16x8& lo) __attribute__((always_inline)) {
+            constexpr int PV = BLOCKS * 4;  // probabilities of a lane
+            typedef __attribute__((ext_vector_type(PV))) __bf16 bf16xp;
+            auto halves = [](float x, int e, bf16xp& hi, bf16xp& lo) __attribute__((always_inline)) {
                 const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
                 hi[e] = (__bf16)h;
                 lo[e] = (__bf16)fmaxf(x - h, x * 0x1p-20f);
             };
-            auto v_frag = [&](int i) __attribute__((always_inline)) {
-                const uint32_t src = v_at[i] + off;
-                const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)src);
-                const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(src + 16 * ROW));
-                return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            bf16x4 vf[OB][BLOCKS];  // all on their way before the first is used
+#pragma unroll
+            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) vf[i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(v_at[i] + off + t * 16 * ROW));
+            __builtin_amdgcn_sched_barrier(0);
+            // x + V^T . P^T of 16 features, P one of its halves
+            auto multiply = [&](int i, const bf16xp& half, f32x4 x) __attribute__((always_inline)) {
+                if constexpr (BLOCKS == 2)
+                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
+                else
+                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vf[i][0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
             };
             // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64
-            bool small = false;
+            bf16xp hi, lo;
+            if (__builtin_expect(small, 0)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) small = small | ((p[e / 4][e % 4] < kSmall) & (p[e / 4][e % 4] > 0.f));
-            bf16x8 hi, lo;
-            if (__builtin_expect(__any(small), 0)) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < PV; ++e) {
                     float& x = p[e / 4][e % 4];
                     halves(x < kSmall ? x * 0x1p64f : 0.f, e, hi, lo);
                     x = x < kSmall ? 0.f : x;
                 }
 #pragma unroll
                 for (int i = 0; i < OB; ++i) {
-                    const bf16x8 vf = v_frag(i);
-                    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi, x, 0, 0, 0);
-                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, x, 0, 0, 0);
+                    const f32x4 x = multiply(i, lo, multiply(i, hi, f32x4{0.f, 0.f, 0.f, 0.f}));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[i][r] = fmaf(x[r], 0x1p-64f, o[i][r]);
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) halves(p[e / 4][e % 4], e, hi, lo);
+            for (int e = 0; e < PV; ++e) halves(p[e / 4][e % 4], e, hi, lo);
 #pragma unroll
-            for (int i = 0; i < OB; ++i) {
-                const bf16x8 vf = v_frag(i);
-                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi, o[i], 0, 0, 0);
-                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, o[i], 0, 0, 0);
-            }
+            for (int i = 0; i < OB; ++i) o[i] = multiply(i, hi, o[i]);
+#pragma unroll
+            for (int i = 0; i < OB; ++i) o[i] = multiply(i, lo, o[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4
@@ -454,29 +468,80 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
             }
         }
         wait_lds();
-        issue_v(mine + 2 * T::BYTES + off, later);
+        if (more) issue_v(mine + 2 * T::BYTES + off, later);
     };
     {
-        int row = (at.first * WAVES + wave) * TR;
-        const Places first = places_of(row, pages_of(row)), second = places_of(row + ROUND, pages_of(row + ROUND));
+        int row = (at.first * WAVES + wave) * TR, left = at.last - at.first;  // rounds
+        const Places first = places_of(row, pages_of(row));
+        issue_q(mine + 3 * T::BYTES);  // the queries pass through the place of the second tile of V
         issue_k(mine, first);
         issue_v(mine + 2 * T::BYTES, first);
-        issue_k(mine + T::BYTES, second);
-        issue_v(mine + 3 * T::BYTES, second);
-        Places later = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+        Places next = places_of(row + ROUND, pages_of(row + ROUND));
+        issue_k(mine + T::BYTES, next);  // (nothing, where the segment has one round)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory");
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) qf[kb] = *(lds_u32x4*)(uintptr_t)(k_at[kb] + 3 * T::BYTES);
+        wait_lds();
+        issue_v(mine + 3 * T::BYTES, next);
+        if constexpr (T::kHalf) {
+            // a power of two, added to the exponents, unless that takes an element out of the range of normal numbers
+            u16x2 least = {0xffff, 0xffff}, most = {0, 0};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const u16x2 x = __builtin_bit_cast(u16x2, qf[kb][e] & 0x7fff7fffu);
+                    least = __builtin_elementwise_min(least, x - (u16x2){1, 1}), most = __builtin_elementwise_max(most, x);  // zeros count as large
+                }
+            const int lo = (min((int)least.x, (int)least.y) + 1) >> 7, hi = max((int)most.x, (int)most.y) >> 7, up = a.scale.exponent;
+            if (__all((lo + up >= 1) & (hi + up <= 253) & (hi < 255))) {
+                const u16x2 add = {(uint16_t)(up * 128), (uint16_t)(up * 128)};
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t word = qf[kb][e];  // (a cast of the element itself takes the vector's first)
+                        const u16x2 x = __builtin_bit_cast(u16x2, word);
+                        const u16x2 some = __builtin_elementwise_min(x & (u16x2){0x7fff, 0x7fff}, (u16x2){1, 1});
+                        qf[kb][e] = __builtin_bit_cast(uint32_t, (u16x2)(x + some * add));
+                    }
+            } else {
+                of_diff = a.scale.whole;
+            }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[kb][e] = __float_as_uint(__uint_as_float(qf[kb][e]) * a.scale.whole);
+        }
         uint32_t off = 0;
-        for (int left = at.last - at.first, bad = first.bad, next_bad = second.bad; left > 0; --left) {
-            const Ids ids = pages_of(row + 3 * ROUND);
-            tile(off, row, bad, later);
-            bad = next_bad, next_bad = later.bad;
+        int bad = first.bad, next_bad = next.bad;
+        if (left > 2) next = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+        for (;; --left) {
+            Ids ids;
+            if (left > 3) ids = pages_of(row + 3 * ROUND);
+            tile(off, row, bad, left > 2, next);
+            if (left == 1) break;
+            bad = next_bad, next_bad = next.bad;
             row += ROUND, off ^= T::BYTES;
-            later = places_of(row + 2 * ROUND, ids);
+            if (left > 3) next = places_of(row + 2 * ROUND, ids);
         }
     }
 
     // ------------------------------------------------------------------ the waves' results together
     l = head_sum(l);
     wait_loads();  // nothing more arrives in the tiles, whose place the sums take
+    if (at.last * ROUND > n && block == 0 && wave == 0) {  // the new row; nobody reads its slot in this launch
+        const int id = table[n >> shift];
+        if ((unsigned)id < (unsigned)a.pages.n_pages) {
+            if (lane < CH) {
+                const size_t to = a.pages.row(id, a.Hkv, hk, n) * CH + lane;
+                static_cast<u32x4*>(a.k_pages)[to] = new_k;
+                static_cast<u32x4*>(a.v_pages)[to] = new_v;
+            }
+            if (lane == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(id, a.G, a.G > 1 ? hk : 0, n)] = a.new_pos_b[at.b];
+        }
+    }
     if (quarter == 0) sh_m[wave][c16] = m, sh_l[wave][c16] = l;
 #pragma unroll
     for (int i = 0; i < OB; ++i) {
@@ -497,7 +562,7 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     auto statistics = [&](int h, float top, float sum) {
         if constexpr (EMIT) *reinterpret_cast<float2*>(a.stats + ((size_t)at.b * a.H + head0 + h) * 2) = make_float2(top * of_diff, sum);
     };
-    unsigned long long* part = a.partials + (size_t)at.split * (kHeadBlock * PART);
+    unsigned long long* part = a.partials + (size_t)at.split * PART;
     for (int i = tid; i < heads * (D / 2); i += WAVES * kWave) {
         const int h = i / (D / 2), d = i % (D / 2) * 2;
         float top = sh_m[0][h], sum = 0.f, x = 0.f, y = 0.f;
@@ -513,19 +578,8 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
             write(h, d, x / sum, y / sum);
             if (d == 0) statistics(h, top, sum);
         } else {
-            put(part + h * PART + 1 + d / 2, x, y);
-            if (d == 0) put(part + h * PART, top, sum);
-        }
-    }
-    if (at.last * ROUND > n && block == 0) {  // the new row; nobody reads its slot in this launch
-        const int id = a.pages.page_of(at.b, n);
-        if (id >= 0) {
-            const size_t to = a.pages.row(id, a.Hkv, hk, n) * CH;
-            if (tid < 2 * CH) {
-                const u32x4 x = reinterpret_cast<const u32x4*>(tid < CH ? k_new : v_new)[tid % CH];
-                (static_cast<u32x4*>(tid < CH ? a.k_pages : a.v_pages))[to + tid % CH] = x;
-            }
-            if (tid == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(id, a.G, a.G > 1 ? hk : 0, n)] = a.new_pos_b[at.b];
+            put(part + kHeadBlock + i, x, y);
+            if (d == 0) put(part + h, top, sum);
         }
     }
     if (at.count == 1) return;
@@ -536,19 +590,59 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     if (tid == 0) sh_ticket = atomicInc(a.tickets + at.split0, at.count - 1);  // back at 0 with the last
     __syncthreads();
     if (sh_ticket != (unsigned)at.count - 1) return;
-    const unsigned long long* parts = a.partials + (size_t)at.split0 * (kHeadBlock * PART);
-    for (int i = tid; i < heads * (D / 2); i += WAVES * kWave) {
-        const int h = i / (D / 2), d = i % (D / 2) * 2;
-        float top = kLowest, sum = 0.f, x = 0.f, y = 0.f;
-        for (int s = 0; s < at.count; ++s) top = fmaxf(top, get(parts + (size_t)s * (kHeadBlock * PART) + h * PART).x);
-        for (int s = 0; s < at.count; ++s) {
-            const unsigned long long* from = parts + (size_t)s * (kHeadBlock * PART) + h * PART;
-            const float2 ml = get(from), v = get(from + 1 + d / 2);
-            const float c = exp2f((ml.x - top) * of_diff);
-            sum += ml.y * c, x += v.x * c, y += v.y * c;
+    const unsigned long long* parts = a.partials + (size_t)at.split0 * PART;
+    constexpr int THREADS = WAVES * kWave, AHEAD = 8;  // loads in flight: each comes from beyond the caches
+    float2* weights = reinterpret_cast<float2*>(tiles[0]);  // [segment][head]: (maximum, sum), then the first is the weight
+    static_assert(kMostSegments * kHeadBlock * 8 <= (int)sizeof(tiles), "all segments of a pair");
+    // (segments behind the last one are behind the end of the buffer: nothing is fetched for them)
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)parts, 0, at.count * PART * 8, 0x00020000);
+    for (int i0 = tid; i0 < at.count * kHeadBlock; i0 += THREADS * AHEAD) {
+        u32x2 x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = i0 + u * THREADS, h = i % kHeadBlock;
+            x[u] = __builtin_amdgcn_raw_buffer_load_b64(rsrc, h < heads ? (i / kHeadBlock * PART + h) * 8 : 0x7ffffff0, 0, kDeviceScope);
         }
-        write(h, d, x / sum, y / sum);
-        if (d == 0) statistics(h, top, sum);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (i0 + u * THREADS < at.count * kHeadBlock) weights[i0 + u * THREADS] = make_float2(__uint_as_float(x[u].x), __uint_as_float(x[u].y));
+    }
+    __syncthreads();
+    for (int h = wave; h < heads; h += WAVES) {
+        float top = kLowest, sum = 0.f;
+        for (int s = lane; s < at.count; s += kWave) top = fmaxf(top, weights[s * kHeadBlock + h].x);
+        top = wave_max(top);
+        for (int s = lane; s < at.count; s += kWave) {
+            float2& x = weights[s * kHeadBlock + h];
+            x.x = exp2f((x.x - top) * of_diff);
+            sum += x.x * x.y;
+        }
+        sum = group_sum<kWave>(sum);
+        if (lane == 0) {
+            sh_l[0][h] = sum;
+            statistics(h, top, sum);
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < heads * (D / 4); i += THREADS) {
+        const int h = i / (D / 4);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int s0 = 0; s0 < at.count; s0 += AHEAD) {
+            u32x4 v[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                v[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, ((s0 + u) * PART + kHeadBlock + i * 2) * 8, 0, kDeviceScope);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (s0 + u < at.count) {
+                    const float w = weights[(s0 + u) * kHeadBlock + h].x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = fmaf(__uint_as_float(v[u][e]), w, x[e]);
+                }
+        }
+        const float sum = sh_l[0][h];
+        write(h, i % (D / 4) * 4, x[0] / sum, x[1] / sum);
+        write(h, i % (D / 4) * 4 + 2, x[2] / sum, x[3] / sum);
     }
 }
 
@@ -584,8 +678,7 @@ size_t paged_step_ws(int B, int H, int slots, int D, bool emit)
 template <int DT, int D> static int launch(const PagedStep& a, float* mass_pages, hipStream_t stream)
 {
     constexpr int ROUND = kPagedWaves * PagedTile<DT, D>::TR;
-    const int g = a.H / a.Hkv;
-    const long long pairs = (long long)a.B * a.Hkv * ((g + kHeadBlock - 1) / kHeadBlock), rounds = (a.pages.slots() + ROUND - 1) / ROUND;
+    const long long pairs = (long long)a.B * a.Hkv * a.blocks, rounds = (a.pages.slots() + ROUND - 1) / ROUND;
     const dim3 grid((unsigned)std::min(kPagedSegments + pairs, rounds * pairs));
     if (!mass_pages) {
         hipLaunchKernelGGL((paged_step_kernel<DT, D, false>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
@@ -603,7 +696,7 @@ int paged_step_dispatch(const void* q, const void* k_new, const void* v_new, voi
                         void* out, void* ws, hipStream_t stream)
 {
     char* at = static_cast<char*>(ws);
-    const PagedStep a{q, k_new, v_new, k_pages, v_pages, out, pos_pages, len_b, new_pos_b, pages, B, H, Hkv, G, paged_scale(scale, dt),
+    const PagedStep a{q, k_new, v_new, k_pages, v_pages, out, pos_pages, len_b, new_pos_b, pages, B, H, Hkv, G, H / Hkv, (H / Hkv + kHeadBlock - 1) / kHeadBlock, paged_scale(scale, dt),
                       reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D)),
                       reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D) + up256((size_t)B * H * pages.slots() * 4)),
                       reinterpret_cast<unsigned int*>(at), reinterpret_cast<unsigned long long*>(at + kTicketBytes)};
