@@ -34,6 +34,7 @@ _lib = None
 _fast = None  # the usual calls in native code (csrc/fastcall.cpp); None in an answer of theirs: not a usual call
 _FAST = ("prefill_score", "prefill_score_varlen", "chunk_score", "select_anchors", "merge_compact", "remerge_compact",
          "decode_step", "decode_step_varlen", "decode_score_step", "evict_min")  # in the order of its table
+_FAST_PAGED = ("paged_store", "paged_decode_step", "paged_decode_score_step", "paged_evict_min")  # and of its second one
 
 
 class EcError(RuntimeError):
@@ -120,6 +121,7 @@ def _load_fast(lib):
         if built_for == str(torch.__version__):
             _fastcall.bind(_raw_stream, _device,
                            tuple(ctypes.cast(getattr(lib, "ec_" + n), ctypes.c_void_p).value for n in _FAST))
+            _fastcall.bind_paged(tuple(ctypes.cast(getattr(lib, "ec_" + n), ctypes.c_void_p).value for n in _FAST_PAGED))
             return _fastcall
         why = f"it was built for torch {built_for}"
     warnings.warn(f"the native half of the binding is not used, calls take 4 to 10 us longer: {why}", RuntimeWarning, stacklevel=3)
@@ -582,6 +584,10 @@ def ec_paged_store(k, v, pos, mass, page_table, k_pages, v_pages, pos_pages, mas
                    T: int | None = None, check=True) -> int:
     """k,v [B,Hkv,src_rows,D], pos [B,G,src_rows] int32, mass [B,G,src_rows] f32, each or None -> rows 0..T-1 (n_rows_b of them) to the slots
     from start_b on; k_pages,v_pages [N,Hkv,page,D], pos_pages, mass_pages [N,G,page], page_table int32 [B,max_pages]."""
+    if _fast is not None:
+        rc = _fast.paged_store(k, v, pos, mass, page_table, k_pages, v_pages, pos_pages, mass_pages, start_b, n_rows_b, T)
+        if rc is not None:
+            return _status("ec_paged_store", rc, check)
     B, max_pages = _paged_table(page_table, "ec_paged_store")
     i32, f32 = torch.int32, torch.float32
     if (k is None) != (v is None):
@@ -636,6 +642,10 @@ def _paged_step(fn, q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, pa
 def ec_paged_decode_step(q, k_new, v_new, k_pages, v_pages, pos_pages, page_table, cache_len_b, new_pos_b, scale: float, out, ws,
                          check=True) -> int:
     """q,out [B,H,D]; k_new,v_new [B,Hkv,D]; pools as in ec_paged_store (pos_pages or None); cache_len_b, new_pos_b int32 [B] on the device."""
+    if _fast is not None:
+        rc = _fast.paged_decode_step(q, k_new, v_new, k_pages, v_pages, pos_pages, page_table, cache_len_b, new_pos_b, scale, out, ws)
+        if rc is not None:
+            return _status("ec_paged_decode_step", rc, check)
     return _paged_step("ec_paged_decode_step", q, k_new, v_new, k_pages, v_pages, pos_pages, None, page_table, cache_len_b, new_pos_b, scale, out, ws,
                        check)
 
@@ -643,6 +653,11 @@ def ec_paged_decode_step(q, k_new, v_new, k_pages, v_pages, pos_pages, page_tabl
 def ec_paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale: float, out,
                                ws, check=True) -> int:
     """ec_paged_decode_step that also adds the attention every row receives to mass_pages [N,G,page] f32."""
+    if _fast is not None:
+        rc = _fast.paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale, out,
+                                           ws)
+        if rc is not None:
+            return _status("ec_paged_decode_score_step", rc, check)
     if mass_pages is None:
         raise ValueError("mass_pages is required")
     return _paged_step("ec_paged_decode_score_step", q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b,
@@ -652,6 +667,11 @@ def ec_paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mas
 def ec_paged_evict_min(k_pages, v_pages, pos_pages, mass_pages, page_table, len_b, keep_b, seen_b, max_evict: int, protect_first: int,
                        protect_recent: int, ws, check=True) -> int:
     """Rows of least mass go until keep_b are left of the len_b (no more than max_evict); the holes are filled from behind."""
+    if _fast is not None:
+        rc = _fast.paged_evict_min(k_pages, v_pages, pos_pages, mass_pages, page_table, len_b, keep_b, seen_b, max_evict, protect_first,
+                                   protect_recent, ws)
+        if rc is not None:
+            return _status("ec_paged_evict_min", rc, check)
     B, max_pages = _paged_table(page_table, "ec_paged_evict_min")
     if k_pages.dim() != 4 or mass_pages.dim() != 3:
         raise ValueError("ec_paged_evict_min: k_pages must be [N,Hkv,page,D] and mass_pages [N,G,page]")

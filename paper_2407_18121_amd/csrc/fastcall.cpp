@@ -33,6 +33,16 @@ struct Functions {
                              void*, void*, size_t, void*);
     int (*evict_min)(void*, void*, int32_t*, float*, int, int, int, int, int, int, int, int, int, int32_t*, void*);
 } fn;
+struct PagedFunctions {  // of the calls on paged caches
+    int (*store)(const void*, const void*, const int32_t*, const float*, const int32_t*, const int32_t*, const int32_t*, int, int, int, int, int, int, int,
+                 int, int, int, void*, void*, int32_t*, float*, void*);
+    int (*decode_step)(const void*, const void*, const void*, void*, void*, int32_t*, const int32_t*, const int32_t*, const int32_t*, int, int, int, int,
+                       int, int, int, int, float, int, void*, void*, size_t, void*);
+    int (*decode_score_step)(const void*, const void*, const void*, void*, void*, int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, int,
+                             int, int, int, int, int, int, int, float, int, void*, void*, size_t, void*);
+    int (*evict_min)(void*, void*, int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, const int32_t*, int, int, int, int, int, int, int, int,
+                     int, int, int, void*, size_t, void*);
+} paged;
 PyObject *raw_stream, *current_device;  // of torch: the current stream's handle, the current device's number
 
 struct Unusual {};  // thrown for whatever binding.py has to look at
@@ -315,18 +325,173 @@ PyObject* evict_min(PyObject*, PyObject* const* args, Py_ssize_t n)  // k_cache 
     });
 }
 
+// ------------------------------------------------------------------ paged caches: tensors of the current device only
+struct Here {
+    int device;
+    void* stream;
+    Here()
+    {
+        PyObject* d = PyObject_CallNoArgs(current_device);
+        PyObject* handle = d ? PyObject_CallOneArg(raw_stream, d) : nullptr;
+        device = d ? static_cast<int>(PyLong_AsLong(d)) : -1;
+        stream = handle ? PyLong_AsVoidPtr(handle) : nullptr;
+        const bool failed = !handle || PyErr_Occurred();
+        Py_XDECREF(d), Py_XDECREF(handle);
+        if (failed) throw Unusual{};
+    }
+    void* at(const at::Tensor& t) const
+    {
+        if (!t.is_cuda() || t.device().index() != device || !t.is_contiguous()) throw Unusual{};
+        return t.data_ptr();
+    }
+    template <typename T = void> T* fits(const at::Tensor* t, at::ScalarType type, std::initializer_list<int64_t> shape, bool optional = false) const
+    {
+        if (!t && optional) return nullptr;
+        if (!t || t->scalar_type() != type || !t->sizes().equals(at::IntArrayRef(shape.begin(), shape.size()))) throw Unusual{};
+        return static_cast<T*>(at(*t));
+    }
+    template <typename T = void> T* fits(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> shape, bool optional = false) const
+    {
+        return fits<T>(tensor(o), type, shape, optional);
+    }
+    int32_t* counters(PyObject* o, int64_t n, bool optional = false) const
+    {
+        const at::Tensor* t = tensor(o);
+        if (!t && optional) return nullptr;
+        if (!t || t->scalar_type() != at::kInt || t->numel() != n) throw Unusual{};
+        return static_cast<int32_t*>(at(*t));
+    }
+    Workspace workspace(PyObject* o) const
+    {
+        if (const at::Tensor* t = tensor(o)) at(*t);
+        return Workspace(o);
+    }
+};
+
+// k v pos mass page_table k_pages v_pages pos_pages mass_pages start_b n_rows_b T
+PyObject* paged_store(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject* const* a) {
+        const Here here;
+        const at::Tensor &table = required(a[4], 2), *k = tensor(a[0]), *pos = tensor(a[2]), *mass = tensor(a[3]), *meta = pos ? pos : mass;
+        if ((k && k->dim() != 4) || (meta && meta->dim() != 3) || (!k && (!meta || a[1] != Py_None))) throw Unusual{};
+        const at::Tensor& pool = k ? required(a[5], 4) : required(pos ? a[7] : a[8], 3);
+        const int64_t B = table.size(0), max_pages = table.size(1), rows = k ? k->size(2) : meta->size(2), N = pool.size(0), page = pool.size(2);
+        const int64_t G = meta ? meta->size(1) : 1, Hkv = k ? k->size(1) : G, D = k ? k->size(3) : 64;
+        groups(G, Hkv);
+        const auto dt = k ? k->scalar_type() : at::kFloat;
+        return [=, kp = here.fits(k, dt, {B, Hkv, rows, D}, true), v = here.fits(a[1], dt, {B, Hkv, rows, D}, !k),
+                pp = here.fits<int32_t>(pos, at::kInt, {B, G, rows}, true), mp = here.fits<float>(mass, at::kFloat, {B, G, rows}, true),
+                tp = here.fits<int32_t>(&table, at::kInt, {B, max_pages}), start = here.counters(a[9], B, true), count = here.counters(a[10], B, true),
+                to_k = k ? here.fits(a[5], dt, {N, Hkv, page, D}) : nullptr, to_v = k ? here.fits(a[6], dt, {N, Hkv, page, D}) : nullptr,
+                to_pos = pos ? here.fits<int32_t>(a[7], at::kInt, {N, G, page}) : nullptr,
+                to_mass = mass ? here.fits<float>(a[8], at::kFloat, {N, G, page}) : nullptr, code = k ? type_code(*k) : 0,
+                T = a[11] == Py_None ? size(rows) : integer(a[11]), iB = size(B), iH = size(Hkv), iG = size(G), ir = size(rows), iD = size(D),
+                ip = size(page), iN = size(N), im = size(max_pages), s = here.stream] {
+            return paged.store(kp, v, pp, mp, tp, start, count, iB, iH, iG, T, ir, iD, ip, iN, im, code, to_k, to_v, to_pos, to_mass, s);
+        };
+    });
+}
+
+// The tensors of both attention calls; `rest` is what follows pos_pages and mass_pages: page_table cache_len_b new_pos_b scale out ws
+struct PagedStep {
+    Here here;
+    int B, H, Hkv, G, D, page, N, max_pages, code;
+    void *q, *kn, *vn, *kp, *vp, *out;
+    int32_t *pos, *table, *len, *new_pos;
+    float* mass;
+    float scale;
+    Workspace ws;
+    PagedStep(PyObject* const* a, PyObject* mass_, PyObject* const* rest) : ws(here.workspace(rest[5]))
+    {
+        const at::Tensor &table_ = required(rest[0], 2), &q_ = required(a[0], 3), &k = required(a[3], 4);
+        const int64_t b = table_.size(0), h = q_.size(1), n = k.size(0), hkv = k.size(1), p = k.size(2), d = k.size(3);
+        PyObject* grouped = mass_ ? mass_ : a[5];
+        const int64_t g = groups(grouped != Py_None ? required(grouped, 3).size(1) : 1, hkv);
+        const auto dt = k.scalar_type();
+        q = here.fits(&q_, dt, {b, h, d}), kn = here.fits(a[1], dt, {b, hkv, d}), vn = here.fits(a[2], dt, {b, hkv, d});
+        kp = here.fits(&k, dt, {n, hkv, p, d}), vp = here.fits(a[4], dt, {n, hkv, p, d});
+        pos = here.fits<int32_t>(a[5], at::kInt, {n, g, p}, true);
+        mass = mass_ ? here.fits<float>(mass_, at::kFloat, {n, g, p}) : nullptr;
+        table = here.fits<int32_t>(&table_, at::kInt, {b, table_.size(1)});
+        len = here.counters(rest[1], b), new_pos = here.counters(rest[2], b, !pos);
+        scale = number(rest[3]);
+        out = here.fits(rest[4], dt, {b, h, d});
+        code = type_code(k);
+        B = size(b), H = size(h), Hkv = size(hkv), G = size(g), D = size(d), page = size(p), N = size(n), max_pages = size(table_.size(1));
+    }
+};
+
+// q k_new v_new k_pages v_pages pos_pages page_table cache_len_b new_pos_b scale out ws
+PyObject* paged_decode_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject* const* a) {
+        return [t = PagedStep(a, nullptr, a + 6)] {
+            return paged.decode_step(t.q, t.kn, t.vn, t.kp, t.vp, t.pos, t.table, t.len, t.new_pos, t.B, t.H, t.Hkv, t.G, t.D, t.page, t.N, t.max_pages,
+                                     t.scale, t.code, t.out, t.ws.p, t.ws.bytes, t.here.stream);
+        };
+    });
+}
+
+// q k_new v_new k_pages v_pages pos_pages mass_pages page_table cache_len_b new_pos_b scale out ws
+PyObject* paged_decode_score_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<13>(args, n, [](PyObject* const* a) {
+        return [t = PagedStep(a, a[6], a + 7)] {
+            return paged.decode_score_step(t.q, t.kn, t.vn, t.kp, t.vp, t.pos, t.mass, t.table, t.len, t.new_pos, t.B, t.H, t.Hkv, t.G, t.D, t.page, t.N,
+                                           t.max_pages, t.scale, t.code, t.out, t.ws.p, t.ws.bytes, t.here.stream);
+        };
+    });
+}
+
+// k_pages v_pages pos_pages mass_pages page_table len_b keep_b seen_b max_evict protect_first protect_recent ws
+PyObject* paged_evict_min(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<12>(args, n, [](PyObject* const* a) {
+        const Here here;
+        const at::Tensor &k = required(a[0], 4), &mass = required(a[3], 3), &table = required(a[4], 2);
+        const int64_t N = k.size(0), Hkv = k.size(1), page = k.size(2), D = k.size(3), G = groups(mass.size(1), Hkv), B = table.size(0);
+        const int64_t max_pages = table.size(1);
+        const auto dt = k.scalar_type();
+        return [=, ws = here.workspace(a[11]), kp = here.fits(&k, dt, {N, Hkv, page, D}), v = here.fits(a[1], dt, {N, Hkv, page, D}),
+                pos = here.fits<int32_t>(a[2], at::kInt, {N, G, page}, true), mp = here.fits<float>(&mass, at::kFloat, {N, G, page}),
+                tp = here.fits<int32_t>(&table, at::kInt, {B, max_pages}), len = here.counters(a[5], B), keep = here.counters(a[6], B),
+                seen = here.counters(a[7], B, true), most = integer(a[8]), first = integer(a[9]), recent = integer(a[10]), code = type_code(k),
+                iB = size(B), iH = size(Hkv), iG = size(G), iD = size(D), ip = size(page), iN = size(N), im = size(max_pages), s = here.stream] {
+            return paged.evict_min(kp, v, pos, mp, tp, len, keep, seen, iB, iH, iG, iD, ip, iN, im, most, first, recent, code, ws.p, ws.bytes, s);
+        };
+    });
+}
+
+template <typename F> bool take_addresses(PyObject* addresses, F& to)
+{
+    constexpr Py_ssize_t kCount = sizeof(F) / sizeof(void*);
+    if (PyTuple_GET_SIZE(addresses) != kCount) return PyErr_Format(PyExc_ValueError, "%zd addresses expected", kCount), false;
+    void* at[kCount];
+    for (Py_ssize_t i = 0; i < kCount; ++i)
+        if (!(at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i)))) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no address");
+            return false;
+        }
+    static_assert(sizeof(F) == sizeof(at), "function pointers only");
+    memcpy(static_cast<void*>(&to), at, sizeof(at));
+    return true;
+}
+
+// bind_paged(addresses in the order of PagedFunctions), after bind
+PyObject* bind_paged(PyObject*, PyObject* args)
+{
+    PyObject* addresses;
+    if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses) || !take_addresses(addresses, paged)) return nullptr;
+    Py_RETURN_NONE;
+}
+
 // bind(raw_stream, current_device, addresses in the order of Functions)
 PyObject* bind(PyObject*, PyObject* args)
 {
     PyObject *stream_, *device_, *addresses;
     if (!PyArg_ParseTuple(args, "OOO!", &stream_, &device_, &PyTuple_Type, &addresses)) return nullptr;
-    constexpr Py_ssize_t kCount = sizeof(Functions) / sizeof(void*);
-    if (PyTuple_GET_SIZE(addresses) != kCount) return PyErr_Format(PyExc_ValueError, "%zd addresses expected", kCount);
-    void* at[kCount];
-    for (Py_ssize_t i = 0; i < kCount; ++i)
-        if (!(at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i)))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "no address");
-    static_assert(sizeof(Functions) == sizeof(at), "function pointers only");
-    memcpy(static_cast<void*>(&fn), at, sizeof(at));
+    if (!take_addresses(addresses, fn)) return nullptr;
     Py_INCREF(stream_), Py_INCREF(device_);
     raw_stream = stream_, current_device = device_;
     Py_RETURN_NONE;
@@ -335,7 +500,9 @@ PyObject* bind(PyObject*, PyObject* args)
 #define EC_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {EC_FAST(prefill_score),   EC_FAST(prefill_score_varlen), EC_FAST(chunk_score),       EC_FAST(select_anchors),
                          EC_FAST(merge_compact),   EC_FAST(remerge_compact),      EC_FAST(decode_step),       EC_FAST(decode_step_varlen),
-                         EC_FAST(decode_score_step), EC_FAST(evict_min),          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         EC_FAST(decode_score_step), EC_FAST(evict_min),          EC_FAST(paged_store),       EC_FAST(paged_decode_step),
+                         EC_FAST(paged_decode_score_step), EC_FAST(paged_evict_min), {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_paged", bind_paged, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
