@@ -387,7 +387,7 @@ int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B,
  *   page_table       DEVICE [B,max_pages] int32           mass_pages  DEVICE [n_pages,G,page] float, accumulated attention
  * and slot s of sequence b (0 <= s < max_pages * page) is row s % page of page page_table[b][s / page].  A cache is a SET of
  * rows in slots 0 .. len-1: attention does not see their order, positions go with them.  Common to the calls:
- *  - page is a power of two from 8 to 256, max_pages * page at most 2^28.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
+ *  - page is a power of two from 8 to 256, max_pages * page at most 2^28, n_pages * page below 2^32.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
  *    h reads key/value head h / (H / Hkv).
  *  - Everything that changes from token to token is read on the device, so the calls can be captured and replayed.
  *  - A table entry outside 0 .. n_pages-1 names no page (entries behind a sequence's last page are not read at all): rows there are
@@ -436,7 +436,7 @@ int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, vo
  * ec_decode_score_step):
  *     mass_j += p_j for rows j < L,   mass_L = p_L
  * where p is the mean of the step's softmax rows over all query heads (G == 1) or over the query heads of the key/value head
- * (G == Hkv), added in ascending head order.
+ * (G == Hkv), added in a fixed order.
  *   mass_pages     updated
  *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_SCORE_STEP, B,H, max_pages * page, D,dt)
  */

@@ -442,6 +442,7 @@ int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int pag
     if (!page_table || B < 1 || Hkv < 1 || D < 1 || page < 1 || n_pages < 1 || max_pages < 1) return EC_EINVAL;
     if (G != 1 && G != Hkv) return EC_EINVAL;
     if ((page & (page - 1)) || page < 8 || page > 256 || (long long)max_pages * page > 1 << 28) return EC_EUNSUPPORTED;
+    if ((long long)n_pages * page >= 1LL << 32) return EC_EUNSUPPORTED;
     if ((long long)B * Hkv > 65535) return EC_EUNSUPPORTED;
     if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
     pages = {page_table, n_pages, max_pages, __builtin_ctz((unsigned)page)};
@@ -509,7 +510,7 @@ int ec_paged_evict_min(void* k_pages, void* v_pages, int32_t* pos_pages, float* 
     ec::Pages pages;
     if (const int rc = paged_shape(page_table, B, Hkv, G, D, page, n_pages, max_pages, dt, pages)) return rc;
     if (max_evict > pages.slots()) return EC_EINVAL;
-    if (!aligned16({k_pages, v_pages})) return EC_EUNSUPPORTED;
+    if (!aligned16({k_pages, v_pages, pos_pages, mass_pages})) return EC_EUNSUPPORTED;
     if (!ws || ws_bytes < ec_workspace_bytes(EC_FN_PAGED_EVICT_MIN, B, G, max_evict, D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
     return ec::paged_evict_dispatch(k_pages, v_pages, pos_pages, mass_pages, pages, len_b, keep_b, seen_b, B, Hkv, G, row_bytes(D, dt), max_evict,
                                     protect_first, protect_recent, ws, reinterpret_cast<hipStream_t>(stream));

@@ -78,111 +78,270 @@ __device__ __forceinline__ uint32_t evict_key(float mass, bool kept)
 }
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+constexpr int kRun = 8;  // consecutive slots that a thread looks at: one page, one table entry, two 16-byte loads each of masses and positions
 
-// Sum over the threads before this one (in lane order), and the sum over all of them in `total`.
-__device__ __forceinline__ uint32_t scan_block(uint32_t x, uint32_t* sh, uint32_t& total)
+// What an eviction looks at in one (sequence, score group).
+struct EvictRows {
+    const int32_t* pos_pages;
+    const float* mass_pages;
+    const Pages& pages;
+    int b, G, g, n, first;
+    int64_t recent;
+    __device__ __forceinline__ EvictRows(const int32_t* pos, const float* mass, const Pages& p, const EvictGoal& goal, int G_, int bg)
+        : pos_pages(pos), mass_pages(mass), pages(p), b(bg / G_), G(G_), g(bg % G_), n(goal.length(b, p.slots())), first(goal.protect_first),
+          recent(goal.protect_recent ? (int64_t)goal.seen_b[b] - goal.protect_recent : INT64_MAX)
+    {
+    }
+    // Keys of slots j .. j + 7 (j a multiple of 8); those from n on get the largest there is, like protected ones. Returns the run's page or -1.
+    __device__ __forceinline__ int keys(int j, uint32_t (&key)[kRun]) const
+    {
+        const int id = j < n ? pages.page_of(b, j) : -1;
+        const size_t at = pages.row(max(id, 0), G, g, j);
+        u32x4 m[2], p[2] = {};
+        m[0] = reinterpret_cast<const u32x4*>(mass_pages + at)[0], m[1] = reinterpret_cast<const u32x4*>(mass_pages + at)[1];
+        if (pos_pages) p[0] = reinterpret_cast<const u32x4*>(pos_pages + at)[0], p[1] = reinterpret_cast<const u32x4*>(pos_pages + at)[1];
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const int where = (int)p[i / 4][i % 4];
+            key[i] = evict_key(__uint_as_float(m[i / 4][i % 4]), id < 0 || j + i >= n || (pos_pages && (where < first || where >= recent)));
+        }
+        return id;
+    }
+};
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x_)
+{
+    int x = (int)x_;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next one (rows 1, 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
+    return (uint32_t)x;
+}
+
+// Sum over the threads before this one, and the sum over all of them in `total`. `sh`: a place of its own for every call between two barriers.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sh, uint32_t& total)
 {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    uint32_t in = x;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const uint32_t y = __shfl_up(in, off, kWave);
-        if (lane >= off) in += y;
-    }
-    __syncthreads();
+    const uint32_t in = wave_scan(x);
     if (lane == kWave - 1) sh[wave] = in;
     __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kEvictWaves; ++w) {
-        if (w < wave) before += sh[w];
-        total += sh[w];
-    }
-    return before + in - x;
+    const uint32_t sums = wave_scan(lane < kEvictWaves ? sh[lane] : 0);
+    total = __builtin_amdgcn_readlane(sums, kEvictWaves - 1);
+    const uint32_t before = __builtin_amdgcn_readlane(sums, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
+    return (wave ? before : 0) + in - x;
 }
 
-// One workgroup per (sequence, score group): which rows go, the list of moves, and the moves of positions and masses.
-__global__ __launch_bounds__(kEvictThreads) void paged_evict_select_kernel(int32_t* pos_pages, float* mass_pages, Pages pages, EvictGoal goal, int G,
-                                                                           int32_t* __restrict__ counts, int2* __restrict__ moves)
+// One workgroup per (sequence, score group): which rows go, and the list of moves. A thread holds runs of 8 consecutive slots. The gone-th smallest
+// key is found digit by digit, 8 bits at a time from the highest bit in which two keys differ (masses share their upper bits, and a
+// histogram of those is one counter that all lanes wait for). HELD: keys stay in registers, for sequences of up to 8192 rows; longer ones are read
+// again for every digit.
+template <bool HELD> __device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list)
 {
-    __shared__ uint32_t hist[256], sh[kEvictWaves], sh_prefix, sh_need;
-    const int b = blockIdx.x / G, g = blockIdx.x % G, tid = threadIdx.x;
-    const int n = goal.length(b, pages.slots()), gone = goal.victims(b, n), m = n - gone;
+    __shared__ __align__(16) uint32_t hist[4][256];
+    __shared__ uint32_t sh[3][kEvictWaves], sh_lo[kEvictWaves], sh_hi[kEvictWaves];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = rows.n, m = n - gone;
+    const int runs = (n + kRun - 1) / kRun;
+    uint32_t held[kRun];
+    int held_page = -1;
+    if constexpr (HELD) held_page = rows.keys(tid * kRun, held);
+    // f(first slot, keys, page) for every run of this thread
+    auto each_run = [&](auto&& f) __attribute__((always_inline)) {
+        if constexpr (HELD) {
+            f(tid * kRun, held, held_page);
+        } else {
+            for (int r0 = 0; r0 < runs; r0 += kEvictThreads) {  // all threads in every round
+                uint32_t key[kRun];
+                const int page = rows.keys((r0 + tid) * kRun, key);
+                f((r0 + tid) * kRun, key, page);
+            }
+        }
+    };
+    hist[tid / 256][tid % 256] = 0;
+    // how many rows are not protected, and the bits in which their keys differ
+    uint32_t lo = 0xffffffffu, hi = 0, free_rows = 0;
+    each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const bool open = key[i] != 0xffffffffu;
+            lo = min(lo, key[i]), hi = max(hi, open ? key[i] : 0u), free_rows += open;
+        }
+    });
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, off, kWave)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, off, kWave));
+    if (lane == 0) sh_lo[wave] = lo, sh_hi[wave] = hi;
+    uint32_t all_free;
+    block_scan(free_rows, sh[0], all_free);
+#pragma unroll
+    for (int w = 0; w < kEvictWaves; ++w) lo = min(lo, sh_lo[w]), hi = max(hi, sh_hi[w]);
+
+    // victims: keys below `last`, and the first `need` rows whose key is `last` (its bits from `shift` on)
+    uint32_t last, need = gone;
+    int shift = 0;
+    if ((uint32_t)gone >= all_free) {
+        last = 0xffffffffu, need = gone - all_free;  // all that are not protected, and protected ones by their slots
+    } else {
+        last = lo;
+        if (lo != hi) {
+            shift = 32 - __clz(lo ^ hi);
+            last = shift == 32 ? 0 : hi >> shift << shift;
+            for (int pass = 0; shift > 0; ++pass) {
+                const int bits = min(shift, 8), down = shift - bits;
+                each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < kRun; ++i)
+                        if (key[i] != 0xffffffffu && ((uint64_t)(key[i] ^ last) >> shift) == 0) atomicAdd(&hist[pass][key[i] >> down & ((1u << bits) - 1)], 1u);
+                });
+                __syncthreads();
+                // every wave finds the digit for itself: four counters a lane
+                const uint4 c = reinterpret_cast<const uint4*>(hist[pass])[lane];
+                const uint32_t upto = wave_scan(c.x + c.y + c.z + c.w);
+                const unsigned long long reached = __ballot(upto >= need);
+                const int at = reached ? __ffsll(reached) - 1 : kWave - 1;  // (always, unless masses change while they are read)
+                const uint32_t x = __builtin_amdgcn_readlane(c.x, at), y = __builtin_amdgcn_readlane(c.y, at), z = __builtin_amdgcn_readlane(c.z, at),
+                               w = __builtin_amdgcn_readlane(c.w, at);
+                need -= __builtin_amdgcn_readlane(upto, at) - (x + y + z + w);
+                uint32_t digit = at * 4, count = x;
+                if (need > count) need -= count, ++digit, count = y;
+                if (need > count && digit % 4 == 1) need -= count, ++digit, count = z;
+                if (need > count && digit % 4 == 2) need -= count, ++digit, count = w;
+                last |= digit << down, shift = down;
+                if (need == count) break;  // all rows with these digits go
+            }
+        }
+    }
+
+    // (a protected row's key can share the upper bits of a NaN's)
+    auto ties_with = [&](uint32_t key) { return ((uint64_t)(key ^ last) >> shift) == 0 && (shift == 0 || key != 0xffffffffu); };
+    uint32_t ties = 0, holes = 0, movers = 0;
+    each_run([&](int j, uint32_t (&key)[kRun], int page) __attribute__((always_inline)) {
+        uint32_t mine = 0, total;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) mine += j + i < n && ties_with(key[i]);
+        uint32_t rank = ties + block_scan(mine, sh[1], total);
+        ties += total;
+        uint32_t flags = 0, both = 0;  // bit i: a hole; bit 8 + i: a mover
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const bool there = j + i < n, tie = there && ties_with(key[i]);
+            const bool victim = there && (tie ? rank < need : key[i] < last);
+            rank += tie;
+            const bool hole = victim && j + i < m, mover = there && !victim && j + i >= m;
+            flags |= (uint32_t)hole << i | (uint32_t)mover << (8 + i);
+            both += (uint32_t)hole | (uint32_t)mover << 16;
+        }
+        uint32_t at = block_scan(both, sh[2], total);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const uint32_t row = page < 0 ? 0xffffffffu : ((uint32_t)page << rows.pages.shift) + ((j + i) & (rows.pages.page() - 1));
+            if (flags >> i & 1) list[holes + (at & 0xffff)].x = row;
+            if (flags >> (8 + i) & 1) list[movers + (at >> 16)].y = row;
+            at += (flags >> i & 1) | (flags >> (8 + i) & 1) << 16;
+        }
+        holes += total & 0xffff, movers += total >> 16;
+        if constexpr (!HELD) __syncthreads();  // sh is written again
+    });
+    if (tid == 0) *counts = min(holes, movers);  // equal, unless masses change while they are read
+}
+
+__global__ __launch_bounds__(kEvictThreads) void paged_evict_select_kernel(const int32_t* __restrict__ pos_pages, const float* __restrict__ mass_pages,
+                                                                           Pages pages, EvictGoal goal, int G, int32_t* __restrict__ counts,
+                                                                           uint2* __restrict__ moves)
+{
+    const EvictRows rows(pos_pages, mass_pages, pages, goal, G, blockIdx.x);
+    const int gone = goal.victims(rows.b, rows.n);
     if (gone == 0) {
-        if (tid == 0) counts[blockIdx.x] = 0;
+        if (threadIdx.x == 0) counts[blockIdx.x] = 0;
         return;
     }
-    const int64_t recent = goal.protect_recent ? (int64_t)goal.seen_b[b] - goal.protect_recent : INT64_MAX;
-    auto key_of = [&](int j) {
-        const int id = pages.page_of(b, j);
-        if (id < 0) return 0xffffffffu;
-        const size_t at = pages.row(id, G, g, j);
-        const int p = pos_pages ? pos_pages[at] : 0;
-        return evict_key(mass_pages[at], pos_pages && (p < goal.protect_first || p >= recent));
-    };
-    // the gone-th smallest key, digit by digit
-    uint32_t prefix = 0, need = gone;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += kEvictThreads) {
-            const uint32_t k = key_of(j);
-            if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1u);
+    uint2* list = moves + (size_t)blockIdx.x * goal.max_evict;
+    if (rows.n <= kEvictThreads * kRun) select_victims<true>(rows, gone, counts + blockIdx.x, list);
+    else select_victims<false>(rows, gone, counts + blockIdx.x, list);
+}
+
+// A row number of the list (page and row in it) in a pool of `heads` heads.
+__device__ __forceinline__ size_t pool_row(uint32_t row, const Pages& pages, int heads, int head)
+{
+    return pages.row(row >> pages.shift, heads, head, row);
+}
+
+// Moves: a workgroup takes 4 * 256 / CH rows of K or of V of a head at a time, all their loads in flight; K's of the group's first head take positions
+// and masses along.
+template <int CH>
+__global__ __launch_bounds__(256) void paged_evict_move_kernel(u32x4* k_pages, u32x4* v_pages, int32_t* pos_pages, float* mass_pages, Pages pages,
+                                                               int Hkv, int G, int max_evict, const int32_t* __restrict__ counts,
+                                                               const uint2* __restrict__ moves)
+{
+    constexpr int ROWS = 256 / CH, AHEAD = 4;
+    const int b = blockIdx.z, head = blockIdx.y >> 1, g = G > 1 ? head : 0, count = counts[b * G + g];
+    u32x4* rows = blockIdx.y & 1 ? v_pages : k_pages;
+    const uint2* list = moves + (size_t)(b * G + g) * max_evict;
+    const int sub = threadIdx.x % CH;
+    for (int i0 = blockIdx.x * (ROWS * AHEAD); i0 < count; i0 += gridDim.x * (ROWS * AHEAD)) {
+        uint2 move[AHEAD];
+        u32x4 x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = i0 + u * ROWS + threadIdx.x / CH;
+            move[u] = i < count ? list[i] : make_uint2(~0u, ~0u);
         }
-        __syncthreads();
-        if (tid == 0) {
-            uint32_t d = 0;
-            while (d < 255 && hist[d] < need) need -= hist[d++];
-            sh_prefix = prefix | d << shift, sh_need = need;
-        }
-        __syncthreads();
-        prefix = sh_prefix, need = sh_need;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (move[u].x != ~0u && move[u].y != ~0u) x[u] = __builtin_nontemporal_load(rows + pool_row(move[u].y, pages, Hkv, head) * CH + sub);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (move[u].x != ~0u && move[u].y != ~0u) rows[pool_row(move[u].x, pages, Hkv, head) * CH + sub] = x[u];
     }
-    // victims are the rows below that key and the first `need` rows that have it
-    int2* list = moves + (size_t)blockIdx.x * goal.max_evict;
-    uint32_t ties = 0, holes = 0, movers = 0;
-    for (int j0 = 0; j0 < n; j0 += kEvictThreads) {
-        const int j = j0 + tid;
-        const uint32_t k = j < n ? key_of(j) : 0xffffffffu;
-        const bool tie = j < n && k == prefix;
-        uint32_t total;
-        const uint32_t rank = ties + scan_block(tie, sh, total);
-        ties += total;
-        const bool victim = j < n && (k < prefix || (tie && rank < need));
-        const bool hole = victim && j < m, mover = j < n && !victim && j >= m;
-        const uint32_t at = scan_block((uint32_t)hole | (uint32_t)mover << 16, sh, total);
-        if (hole) list[holes + (at & 0xffff)].x = j;
-        if (mover) list[movers + (at >> 16)].y = j;
-        holes += total & 0xffff, movers += total >> 16;
-    }
-    __threadfence_block();
-    __syncthreads();
-    holes = min(holes, movers);  // equal, unless masses change while they are read
-    if (tid == 0) counts[blockIdx.x] = holes;
-    for (int i = tid; i < (int)holes; i += kEvictThreads) {
-        const int2 move = list[i];
-        const int to = pages.page_of(b, move.x), from = pages.page_of(b, move.y);
-        if (to < 0 || from < 0) continue;
-        const size_t t = pages.row(to, G, g, move.x), f = pages.row(from, G, g, move.y);
-        mass_pages[t] = mass_pages[f];
-        if (pos_pages) pos_pages[t] = pos_pages[f];
+    if ((blockIdx.y & 1) || (G == 1 && head)) return;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
+        const uint2 move = list[i];
+        if (move.x == ~0u || move.y == ~0u) continue;
+        const size_t to = pool_row(move.x, pages, G, g), from = pool_row(move.y, pages, G, g);
+        mass_pages[to] = mass_pages[from];
+        if (pos_pages) pos_pages[to] = pos_pages[from];
     }
 }
 
+// One row of every sequence, the step of a generation loop, in one launch: the workgroup that finds the least row fills its place.
 template <int CH>
-__global__ __launch_bounds__(256) void paged_evict_move_kernel(u32x4* k_pages, u32x4* v_pages, Pages pages, int Hkv, int G, int max_evict,
-                                                               const int32_t* __restrict__ counts, const int2* __restrict__ moves)
+__global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k_pages, u32x4* v_pages, int32_t* pos_pages, float* mass_pages, Pages pages,
+                                                                        EvictGoal goal, int Hkv, int G)
 {
-    constexpr int ROWS = 256 / CH;
-    const int b = blockIdx.z, head = blockIdx.y >> 1, bg = b * G + (G > 1 ? head : 0), count = counts[bg];
-    u32x4* rows = blockIdx.y & 1 ? v_pages : k_pages;
-    const int2* list = moves + (size_t)bg * max_evict;
-    for (int i = blockIdx.x * ROWS + threadIdx.x / CH; i < count; i += gridDim.x * ROWS) {
-        const int2 move = list[i];
-        const int to = pages.page_of(b, move.x), from = pages.page_of(b, move.y);
-        if (to < 0 || from < 0) continue;
-        rows[pages.row(to, Hkv, head, move.x) * CH + threadIdx.x % CH] = rows[pages.row(from, Hkv, head, move.y) * CH + threadIdx.x % CH];
+    __shared__ unsigned long long sh_best[kEvictWaves];
+    const EvictRows rows(pos_pages, mass_pages, pages, goal, G, blockIdx.x);
+    const int n = rows.n, b = rows.b, tid = threadIdx.x;
+    if (goal.victims(b, n) == 0) return;
+    const int from = pages.page_of(b, n - 1);
+    unsigned long long best = ~0ull;  // (key, slot)
+    for (int j = tid * kRun; j < n; j += kEvictThreads * kRun) {
+        uint32_t key[kRun];
+        rows.keys(j, key);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+            if (j + i < n) best = min(best, (unsigned long long)key[i] << 32 | (uint32_t)(j + i));
+    }
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
+    if (tid % kWave == 0) sh_best[tid / kWave] = best;
+    __syncthreads();
+    best = sh_best[tid % kEvictWaves];
+#pragma unroll
+    for (int off = 1; off < kEvictWaves; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
+    const int hole = (int)(uint32_t)best, to = pages.page_of(b, hole);
+    if (hole == n - 1 || to < 0 || from < 0) return;
+    const int heads = G > 1 ? 1 : Hkv, head0 = G > 1 ? rows.g : 0;
+    for (int i = tid; i < heads * 2 * CH; i += kEvictThreads) {
+        const int head = head0 + i / (2 * CH), c = i % CH;
+        u32x4* pool = i / CH & 1 ? v_pages : k_pages;
+        pool[pages.row(to, Hkv, head, hole) * CH + c] = pool[pages.row(from, Hkv, head, n - 1) * CH + c];
+    }
+    if (tid == 0) {
+        const size_t t = pages.row(to, G, rows.g, hole), f = pages.row(from, G, rows.g, n - 1);
+        mass_pages[t] = mass_pages[f];
+        if (pos_pages) pos_pages[t] = pos_pages[f];
     }
 }
 
@@ -196,15 +355,26 @@ int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float
                          int protect_recent, void* ws, hipStream_t stream)
 {
     int32_t* counts = static_cast<int32_t*>(ws);
-    int2* moves = reinterpret_cast<int2*>(static_cast<char*>(ws) + (((size_t)B * G * 4 + 255) & ~(size_t)255));
+    uint2* moves = reinterpret_cast<uint2*>(static_cast<char*>(ws) + (((size_t)B * G * 4 + 255) & ~(size_t)255));
     const EvictGoal goal{len_b, keep_b, seen_b, max_evict, protect_first, protect_recent};
+    u32x4 *k = static_cast<u32x4*>(k_pages), *v = static_cast<u32x4*>(v_pages);
+    if (max_evict == 1) {
+#define EC_ONE(CH_)                  \
+    if (row_bytes == CH_ * 16)       \
+        hipLaunchKernelGGL(paged_evict_one_kernel<CH_>, dim3(B * G), dim3(kEvictThreads), 0, stream, k, v, pos_pages, mass_pages, pages, goal, Hkv, G)
+        EC_ONE(8);
+        EC_ONE(16);
+        EC_ONE(32);
+#undef EC_ONE
+        return status_from_hip(hipGetLastError());
+    }
     hipLaunchKernelGGL(paged_evict_select_kernel, dim3(B * G), dim3(kEvictThreads), 0, stream, pos_pages, mass_pages, pages, goal, G, counts, moves);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
-    const int most = std::max(1, 4096 / (2 * Hkv * B));
-#define EC_MOVE(CH_)                                                                                                                          \
-    if (row_bytes == CH_ * 16)                                                                                                                \
-        hipLaunchKernelGGL(paged_evict_move_kernel<CH_>, dim3(std::min((max_evict + 256 / CH_ - 1) / (256 / CH_), most), 2 * Hkv, B), dim3(256), 0, \
-                           stream, (u32x4*)k_pages, (u32x4*)v_pages, pages, Hkv, G, max_evict, counts, moves)
+    const int most = std::max(1, 4096 / (2 * Hkv * B));  // the lists' lengths are on the device: workgroups go over them
+#define EC_MOVE(CH_)                                                                                                                             \
+    if (row_bytes == CH_ * 16)                                                                                                                   \
+        hipLaunchKernelGGL(paged_evict_move_kernel<CH_>, dim3(std::min((max_evict * CH_ + 1023) / 1024, most), 2 * Hkv, B), dim3(256), 0, stream, k, v, \
+                           pos_pages, mass_pages, pages, Hkv, G, max_evict, counts, moves)
     EC_MOVE(8);
     EC_MOVE(16);
     EC_MOVE(32);

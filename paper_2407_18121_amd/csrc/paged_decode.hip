@@ -646,23 +646,47 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     }
 }
 
-// mass of every row += the mean of its group's probabilities; a thread a row, heads in ascending order.
-__global__ __launch_bounds__(256) void paged_mass_kernel(const float* __restrict__ raw, const float* __restrict__ stats, float* mass_pages,
-                                                         const int32_t* __restrict__ len_b, Pages pages, int H, int G)
+// mass of every row += the mean of its group's probabilities. A workgroup takes 64 rows at a time, a lane each; its four waves share the group's
+// heads (eight reads of each in flight) and add up in LDS, in an order of their own: the same bits every time. Bound by latency up to some
+// thousand rows, by the scores' bytes beyond.
+constexpr int kMassRows = kWave, kMassWaves = 4, kMassAhead = 8;
+__global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const float* __restrict__ raw, const float* __restrict__ stats, float* mass_pages,
+                                                                          const int32_t* __restrict__ len_b, Pages pages, int H, int G)
 {
-    const int b = blockIdx.y / G, g = blockIdx.y % G, n = len_b[b];
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (n < 0 || n >= pages.slots() || j > n) return;
-    const int id = pages.page_of(b, j);
-    if (id < 0) return;
-    const int heads = H / G;
-    float sum = 0.f;
-    for (int h = g * heads; h < (g + 1) * heads; ++h) {
-        const size_t bh = (size_t)b * H + h;
-        sum += exp2f(raw[bh * pages.slots() + j] - stats[bh * 2]) / stats[bh * 2 + 1];
+    __shared__ float part[kMassWaves][kMassRows];
+    const int b = blockIdx.y / G, g = blockIdx.y % G, n = len_b[b], slots = pages.slots();
+    if (n < 0 || n >= slots) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int heads = H / G, per = (heads + kMassWaves - 1) / kMassWaves, h0 = wave * per, h1 = min(h0 + per, heads);
+    const size_t first = (size_t)b * H + g * heads;
+    for (int j0 = blockIdx.x * kMassRows; j0 <= n; j0 += gridDim.x * kMassRows) {
+        const int j = j0 + lane;
+        float sum = 0.f;
+        for (int h = h0; h < h1; h += kMassAhead) {
+            float x[kMassAhead];
+#pragma unroll
+            for (int u = 0; u < kMassAhead; ++u) x[u] = h + u < h1 && j <= n ? raw[(first + h + u) * slots + j] : 0.f;
+#pragma unroll
+            for (int u = 0; u < kMassAhead; ++u)
+                if (h + u < h1) {
+                    const float2 of = reinterpret_cast<const float2*>(stats)[first + h + u];
+                    sum += exp2f(x[u] - of.x) / of.y;
+                }
+        }
+        part[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && j <= n) {
+            const int id = pages.page_of(b, j);
+            if (id >= 0) {
+                float all = part[0][lane];
+#pragma unroll
+                for (int w = 1; w < kMassWaves; ++w) all += part[w][lane];
+                float* m = mass_pages + pages.row(id, G, g, j);
+                *m = (j == n ? 0.f : *m) + all / (float)heads;
+            }
+        }
+        __syncthreads();
     }
-    float* m = mass_pages + pages.row(id, G, g, j);
-    *m = (j == n ? 0.f : *m) + sum / (float)heads;
 }
 
 // Workspace: tickets, partial results of cut pairs (a pair of r rounds is cut into less than 2 r / most segments, so there are less than twice
@@ -686,8 +710,9 @@ template <int DT, int D> static int launch(const PagedStep& a, float* mass_pages
     }
     hipLaunchKernelGGL((paged_step_kernel<DT, D, true>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
-    hipLaunchKernelGGL(paged_mass_kernel, dim3((a.pages.slots() + 255) / 256, a.B * a.G), dim3(256), 0, stream, a.raw, a.stats, mass_pages, a.len_b,
-                       a.pages, a.H, a.G);
+    const int groups = a.B * a.G, most = std::max(1, 4096 / groups);  // the lengths are on the device: workgroups go over the rows
+    hipLaunchKernelGGL(paged_mass_kernel, dim3(std::min((a.pages.slots() + kMassRows - 1) / kMassRows, most), groups), dim3(kMassRows * kMassWaves), 0, stream,
+                       a.raw, a.stats, mass_pages, a.len_b, a.pages, a.H, a.G);
     return status_from_hip(hipGetLastError());
 }
 

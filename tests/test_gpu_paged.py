@@ -310,7 +310,7 @@ EVICTS = [  # dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent
 
 
 @pytest.mark.parametrize("case", range(len(EVICTS)))
-@pytest.mark.parametrize("masses", ["any", "ties", "ends", "same"])
+@pytest.mark.parametrize("masses", ["any", "ties", "ends", "same", "nan", "close"])
 def test_evict(case, masses):
     dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent = EVICTS[case]
     rng = np.random.default_rng(50 + case)
@@ -327,6 +327,10 @@ def test_evict(case, masses):
         pool.mass = rng.choice(np.float32([0.0, -0.0, 1e-45, -1e-45, np.inf, -np.inf, np.nan, -np.nan, 3.4e38, -2.0]), pool.mass.shape)
     elif masses == "same":
         pool.mass[:] = 0.25
+    elif masses == "nan":
+        pool.mass = np.where(rng.random(pool.mass.shape) < 0.5, np.nan, rng.random(pool.mass.shape).astype(np.float32))
+    elif masses == "close":  # differ in their last bits only
+        pool.mass = np.nextafter(np.float32(1.5), np.float32(2)) + rng.integers(0, 300, pool.mass.shape).astype(np.float32) * np.float32(2.0 ** -23)
     seen = [int(np.quantile(pool.pos, 0.9))] * len(lens)
     dev = Dev(pool, dtype)
     ws = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, len(lens), G, max_evict, D, ec.dtype_code(dev.k))

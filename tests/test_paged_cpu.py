@@ -35,7 +35,7 @@ def _evict(**other):
 SHAPE = [(dict(B=0), ec.EC_EINVAL), (dict(Hkv=0), ec.EC_EINVAL), (dict(G=2), ec.EC_EINVAL), (dict(D=0), ec.EC_EINVAL), (dict(page=0), ec.EC_EINVAL),
          (dict(page=-16), ec.EC_EINVAL), (dict(n_pages=0), ec.EC_EINVAL), (dict(max_pages=0), ec.EC_EINVAL), (dict(table=None), ec.EC_EINVAL),
          (dict(page=24), ec.EC_EUNSUPPORTED), (dict(page=4), ec.EC_EUNSUPPORTED), (dict(page=512), ec.EC_EUNSUPPORTED),
-         (dict(max_pages=1 << 27), ec.EC_EUNSUPPORTED), (dict(D=96), ec.EC_EUNSUPPORTED), (dict(dt=2), ec.EC_EUNSUPPORTED),
+         (dict(max_pages=1 << 27), ec.EC_EUNSUPPORTED), (dict(n_pages=1 << 28), ec.EC_EUNSUPPORTED), (dict(D=96), ec.EC_EUNSUPPORTED), (dict(dt=2), ec.EC_EUNSUPPORTED),
          (dict(B=20000), ec.EC_EUNSUPPORTED), (dict(k_pages=ODD), ec.EC_EUNSUPPORTED), (dict(v_pages=ODD), ec.EC_EUNSUPPORTED)]
 
 
@@ -87,6 +87,8 @@ def test_evict_refusals():
         assert _evict(**{p: None}) == ec.EC_EINVAL, p
     assert _evict(max_evict=0) == ec.EC_EINVAL
     assert _evict(max_evict=65) == ec.EC_EINVAL                          # more than the slots of a sequence
+    for p in ("pos_pages", "mass_pages"):
+        assert _evict(**{p: ODD}) == ec.EC_EUNSUPPORTED, p
     assert _evict(first=-1) == ec.EC_EINVAL
     assert _evict(recent=-1) == ec.EC_EINVAL
     assert _evict(seen_b=None, recent=0) == ec.EC_EWORKSPACE
