@@ -28,6 +28,7 @@ typedef __attribute__((address_space(4))) const int32_t const_i32;  // read thro
 
 constexpr int kPagedWaves = 4;
 constexpr int kPagedSegments = 256;  // workgroups that a launch of few pairs aims at: one a compute unit
+constexpr int kWholeRounds = 3;       // a pair of so many rounds is not cut: 60, 120 rows of one sequence, H32 5.4, 5.9 us a step, joined 7.9
 constexpr int kMostSegments = 256;   // of a pair, whose weights have to fit into LDS when they are joined
 constexpr int kHeadBlock = 16;       // query heads of a pair, at most
 constexpr float kSmallExponent = -100.f, kSmall = 0x1p-100f;  // probabilities below it are looked at apart
@@ -61,11 +62,20 @@ struct PagedStep {
     unsigned long long* partials;  // of the segments of such pairs
 };
 
-// load_lds_16 of data that is read once: the non-temporal hint keeps it from displacing cache lines (B16 H32 870 rows 46.8 -> 42.3 us a step, one
-// cache of 131071 rows 105 -> 91)
-__device__ __forceinline__ void load_once_lds_16(u32x4 rsrc, uint32_t lds, uint32_t byte_offset)
+// N load instructions of consecutive rows into consecutive LDS (see load_lds_16): the instruction's offset moves both by 1 KB. The non-temporal hint
+// keeps data that is read once from displacing cache lines (B16 H32 870 rows 46.8 -> 42.3 us a step, one cache of 131071 rows 105 -> 91).
+template <int N> __device__ __forceinline__ void load_run_lds(u32x4 rsrc, uint32_t lds, const uint32_t* offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(byte_offset), "s"(rsrc) : "memory");
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(offset[0]), "s"(rsrc) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %3, 0 offen nt lds\n\t"
+                     "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 nt lds" ::"s"(lds), "v"(offset[0]), "v"(offset[1]), "s"(rsrc) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, 0 offen nt lds\n\t"
+                     "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 nt lds\n\tbuffer_load_dwordx4 %3, %5, 0 offen offset:2048 nt lds\n\t"
+                     "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 nt lds"
+                     ::"s"(lds), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(rsrc) : "memory");
 }
 
 template <int DT, int D> struct PagedTile {
@@ -138,7 +148,7 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
     if (B == 1) {  // nothing to look through
         const int n = ((const const_i32*)(uintptr_t)len_b)[0];
         const bool live = n >= 0 && n < slots;
-        const int rounds = live ? n / ROUND + 1 : 1, count = min(min(rounds, kMostSegments), max(scalar(divided(kPagedSegments, pairs)), 1));
+        const int rounds = live ? n / ROUND + 1 : 1, count = min(min(rounds, kMostSegments), min(max(scalar(divided(kPagedSegments, pairs)), 1), rounds <= kWholeRounds ? 1 : max(rounds / 2, 16)));
         const int seg = scalar(divided(id, pairs));
         if (seg >= count) return {-1, 0, 0, 0, 0, 0, 0, 0};
         const int pair = id - seg * pairs;
@@ -158,6 +168,16 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
         all += last_lane(scan_wave(rounds_of(b0 + lane, n)));
     }
     int most = (int)((all * pairs + kPagedSegments - 1) / kPagedSegments);
+    // Sequences of different lengths that are cut into two or not at all leave some compute units with much and others with little: twice as many
+    // segments there, as many as the chip holds at once (us a step, 256 about / 512 at most: 192 pairs of 1450 .. 2900 rows 52.0 / 45.8, 128 of 750 ..
+    // 1500 22.2 / 18.8; pairs that are cut further, one length and single sequences gain nothing, and joining takes longer: 64 pairs of 2000 .. 4000 rows
+    // 19.6 / 21.6, 8 of 131071 91 / 98).
+    if (B <= kWave && most >= 8 && B * pairs > kPagedSegments / 3 && B * pairs <= 2 * kPagedSegments &&
+        wave_max((float)rounds_of(lane, n)) * B > 1.125f * all) {
+        most = max((int)((all * pairs + 2 * kPagedSegments - 1) / (2 * kPagedSegments)), kWholeRounds);
+        while (last_lane(scan_wave(divided(rounds_of(lane, n) + most - 1, most))) * pairs > 2 * kPagedSegments) most += (most + 7) / 8;
+    }
+    most = max(most, kWholeRounds);
     int before = 0, cut = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
         if (B > kWave) n = rows(b0 + lane);
@@ -183,7 +203,8 @@ __device__ __forceinline__ void put(unsigned long long* p, float x, float y)
 {
     __hip_atomic_store(p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kWave) void paged_step_kernel(PagedStep a)
+template <int DT, int D, bool EMIT>
+__global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(PagedStep a)
 {
     using T = PagedTile<DT, D>;
     constexpr int WAVES = kPagedWaves, TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
@@ -223,37 +244,45 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles[wave]));
     const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
     const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(n, at.last * ROUND);  // rows of the cache in the segment end there
-    uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in a run of 8 rows, K: of even and odd runs
+    uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in the rows of a load instruction, K: of even and odd runs
 #pragma unroll
     for (int i = 0; i < T::IPG; ++i) {
         const int r = i * RPI + lane / CH;
-        k_part[0][i] = r * ROW + (lane % CH ^ T::swz_k(r)) * 16;
-        k_part[1][i] = r * ROW + (lane % CH ^ T::swz_k(r + 8)) * 16;
-        v_part[i] = r * ROW + (lane % CH ^ T::swz_v(r)) * 16;
+        k_part[0][i] = lane / CH * ROW + (lane % CH ^ T::swz_k(r)) * 16;
+        k_part[1][i] = lane / CH * ROW + (lane % CH ^ T::swz_k(r + 8)) * 16;
+        v_part[i] = lane / CH * ROW + (lane % CH ^ T::swz_v(r)) * 16;
     }
+    // Where the runs of a tile lie in the pools, and how many bytes of them are there: none behind the segment or on no page, and what is not
+    // there becomes zeros in LDS. A run in the page of the one before it needs no table entry.
     struct Ids {
         int id[T::GROUPS];
     };
+    const int page_rows = 1 << shift;
     auto pages_of = [&](int row) __attribute__((always_inline)) {
         Ids ids;
 #pragma unroll
-        for (int u = 0; u < T::GROUPS; ++u) ids.id[u] = table[min((row + u * 8) >> shift, a.pages.max_pages - 1)];
+        for (int u = 0; u < T::GROUPS; ++u)
+            if (u == 0 || u * 8 % page_rows == 0) ids.id[u] = table[min((row + u * 8) >> shift, a.pages.max_pages - 1)];
         return ids;
     };
-    // Where the runs of a tile lie in the pools, and how many bytes of them are there: none behind the segment or on no page, and what is not
-    // there becomes zeros in LDS.
     struct Places {
         size_t from[T::GROUPS];
         int bytes[T::GROUPS], bad;  // bit u: run u has rows, but no page
     };
+    const uint32_t head_bytes = (uint32_t)ROW << shift, page_bytes = head_bytes * (uint32_t)a.Hkv;
     auto places_of = [&](int row, const Ids& ids) __attribute__((always_inline)) {
         Places pl;
         pl.bad = 0;
+        bool page = false;
 #pragma unroll
         for (int u = 0; u < T::GROUPS; ++u) {
             const int r = row + u * 8, left = end - r;
-            const bool page = (unsigned)ids.id[u] < (unsigned)a.pages.n_pages;
-            pl.from[u] = ((((size_t)(unsigned)(page ? ids.id[u] : 0) * (unsigned)a.Hkv + (unsigned)hk) << shift) + (r & mask)) * ROW;
+            if (u == 0 || u * 8 % page_rows == 0) {
+                page = (unsigned)ids.id[u] < (unsigned)a.pages.n_pages;
+                pl.from[u] = (size_t)(uint32_t)(page ? ids.id[u] : 0) * page_bytes + (hk * head_bytes + (uint32_t)(r & mask) * ROW);
+            } else {
+                pl.from[u] = pl.from[u ? u - 1 : 0] + 8 * ROW;
+            }
             pl.bytes[u] = page ? max(min(left, 8), 0) * ROW : 0;
             pl.bad |= page || left <= 0 ? 0 : 1 << u;
         }
@@ -262,38 +291,30 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     auto issue_k = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::GROUPS; ++u)
+            load_run_lds<T::IPG>(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, k_part[u & 1]);
+    };
+    auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < T::IPG; ++i)
-                load_once_lds_16(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
+        for (int u = 0; u < T::GROUPS; ++u)
+            load_run_lds<T::IPG>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, v_part);
     };
     auto issue_q = [&](uint32_t lds) __attribute__((always_inline)) {  // rows of queries like rows of K; zeros for heads that do not exist
         const char* q = static_cast<const char*>(a.q) + out_at * Elem<DT>::kBytes;
 #pragma unroll
         for (int u = 0; u < kHeadBlock / 8; ++u)
-#pragma unroll
-            for (int i = 0; i < T::IPG; ++i)
-                load_lds_16(tile_rsrc(q + u * 8 * ROW, max(heads - u * 8, 0) * ROW), lds + (u * 8 + i * RPI) * ROW, k_part[u & 1][i]);
-    };
-    auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < T::GROUPS; ++u)
-#pragma unroll
-            for (int i = 0; i < T::IPG; ++i)
-                load_once_lds_16(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + (u * 8 + i * RPI) * ROW, v_part[i]);
+            load_run_lds<T::IPG>(tile_rsrc(q + u * 8 * ROW, max(heads - u * 8, 0) * ROW), lds + u * 8 * ROW, k_part[u & 1]);
     };
     // the new row, where the tile has it: into the place that its loads left at zero
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-    auto add_new = [&](uint32_t lds, int row, const u32x4& chunk, int swizzle) __attribute__((always_inline)) {
+    auto add_new = [&](uint32_t off, int row) __attribute__((always_inline)) {
         const int r = n - row;
         if (r >= 0 && r < TR) {
-            if (lane < CH) *(lds_u32x4*)(uintptr_t)(lds + r * ROW + (lane ^ swizzle) * 16) = chunk;
+            if (lane < CH) {
+                *(lds_u32x4*)(uintptr_t)(mine + off + r * ROW + (lane ^ T::swz_k(r)) * 16) = new_k;
+                *(lds_u32x4*)(uintptr_t)(mine + 2 * T::BYTES + off + r * ROW + (lane ^ T::swz_v(r)) * 16) = new_v;
+            }
             wait_lds();
         }
-    };
-    // loads of the wave but the newest three tiles' have landed; or all of them, where no tile is issued any more
-    auto wait_tile = [&](bool more) __attribute__((always_inline)) {
-        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory");
-        else wait_loads();
     };
 
     // ------------------------------------------------------------------ one tile after the other
@@ -317,40 +338,60 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
     }
     constexpr int BLOCKS = TR / 16;  // of 16 rows
 
-    // off: which of the two places; later: the tile after the next, whose loads are issued as this one's place becomes free
-    auto tile = [&](uint32_t off, int row, int bad, bool more, const Places& later) __attribute__((always_inline)) {
+    // off: which of the two places; left: tiles with this one; later: the tile after the next, whose loads are issued once this one is in registers
+    auto tile = [&](uint32_t off, int row, int bad, int left, const Places& later) __attribute__((always_inline)) {
+        if (left > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");  // all loads but the next tile's have landed
+        else wait_loads();
+        add_new(off, row);
+        f32x4 kf[KB][BLOCKS];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t) kf[kb][t] = *(lds_f32x4*)(uintptr_t)(k_at[kb] + off + t * 16 * ROW);
+        bf16x4 vh[OB][BLOCKS];  // V, bf16
+        f32x4 vw[OB];           // V, fp32
+#pragma unroll
+        for (int i = 0; i < OB; ++i) {
+            if constexpr (T::kHalf) {
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) vh[i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(v_at[i] + off + t * 16 * ROW));
+            } else {
+                vw[i] = *(lds_f32x4*)(uintptr_t)(v_at[i] + off);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
         f32x4 s[BLOCKS];
-#pragma unroll
-        for (int t = 0; t < BLOCKS; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        wait_tile(more);
-        add_new(mine + off, row, new_k, T::swz_k(n - row));
         if constexpr (T::kHalf) {
-            bf16x8 kf[KB][BLOCKS];
+            f32x4 part[BLOCKS][2];  // two chains
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int t = 0; t < BLOCKS; ++t) kf[kb][t] = *(lds_bf16x8*)(uintptr_t)(k_at[kb] + off + t * 16 * ROW);
+            for (int t = 0; t < BLOCKS; ++t) part[t][0] = part[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int t = 0; t < BLOCKS; ++t)
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][t], __builtin_bit_cast(bf16x8, qf[kb]), s[t], 0, 0, 0);
-        } else {
-            f32x4 kf[KB], part[4];  // four chains, so that every partial sum is short
+                    part[t][kb % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[kb][t]), __builtin_bit_cast(bf16x8, qf[kb]),
+                                                                             part[t][kb % 2], 0, 0, 0);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) kf[kb] = *(lds_f32x4*)(uintptr_t)(k_at[kb] + off);
+            for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][r] = part[t][0][r] + part[t][1][r];
+        } else {
+            f32x4 part[4];  // four chains, so that every partial sum is short
 #pragma unroll
             for (int e = 0; e < 4; ++e) part[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][e], __uint_as_float(qf[kb][e]), part[e], 0, 0, 0);
+                    part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][0][e], __uint_as_float(qf[kb][e]), part[e], 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[0][r] = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
         }
         wait_lds();
-        if (more) issue_k(mine + off, later);
+        if (left > 2) {
+            issue_k(mine + off, later);
+            issue_v(mine + 2 * T::BYTES + off, later);
+        }
 
         if (bad || row + TR > n + 1) {
 #pragma unroll
@@ -412,8 +453,6 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
             for (int r = 0; r < 4; ++r) sum += p[t][r];
         l += sum;
 
-        wait_tile(more);
-        add_new(mine + 2 * T::BYTES + off, row, new_v, T::swz_v(n - row));
         if constexpr (T::kHalf) {
             // a probability is the sum of two bf16 numbers, its upper half (cut, so that the rest is not negative) and the rest, together
             // 2^-16 of it off; the rest of one that is not 0 is not 0 either, so that an infinite V stays infinite
@@ -424,18 +463,12 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
                 hi[e] = (__bf16)h;
                 lo[e] = (__bf16)fmaxf(x - h, x * 0x1p-20f);
             };
-            bf16x4 vf[OB][BLOCKS];  // all on their way before the first is used
-#pragma unroll
-            for (int i = 0; i < OB; ++i)
-#pragma unroll
-                for (int t = 0; t < BLOCKS; ++t) vf[i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(v_at[i] + off + t * 16 * ROW));
-            __builtin_amdgcn_sched_barrier(0);
             // x + V^T . P^T of 16 features, P one of its halves
             auto multiply = [&](int i, const bf16xp& half, f32x4 x) __attribute__((always_inline)) {
                 if constexpr (BLOCKS == 2)
-                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(vh[i][0], vh[i][1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
                 else
-                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vf[i][0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vh[i][0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
             };
             // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64
             bf16xp hi, lo;
@@ -462,13 +495,10 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
         } else {
 #pragma unroll
             for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4
-                const f32x4 vf = *(lds_f32x4*)(uintptr_t)(v_at[i] + off);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e], p[0][i % 4], o[i / 4 * 4 + e], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) o[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw[i][e], p[0][i % 4], o[i / 4 * 4 + e], 0, 0, 0);
             }
         }
-        wait_lds();
-        if (more) issue_v(mine + 2 * T::BYTES + off, later);
     };
     {
         int row = (at.first * WAVES + wave) * TR, left = at.last - at.first;  // rounds
@@ -520,7 +550,7 @@ template <int DT, int D, bool EMIT> __global__ __launch_bounds__(kPagedWaves* kW
         for (;; --left) {
             Ids ids;
             if (left > 3) ids = pages_of(row + 3 * ROUND);
-            tile(off, row, bad, left > 2, next);
+            tile(off, row, bad, left, next);
             if (left == 1) break;
             bad = next_bad, next_bad = next.bad;
             row += ROUND, off ^= T::BYTES;
@@ -703,7 +733,9 @@ template <int DT, int D> static int launch(const PagedStep& a, float* mass_pages
 {
     constexpr int ROUND = kPagedWaves * PagedTile<DT, D>::TR;
     const long long pairs = (long long)a.B * a.Hkv * a.blocks, rounds = (a.pages.slots() + ROUND - 1) / ROUND;
-    const dim3 grid((unsigned)std::min(kPagedSegments + pairs, rounds * pairs));
+    // as many workgroups as there can be segments (see find_segment); those without one leave at once
+    const long long segments = a.B == 1 ? std::max<long long>(kPagedSegments, pairs) : std::max<long long>(2 * kPagedSegments, kPagedSegments + pairs);
+    const dim3 grid((unsigned)std::min(segments, rounds * pairs));
     if (!mass_pages) {
         hipLaunchKernelGGL((paged_step_kernel<DT, D, false>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
         return status_from_hip(hipGetLastError());

@@ -125,6 +125,29 @@ def test_step_long_or_many(dtype, H, Hkv, B, n, page, scored):
     run_step(pool, dtype, H, lens, n, scored)
 
 
+def quick(rng, dtype, Hkv, G, D, page, lens):
+    """A pool of normal numbers all over: long sequences are made quickly."""
+    used = [max(n, 0) // page + 1 for n in lens]
+    N = sum(used)
+    order, table, at = rng.permutation(N), np.full((len(lens), max(used)), -1, np.int64), 0
+    for b, u in enumerate(used):
+        table[b, :u] = order[at:at + u]
+        at += u
+    k, v = (quantize(rng.standard_normal((N, Hkv, page, D), np.float32), dtype) for _ in range(2))
+    return ref.Pool(k, v, rng.integers(0, 5000, (N, G, page)).astype(np.int32), rng.random((N, G, page)).astype(np.float32), table)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,page,B,n", [("bf16", 4, 2, 128, 16, 24, 4200), ("bf16", 2, 2, 64, 64, 30, 6000), ("f32", 4, 4, 64, 32, 40, 700),
+                                                    ("bf16", 3, 1, 128, 8, 64, 3900), ("bf16", 2, 1, 128, 256, 63, 5000), ("bf16", 1, 1, 64, 16, 70, 2000)])
+@pytest.mark.parametrize("spread", ["alike", "mixed", "one long"])
+def test_batches_whose_sequences_are_cut(dtype, H, Hkv, D, page, B, n, spread):
+    """Every rule by which a batch is divided over workgroups: no row is left out or counted twice."""
+    rng = np.random.default_rng(B + n)
+    lens = [n] * B if spread == "alike" else [int(x) for x in rng.integers(-1, n + 1, B)] if spread == "mixed" else [n * 3] + [int(x) for x in rng.integers(0, 200, B - 1)]
+    pool = quick(rng, dtype, Hkv, 1, D, page, lens)
+    run_step(pool, dtype, H, lens, n, with_pos=False)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scored", [False, True])
 def test_pages_that_do_not_exist(dtype, scored):
