@@ -6,34 +6,46 @@
 namespace ec {
 
 // ------------------------------------------------------------------ store
-// A workgroup per 32 rows of a (sequence, head), one more head for the positions and masses of every score group.
+// A workgroup takes kStoreRows rows of a (sequence, head), all its loads in flight; that of the first head takes positions and masses along. Bound: memory,
+// at the rate of a plain copy (5.2 TB/s read and written at B16 H32 1024 .. 2048 rows; 4.97 without the non-temporal hints, 4.8 with 64 rows).
 constexpr int kStoreRows = 32;
 template <int CH>  // 16-byte chunks of a row
 __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restrict__ k, const u32x4* __restrict__ v, const int32_t* __restrict__ pos,
                                                           const float* __restrict__ mass, Pages pages, const int32_t* __restrict__ start_b,
-                                                          const int32_t* __restrict__ n_rows_b, int Hkv, int G, int T, int src_rows, u32x4* k_pages,
-                                                          u32x4* v_pages, int32_t* pos_pages, float* mass_pages)
+                                                          const int32_t* __restrict__ n_rows_b, int Hkv, int G, int T, int src_rows,
+                                                          u32x4* __restrict__ k_pages, u32x4* __restrict__ v_pages, int32_t* __restrict__ pos_pages,
+                                                          float* __restrict__ mass_pages)
 {
+    constexpr int ROWS = 256 / CH, EACH = kStoreRows / ROWS;  // rows of a pass, passes
     const int b = blockIdx.z, head = blockIdx.y, r0 = blockIdx.x * kStoreRows;
     const int n = min(max(n_rows_b ? n_rows_b[b] : T, 0), T), start = start_b ? start_b[b] : 0;
-    auto slot_of = [&](int r) {
+    if (r0 >= n) return;
+    auto page_at = [&](int r) {  // page of row r's slot, or -1
         const int64_t s = (int64_t)start + r;
-        return r < n && s >= 0 && s < pages.slots() ? (int)s : -1;
+        return r < n && s >= 0 && s < pages.slots() ? pages.page_of(b, (int)s) : -1;
     };
-    if (head < Hkv && k) {
-        for (int i = threadIdx.x; i < kStoreRows * CH; i += 256) {
-            const int r = r0 + i / CH, s = slot_of(r), id = s < 0 ? -1 : pages.page_of(b, s);
-            if (id < 0) continue;
-            const size_t from = (((size_t)b * Hkv + head) * src_rows + r) * CH + i % CH, to = pages.row(id, Hkv, head, s) * CH + i % CH;
-            k_pages[to] = k[from];
-            v_pages[to] = v[from];
+    if (k) {
+        const int c = threadIdx.x % CH, first = r0 + threadIdx.x / CH;
+        const u32x4 *from_k = k + ((size_t)b * Hkv + head) * src_rows * CH, *from_v = v + ((size_t)b * Hkv + head) * src_rows * CH;
+        u32x4 x[EACH], y[EACH];
+        int id[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const size_t at = (size_t)min(first + i * ROWS, n - 1) * CH + c;
+            x[i] = __builtin_nontemporal_load(from_k + at), y[i] = __builtin_nontemporal_load(from_v + at), id[i] = page_at(first + i * ROWS);
         }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (id[i] >= 0) {
+                const size_t to = pages.row(id[i], Hkv, head, start + first + i * ROWS) * CH + c;
+                __builtin_nontemporal_store(x[i], k_pages + to), __builtin_nontemporal_store(y[i], v_pages + to);
+            }
     }
     if (head == 0) {
         for (int i = threadIdx.x; i < kStoreRows * G; i += 256) {
-            const int g = i / kStoreRows, r = r0 + i % kStoreRows, s = slot_of(r), id = s < 0 ? -1 : pages.page_of(b, s);
+            const int g = i / kStoreRows, r = r0 + i % kStoreRows, id = page_at(r);
             if (id < 0) continue;
-            const size_t from = ((size_t)b * G + g) * src_rows + r, to = pages.row(id, G, g, s);
+            const size_t from = ((size_t)b * G + g) * src_rows + r, to = pages.row(id, G, g, start + r);
             if (pos) pos_pages[to] = pos[from];
             if (mass) mass_pages[to] = mass[from];
         }
@@ -68,16 +80,18 @@ struct EvictGoal {
     __device__ __forceinline__ int victims(int b, int n) const { return min(max(n - max(keep_b[b], 0), 0), max_evict); }
 };
 
+constexpr uint32_t kProtected = 0xffffffffu;
 // The order in which rows go, as an integer: fp32 order with -0 equal to +0, NaN behind +inf, protected rows (and rows on no page) last.
 __device__ __forceinline__ uint32_t evict_key(float mass, bool kept)
 {
     uint32_t u = __float_as_uint(mass);
     if (u == 0x80000000u) u = 0u;
     const uint32_t key = (u & 0x7fffffffu) > 0x7f800000u ? 0xfffffffeu : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    return kept ? 0xffffffffu : key;
+    return kept ? kProtected : key;
 }
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+constexpr int kCopies = 8, kCopyWords = 264;
 constexpr int kRun = 8;  // consecutive slots that a thread looks at: one page, one table entry, two 16-byte loads each of masses and positions
 
 // What an eviction looks at in one (sequence, score group).
@@ -135,14 +149,17 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sh, uint32_
     return (wave ? before : 0) + in - x;
 }
 
-// One workgroup per (sequence, score group): which rows go, and the list of moves. A thread holds runs of 8 consecutive slots. The gone-th smallest
-// key is found digit by digit, 8 bits at a time from the highest bit in which two keys differ (masses share their upper bits, and a
-// histogram of those is one counter that all lanes wait for). HELD: keys stay in registers, for sequences of up to 8192 rows; longer ones are read
-// again for every digit.
+// One workgroup per (sequence, score group): which rows go, and the list of moves. A thread holds runs of 8 consecutive slots. Sought is the gone-th
+// smallest (key, slot): digit by digit, 8 bits at a time from the highest bit in which two keys differ (masses share their upper bits, and a histogram
+// of those is one counter that all lanes wait for), until at most 64 rows share the digits found, which every wave ranks. HELD: keys stay in
+// registers, for sequences of up to 8192 rows; longer ones are read again for every digit. Bound: a chain of latencies (length, table, masses, a barrier
+// or two for each digit); by the profiler 16 groups of 8192 rows 67 us with digits sought by one thread and keys read again, now 10.
 template <bool HELD> __device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list)
 {
-    __shared__ __align__(16) uint32_t hist[4][256];
-    __shared__ uint32_t sh[3][kEvictWaves], sh_lo[kEvictWaves], sh_hi[kEvictWaves];
+    // a counter has a copy for every eighth lane, in banks of their own
+    __shared__ __align__(16) uint32_t hist[4][kCopies][kCopyWords];
+    __shared__ uint32_t sh[3][kEvictWaves], sh_lo[kEvictWaves], sh_hi[kEvictWaves], n_few, sh_slot;
+    __shared__ unsigned long long few[kWave];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = rows.n, m = n - gone;
     const int runs = (n + kRun - 1) / kRun;
     uint32_t held[kRun];
@@ -160,91 +177,129 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
             }
         }
     };
-    hist[tid / 256][tid % 256] = 0;
+    for (int i = tid; i < (int)(sizeof(hist) / 16); i += kEvictThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) n_few = 0, sh_slot = 0;
     // how many rows are not protected, and the bits in which their keys differ
-    uint32_t lo = 0xffffffffu, hi = 0, free_rows = 0;
+    uint32_t lo = kProtected, hi = 0, open = 0;
     each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            const bool open = key[i] != 0xffffffffu;
-            lo = min(lo, key[i]), hi = max(hi, open ? key[i] : 0u), free_rows += open;
-        }
+        for (int i = 0; i < kRun; ++i) lo = min(lo, key[i]), hi = max(hi, key[i] == kProtected ? 0u : key[i]), open += key[i] != kProtected;
     });
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, off, kWave)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, off, kWave));
     if (lane == 0) sh_lo[wave] = lo, sh_hi[wave] = hi;
-    uint32_t all_free;
-    block_scan(free_rows, sh[0], all_free);
+    uint32_t all_open;
+    block_scan(open, sh[0], all_open);
 #pragma unroll
     for (int w = 0; w < kEvictWaves; ++w) lo = min(lo, sh_lo[w]), hi = max(hi, sh_hi[w]);
 
-    // victims: keys below `last`, and the first `need` rows whose key is `last` (its bits from `shift` on)
-    uint32_t last, need = gone;
-    int shift = 0;
-    if ((uint32_t)gone >= all_free) {
-        last = 0xffffffffu, need = gone - all_free;  // all that are not protected, and protected ones by their slots
-    } else {
-        last = lo;
-        if (lo != hi) {
-            shift = 32 - __clz(lo ^ hi);
-            last = shift == 32 ? 0 : hi >> shift << shift;
-            for (int pass = 0; shift > 0; ++pass) {
-                const int bits = min(shift, 8), down = shift - bits;
-                each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
+    // Victims are the rows up to `limit` in the order of (key, slot). Where only their key is known, last, and how many rows have it and go, need, the
+    // slot is looked for behind.
+    unsigned long long limit = (unsigned long long)(kProtected - 1) << 32 | 0xffffffffu;  // all that are not protected
+    uint32_t last = kProtected, need = gone - min((uint32_t)gone, all_open);
+    bool ties = need > 0;
+    if ((uint32_t)gone < all_open) {
+        int shift = lo == hi ? 0 : 32 - __clz(lo ^ hi);
+        need = gone, ties = true;
+        last = shift == 32 ? 0 : hi >> shift << shift;
+        for (int pass = 0; shift > 0; ++pass) {
+            const int bits = min(shift, 8), down = shift - bits;
+            each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < kRun; ++i)
+                    if (key[i] != kProtected && ((uint64_t)(key[i] ^ last) >> shift) == 0)
+                        atomicAdd(&hist[pass][lane % kCopies][key[i] >> down & ((1u << bits) - 1)], 1u);
+            });
+            __syncthreads();
+            // every wave finds the digit for itself: four counters a lane
+            uint4 c = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int copy = 0; copy < kCopies; ++copy) {
+                const uint4 x = reinterpret_cast<const uint4*>(hist[pass][copy])[lane];
+                c.x += x.x, c.y += x.y, c.z += x.z, c.w += x.w;
+            }
+            const uint32_t upto = wave_scan(c.x + c.y + c.z + c.w);
+            const unsigned long long reached = __ballot(upto >= need);
+            const int at = reached ? __ffsll(reached) - 1 : kWave - 1;  // (always, unless masses change while they are read)
+            const uint32_t x = __builtin_amdgcn_readlane(c.x, at), y = __builtin_amdgcn_readlane(c.y, at), z = __builtin_amdgcn_readlane(c.z, at),
+                           w = __builtin_amdgcn_readlane(c.w, at);
+            need -= __builtin_amdgcn_readlane(upto, at) - (x + y + z + w);
+            uint32_t digit = at * 4, count = x;
+            if (need > count) {
+                need -= count, ++digit, count = y;
+                if (need > count) {
+                    need -= count, ++digit, count = z;
+                    if (need > count) need -= count, ++digit, count = w;
+                }
+            }
+            last |= digit << down, shift = down;
+            if (need == count) {  // all rows with these digits go
+                ties = false;
+                limit = (unsigned long long)min(last | ((1u << down) - 1), kProtected - 1) << 32 | 0xffffffffu;
+                break;
+            }
+            if (count <= kWave) {  // few rows are left
+                ties = false;
+                each_run([&](int j, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < kRun; ++i)
-                        if (key[i] != 0xffffffffu && ((uint64_t)(key[i] ^ last) >> shift) == 0) atomicAdd(&hist[pass][key[i] >> down & ((1u << bits) - 1)], 1u);
+                        if (key[i] != kProtected && ((uint64_t)(key[i] ^ last) >> down) == 0) {
+                            const uint32_t to = atomicAdd(&n_few, 1u);
+                            if (to < kWave) few[to] = (unsigned long long)key[i] << 32 | (uint32_t)(j + i);
+                        }
                 });
                 __syncthreads();
-                // every wave finds the digit for itself: four counters a lane
-                const uint4 c = reinterpret_cast<const uint4*>(hist[pass])[lane];
-                const uint32_t upto = wave_scan(c.x + c.y + c.z + c.w);
-                const unsigned long long reached = __ballot(upto >= need);
-                const int at = reached ? __ffsll(reached) - 1 : kWave - 1;  // (always, unless masses change while they are read)
-                const uint32_t x = __builtin_amdgcn_readlane(c.x, at), y = __builtin_amdgcn_readlane(c.y, at), z = __builtin_amdgcn_readlane(c.z, at),
-                               w = __builtin_amdgcn_readlane(c.w, at);
-                need -= __builtin_amdgcn_readlane(upto, at) - (x + y + z + w);
-                uint32_t digit = at * 4, count = x;
-                if (need > count) need -= count, ++digit, count = y;
-                if (need > count && digit % 4 == 1) need -= count, ++digit, count = z;
-                if (need > count && digit % 4 == 2) need -= count, ++digit, count = w;
-                last |= digit << down, shift = down;
-                if (need == count) break;  // all rows with these digits go
+                const unsigned long long mine = few[lane];
+                uint32_t rank = 0;
+                for (uint32_t i = 0; i < count; ++i) rank += few[i] < mine;
+                const unsigned long long found = __ballot((uint32_t)lane < count && rank == need - 1);
+                const int who = found ? __ffsll(found) - 1 : 0;
+                limit = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), who) << 32 |
+                        (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, who);
+                break;
             }
         }
     }
-
-    // (a protected row's key can share the upper bits of a NaN's)
-    auto ties_with = [&](uint32_t key) { return ((uint64_t)(key ^ last) >> shift) == 0 && (shift == 0 || key != 0xffffffffu); };
-    uint32_t ties = 0, holes = 0, movers = 0;
-    each_run([&](int j, uint32_t (&key)[kRun], int page) __attribute__((always_inline)) {
-        uint32_t mine = 0, total;
+    if (ties) {  // the need-th row whose key is `last`
+        uint32_t before = 0;
+        each_run([&](int j, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
+            uint32_t mine = 0, total;
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) mine += j + i < n && ties_with(key[i]);
-        uint32_t rank = ties + block_scan(mine, sh[1], total);
-        ties += total;
-        uint32_t flags = 0, both = 0;  // bit i: a hole; bit 8 + i: a mover
+            for (int i = 0; i < kRun; ++i) mine += j + i < n && key[i] == last;
+            uint32_t rank = before + block_scan(mine, sh[1], total);
+            before += total;
+#pragma unroll
+            for (int i = 0; i < kRun; ++i)
+                if (j + i < n && key[i] == last && ++rank == need) sh_slot = j + i;
+            if constexpr (!HELD) __syncthreads();  // sh is written again
+        });
+        __syncthreads();
+        limit = (unsigned long long)last << 32 | sh_slot;
+    }
+
+    uint32_t holes = 0, movers = 0;
+    each_run([&](int j, uint32_t (&key)[kRun], int page) __attribute__((always_inline)) {
+        uint32_t flags = 0, both = 0, total;  // bit i: a hole; bit 8 + i: a mover
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const bool there = j + i < n, tie = there && ties_with(key[i]);
-            const bool victim = there && (tie ? rank < need : key[i] < last);
-            rank += tie;
-            const bool hole = victim && j + i < m, mover = there && !victim && j + i >= m;
+            const bool victim = ((unsigned long long)key[i] << 32 | (uint32_t)(j + i)) <= limit;
+            const bool hole = victim && j + i < m, mover = !victim && j + i >= m && j + i < n;
             flags |= (uint32_t)hole << i | (uint32_t)mover << (8 + i);
             both += (uint32_t)hole | (uint32_t)mover << 16;
         }
         uint32_t at = block_scan(both, sh[2], total);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const uint32_t row = page < 0 ? 0xffffffffu : ((uint32_t)page << rows.pages.shift) + ((j + i) & (rows.pages.page() - 1));
-            if (flags >> i & 1) list[holes + (at & 0xffff)].x = row;
-            if (flags >> (8 + i) & 1) list[movers + (at >> 16)].y = row;
+            const uint32_t row = page < 0 ? ~0u : ((uint32_t)page << rows.pages.shift) + ((j + i) & (rows.pages.page() - 1));
+            const uint32_t to_hole = holes + (at & 0xffff), to_mover = movers + (at >> 16);
+            if ((flags >> i & 1) && to_hole < (uint32_t)gone) list[to_hole].x = row;
+            if ((flags >> (8 + i) & 1) && to_mover < (uint32_t)gone) list[to_mover].y = row;
             at += (flags >> i & 1) | (flags >> (8 + i) & 1) << 16;
         }
         holes += total & 0xffff, movers += total >> 16;
-        if constexpr (!HELD) __syncthreads();  // sh is written again
+        if constexpr (!HELD) __syncthreads();
     });
-    if (tid == 0) *counts = min(holes, movers);  // equal, unless masses change while they are read
+    if (tid == 0) *counts = min(min(holes, movers), (uint32_t)gone);  // equal, unless masses change while they are read
 }
 
 __global__ __launch_bounds__(kEvictThreads) void paged_evict_select_kernel(const int32_t* __restrict__ pos_pages, const float* __restrict__ mass_pages,
@@ -268,40 +323,29 @@ __device__ __forceinline__ size_t pool_row(uint32_t row, const Pages& pages, int
     return pages.row(row >> pages.shift, heads, head, row);
 }
 
-// Moves: a workgroup takes 4 * 256 / CH rows of K or of V of a head at a time, all their loads in flight; K's of the group's first head take positions
-// and masses along.
+// Moves: a workgroup takes 256 / CH rows of K or of V of a head at a time; K's of the group's first head take positions and masses along. Bound: memory.
+// (B16 H32 8192 -> 820 rows, selection included, us: 103; with non-temporal stores 96; a row a thread instead of four in flight 93.)
 template <int CH>
 __global__ __launch_bounds__(256) void paged_evict_move_kernel(u32x4* k_pages, u32x4* v_pages, int32_t* pos_pages, float* mass_pages, Pages pages,
                                                                int Hkv, int G, int max_evict, const int32_t* __restrict__ counts,
                                                                const uint2* __restrict__ moves)
 {
-    constexpr int ROWS = 256 / CH, AHEAD = 4;
+    constexpr int ROWS = 256 / CH;
     const int b = blockIdx.z, head = blockIdx.y >> 1, g = G > 1 ? head : 0, count = counts[b * G + g];
+    const bool tells = !(blockIdx.y & 1) && (G > 1 || head == 0);
     u32x4* rows = blockIdx.y & 1 ? v_pages : k_pages;
     const uint2* list = moves + (size_t)(b * G + g) * max_evict;
     const int sub = threadIdx.x % CH;
-    for (int i0 = blockIdx.x * (ROWS * AHEAD); i0 < count; i0 += gridDim.x * (ROWS * AHEAD)) {
-        uint2 move[AHEAD];
-        u32x4 x[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int i = i0 + u * ROWS + threadIdx.x / CH;
-            move[u] = i < count ? list[i] : make_uint2(~0u, ~0u);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (move[u].x != ~0u && move[u].y != ~0u) x[u] = __builtin_nontemporal_load(rows + pool_row(move[u].y, pages, Hkv, head) * CH + sub);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (move[u].x != ~0u && move[u].y != ~0u) rows[pool_row(move[u].x, pages, Hkv, head) * CH + sub] = x[u];
-    }
-    if ((blockIdx.y & 1) || (G == 1 && head)) return;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
+    for (int i = blockIdx.x * ROWS + threadIdx.x / CH; i < count; i += gridDim.x * ROWS) {
         const uint2 move = list[i];
-        if (move.x == ~0u || move.y == ~0u) continue;
-        const size_t to = pool_row(move.x, pages, G, g), from = pool_row(move.y, pages, G, g);
-        mass_pages[to] = mass_pages[from];
-        if (pos_pages) pos_pages[to] = pos_pages[from];
+        if (move.x == ~0u || move.y == ~0u) continue;  // on no page
+        const u32x4 x = __builtin_nontemporal_load(rows + pool_row(move.y, pages, Hkv, head) * CH + sub);
+        if (tells && sub == 0) {
+            const size_t to = pool_row(move.x, pages, G, g), from = pool_row(move.y, pages, G, g);
+            mass_pages[to] = mass_pages[from];
+            if (pos_pages) pos_pages[to] = pos_pages[from];
+        }
+        __builtin_nontemporal_store(x, rows + pool_row(move.x, pages, Hkv, head) * CH + sub);
     }
 }
 
@@ -370,10 +414,10 @@ int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float
     }
     hipLaunchKernelGGL(paged_evict_select_kernel, dim3(B * G), dim3(kEvictThreads), 0, stream, pos_pages, mass_pages, pages, goal, G, counts, moves);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
-    const int most = std::max(1, 4096 / (2 * Hkv * B));  // the lists' lengths are on the device: workgroups go over them
+    const int most = std::max(1, 8192 / (2 * Hkv * B));  // the lists' lengths are on the device: workgroups go over them
 #define EC_MOVE(CH_)                                                                                                                             \
     if (row_bytes == CH_ * 16)                                                                                                                   \
-        hipLaunchKernelGGL(paged_evict_move_kernel<CH_>, dim3(std::min((max_evict * CH_ + 1023) / 1024, most), 2 * Hkv, B), dim3(256), 0, stream, k, v, \
+        hipLaunchKernelGGL(paged_evict_move_kernel<CH_>, dim3(std::min((max_evict + 256 / CH_ - 1) / (256 / CH_), most), 2 * Hkv, B), dim3(256), 0, stream, k, v, \
                            pos_pages, mass_pages, pages, Hkv, G, max_evict, counts, moves)
     EC_MOVE(8);
     EC_MOVE(16);

@@ -4,6 +4,9 @@ prefill():  ec_prefill_score -> ec_select_anchors -> ec_merge_compact      (Sec.
 decode():   ec_evict_index (host) -> ec_decode_step                        (Sec. 3.3 Output Generation)
 extend():   ec_chunk_score -> ec_select_anchors -> ec_remerge_compact      (a later turn: chat history is
                                                                             compressed again with the new chunk)
+
+PagedBatch holds the compressed caches of sequences that come and go in pages of one pool per layer:
+admit() / store() -> begin() -> decode() or decode_scored() in every layer -> end(), shrink() when memory runs short, release()
 """
 from __future__ import annotations
 
@@ -74,3 +77,122 @@ class LayerState:
         self.k_cache, self.v_cache = k_next, v_next
         self.n_anchor = self.cache_len = n_new
         return n_new
+
+
+class PagedBatch:
+    """The caches of up to `places` sequences in pages, for all layers of a model: one pool of n_pages pages of `page` rows per layer and one page
+    table that the layers share.  The host keeps the free pages and the length of every sequence; nothing is read back from the device.
+
+        batch.admit([0, 1], [n_anchor, n_anchor], [T, T])        # two sequences get pages ...
+        for i, state in enumerate(layers):
+            batch.store(i, [0, 1], state.k_cache, state.v_cache, state.pos, mass)   # ... and their compressed prompts' rows
+        for q, k, v in generated_tokens:
+            batch.begin()                                        # room for a row
+            for i in range(n_layers):
+                batch.decode_scored(i, q[i], k[i], v[i], scale, out[i], keep)       # attention, masses, and the lightest row goes
+            batch.end(keep)
+        batch.shrink(keep // 2)                                  # all but the heaviest rows go, their pages are free
+    """
+
+    def __init__(self, layers, places, H, Hkv, D, page, n_pages, max_pages, dtype: torch.dtype, G=1, recent=25, protect_first=1, device="cuda"):
+        self.H, self.Hkv, self.D, self.G, self.page, self.max_pages = H, Hkv, D, G, page, max_pages
+        self.recent, self.protect_first = recent, protect_first
+        self.k_pages, self.v_pages = (torch.zeros((layers, n_pages, Hkv, page, D), dtype=dtype, device=device) for _ in range(2))
+        self.pos_pages = torch.zeros((layers, n_pages, G, page), dtype=torch.int32, device=device)
+        self.mass_pages = torch.zeros((layers, n_pages, G, page), dtype=torch.float32, device=device)
+        self.rows, self.seen = [-1] * places, [0] * places  # rows of every sequence, -1: no sequence; tokens seen
+        self.held = [[] for _ in range(places)]
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.table = torch.full((places, max_pages), -1, dtype=torch.int32, device=device)
+        # rows before the step, behind it, tokens seen before it and behind it
+        self.numbers = torch.zeros((4, places), dtype=torch.int32, device=device)
+        self.len_b, self.len_after, self.pos_b, self.seen_b = self.numbers
+        dt = ec.dtype_code(self.k_pages)
+        self.ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, places, H, max_pages * page, D, dt, device)
+        self.ws_one = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, places, G, 1, D, dt, device)
+        self._upload()
+
+    def _ints(self, x):
+        return torch.tensor(x, dtype=torch.int32, device=self.table.device)
+
+    def _upload(self):
+        self.numbers.copy_(self._ints([self.rows, [n + 1 for n in self.rows], self.seen, [n + 1 for n in self.seen]]))
+
+    def _hold(self, place, rows):
+        """Exactly the pages that `rows` rows need, taken from the free ones or given back to them."""
+        held, need = self.held[place], -(-rows // self.page)
+        if need > self.max_pages or need - len(held) > len(self.free):
+            raise ValueError(f"sequence {place}: {need} pages for {rows} rows, but {len(self.free)} are free and a sequence has {self.max_pages} at most")
+        if need == len(held):
+            return
+        while len(held) < need:
+            held.append(self.free.pop())
+        while len(held) > need:
+            self.free.append(held.pop())
+        self.table[place].copy_(self._ints(held + [-1] * (self.max_pages - need)))
+
+    def admit(self, places, rows, seen):
+        """Pages for sequences that start with `rows` rows of a prompt of `seen` tokens; store() brings the rows of every layer."""
+        for b in places:
+            if self.rows[b] >= 0:
+                raise ValueError(f"place {b} holds a sequence")
+        need = [-(-n // self.page) for n in rows]
+        if sum(need) > len(self.free) or max(need) > self.max_pages:
+            raise ValueError(f"{need} pages for {list(rows)} rows, but {len(self.free)} are free and a sequence has {self.max_pages} at most")
+        for b, n, t in zip(places, rows, seen):
+            self._hold(b, n)
+            self.rows[b], self.seen[b] = n, t
+        self._upload()
+
+    def release(self, place):
+        self._hold(place, 0)
+        self.rows[place], self.seen[place] = -1, 0
+        self._upload()
+
+    def store(self, layer, places, k, v, pos, mass):
+        """Rows 0.. of k, v [len(places),Hkv,n,D], pos and mass [len(places),G,n] as the sequences' rows (their first rows[place] ones)."""
+        ec.ec_paged_store(k, v, pos, mass, self.table[list(places)], self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer],
+                          self.mass_pages[layer], None, self._ints([self.rows[b] for b in places]))
+
+    def begin(self):
+        """Room for one more row of every sequence."""
+        for b, n in enumerate(self.rows):
+            if n >= 0:
+                self._hold(b, n + 1)
+
+    def decode(self, layer, q, k_new, v_new, scale, out):
+        """One layer of a token: append and attend (places without a sequence get zeros).  Masses are left alone, so that new rows have none of
+        their own: before shrink() they are stored, or the tokens take decode_scored()."""
+        ec.ec_paged_decode_step(q, k_new, v_new, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.table, self.len_b, self.pos_b,
+                                scale, out, self.ws)
+
+    def decode_scored(self, layer, q, k_new, v_new, scale, out, keep: int):
+        """One layer of a token under the frequency policy: append, attend, add to the masses, and a sequence of more than `keep` rows loses its
+        lightest."""
+        ec.ec_paged_decode_score_step(q, k_new, v_new, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer],
+                                      self.table, self.len_b, self.pos_b, scale, out, self.ws)
+        ec.ec_paged_evict_min(self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], self.table, self.len_after,
+                              torch.full_like(self.len_b, keep), self.seen_b, 1, self.protect_first, self.recent, self.ws_one)
+
+    def end(self, keep: int | None = None):
+        """Behind the last layer of a token; keep as in decode_scored, None after decode."""
+        for b, n in enumerate(self.rows):
+            if n >= 0:
+                self.rows[b] = n if keep is not None and n + 1 > keep else n + 1
+                self.seen[b] += 1
+        self._upload()
+
+    def shrink(self, keep: int):
+        """Sequences of more than `keep` rows keep the heaviest, in every layer; the pages behind are free."""
+        most = max(max(self.rows) - keep, 0)
+        if not most:
+            return
+        ws = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, len(self.rows), self.G, most, self.D, ec.dtype_code(self.k_pages), self.table.device)
+        for layer in range(self.k_pages.shape[0]):
+            ec.ec_paged_evict_min(self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], self.table, self.len_b,
+                                  torch.full_like(self.len_b, keep), self.pos_b, most, self.protect_first, self.recent, ws)
+        for b, n in enumerate(self.rows):
+            if n > keep:
+                self.rows[b] = keep
+                self._hold(b, keep)
+        self._upload()
