@@ -237,12 +237,13 @@ __global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(Paged
     const char* k_new = static_cast<const char*>(a.k_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
     const char* v_new = static_cast<const char*>(a.v_new) + ((size_t)at.b * a.Hkv + hk) * ROW;
 
-    // the new row's chunk of this lane (the first CH lanes have one)
+    // what storing the new row takes, asked for early: its page, its position, its chunk of this lane (the first CH lanes have one)
+    const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
+    const int new_page = table[n >> a.pages.shift], new_pos = a.pos_pages ? ((const const_i32*)(uintptr_t)a.new_pos_b)[at.b] : 0;
     const u32x4 new_k = reinterpret_cast<const u32x4*>(k_new)[lane % CH], new_v = reinterpret_cast<const u32x4*>(v_new)[lane % CH];
 
     // ------------------------------------------------------------------ rows into LDS
     const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles[wave]));
-    const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
     const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(n, at.last * ROUND);  // rows of the cache in the segment end there
     uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in the rows of a load instruction, K: of even and odd runs
 #pragma unroll
@@ -562,14 +563,13 @@ __global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(Paged
     l = head_sum(l);
     wait_loads();  // nothing more arrives in the tiles, whose place the sums take
     if (at.last * ROUND > n && block == 0 && wave == 0) {  // the new row; nobody reads its slot in this launch
-        const int id = table[n >> shift];
-        if ((unsigned)id < (unsigned)a.pages.n_pages) {
+        if ((unsigned)new_page < (unsigned)a.pages.n_pages) {
             if (lane < CH) {
-                const size_t to = a.pages.row(id, a.Hkv, hk, n) * CH + lane;
+                const size_t to = a.pages.row(new_page, a.Hkv, hk, n) * CH + lane;
                 static_cast<u32x4*>(a.k_pages)[to] = new_k;
                 static_cast<u32x4*>(a.v_pages)[to] = new_v;
             }
-            if (lane == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(id, a.G, a.G > 1 ? hk : 0, n)] = a.new_pos_b[at.b];
+            if (lane == 0 && a.pos_pages && (a.G > 1 || hk == 0)) a.pos_pages[a.pages.row(new_page, a.G, a.G > 1 ? hk : 0, n)] = new_pos;
         }
     }
     if (quarter == 0) sh_m[wave][c16] = m, sh_l[wave][c16] = l;
@@ -626,13 +626,19 @@ __global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(Paged
     static_assert(kMostSegments * kHeadBlock * 8 <= (int)sizeof(tiles), "all segments of a pair");
     // (segments behind the last one are behind the end of the buffer: nothing is fetched for them)
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)parts, 0, at.count * PART * 8, 0x00020000);
-    for (int i0 = tid; i0 < at.count * kHeadBlock; i0 += THREADS * AHEAD) {
+    u32x4 v[AHEAD];  // four sums of a head each, of as many segments
+    auto fetch = [&](int i, int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) v[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, ((s0 + u) * PART + kHeadBlock + i * 2) * 8, 0, kDeviceScope);
+    };
+    for (int i0 = tid; i0 < max(at.count * kHeadBlock, THREADS); i0 += THREADS * AHEAD) {  // (every thread goes round once)
         u32x2 x[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int i = i0 + u * THREADS, h = i % kHeadBlock;
             x[u] = __builtin_amdgcn_raw_buffer_load_b64(rsrc, h < heads ? (i / kHeadBlock * PART + h) * 8 : 0x7ffffff0, 0, kDeviceScope);
         }
+        if (i0 == tid) fetch(tid, 0);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (i0 + u * THREADS < at.count * kHeadBlock) weights[i0 + u * THREADS] = make_float2(__uint_as_float(x[u].x), __uint_as_float(x[u].y));
@@ -658,10 +664,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(Paged
         const int h = i / (D / 4);
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int s0 = 0; s0 < at.count; s0 += AHEAD) {
-            u32x4 v[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                v[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, ((s0 + u) * PART + kHeadBlock + i * 2) * 8, 0, kDeviceScope);
+            if (i != tid || s0) fetch(i, s0);  // the first have been asked for with the statistics
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
                 if (s0 + u < at.count) {
