@@ -387,8 +387,8 @@ int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B,
  *   page_table       DEVICE [B,max_pages] int32           mass_pages  DEVICE [n_pages,G,page] float, accumulated attention
  * and slot s of sequence b (0 <= s < max_pages * page) is row s % page of page page_table[b][s / page].  A cache is a SET of
  * rows in slots 0 .. len-1: attention does not see their order, positions go with them.  Common to the calls:
- *  - page is a power of two from 8 to 256, max_pages * page at most 2^28, n_pages * page below 2^32.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head
- *    h reads key/value head h / (H / Hkv).
+ *  - page is a power of two from 8 to 256, max_pages * page at most 2^28, n_pages * page below 2^32, a page of all heads of K below 4
+ *    GiB.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head h reads key/value head h / (H / Hkv).
  *  - Everything that changes from token to token is read on the device, so the calls can be captured and replayed.
  *  - A table entry outside 0 .. n_pages-1 names no page (entries behind a sequence's last page are not read at all): rows there are
  *    not read, not written and weigh nothing.  Pages that a call only reads may be shared by sequences (a common prefix); a
@@ -417,7 +417,8 @@ int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float
  *   2. out = softmax_j(scale * <q, k_j>) . v_j over rows 0 .. L of the query head's key/value head
  * Where L is outside 0 .. max_pages * page - 1 the place b of the batch holds no sequence: its out is zeros and nothing is stored.  The
  * new row always counts, also where the table names no page for it.  cache_len_b is read only (all layers share it).
- *   q,out          DEVICE [B,H,D] dt           k_new,v_new    DEVICE [B,Hkv,D] dt
+ *   q,out          DEVICE [B,H,D] dt; out must not overlap q, k_new or v_new
+ *   k_new,v_new    DEVICE [B,Hkv,D] dt
  *   pos_pages      may be NULL, new_pos_b then too
  *   cache_len_b,new_pos_b  DEVICE [B] int32
  *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_STEP, B,H, max_pages * page, D,dt); all zeros before its first

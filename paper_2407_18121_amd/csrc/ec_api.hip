@@ -436,6 +436,8 @@ bool aligned16(std::initializer_list<const void*> ptrs)
     return all % 16 == 0;
 }
 
+int row_bytes(int D, int dt) { return D * (dt == EC_BF16 ? 2 : 4); }
+
 // What every call on paged caches is checked for; EC_OK, and the pages then.
 int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int page, int n_pages, int max_pages, int dt, ec::Pages& pages)
 {
@@ -445,11 +447,10 @@ int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int pag
     if ((long long)n_pages * page >= 1LL << 32) return EC_EUNSUPPORTED;
     if ((long long)B * Hkv > 65535) return EC_EUNSUPPORTED;
     if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
+    if ((long long)Hkv * page * row_bytes(D, dt) >= 1LL << 32) return EC_EUNSUPPORTED;
     pages = {page_table, n_pages, max_pages, __builtin_ctz((unsigned)page)};
     return EC_OK;
 }
-
-int row_bytes(int D, int dt) { return D * (dt == EC_BF16 ? 2 : 4); }
 
 int paged_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages,
                const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv, int G, int D, int page,

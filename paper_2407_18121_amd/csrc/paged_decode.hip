@@ -29,6 +29,7 @@ typedef __attribute__((address_space(4))) const int32_t const_i32;  // read thro
 constexpr int kPagedWaves = 4;
 constexpr int kPagedSegments = 256;  // workgroups that a launch of few pairs aims at: one a compute unit
 constexpr int kWholeRounds = 3;       // a pair of so many rounds is not cut: 60, 120 rows of one sequence, H32 5.4, 5.9 us a step, joined 7.9
+constexpr int kLengths = 1024;        // of a batch that are held in LDS
 constexpr int kMostSegments = 256;   // of a pair, whose weights have to fit into LDS when they are joined
 constexpr int kHeadBlock = 16;       // query heads of a pair, at most
 constexpr float kSmallExponent = -100.f, kSmall = 0x1p-100f;  // probabilities below it are looked at apart
@@ -142,7 +143,7 @@ __device__ __forceinline__ Segment segment_of(int b, int n, int pair, int seg, i
     const int first = seg * each + min(seg, more);
     return {b, n, pair, first, first + each + (seg < more), count, split0 + seg, split0};
 }
-template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32_t* __restrict__ len_b, int B, int pairs, int slots, int id)
+template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32_t* __restrict__ len_b, int B, int pairs, int slots, int id, int* sh_len)
 {
     const int lane = threadIdx.x % kWave;
     if (B == 1) {  // nothing to look through
@@ -155,10 +156,15 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
         return segment_of(0, live ? n : -1, pair, seg, rounds, count, pair * count);
     }
     // rows before the step, or -1 for a place without a sequence, which has one round all the same (somebody has to write its zeros)
+    const bool kept = B > kWave && B <= kLengths;  // in LDS, as every wave looks through them twice
     auto rows = [&](int b) {
-        const int n = b < B ? len_b[b] : -1;
+        const int n = b >= B ? -1 : kept ? sh_len[b] : len_b[b];
         return n >= 0 && n < slots ? n : -1;
     };
+    if (kept) {
+        for (int i = threadIdx.x; i < B; i += blockDim.x) sh_len[i] = len_b[i];
+        __syncthreads();
+    }
     auto rounds_of = [&](int b, int n) { return b >= B ? 0 : n < 0 ? 1 : n / ROUND + 1; };
     // (loops over scalars, so that all lanes are there for what passes between lanes)
     int n = -1;
@@ -217,9 +223,10 @@ __global__ __launch_bounds__(kPagedWaves* kWave, 2) void paged_step_kernel(Paged
     __shared__ __align__(256) unsigned char tiles[WAVES][4 * T::BYTES];  // of every wave: two tiles of K, two of V
     __shared__ float sh_m[WAVES][kHeadBlock], sh_l[WAVES][kHeadBlock];
     __shared__ unsigned int sh_ticket;
+    __shared__ int sh_len[kLengths];
 
     const int slots = a.pages.slots();
-    const Segment at = find_segment<ROUND>(a.len_b, a.B, a.Hkv * a.blocks, slots, blockIdx.x);
+    const Segment at = find_segment<ROUND>(a.len_b, a.B, a.Hkv * a.blocks, slots, blockIdx.x, sh_len);
     if (at.b < 0) return;
     const int hk = a.blocks == 1 ? at.pair : at.pair / a.blocks, block = at.pair - hk * a.blocks, heads = min(a.group - block * kHeadBlock, kHeadBlock);
     const int head0 = hk * a.group + block * kHeadBlock;  // first query head

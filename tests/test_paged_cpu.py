@@ -36,13 +36,14 @@ SHAPE = [(dict(B=0), ec.EC_EINVAL), (dict(Hkv=0), ec.EC_EINVAL), (dict(G=2), ec.
          (dict(page=-16), ec.EC_EINVAL), (dict(n_pages=0), ec.EC_EINVAL), (dict(max_pages=0), ec.EC_EINVAL), (dict(table=None), ec.EC_EINVAL),
          (dict(page=24), ec.EC_EUNSUPPORTED), (dict(page=4), ec.EC_EUNSUPPORTED), (dict(page=512), ec.EC_EUNSUPPORTED),
          (dict(max_pages=1 << 27), ec.EC_EUNSUPPORTED), (dict(n_pages=1 << 28), ec.EC_EUNSUPPORTED), (dict(D=96), ec.EC_EUNSUPPORTED), (dict(dt=2), ec.EC_EUNSUPPORTED),
-         (dict(B=20000), ec.EC_EUNSUPPORTED), (dict(k_pages=ODD), ec.EC_EUNSUPPORTED), (dict(v_pages=ODD), ec.EC_EUNSUPPORTED)]
+         (dict(B=20000), ec.EC_EUNSUPPORTED), (dict(B=1, Hkv=65535, H=65535, page=256, dt=0), ec.EC_EUNSUPPORTED), (dict(k_pages=ODD), ec.EC_EUNSUPPORTED), (dict(v_pages=ODD), ec.EC_EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("other,status", SHAPE)
 def test_shapes_are_refused(other, status):
     for fn in ("ec_paged_decode_step", "ec_paged_decode_score_step"):
         assert _step(fn, **other) == status
+    other = {p: x for p, x in other.items() if p != "H"}
     assert _store(**other) == status
     assert _evict(**other) == status
 
