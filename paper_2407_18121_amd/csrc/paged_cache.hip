@@ -349,24 +349,45 @@ __global__ __launch_bounds__(256) void paged_evict_move_kernel(u32x4* k_pages, u
     }
 }
 
-// One row of every sequence, the step of a generation loop, in one launch: the workgroup that finds the least row fills its place.
+// One row of every sequence, the step of a generation loop, in one launch: the workgroup that finds the least row fills its place. Only the last row can be
+// the one that moves, so it is fetched while the least one is sought; what is left of the chain is length, table, masses, the reduction and the store.
 template <int CH>
 __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k_pages, u32x4* v_pages, int32_t* pos_pages, float* mass_pages, Pages pages,
                                                                         EvictGoal goal, int Hkv, int G)
 {
+    constexpr int HELD = 3;  // chunks of a thread that are fetched early: 48 heads of 512 bytes
     __shared__ unsigned long long sh_best[kEvictWaves];
+    __shared__ int sh_page;
     const EvictRows rows(pos_pages, mass_pages, pages, goal, G, blockIdx.x);
     const int n = rows.n, b = rows.b, tid = threadIdx.x;
     if (goal.victims(b, n) == 0) return;
     const int from = pages.page_of(b, n - 1);
+    const int heads = G > 1 ? 1 : Hkv, head0 = G > 1 ? rows.g : 0, chunks = heads * 2 * CH;
+    auto place = [&](int i, int id, int slot) {  // chunk i of the heads' K and V rows in a slot
+        return (i / CH & 1 ? v_pages : k_pages) + pages.row(id, Hkv, head0 + i / (2 * CH), slot) * CH + i % CH;
+    };
     unsigned long long best = ~0ull;  // (key, slot)
+    int page = -1;                    // of this thread's best
     for (int j = tid * kRun; j < n; j += kEvictThreads * kRun) {
         uint32_t key[kRun];
-        rows.keys(j, key);
+        const int id = rows.keys(j, key);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i)
-            if (j + i < n) best = min(best, (unsigned long long)key[i] << 32 | (uint32_t)(j + i));
+        for (int i = 0; i < kRun; ++i) {
+            const unsigned long long x = (unsigned long long)key[i] << 32 | (uint32_t)(j + i);
+            if (j + i < n && x < best) best = x, page = id;
+        }
     }
+    u32x4 row[HELD];
+    float mass = 0.f;
+    int pos = 0;
+    if (from >= 0) {
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+            if (tid + u * kEvictThreads < chunks) row[u] = *place(tid + u * kEvictThreads, from, n - 1);
+        mass = mass_pages[pages.row(from, G, rows.g, n - 1)];
+        if (pos_pages) pos = pos_pages[pages.row(from, G, rows.g, n - 1)];
+    }
+    const unsigned long long mine = best;
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
     if (tid % kWave == 0) sh_best[tid / kWave] = best;
@@ -374,18 +395,17 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
     best = sh_best[tid % kEvictWaves];
 #pragma unroll
     for (int off = 1; off < kEvictWaves; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
-    const int hole = (int)(uint32_t)best, to = pages.page_of(b, hole);
+    if (mine == best) sh_page = page;  // one thread's: slots differ
+    __syncthreads();
+    const int hole = (int)(uint32_t)best, to = sh_page;
     if (hole == n - 1 || to < 0 || from < 0) return;
-    const int heads = G > 1 ? 1 : Hkv, head0 = G > 1 ? rows.g : 0;
-    for (int i = tid; i < heads * 2 * CH; i += kEvictThreads) {
-        const int head = head0 + i / (2 * CH), c = i % CH;
-        u32x4* pool = i / CH & 1 ? v_pages : k_pages;
-        pool[pages.row(to, Hkv, head, hole) * CH + c] = pool[pages.row(from, Hkv, head, n - 1) * CH + c];
-    }
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+        if (tid + u * kEvictThreads < chunks) *place(tid + u * kEvictThreads, to, hole) = row[u];
+    for (int i = tid + HELD * kEvictThreads; i < chunks; i += kEvictThreads) *place(i, to, hole) = *place(i, from, n - 1);
     if (tid == 0) {
-        const size_t t = pages.row(to, G, rows.g, hole), f = pages.row(from, G, rows.g, n - 1);
-        mass_pages[t] = mass_pages[f];
-        if (pos_pages) pos_pages[t] = pos_pages[f];
+        mass_pages[pages.row(to, G, rows.g, hole)] = mass;
+        if (pos_pages) pos_pages[pages.row(to, G, rows.g, hole)] = pos;
     }
 }
 

@@ -700,12 +700,14 @@ __global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const
     const int heads = H / G, per = (heads + kMassWaves - 1) / kMassWaves, h0 = wave * per, h1 = min(h0 + per, heads);
     const size_t first = (size_t)b * H + g * heads;
     for (int j0 = blockIdx.x * kMassRows; j0 <= n; j0 += gridDim.x * kMassRows) {
-        const int j = j0 + lane;
+        const int j = j0 + lane, id = pages.page_of(b, min(j, n));
+        float* at = mass_pages + pages.row(max(id, 0), G, g, min(j, n));
+        const float old = *at;  // on its way with the scores
         float sum = 0.f;
         for (int h = h0; h < h1; h += kMassAhead) {
             float x[kMassAhead];
 #pragma unroll
-            for (int u = 0; u < kMassAhead; ++u) x[u] = h + u < h1 && j <= n ? raw[(first + h + u) * slots + j] : 0.f;
+            for (int u = 0; u < kMassAhead; ++u) x[u] = raw[(first + min(h + u, h1 - 1)) * slots + min(j, n)];
 #pragma unroll
             for (int u = 0; u < kMassAhead; ++u)
                 if (h + u < h1) {
@@ -715,15 +717,11 @@ __global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const
         }
         part[wave][lane] = sum;
         __syncthreads();
-        if (wave == 0 && j <= n) {
-            const int id = pages.page_of(b, j);
-            if (id >= 0) {
-                float all = part[0][lane];
+        if (wave == 0 && j <= n && id >= 0) {
+            float all = part[0][lane];
 #pragma unroll
-                for (int w = 1; w < kMassWaves; ++w) all += part[w][lane];
-                float* m = mass_pages + pages.row(id, G, g, j);
-                *m = (j == n ? 0.f : *m) + all / (float)heads;
-            }
+            for (int w = 1; w < kMassWaves; ++w) all += part[w][lane];
+            *at = (j == n ? 0.f : old) + all / (float)heads;
         }
         __syncthreads();
     }
