@@ -4,6 +4,7 @@
     python -m paper_2407_18121_amd.tune merge    # ec_merge_compact on three anchor distributions
     python -m paper_2407_18121_amd.tune select   # ec_select_anchors
     python -m paper_2407_18121_amd.tune score    # ec_prefill_score
+    python -m paper_2407_18121_amd.tune paged    # attention, storing and eviction over pages
 
 Every measurement replays one HIP graph that walks several distinct sets of buffers (so that nothing is served
 from a cache a real layer loop would not have), 100 ms of it before anything is timed, and reports microseconds per call by HIP
@@ -169,9 +170,76 @@ def tune_score():
         print(f"score {name}: {ms * 1e3:9.1f} us {3.0 * D * T * (T + 1) * B * H / (ms * 1e-3) / 1e12:7.1f} TFLOP/s", flush=True)
 
 
+def paged_timer(B, H, Hkv, D, rows, page, dtype=BF16, sets=8, G=1):
+    """us per call of ec_paged_decode_step, of ec_paged_decode_score_step with the removal of one row, and of storing `rows` rows, over caches of
+    `rows` rows in pages of any order; GB/s of the rows' bytes in the first and of both ways in the last."""
+    per = rows // page + 1
+    n_pages = B * per
+    k, v = (torch.randn(sets, n_pages, Hkv, page, D, device="cuda").to(dtype) for _ in range(2))
+    table = torch.randperm(n_pages, device="cuda").to(torch.int32).view(B, per)
+    pos, mass = torch.zeros(sets, n_pages, G, page, dtype=torch.int32, device="cuda"), torch.rand(sets, n_pages, G, page, device="cuda")
+    q, kn, vn = (torch.randn(B, h, D, device="cuda").to(dtype) for h in (H, Hkv, Hkv))
+    out, n, one = torch.empty_like(q), torch.full((B,), rows, dtype=torch.int32, device="cuda"), torch.full((B,), rows + 1, dtype=torch.int32, device="cuda")
+    dt = ec.dtype_code(q)
+    ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, B, H, per * page, D, dt)
+    ws_one = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, B, G, 1, D, dt)
+    src, spos, smass = torch.randn(B, Hkv, rows, D, device="cuda").to(dtype), torch.zeros(B, G, rows, dtype=torch.int32, device="cuda"), torch.rand(B, G, rows, device="cuda")
+
+    def step():
+        for i in range(sets):
+            ec.ec_paged_decode_step(q, kn, vn, k[i], v[i], pos[i], table, n, n, 0.088, out, ws)
+
+    def scored():
+        for i in range(sets):
+            ec.ec_paged_decode_score_step(q, kn, vn, k[i], v[i], pos[i], mass[i], table, n, n, 0.088, out, ws)
+            ec.ec_paged_evict_min(k[i], v[i], pos[i], mass[i], table, one, n, one, 1, 1, 25, ws_one)
+
+    def store():
+        for i in range(sets):
+            ec.ec_paged_store(src, src, spos, smass, table, k[i], v[i], pos[i], mass[i])
+
+    us = [graph_time_ms(f) * 1e3 / sets for f in (step, scored, store)]
+    rows_bytes = 2 * B * Hkv * D * k.element_size() * rows
+    return us, rows_bytes / us[0] / 1e3, 2 * rows_bytes / us[2] / 1e3
+
+
+def time_paged_evict(B, Hkv, D, rows, keep, page, sets=4, G=1):
+    """us per call of ec_paged_evict_min, the masses written anew before every call (their copy is timed by itself and taken off)."""
+    per = rows // page + 1
+    k, v = (torch.randn(sets, B * per, Hkv, page, D, device="cuda").to(BF16) for _ in range(2))
+    table = torch.randperm(B * per, device="cuda").to(torch.int32).view(B, per)
+    fresh = torch.rand(B * per, G, page, device="cuda")
+    mass, n, kept = fresh.clone().expand(sets, -1, -1, -1).contiguous(), torch.full((B,), rows, dtype=torch.int32, device="cuda"), torch.full((B,), keep, dtype=torch.int32, device="cuda")
+    ws = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, B, G, rows - keep, D, ec.EC_BF16)
+
+    def copies():
+        for i in range(sets):
+            mass[i].copy_(fresh)
+
+    def evict():
+        for i in range(sets):
+            mass[i].copy_(fresh)
+            ec.ec_paged_evict_min(k[i], v[i], None, mass[i], table, n, kept, None, rows - keep, 0, 0, ws)
+
+    return (graph_time_ms(evict) - graph_time_ms(copies)) * 1e3 / sets
+
+
+def tune_paged():
+    print("shape: us of a step | its rows' TB/s | a step with masses and the removal of a row | storing the rows | TB/s read and written")
+    for B, H, Hkv, D, rows, page, dtype in ((1, 4, 4, 64, 100, 16, torch.float32), (1, 32, 32, 128, 640, 16, BF16), (1, 32, 8, 128, 2048, 16, BF16),
+                                            (8, 32, 8, 128, 1500, 16, BF16), (8, 32, 32, 128, 1000, 16, torch.float32), (16, 32, 32, 128, 870, 16, BF16),
+                                            (16, 32, 32, 128, 870, 64, BF16), (8, 32, 32, 64, 1000, 16, BF16), (64, 32, 8, 128, 1000, 16, BF16),
+                                            (1, 40, 8, 128, 131072, 64, BF16)):
+        us, gbps, copy = paged_timer(B, H, Hkv, D, rows, page, dtype, 8 if rows < 10000 else 2)
+        name = f"B{B} H{H}/{Hkv} D{D} {rows} rows, pages of {page}, {'bf16' if dtype == BF16 else 'fp32'}"
+        print(f"{name}: {us[0]:8.2f} | {gbps / 1e3:5.2f} | {us[1]:8.2f} | {us[2]:8.2f} | {copy / 1e3:5.2f}", flush=True)
+    for B, Hkv, rows, keep in ((1, 32, 640, 512), (8, 8, 3000, 1000), (16, 32, 8192, 820), (16, 32, 8192, 8000)):
+        print(f"eviction B{B} Hkv{Hkv} D128 {rows} -> {keep} rows, pages of 16: {time_paged_evict(B, Hkv, 128, rows, keep, 16):8.2f} us", flush=True)
+
+
 def main(argv):
     what = argv[1] if len(argv) > 1 else ""
-    table = {"decode": tune_decode, "merge": tune_merge, "select": tune_select, "score": tune_score}
+    table = {"decode": tune_decode, "merge": tune_merge, "select": tune_select, "score": tune_score, "paged": tune_paged}
     if what not in table:
         print(__doc__)
         return 2
