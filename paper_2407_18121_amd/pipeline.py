@@ -131,13 +131,23 @@ class PagedBatch:
             self.free.append(held.pop())
         self.table[place].copy_(self._ints(held + [-1] * (self.max_pages - need)))
 
+    def _places(self, places):
+        """Places of the batch, each named once."""
+        places = list(places)
+        if len(set(places)) != len(places) or any(not 0 <= b < len(self.rows) for b in places):
+            raise ValueError(f"{places} are not different places of 0 .. {len(self.rows) - 1}")
+        return places
+
     def admit(self, places, rows, seen):
         """Pages for sequences that start with `rows` rows of a prompt of `seen` tokens; store() brings the rows of every layer."""
+        places = self._places(places)
+        if not len(places) == len(rows) == len(seen) or any(n < 0 for n in rows):
+            raise ValueError(f"places {places}, rows {list(rows)} and seen {list(seen)} do not belong together")
         for b in places:
             if self.rows[b] >= 0:
                 raise ValueError(f"place {b} holds a sequence")
         need = [-(-n // self.page) for n in rows]
-        if sum(need) > len(self.free) or max(need) > self.max_pages:
+        if sum(need) > len(self.free) or max(need, default=0) > self.max_pages:
             raise ValueError(f"{need} pages for {list(rows)} rows, but {len(self.free)} are free and a sequence has {self.max_pages} at most")
         for b, n, t in zip(places, rows, seen):
             self._hold(b, n)
@@ -145,13 +155,17 @@ class PagedBatch:
         self._upload()
 
     def release(self, place):
+        self._places([place])
         self._hold(place, 0)
         self.rows[place], self.seen[place] = -1, 0
         self._upload()
 
     def store(self, layer, places, k, v, pos, mass):
         """Rows 0.. of k, v [len(places),Hkv,n,D], pos and mass [len(places),G,n] as the sequences' rows (their first rows[place] ones)."""
-        ec.ec_paged_store(k, v, pos, mass, self.table[list(places)], self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer],
+        places = self._places(places)
+        if any(self.rows[b] > k.shape[2] for b in places):
+            raise ValueError(f"{k.shape[2]} rows for sequences of {[self.rows[b] for b in places]}")
+        ec.ec_paged_store(k, v, pos, mass, self.table[places], self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer],
                           self.mass_pages[layer], None, self._ints([self.rows[b] for b in places]))
 
     def begin(self):
@@ -176,6 +190,8 @@ class PagedBatch:
 
     def end(self, keep: int | None = None):
         """Behind the last layer of a token; keep as in decode_scored, None after decode."""
+        if any(n >= len(held) * self.page for n, held in zip(self.rows, self.held)):
+            raise ValueError("a token ends, but begin() has not made room for its row")
         for b, n in enumerate(self.rows):
             if n >= 0:
                 self.rows[b] = n if keep is not None and n + 1 > keep else n + 1
@@ -184,6 +200,8 @@ class PagedBatch:
 
     def shrink(self, keep: int):
         """Sequences of more than `keep` rows keep the heaviest, in every layer; the pages behind are free."""
+        if keep < 0:
+            raise ValueError(f"keep is {keep}")
         most = max(max(self.rows) - keep, 0)
         if not most:
             return

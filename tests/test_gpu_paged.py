@@ -330,6 +330,9 @@ EVICTS = [  # dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent
     ("bf16", 64, 1, 1, 256, [5000], [17], 3000, 4, 100),          # the cap on what may go is reached
     ("bf16", 64, 1, 1, 8, [20, 20], [3, 10], 20, 30, 500),        # more protected than kept
     ("f32", 64, 1, 1, 256, [70001], [30000], 65000, 1, 25),
+    ("bf16", 64, 1, 1, 128, [32768], [20000], 12768, 3, 50),
+    ("bf16", 64, 1, 1, 64, [8193], [8000], 1000, 1, 25),
+    ("bf16", 128, 1, 1, 32, [40009], [40008], 1, 1, 25),
 ]
 
 

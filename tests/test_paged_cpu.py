@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2407_18121_amd import binding as ec
+from paper_2407_18121_amd.pipeline import PagedBatch
 
 ONE, ODD = ctypes.c_void_p(256), ctypes.c_void_p(264)  # never dereferenced: validation fails first
 
@@ -160,3 +161,31 @@ def test_binding_refuses_what_does_not_fit():
         store(mass=torch.zeros((B, 1, 4)), mass_pages=mass)
     with pytest.raises(ValueError, match="pos_pages is required"):
         store(pos=torch.zeros((B, 1, 5), dtype=i32))
+
+
+def test_places_and_pages_of_a_batch():
+    """What PagedBatch keeps on the host: pages taken and given back, and what it refuses without changing anything."""
+    batch = PagedBatch(1, 3, 4, 2, 64, 16, 8, 3, torch.float32, device="cpu")
+    batch.admit([2, 0], [17, 0], [40, 0])
+    assert batch.rows == [0, -1, 17] and [len(h) for h in batch.held] == [0, 0, 2] and len(batch.free) == 6
+    state = lambda: (list(batch.rows), list(batch.seen), [list(h) for h in batch.held], list(batch.free), batch.table.tolist())
+    before = state()
+    for places, rows, seen in (([1, 1], [5, 5], [5, 5]), ([-2], [5], [5]), ([3], [5], [5]), ([1], [5, 6], [5, 6]), ([1], [-1], [5]), ([1], [49], [49]),
+                               ([2], [5], [5])):
+        with pytest.raises(ValueError):
+            batch.admit(places, rows, seen)
+    x = torch.zeros(1, 2, 16, 64)
+    for places in ([2], [-1], [3]):  # 17 rows, but 16 given; no such places
+        with pytest.raises(ValueError):
+            batch.store(0, places, x, x, torch.zeros(1, 1, 16, dtype=torch.int32), torch.zeros(1, 1, 16))
+    for call in (lambda: batch.release(-1), lambda: batch.shrink(-1), batch.end):  # end(): no room has been made for a token
+        with pytest.raises(ValueError):
+            call()
+    assert state() == before
+    batch.admit([], [], [])
+    batch.begin()
+    assert [len(h) for h in batch.held] == [1, 0, 2] and state()[4][0][0] == batch.held[0][0]
+    batch.end()
+    assert batch.rows == [1, -1, 18] and batch.seen == [1, 0, 41] and batch.len_b.tolist() == [1, -1, 18] and batch.len_after.tolist() == [2, 0, 19]
+    batch.release(2)
+    assert batch.table[2].tolist() == [-1] * 3 and len(batch.free) == 7
