@@ -417,7 +417,7 @@ int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float
  *   2. out = softmax_j(scale * <q, k_j>) . v_j over rows 0 .. L of the query head's key/value head
  * Where L is outside 0 .. max_pages * page - 1 the place b of the batch holds no sequence: its out is zeros and nothing is stored.  The
  * new row always counts, also where the table names no page for it.  cache_len_b is read only (all layers share it).
- *   q,out          DEVICE [B,H,D] dt; out must not overlap q, k_new or v_new
+ *   q,out          DEVICE [B,H,D] dt; out must not overlap q, k_new or v_new (EC_EINVAL)
  *   k_new,v_new    DEVICE [B,Hkv,D] dt
  *   pos_pages      may be NULL, new_pos_b then too
  *   cache_len_b,new_pos_b  DEVICE [B] int32

@@ -464,6 +464,10 @@ int paged_step(const void* q, const void* k_new, const void* v_new, void* k_page
     if (const int rc = paged_shape(page_table, B, Hkv, G, D, page, n_pages, max_pages, dt, pages)) return rc;
     if ((long long)B * H > 65535 || !aligned16({q, k_new, v_new, k_pages, v_pages, out})) return EC_EUNSUPPORTED;
     if (!ws || ws_bytes < ec_workspace_bytes(fn, B, H, pages.slots(), D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
+    // out is written while other workgroups still read what comes in
+    const uintptr_t head = (size_t)row_bytes(D, dt) * B, o = (uintptr_t)out, qs = (uintptr_t)q, ks = (uintptr_t)k_new, vs = (uintptr_t)v_new;
+    auto overlap = [&](uintptr_t in, int heads) { return in < o + head * H && o < in + head * heads; };
+    if (overlap(qs, H) || overlap(ks, Hkv) || overlap(vs, Hkv)) return EC_EINVAL;
     return ec::paged_step_dispatch(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, pages, cache_len_b, new_pos_b, B, H, Hkv, G, D, scale, dt,
                                    out, ws, reinterpret_cast<hipStream_t>(stream));
 }

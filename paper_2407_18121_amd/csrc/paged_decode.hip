@@ -6,6 +6,12 @@
 //   O^T += V^T . P^T   the probabilities are the second operand as they stand; V is transposed on its way out of LDS (bf16)
 // Every row of K and V is read once for all query heads of its head, straight from its page into LDS; a tile is in flight while the
 // one before it is used.  The new row takes part as the last row of the last tile and is stored by that tile's workgroup.
+// The segments' results meet by the rule of the softmax: with M the largest of their maxima m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
+//
+// Bound by the bytes of the rows, of which the counters see 1.002 .. 1.003 times what has to be read (a large copy on this card moves 5.0 .. 5.5 TB/s):
+//   bf16 D128 B16 H32/32 870 rows 39.0 us, 5.9 TB/s; one cache of 131071 rows, H40/8 89.3, 6.0; fp32 B8 H32/32 1000 rows 48.9, 5.4.
+// Short caches by a chain of latencies, 8 us of B1 H32/32 640 rows: lengths and pages 0.6, first rows 1.1, a tile 0.8 and 0.5 for each further one,
+// the waves' results 1.0, the ticket 0.5, the other segments' results 2.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -26,7 +32,7 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 typedef __attribute__((address_space(4))) const int32_t const_i32;  // read through the scalar cache: nothing that a launch writes
 
-constexpr int kPagedWaves = 4;
+constexpr int kPagedWaves = 4;         // with 2: 41.1, one long cache 110 us
 constexpr int kPagedSegments = 256;  // workgroups that a launch of few pairs aims at: one a compute unit
 constexpr int kWholeRounds = 3;       // a pair of so many rounds is not cut: 60, 120 rows of one sequence, H32 5.4, 5.9 us a step, joined 7.9
 constexpr int kLengths = 1024;        // of a batch that are held in LDS
@@ -64,7 +70,7 @@ struct PagedStep {
 };
 
 // N load instructions of consecutive rows into consecutive LDS (see load_lds_16): the instruction's offset moves both by 1 KB. The non-temporal hint
-// keeps data that is read once from displacing cache lines (B16 H32 870 rows 46.8 -> 42.3 us a step, one cache of 131071 rows 105 -> 91).
+// keeps data that is read once from displacing cache lines (B16 H32 870 rows 39.0 us a step, 44.1 without; one cache of 131071 rows 89.3, 100.5).
 template <int N> __device__ __forceinline__ void load_run_lds(u32x4 rsrc, uint32_t lds, const uint32_t* offset)
 {
     if constexpr (N == 1)
@@ -84,7 +90,9 @@ template <int DT, int D> struct PagedTile {
     static constexpr int kRowBytes = D * Elem<DT>::kBytes;
     static constexpr int CH = kRowBytes / 16;      // 16-byte chunks of a row
     static constexpr int RPI = kWave / CH;         // rows of a load instruction
-    static constexpr int TR = kHalf && D < 128 ? 32 : 16;  // rows of a tile
+    // Rows of a tile: 32 KB of tiles a wave and more leave a compute unit one workgroup (B16 H32 D128 870 rows 39.0 us with 16, 44.2 with 32); shorter
+    // rows have the room, and 32 of them fill the matrix instruction of 32 (B8 H32 D64 1000 rows 15.4 us, 16.6 with 16)
+    static constexpr int TR = kHalf && D < 128 ? 32 : 16;
     static constexpr int GROUPS = TR / 8;          // runs of 8 rows, which lie in one page
     static constexpr int IPG = 8 / RPI;            // load instructions of a run
     static constexpr int NI = GROUPS * IPG;        // of a tile of K or V
@@ -629,7 +637,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
     __syncthreads();
     if (sh_ticket != (unsigned)at.count - 1) return;
     const unsigned long long* parts = a.partials + (size_t)at.split0 * PART;
-    constexpr int THREADS = WAVES * kWave, AHEAD = 8;  // loads in flight: each comes from beyond the caches
+    constexpr int THREADS = WAVES * kWave, AHEAD = 8;  // loads in flight: each comes from beyond the caches (16: B1 H32 641 rows 9.7 us instead of 8.9)
     float2* weights = reinterpret_cast<float2*>(tiles[0]);  // [segment][head]: (maximum, sum), then the first is the weight
     static_assert(kMostSegments * kHeadBlock * 8 <= (int)sizeof(tiles), "all segments of a pair");
     // (segments behind the last one are behind the end of the buffer: nothing is fetched for them)

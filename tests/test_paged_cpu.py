@@ -189,3 +189,14 @@ def test_places_and_pages_of_a_batch():
     assert batch.rows == [1, -1, 18] and batch.seen == [1, 0, 41] and batch.len_b.tolist() == [1, -1, 18] and batch.len_after.tolist() == [2, 0, 19]
     batch.release(2)
     assert batch.table[2].tolist() == [-1] * 3 and len(batch.free) == 7
+
+
+@pytest.mark.parametrize("fn", ["ec_paged_decode_step", "ec_paged_decode_score_step"])
+def test_outputs_over_inputs_are_refused(fn):
+    code = ec.EC_FN_PAGED_DECODE_STEP if fn == "ec_paged_decode_step" else ec.EC_FN_PAGED_DECODE_SCORE_STEP
+    need = ec.ec_workspace_bytes(code, 2, 8, 64, 128, ec.EC_BF16)
+    at = {p: 1 << 20 << i for i, p in enumerate(("out", "q", "k_new", "v_new"))}
+    for p, rows in (("q", 16), ("k_new", 8), ("v_new", 8)):  # out has 16 rows of 256 bytes
+        for off in (0, 16, 15 * 256, -16, -(rows * 256 - 16)):
+            x = {k: ctypes.c_void_p(v) for k, v in {**at, p: at["out"] + off}.items()}
+            assert _step(fn, ws_bytes=need, **x) == ec.EC_EINVAL, (p, off)
