@@ -136,29 +136,51 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x_)
     return (uint32_t)x;
 }
 
+// The smallest, the largest over the wave's lanes.
+template <bool LARGEST> __device__ __forceinline__ uint32_t wave_end(uint32_t x)
+{
+    constexpr int NONE = LARGEST ? 0 : -1;
+    auto step = [&](uint32_t y) __attribute__((always_inline)) { x = LARGEST ? max(x, y) : min(x, y); };
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x111, 0xf, 0xf, false));  // (the lanes as in wave_scan)
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(NONE, (int)x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane((int)x, kWave - 1);
+}
+// The smallest (key, slot) over the wave's lanes.
+__device__ __forceinline__ unsigned long long wave_least(unsigned long long x)
+{
+    const uint32_t hi = wave_end<false>((uint32_t)(x >> 32));
+    return (unsigned long long)hi << 32 | wave_end<false>((uint32_t)(x >> 32) == hi ? (uint32_t)x : ~0u);
+}
+
 // Sum over the threads before this one, and the sum over all of them in `total`. `sh`: a place of its own for every call between two barriers.
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sh, uint32_t& total)
+template <int WAVES> __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sh, uint32_t& total)
 {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const uint32_t in = wave_scan(x);
     if (lane == kWave - 1) sh[wave] = in;
     __syncthreads();
-    const uint32_t sums = wave_scan(lane < kEvictWaves ? sh[lane] : 0);
-    total = __builtin_amdgcn_readlane(sums, kEvictWaves - 1);
+    const uint32_t sums = wave_scan(lane < WAVES ? sh[lane] : 0);
+    total = __builtin_amdgcn_readlane(sums, WAVES - 1);
     const uint32_t before = __builtin_amdgcn_readlane(sums, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
     return (wave ? before : 0) + in - x;
 }
 
 // One workgroup per (sequence, score group): which rows go, and the list of moves. A thread holds runs of 8 consecutive slots. Sought is the gone-th
 // smallest (key, slot): digit by digit, 8 bits at a time from the highest bit in which two keys differ (masses share their upper bits, and a histogram
-// of those is one counter that all lanes wait for), until at most 64 rows share the digits found, which every wave ranks. HELD: keys stay in
-// registers, for sequences of up to 8192 rows; longer ones are read again for every digit. Bound: a chain of latencies (length, table, masses, a barrier
-// or two for each digit); by the profiler 16 groups of 8192 rows 67 us with digits sought by one thread and keys read again, now 10.
-template <bool HELD> __device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list)
+// of those is one counter that all lanes wait for), until at most 64 rows share the digits found, which the waves rank, a share of the
+// comparisons each (all in every wave: 1500 rows 8.2 us instead of 6.0). HELD: keys stay in registers, for sequences of up to 8192 rows; longer ones are
+// read again for every digit. Bound: a chain of latencies (length, table, masses, a barrier or two for each digit); 16 groups of 8192 rows 67 us with
+// digits sought by one thread and keys read again, now 10.
+template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list)
 {
     // a counter has a copy for every eighth lane, in banks of their own
     __shared__ __align__(16) uint32_t hist[4][kCopies][kCopyWords];
-    __shared__ uint32_t sh[3][kEvictWaves], sh_lo[kEvictWaves], sh_hi[kEvictWaves], n_few, sh_slot;
+    constexpr int WAVES = THREADS / kWave;
+    __shared__ uint32_t sh[3][WAVES], sh_lo[WAVES], sh_hi[WAVES], ranks[kWave], n_few, sh_slot;
     __shared__ unsigned long long few[kWave];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = rows.n, m = n - gone;
     const int runs = (n + kRun - 1) / kRun;
@@ -170,14 +192,15 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
         if constexpr (HELD) {
             f(tid * kRun, held, held_page);
         } else {
-            for (int r0 = 0; r0 < runs; r0 += kEvictThreads) {  // all threads in every round
+            for (int r0 = 0; r0 < runs; r0 += THREADS) {  // all threads in every round
                 uint32_t key[kRun];
                 const int page = rows.keys((r0 + tid) * kRun, key);
                 f((r0 + tid) * kRun, key, page);
             }
         }
     };
-    for (int i = tid; i < (int)(sizeof(hist) / 16); i += kEvictThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < (int)(sizeof(hist) / 16); i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    if (tid < kWave) ranks[tid] = 0;
     if (tid == 0) n_few = 0, sh_slot = 0;
     // how many rows are not protected, and the bits in which their keys differ
     uint32_t lo = kProtected, hi = 0, open = 0;
@@ -185,13 +208,11 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
 #pragma unroll
         for (int i = 0; i < kRun; ++i) lo = min(lo, key[i]), hi = max(hi, key[i] == kProtected ? 0u : key[i]), open += key[i] != kProtected;
     });
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, off, kWave)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, off, kWave));
+    lo = wave_end<false>(lo), hi = wave_end<true>(hi);
     if (lane == 0) sh_lo[wave] = lo, sh_hi[wave] = hi;
     uint32_t all_open;
-    block_scan(open, sh[0], all_open);
-#pragma unroll
-    for (int w = 0; w < kEvictWaves; ++w) lo = min(lo, sh_lo[w]), hi = max(hi, sh_hi[w]);
+    block_scan<WAVES>(open, sh[0], all_open);
+    lo = wave_end<false>(sh_lo[lane % WAVES]), hi = wave_end<true>(sh_hi[lane % WAVES]);
 
     // Victims are the rows up to `limit` in the order of (key, slot). Where only their key is known, last, and how many rows have it and go, need, the
     // slot is looked for behind.
@@ -250,9 +271,11 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
                 });
                 __syncthreads();
                 const unsigned long long mine = few[lane];
-                uint32_t rank = 0;
-                for (uint32_t i = 0; i < count; ++i) rank += few[i] < mine;
-                const unsigned long long found = __ballot((uint32_t)lane < count && rank == need - 1);
+                uint32_t smaller = 0;  // a wave's share
+                for (uint32_t i = wave; i < count; i += WAVES) smaller += few[i] < mine;
+                if (smaller) atomicAdd(&ranks[lane], smaller);
+                __syncthreads();
+                const unsigned long long found = __ballot((uint32_t)lane < count && ranks[lane] == need - 1);
                 const int who = found ? __ffsll(found) - 1 : 0;
                 limit = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), who) << 32 |
                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, who);
@@ -266,7 +289,7 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
             uint32_t mine = 0, total;
 #pragma unroll
             for (int i = 0; i < kRun; ++i) mine += j + i < n && key[i] == last;
-            uint32_t rank = before + block_scan(mine, sh[1], total);
+            uint32_t rank = before + block_scan<WAVES>(mine, sh[1], total);
             before += total;
 #pragma unroll
             for (int i = 0; i < kRun; ++i)
@@ -287,7 +310,7 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
             flags |= (uint32_t)hole << i | (uint32_t)mover << (8 + i);
             both += (uint32_t)hole | (uint32_t)mover << 16;
         }
-        uint32_t at = block_scan(both, sh[2], total);
+        uint32_t at = block_scan<WAVES>(both, sh[2], total);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             const uint32_t row = page < 0 ? ~0u : ((uint32_t)page << rows.pages.shift) + ((j + i) & (rows.pages.page() - 1));
@@ -302,7 +325,8 @@ template <bool HELD> __device__ __forceinline__ void select_victims(const EvictR
     if (tid == 0) *counts = min(min(holes, movers), (uint32_t)gone);  // equal, unless masses change while they are read
 }
 
-__global__ __launch_bounds__(kEvictThreads) void paged_evict_select_kernel(const int32_t* __restrict__ pos_pages, const float* __restrict__ mass_pages,
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_evict_select_kernel(const int32_t* __restrict__ pos_pages, const float* __restrict__ mass_pages,
                                                                            Pages pages, EvictGoal goal, int G, int32_t* __restrict__ counts,
                                                                            uint2* __restrict__ moves)
 {
@@ -313,8 +337,9 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_select_kernel(const
         return;
     }
     uint2* list = moves + (size_t)blockIdx.x * goal.max_evict;
-    if (rows.n <= kEvictThreads * kRun) select_victims<true>(rows, gone, counts + blockIdx.x, list);
-    else select_victims<false>(rows, gone, counts + blockIdx.x, list);
+    // fewer than kEvictThreads only where the table ends before
+    if (THREADS < kEvictThreads || rows.n <= kEvictThreads * kRun) select_victims<THREADS, true>(rows, gone, counts + blockIdx.x, list);
+    else select_victims<THREADS, false>(rows, gone, counts + blockIdx.x, list);
 }
 
 // A row number of the list (page and row in it) in a pool of `heads` heads.
@@ -388,13 +413,10 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
         if (pos_pages) pos = pos_pages[pages.row(from, G, rows.g, n - 1)];
     }
     const unsigned long long mine = best;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
+    best = wave_least(best);
     if (tid % kWave == 0) sh_best[tid / kWave] = best;
     __syncthreads();
-    best = sh_best[tid % kEvictWaves];
-#pragma unroll
-    for (int off = 1; off < kEvictWaves; off <<= 1) best = min(best, __shfl_xor(best, off, kWave));
+    best = wave_least(sh_best[tid % kEvictWaves]);
     if (mine == best) sh_page = page;  // one thread's: slots differ
     __syncthreads();
     const int hole = (int)(uint32_t)best, to = sh_page;
@@ -432,7 +454,16 @@ int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float
 #undef EC_ONE
         return status_from_hip(hipGetLastError());
     }
-    hipLaunchKernelGGL(paged_evict_select_kernel, dim3(B * G), dim3(kEvictThreads), 0, stream, pos_pages, mass_pages, pages, goal, G, counts, moves);
+    // Threads for the rows that the tables have room for: fewer waves do less twice and meet sooner (us of a call that moves few bytes, 640 rows 6.4 with
+    // 1024 threads and 5.6 with 256, 24 groups of 3001 9.9 and with 512 8.9).
+    const int threads = pages.slots() <= 256 * kRun ? 256 : pages.slots() <= 512 * kRun ? 512 : kEvictThreads;
+#define EC_SELECT(THREADS_)   \
+    if (threads == THREADS_)  \
+        hipLaunchKernelGGL(paged_evict_select_kernel<THREADS_>, dim3(B * G), dim3(THREADS_), 0, stream, pos_pages, mass_pages, pages, goal, G, counts, moves)
+    EC_SELECT(256);
+    EC_SELECT(512);
+    EC_SELECT(kEvictThreads);
+#undef EC_SELECT
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     const int most = std::max(1, 8192 / (2 * Hkv * B));  // the lists' lengths are on the device: workgroups go over them
 #define EC_MOVE(CH_)                                                                                                                             \
