@@ -152,13 +152,20 @@ __device__ __forceinline__ Segment segment_of(int b, int n, int pair, int seg, i
     const int first = seg * each + min(seg, more);
     return {b, n, pair, first, first + each + (seg < more), count, split0 + seg, split0};
 }
+// Segments that a pair of so many rounds is cut into at most. A few rounds are not cut, others as far as one round each while there are few of them (us a
+// step, against segments of three rounds at least: two sequences, H8/2, fp32 D64, 374 rows 7.4 / 9.0, 758 8.3 / 9.0; bf16 D128 374 rows 8.1 / 9.5; with
+// segments of one round everywhere 2550 rows 10.8, now 10.1).
+__device__ __forceinline__ int most_segments(int rounds)
+{
+    return rounds <= kWholeRounds ? min(rounds, 1) : min(min(rounds, max(rounds / 2, 16)), kMostSegments);
+}
 template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32_t* __restrict__ len_b, int B, int pairs, int slots, int id, int* sh_len)
 {
     const int lane = threadIdx.x % kWave;
     if (B == 1) {  // nothing to look through
         const int n = ((const const_i32*)(uintptr_t)len_b)[0];
         const bool live = n >= 0 && n < slots;
-        const int rounds = live ? n / ROUND + 1 : 1, count = min(min(rounds, kMostSegments), min(max(scalar(divided(kPagedSegments, pairs)), 1), rounds <= kWholeRounds ? 1 : max(rounds / 2, 16)));
+        const int rounds = live ? n / ROUND + 1 : 1, count = min(max(scalar(divided(kPagedSegments, pairs)), 1), most_segments(rounds));
         const int seg = scalar(divided(id, pairs));
         if (seg >= count) return {-1, 0, 0, 0, 0, 0, 0, 0};
         const int pair = id - seg * pairs;
@@ -189,14 +196,13 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
     // 19.6 / 21.6, 8 of 131071 91 / 98).
     if (B <= kWave && most >= 8 && B * pairs > kPagedSegments / 3 && B * pairs <= 2 * kPagedSegments &&
         wave_max((float)rounds_of(lane, n)) * B > 1.125f * all) {
-        most = max((int)((all * pairs + 2 * kPagedSegments - 1) / (2 * kPagedSegments)), kWholeRounds);
+        most = (int)((all * pairs + 2 * kPagedSegments - 1) / (2 * kPagedSegments));
         while (last_lane(scan_wave(divided(rounds_of(lane, n) + most - 1, most))) * pairs > 2 * kPagedSegments) most += (most + 7) / 8;
     }
-    most = max(most, kWholeRounds);
     int before = 0, cut = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
         if (B > kWave) n = rows(b0 + lane);
-        const int rounds = rounds_of(b0 + lane, n), count = min(divided(rounds + most - 1, most), kMostSegments);
+        const int rounds = rounds_of(b0 + lane, n), count = min(divided(rounds + most - 1, most), most_segments(rounds));
         const int upto = scan_wave(count), cut_upto = scan_wave(count > 1 ? count : 0);
         const unsigned long long beyond = __ballot(id < before + upto * pairs);
         if (beyond) {

@@ -139,7 +139,8 @@ def quick(rng, dtype, Hkv, G, D, page, lens):
 
 @pytest.mark.parametrize("dtype,H,Hkv,D,page,B,n", [("bf16", 4, 2, 128, 16, 24, 4200), ("bf16", 2, 2, 64, 64, 30, 6000), ("f32", 4, 4, 64, 32, 40, 700),
                                                     ("bf16", 3, 1, 128, 8, 64, 3900), ("bf16", 2, 1, 128, 256, 63, 5000), ("bf16", 1, 1, 64, 16, 70, 2000), ("f32", 1, 1, 64, 8, 700, 40),
-                                                    ("bf16", 1, 1, 64, 8, 1100, 60)])
+                                                    ("bf16", 1, 1, 64, 8, 1100, 60), ("bf16", 4, 2, 128, 16, 2, 640), ("f32", 8, 2, 64, 8, 3, 1100),
+                                                    ("bf16", 2, 1, 128, 16, 70, 400)])
 @pytest.mark.parametrize("spread", ["alike", "mixed", "one long"])
 def test_batches_whose_sequences_are_cut(dtype, H, Hkv, D, page, B, n, spread):
     """Every rule by which a batch is divided over workgroups: no row is left out or counted twice."""
