@@ -64,7 +64,9 @@ struct PagedStep {
     int B, H, Hkv, G;
     int group, blocks;             // query heads of a key/value head, and pairs that they make
     PagedScale scale;
-    float *raw, *stats;            // EMIT: [B,H,slots] scores in base-2 units, [B,H,2] softmax maximum and denominator
+    float *raw, *stats;            // of a step with masses: [B,H,slots] scores in base-2 units, [B,H,2] softmax maximum and 1 / denominator
+    float* mass_pages;
+    unsigned int* group_tickets;   // kMasses, of the (sequence, score group)s; zeros before and after
     unsigned int* tickets;         // of the pairs with several segments, by their first one's number; zeros before and after
     unsigned long long* partials;  // of the segments of such pairs
 };
@@ -224,7 +226,29 @@ __device__ __forceinline__ void put(unsigned long long* p, float x, float y)
 {
     __hip_atomic_store(p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <int DT, int D, bool EMIT>
+// What becomes of the scores: nothing; they are stored, and paged_mass_kernel adds up the masses; the last workgroup of a (sequence, score group) does.
+enum { kNoScores, kScores, kMasses };
+constexpr int kMassAhead = 8;  // reads in flight of a thread that adds up masses (kMasses: twice)
+// What a kMasses launch takes at most: of a group pairs, slots and scores; groups of several pairs, which have tickets. It saves the host a launch, 2.5 us, and
+// takes about as long (us a step, two launches / one: B1 H32/8, eight groups, 250 rows 10.7 / 10.4, 1000 11.4 / 12.1; B32 likewise 14.2 / 13.3, 34.8 / 31.2;
+// B2 H8/2, one group, fp32 D64, 60 rows 8.25 / 8.2, 500 10.5 / 11.1). The scores come from beyond the caches, which one workgroup is slow at (B1
+// H32, one group, 500 rows 11.9 / 13.4, 2000 rows 15 / 25), and so are many pairs at one ticket (B16 H32, one group, 60 rows 11.8 / 16.1).
+constexpr int kMassPairs = 4, kMassSlots = 2048, kMassScores = 4096, kMassGroups = 512;
+constexpr int kMassHeads = kMassScores / 8;  // a sequence has 8 slots at least
+// 2^x; the exponential instruction gives zero where the result is subnormal, exp2f does not
+__device__ __forceinline__ void weights_of(f32x4& x)
+{
+    const float least = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+    f32x4 p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(x[e]);
+    if (__builtin_expect(__any(least < kSmallExponent), 0)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = exp2f(x[e]);
+    }
+    x = p;
+}
+template <int DT, int D, int EMIT>
 __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) void paged_step_kernel(PagedStep a)
 {
     using T = PagedTile<DT, D>;
@@ -360,6 +384,8 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
         }
     }
     constexpr int BLOCKS = TR / 16;  // of 16 rows
+    [[maybe_unused]] const auto scores = __builtin_amdgcn_make_buffer_rsrc(a.raw + ((size_t)at.b * a.H + head0) * slots, 0,
+                                                                           EMIT == kMasses ? heads * slots * 4 : 0, 0x00020000);
 
     // off: which of the two places; left: tiles with this one; later: the tile after the next, whose loads are issued once this one is in registers
     auto tile = [&](uint32_t off, int row, int bad, int left, const Places& later) __attribute__((always_inline)) {
@@ -425,7 +451,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                     if (j > n || (j < n && (bad >> (t * 2 + quarter / 2) & 1))) s[t][r] = -INFINITY;
                 }
         }
-        if constexpr (EMIT) {
+        if constexpr (EMIT != kNoScores) {
             if (c16 < heads) {
                 float* raw = a.raw + ((size_t)at.b * a.H + head0 + c16) * slots;
 #pragma unroll
@@ -434,7 +460,11 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                     f32x4 x;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[r] = s[t][r] * of_diff;
-                    if (j <= n) *reinterpret_cast<f32x4*>(raw + j) = x;
+                    if constexpr (EMIT == kMasses) {  // written through, like the partial results
+                        if (j <= n) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), scores, (c16 * slots + j) * 4, 0, kDeviceScope);
+                    } else {
+                        if (j <= n) *reinterpret_cast<f32x4*>(raw + j) = x;
+                    }
                 }
             }
         }
@@ -612,7 +642,9 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
         else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + out_at + h * D + d) = make_float2(x, y);
     };
     auto statistics = [&](int h, float top, float sum) {
-        if constexpr (EMIT) *reinterpret_cast<float2*>(a.stats + ((size_t)at.b * a.H + head0 + h) * 2) = make_float2(top * of_diff, sum);
+        float* to = a.stats + ((size_t)at.b * a.H + head0 + h) * 2;
+        if constexpr (EMIT == kMasses) put(reinterpret_cast<unsigned long long*>(to), top * of_diff, 1.f / sum);
+        else if constexpr (EMIT == kScores) *reinterpret_cast<float2*>(to) = make_float2(top * of_diff, 1.f / sum);
     };
     unsigned long long* part = a.partials + (size_t)at.split * PART;
     for (int i = tid; i < heads * (D / 2); i += WAVES * kWave) {
@@ -634,7 +666,100 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
             if (d == 0) put(part + h, top, sum);
         }
     }
-    if (at.count == 1) return;
+    // ------------------------------------------------------------------ the masses of a group, by the last of its pairs
+    auto add_masses = [&]() __attribute__((always_inline)) {
+        constexpr int ROWS = WAVES * kWave, EACH = kMassSlots / ROWS;  // rows of a pass, a row a thread; four a lane where the waves share the heads
+        const int g = a.G > 1 ? hk : 0, all_heads = a.H / a.G, pairs = a.G > 1 ? a.blocks : a.Hkv * a.blocks, passes = n / ROWS + 1;
+        const size_t first = (size_t)at.b * a.H + g * all_heads;
+        int id[EACH];  // pages and masses of this thread's rows, asked for on the way
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) id[u] = u < passes ? a.pages.page_of(at.b, min(u * ROWS + tid, n)) : -1;
+        wait_loads();  // this wave's scores and statistics are where every workgroup sees them
+        float* to[EACH];
+        float old[EACH];
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            to[u] = a.mass_pages + a.pages.row(max(id[u], 0), a.G, g, min(u * ROWS + tid, n));
+            old[u] = u < passes ? *to[u] : 0.f;
+        }
+        __syncthreads();
+        if (pairs > 1) {
+            if (tid == 0) sh_ticket = atomicInc(a.group_tickets + at.b * a.G + g, pairs - 1);
+            __syncthreads();
+            if (sh_ticket != (unsigned)pairs - 1) return;
+        }
+        static_assert(kMassHeads * 8 + WAVES * kMassSlots * 4 <= (int)sizeof(tiles));
+        float2* of = reinterpret_cast<float2*>(tiles[0]);
+        float(*part)[kMassSlots] = reinterpret_cast<float(*)[kMassSlots]>(tiles[0] + kMassHeads * 8);
+        const auto raw = __builtin_amdgcn_make_buffer_rsrc(a.raw + first * slots, 0, all_heads * slots * 4, 0x00020000);
+        const auto stats = __builtin_amdgcn_make_buffer_rsrc(a.stats + first * 2, 0, all_heads * 8, 0x00020000);
+        const int per = (all_heads + WAVES - 1) / WAVES, h0 = wave * per, heads_here = min(per, all_heads - h0);  // (none: 0 or less)
+        u32x4 x[2][kMassAhead];
+        int fetch_pass = 0, fetch_head = 0, pass = 0, head = 0;
+        auto fetch = [&](u32x4(&to)[kMassAhead]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < kMassAhead; ++u) {
+                const int j = fetch_pass * ROWS + lane * 4;
+                to[u] = __builtin_amdgcn_raw_buffer_load_b128(raw, j <= n && heads_here > 0 ? ((h0 + fetch_head) * slots + j) * 4 : 0x7ffffff0, 0, kDeviceScope);
+                if (++fetch_head >= heads_here) fetch_head = 0, ++fetch_pass;
+            }
+        };
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        auto add = [&](const u32x4(&from)[kMassAhead]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < kMassAhead; ++u)
+                if (pass < passes) {
+                    const float2 y = of[h0 + head];
+                    f32x4 p;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t word = from[u][e];
+                        p[e] = __uint_as_float(word) - y.x;
+                    }
+                    weights_of(p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(p[e], y.y, sum[e]);
+                    if (++head >= heads_here) {
+                        *reinterpret_cast<f32x4*>(part[wave] + pass * ROWS + lane * 4) = sum;
+                        sum = f32x4{0.f, 0.f, 0.f, 0.f}, head = 0, ++pass;
+                    }
+                }
+        };
+        for (int h = tid; h < all_heads; h += ROWS) {
+            const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(stats, h * 8, 0, kDeviceScope);
+            of[h] = make_float2(__uint_as_float(y.x), __uint_as_float(y.y));
+        }
+        fetch(x[0]);
+        fetch(x[1]);
+        __syncthreads();
+        if (heads_here > 0) {
+            for (;;) {
+                add(x[0]);
+                if (pass >= passes) break;
+                fetch(x[0]);
+                add(x[1]);
+                if (pass >= passes) break;
+                fetch(x[1]);
+            }
+        } else {
+            for (; pass < passes; ++pass) *reinterpret_cast<f32x4*>(part[wave] + pass * ROWS + lane * 4) = sum;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int j = u * ROWS + tid;
+            if (j <= n && id[u] >= 0) {
+                float all = part[0][j];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) all += part[w][j];
+                *to[u] = (j == n ? 0.f : old[u]) + all / (float)all_heads;
+            }
+        }
+    };
+    if (at.count == 1) {
+        if constexpr (EMIT == kMasses) add_masses();
+        return;
+    }
 
     // ------------------------------------------------------------------ the segments' results together, by the last to arrive
     wait_loads();  // (stores count too) this wave's partial results are where every workgroup sees them
@@ -699,13 +824,13 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
         write(h, i % (D / 4) * 4, x[0] / sum, x[1] / sum);
         write(h, i % (D / 4) * 4 + 2, x[2] / sum, x[3] / sum);
     }
+    if constexpr (EMIT == kMasses) add_masses();
 }
 
 // mass of every row += the mean of its group's probabilities. A workgroup takes 64 rows at a time, a lane each; its four waves share the group's
 // heads (eight reads of each in flight) and add up in LDS, in an order of their own: the same bits every time. Bound by latency up to some
-// thousand rows, by the scores' bytes beyond: 3.5 .. 4.3 us. (A launch of its own: with the masses added up by the last workgroup of a sequence, whose
-// reads have to come from beyond the caches, a layer of the frequency policy took 21.7 instead of 16.5 us at 513 rows, 37.7 instead of 19.6 at 2000.)
-constexpr int kMassRows = kWave, kMassWaves = 4, kMassAhead = 8;
+// thousand rows, by the scores' bytes beyond: 3.5 .. 4.3 us. (Groups of few scores have no launch of their own: see kMassScores.)
+constexpr int kMassRows = kWave, kMassWaves = kPagedWaves;
 __global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const float* __restrict__ raw, const float* __restrict__ stats, float* mass_pages,
                                                                           const int32_t* __restrict__ len_b, Pages pages, int H, int G)
 {
@@ -728,7 +853,7 @@ __global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const
             for (int u = 0; u < kMassAhead; ++u)
                 if (h + u < h1) {
                     const float2 of = reinterpret_cast<const float2*>(stats)[first + h + u];
-                    sum += exp2f(x[u] - of.x) / of.y;
+                    sum = fmaf(exp2f(x[u] - of.x), of.y, sum);
                 }
         }
         part[wave][lane] = sum;
@@ -743,10 +868,10 @@ __global__ __launch_bounds__(kMassRows* kMassWaves) void paged_mass_kernel(const
     }
 }
 
-// Workspace: tickets, partial results of cut pairs (a pair of r rounds is cut into less than 2 r / most segments, so there are less than twice
+// Workspace: tickets of pairs and of groups (where they lie does not hang on the call), partial results of cut pairs (a pair of r rounds is cut into less than 2 r / most segments, so there are less than twice
 // kPagedSegments of them), and for EMIT scores and statistics.
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-constexpr size_t kTicketBytes = 2 * kPagedSegments * sizeof(unsigned int);
+constexpr size_t kTicketBytes = (2 * kPagedSegments + kMassGroups) * sizeof(unsigned int);
 static size_t partial_bytes(int D) { return up256((size_t)2 * kPagedSegments * kHeadBlock * (D / 2 + 1) * 8); }
 size_t paged_step_ws(int B, int H, int slots, int D, bool emit)
 {
@@ -761,10 +886,16 @@ template <int DT, int D> static int launch(const PagedStep& a, float* mass_pages
     const long long segments = a.B == 1 ? std::max<long long>(kPagedSegments, pairs) : std::max<long long>(2 * kPagedSegments, kPagedSegments + pairs);
     const dim3 grid((unsigned)std::min(segments, rounds * pairs));
     if (!mass_pages) {
-        hipLaunchKernelGGL((paged_step_kernel<DT, D, false>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
+        hipLaunchKernelGGL((paged_step_kernel<DT, D, kNoScores>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
         return status_from_hip(hipGetLastError());
     }
-    hipLaunchKernelGGL((paged_step_kernel<DT, D, true>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
+    const int heads = a.H / a.G, slots = a.pages.slots();
+    const int together = a.G > 1 ? a.blocks : a.Hkv * a.blocks;  // pairs of a group
+    if ((together == 1 || (together <= kMassPairs && a.B * a.G <= kMassGroups)) && slots <= kMassSlots && (long long)heads * slots <= kMassScores) {
+        hipLaunchKernelGGL((paged_step_kernel<DT, D, kMasses>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
+        return status_from_hip(hipGetLastError());
+    }
+    hipLaunchKernelGGL((paged_step_kernel<DT, D, kScores>), grid, dim3(kPagedWaves * kWave), 0, stream, a);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     const int groups = a.B * a.G, most = std::max(1, 4096 / groups);  // the lengths are on the device: workgroups go over the rows
     hipLaunchKernelGGL(paged_mass_kernel, dim3(std::min((a.pages.slots() + kMassRows - 1) / kMassRows, most), groups), dim3(kMassRows * kMassWaves), 0, stream,
@@ -780,7 +911,8 @@ int paged_step_dispatch(const void* q, const void* k_new, const void* v_new, voi
     const PagedStep a{q, k_new, v_new, k_pages, v_pages, out, pos_pages, len_b, new_pos_b, pages, B, H, Hkv, G, H / Hkv, (H / Hkv + kHeadBlock - 1) / kHeadBlock, paged_scale(scale, dt),
                       reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D)),
                       reinterpret_cast<float*>(at + kTicketBytes + partial_bytes(D) + up256((size_t)B * H * pages.slots() * 4)),
-                      reinterpret_cast<unsigned int*>(at), reinterpret_cast<unsigned long long*>(at + kTicketBytes)};
+                      mass_pages, reinterpret_cast<unsigned int*>(at) + 2 * kPagedSegments, reinterpret_cast<unsigned int*>(at),
+                      reinterpret_cast<unsigned long long*>(at + kTicketBytes)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, mass_pages, stream) : launch<EC_BF16, 64>(a, mass_pages, stream);
     return D == 128 ? launch<EC_F32, 128>(a, mass_pages, stream) : launch<EC_F32, 64>(a, mass_pages, stream);
 }

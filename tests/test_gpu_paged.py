@@ -56,7 +56,7 @@ class Dev:
         assert (np.isnan(want) | (got == want) | (err <= (0 if mass_tol is None else mass_tol))).all(), np.nanmax(err)
 
 
-def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=None, vn=None, with_pos=True, more=0.0):
+def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=None, vn=None, with_pos=True, more=0.0, ws=None):
     rng = np.random.default_rng(seed)
     B, D = pool.table.shape[0], pool.k.shape[3]
     scale = D ** -0.5 if scale is None else scale
@@ -67,7 +67,7 @@ def run_step(pool, dtype, H, lens, seed, scored=False, scale=None, q=None, kn=No
     dev, code = Dev(pool, dtype), ec.EC_F32 if dtype == "f32" else ec.EC_BF16
     out = torch.full((B, H, D), 3.0, device="cuda", dtype=dev.k.dtype)
     fn = ec.EC_FN_PAGED_DECODE_SCORE_STEP if scored else ec.EC_FN_PAGED_DECODE_STEP
-    ws = ec.new_workspace(fn, B, H, pool.slots, D, code)
+    ws = ec.new_workspace(fn, B, H, pool.slots, D, code) if ws is None else ws
     tq, tk, tv, tl, tp = to_dev(q, dtype), to_dev(kn, dtype), to_dev(vn, dtype), ints(lens), ints(new_pos)
     pos = dev.pos if with_pos else None
     print("step", dtype, q.shape, pool.k.shape, list(lens)[:8], flush=True)
@@ -123,6 +123,43 @@ def test_step_long_or_many(dtype, H, Hkv, B, n, page, scored):
     lens = [n] + [int(x) for x in rng.integers(-1, n + 1, B - 1)]
     pool = make(rng, dtype, B, Hkv, 1, 64 if n > 1000 else 128, page, -(-(n + 1) // page), lens)
     run_step(pool, dtype, H, lens, n, scored)
+
+
+MASSES = [  # dtype, D, H, Hkv, G, page, max_pages, lens: groups of few and of many scores, of one pair and of several, cut and whole
+    ("bf16", 128, 8, 2, 1, 16, 31, [400, -1, 495, 0]),      # two pairs a group
+    ("bf16", 128, 20, 1, 1, 16, 12, [150, 191, 3]),         # two pairs of one key head
+    ("bf16", 64, 68, 2, 2, 8, 14, [111, 30]),               # three pairs of a key head each
+    ("bf16", 64, 51, 1, 1, 8, 9, [71, 2, 60]),              # four pairs
+    ("bf16", 64, 65, 1, 1, 8, 7, [55, 17]),                 # five pairs
+    ("bf16", 128, 4, 4, 4, 8, 256, [2047, 1500]),           # as many slots as one launch takes, one head a group
+    ("bf16", 128, 4, 4, 4, 8, 257, [2055, 1500]),           # and a page more
+    ("bf16", 128, 2, 1, 1, 32, 64, [2040]),                 # as many scores
+    ("bf16", 64, 5, 1, 1, 32, 26, [831, 500]),              # and some more
+    ("f32", 64, 9, 3, 1, 8, 40, [310, 311, 319, 255, 256]),
+    ("f32", 128, 7, 1, 1, 64, 9, [500, 64, 63]),
+    ("f32", 64, 512, 1, 1, 8, 1, [7, 6, 0, -1]),            # as many heads
+    ("f32", 128, 3, 3, 3, 16, 20, [300] * 200),             # more groups than tickets, one pair each
+    ("bf16", 64, 2, 2, 1, 8, 5, [33] * 520),                # and of two pairs
+]
+
+
+@pytest.mark.parametrize("case", range(len(MASSES)))
+def test_masses(case):
+    dtype, D, H, Hkv, G, page, max_pages, lens = MASSES[case]
+    pool = make(np.random.default_rng(900 + case), dtype, len(lens), Hkv, G, D, page, max_pages, lens)
+    if case % 2:
+        pool.table[0, 1 if max_pages > 1 else 0] = -1  # rows that are not there
+    run_step(pool, dtype, H, lens, case, True)
+
+
+def test_one_workspace_for_calls_of_different_sizes():
+    """What a call leaves in a workspace is what any other finds right, whichever way the masses are added up."""
+    ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, 70, 64, 6000, 128, ec.EC_F32)
+    for i, (dtype, D, H, Hkv, G, page, lens) in enumerate([("bf16", 128, 8, 2, 1, 16, [400, 300, 0]), ("bf16", 128, 8, 2, 1, 16, [5000, 300]),
+                                                           ("f32", 64, 3, 3, 1, 8, [500] * 5), ("bf16", 64, 40, 4, 4, 32, [200] * 60),
+                                                           ("bf16", 128, 8, 2, 1, 16, [400, 300, 0]), ("f32", 128, 64, 1, 1, 8, [50, 60])]):
+        for scored in (True, False, True):
+            run_step(quick(np.random.default_rng(i), dtype, Hkv, G, D, page, lens), dtype, H, lens, i, scored, ws=ws)
 
 
 def quick(rng, dtype, Hkv, G, D, page, lens):
