@@ -110,6 +110,7 @@ class PagedBatch:
         dt = ec.dtype_code(self.k_pages)
         self.ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, places, H, max_pages * page, D, dt, device)
         self.ws_one = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, places, G, 1, D, dt, device)
+        self.budget = None
         self._upload()
 
     def _ints(self, x):
@@ -117,6 +118,14 @@ class PagedBatch:
 
     def _upload(self):
         self.numbers.copy_(self._ints([self.rows, [n + 1 for n in self.rows], self.seen, [n + 1 for n in self.seen]]))
+
+    def _budget(self, keep):
+        """`keep` for every place: the layers of a token share the tensor. A graph under capture gets one of its own, filled by its replays."""
+        if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
+            return torch.full_like(self.len_b, keep)
+        if self.budget is None or self.budget[0] != keep:
+            self.budget = (keep, torch.full_like(self.len_b, keep))
+        return self.budget[1]
 
     def _hold(self, place, rows):
         """Exactly the pages that `rows` rows need, taken from the free ones or given back to them."""
@@ -186,7 +195,7 @@ class PagedBatch:
         ec.ec_paged_decode_score_step(q, k_new, v_new, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer],
                                       self.table, self.len_b, self.pos_b, scale, out, self.ws)
         ec.ec_paged_evict_min(self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], self.table, self.len_after,
-                              torch.full_like(self.len_b, keep), self.seen_b, 1, self.protect_first, self.recent, self.ws_one)
+                              self._budget(keep), self.seen_b, 1, self.protect_first, self.recent, self.ws_one)
 
     def end(self, keep: int | None = None):
         """Behind the last layer of a token; keep as in decode_scored, None after decode."""
@@ -208,7 +217,7 @@ class PagedBatch:
         ws = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, len(self.rows), self.G, most, self.D, ec.dtype_code(self.k_pages), self.table.device)
         for layer in range(self.k_pages.shape[0]):
             ec.ec_paged_evict_min(self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], self.table, self.len_b,
-                                  torch.full_like(self.len_b, keep), self.pos_b, most, self.protect_first, self.recent, ws)
+                                  self._budget(keep), self.pos_b, most, self.protect_first, self.recent, ws)
         for b, n in enumerate(self.rows):
             if n > keep:
                 self.rows[b] = keep

@@ -100,3 +100,45 @@ def test_out_of_pages():
     with pytest.raises(ValueError, match="are free"):
         batch.admit([1], [17], [17])
     assert batch.rows == [32, -1] and len(batch.free) == 1
+
+
+def test_tokens_captured_and_replayed():
+    """The layers of a token under the frequency policy as one graph, replayed for several tokens between eager ones, against a batch that runs eagerly."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *shape: torch.randn(shape, device="cuda", generator=g).bfloat16()
+    L, H, Hkv, D, keep, n = 2, 4, 2, 64, 41, 45
+    batches = [PagedBatch(L, 3, H, Hkv, D, 16, 12, 4, torch.bfloat16) for _ in range(2)]
+    k, v, pos, mass = rand(2, Hkv, n, D), rand(2, Hkv, n, D), torch.arange(n, dtype=torch.int32, device="cuda").expand(2, 1, n).contiguous(), torch.rand(2, 1, n, device="cuda", generator=g)
+    for batch in batches:
+        batch.admit([2, 0], [n, n - 6], [n, n])
+        for i in range(L):
+            batch.store(i, [2, 0], k, v, pos, mass)
+    token, outs = [rand(L, 3, H, D), rand(L, 3, Hkv, D), rand(L, 3, Hkv, D)], [torch.empty(L, 3, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def layers(batch, out, keep):
+        for i in range(L):
+            batch.decode_scored(i, token[0][i], token[1][i], token[2][i], 0.125, out[i], keep)
+
+    def step(keep, one, other):
+        for x in token:
+            x.copy_(rand(*x.shape))
+        for batch, run in zip(batches, (one, other)):
+            batch.begin()
+            run()
+            batch.end(keep)
+        assert torch.equal(outs[0], outs[1]) and batches[0].rows == batches[1].rows
+        for name in ("k_pages", "v_pages", "pos_pages", "mass_pages", "table"):
+            assert torch.equal(getattr(batches[0], name), getattr(batches[1], name)), name
+
+    eager = [lambda keep=keep, i=i: layers(batches[i], outs[i], keep) for i in range(2)]
+    step(keep, *eager)
+    graph = torch.cuda.CUDAGraph()
+    saved = [x.clone() for x in (batches[1].k_pages, batches[1].v_pages, batches[1].pos_pages, batches[1].mass_pages)]
+    with torch.cuda.graph(graph):
+        layers(batches[1], outs[1], keep)
+    for x, y in zip((batches[1].k_pages, batches[1].v_pages, batches[1].pos_pages, batches[1].mass_pages), saved):
+        assert torch.equal(x, y)  # capturing runs nothing
+    for t in range(6):
+        if t == 3:  # another budget in between, eagerly
+            step(keep - 2, *[lambda i=i: layers(batches[i], outs[i], keep - 2) for i in range(2)])
+        step(keep, eager[0], graph.replay)
