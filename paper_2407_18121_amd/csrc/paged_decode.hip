@@ -83,8 +83,8 @@ template <int N> __device__ __forceinline__ void load_run_lds(u32x4 rsrc, uint32
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, 0 offen nt lds\n\t"
                      "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 nt lds\n\tbuffer_load_dwordx4 %3, %5, 0 offen offset:2048 nt lds\n\t"
-                     "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 nt lds"
-                     ::"s"(lds), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(rsrc) : "memory");
+                     "buffer_load_dwordx4 %4, %5, 0 offen offset:%6 nt lds"
+                     ::"s"(lds), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(rsrc), "n"(3 * 1024) : "memory");
 }
 
 template <int DT, int D> struct PagedTile {
