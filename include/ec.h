@@ -439,7 +439,8 @@ int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, vo
  * where p is the mean of the step's softmax rows over all query heads (G == 1) or over the query heads of the key/value head
  * (G == Hkv), added in a fixed order.
  *   mass_pages     updated
- *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_SCORE_STEP, B,H, max_pages * page, D,dt)
+ *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_SCORE_STEP, B,H, max_pages * page, D,dt); zeros before its first use and
+ *                  one call at a time, as there
  */
 int ec_paged_decode_score_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
                                float* mass_pages, const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b,
