@@ -106,20 +106,27 @@ struct EvictRows {
           recent(goal.protect_recent ? (int64_t)goal.seen_b[b] - goal.protect_recent : INT64_MAX)
     {
     }
-    // Keys of slots j .. j + 7 (j a multiple of 8); those from n on get the largest there is, like protected ones. Returns the run's page or -1.
-    __device__ __forceinline__ int keys(int j, uint32_t (&key)[kRun]) const
+    // Keys of RUNS runs of 8 slots, each `stride` behind the one before it, all their loads in flight; slots from n on get the largest key there is, like
+    // protected ones. page[u]: the run's page or -1.
+    template <int RUNS> __device__ __forceinline__ void keys(int j0, int stride, uint32_t (&key)[RUNS][kRun], int (&page)[RUNS]) const
     {
-        const int id = j < n ? pages.page_of(b, j) : -1;
-        const size_t at = pages.row(max(id, 0), G, g, j);
-        u32x4 m[2], p[2] = {};
-        m[0] = reinterpret_cast<const u32x4*>(mass_pages + at)[0], m[1] = reinterpret_cast<const u32x4*>(mass_pages + at)[1];
-        if (pos_pages) p[0] = reinterpret_cast<const u32x4*>(pos_pages + at)[0], p[1] = reinterpret_cast<const u32x4*>(pos_pages + at)[1];
+        u32x4 m[RUNS][2], p[RUNS][2] = {};
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            const int where = (int)p[i / 4][i % 4];
-            key[i] = evict_key(__uint_as_float(m[i / 4][i % 4]), id < 0 || j + i >= n || (pos_pages && (where < first || where >= recent)));
+        for (int u = 0; u < RUNS; ++u) page[u] = j0 + u * stride < n ? pages.page_of(b, j0 + u * stride) : -1;
+#pragma unroll
+        for (int u = 0; u < RUNS; ++u) {
+            const size_t at = pages.row(max(page[u], 0), G, g, j0 + u * stride);
+            m[u][0] = reinterpret_cast<const u32x4*>(mass_pages + at)[0], m[u][1] = reinterpret_cast<const u32x4*>(mass_pages + at)[1];
+            if (pos_pages) p[u][0] = reinterpret_cast<const u32x4*>(pos_pages + at)[0], p[u][1] = reinterpret_cast<const u32x4*>(pos_pages + at)[1];
         }
-        return id;
+#pragma unroll
+        for (int u = 0; u < RUNS; ++u)
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                const int where = (int)p[u][i / 4][i % 4];
+                key[u][i] = evict_key(__uint_as_float(m[u][i / 4][i % 4]),
+                                      page[u] < 0 || j0 + u * stride + i >= n || (pos_pages && (where < first || where >= recent)));
+            }
     }
 };
 
@@ -172,36 +179,45 @@ template <int WAVES> __device__ __forceinline__ uint32_t block_scan(uint32_t x, 
 // One workgroup per (sequence, score group): which rows go, and the list of moves. A thread holds runs of 8 consecutive slots. Sought is the gone-th
 // smallest (key, slot): digit by digit, 8 bits at a time from the highest bit in which two keys differ (masses share their upper bits, and a histogram
 // of those is one counter that all lanes wait for), until at most 64 rows share the digits found, which the waves rank, a share of the
-// comparisons each (all in every wave: 1500 rows 8.2 us instead of 6.0). HELD: keys stay in registers, for sequences of up to 8192 rows; longer ones are
-// read again for every digit. Bound: a chain of latencies (length, table, masses, a barrier or two for each digit); 16 groups of 8192 rows 67 us with
-// digits sought by one thread and keys read again, now 10.
-template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list)
+// comparisons each (all in every wave: 1500 rows 8.2 us instead of 6.0). HELD: keys stay in registers, one, two or four
+// runs a thread, up to 32768 rows (us of a call, held / read again for every digit: 12000 rows 15.6 / 26, 30000 rows 23 / 37); longer sequences are read again,
+// a run at a time (70000 rows 96 us, with four in flight 110). Bound: a chain of latencies (length, table, masses, a barrier or two for each digit), for
+// long ones by what one compute unit can read; 16 groups of 8192 rows 10 us.
+template <int THREADS> struct SelectShared {
+    __align__(16) uint32_t hist[4][kCopies][kCopyWords];  // a counter has a copy for every eighth lane, in banks of their own
+    uint32_t sums[3][THREADS / kWave], lo[THREADS / kWave], hi[THREADS / kWave], ranks[kWave], n_few, slot;
+    unsigned long long few[kWave];
+};
+template <int THREADS, int RUNS, bool HELD>
+__device__ __forceinline__ void select_victims(const EvictRows& rows, int gone, int32_t* counts, uint2* list, SelectShared<THREADS>& sh)
 {
-    // a counter has a copy for every eighth lane, in banks of their own
-    __shared__ __align__(16) uint32_t hist[4][kCopies][kCopyWords];
-    constexpr int WAVES = THREADS / kWave;
-    __shared__ uint32_t sh[3][WAVES], sh_lo[WAVES], sh_hi[WAVES], ranks[kWave], n_few, sh_slot;
-    __shared__ unsigned long long few[kWave];
+    constexpr int WAVES = THREADS / kWave, STRIDE = THREADS * kRun;
+    constexpr bool ONCE = HELD && RUNS == 1;  // a thread has one run: what its threads share is written once
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = rows.n, m = n - gone;
-    const int runs = (n + kRun - 1) / kRun;
-    uint32_t held[kRun];
-    int held_page = -1;
-    if constexpr (HELD) held_page = rows.keys(tid * kRun, held);
+    uint32_t held[RUNS][kRun];
+    int held_page[RUNS];
+    if constexpr (HELD) rows.keys<RUNS>(tid * kRun, STRIDE, held, held_page);
     // f(first slot, keys, page) for every run of this thread
     auto each_run = [&](auto&& f) __attribute__((always_inline)) {
         if constexpr (HELD) {
-            f(tid * kRun, held, held_page);
+#pragma unroll
+            for (int u = 0; u < RUNS; ++u) f(tid * kRun + u * STRIDE, held[u], held_page[u]);
         } else {
-            for (int r0 = 0; r0 < runs; r0 += THREADS) {  // all threads in every round
-                uint32_t key[kRun];
-                const int page = rows.keys((r0 + tid) * kRun, key);
-                f((r0 + tid) * kRun, key, page);
+            for (int j0 = 0; j0 < n; j0 += RUNS * STRIDE) {  // all threads in every round
+                uint32_t key[RUNS][kRun];
+                int page[RUNS];
+                rows.keys<RUNS>(j0 + tid * kRun, STRIDE, key, page);
+#pragma unroll
+                for (int u = 0; u < RUNS; ++u) f(j0 + tid * kRun + u * STRIDE, key[u], page[u]);
             }
         }
     };
+    auto& hist = sh.hist;
+    auto& few = sh.few;
+    auto& ranks = sh.ranks;
     for (int i = tid; i < (int)(sizeof(hist) / 16); i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     if (tid < kWave) ranks[tid] = 0;
-    if (tid == 0) n_few = 0, sh_slot = 0;
+    if (tid == 0) sh.n_few = 0, sh.slot = 0;
     // how many rows are not protected, and the bits in which their keys differ
     uint32_t lo = kProtected, hi = 0, open = 0;
     each_run([&](int, uint32_t (&key)[kRun], int) __attribute__((always_inline)) {
@@ -209,10 +225,10 @@ template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims
         for (int i = 0; i < kRun; ++i) lo = min(lo, key[i]), hi = max(hi, key[i] == kProtected ? 0u : key[i]), open += key[i] != kProtected;
     });
     lo = wave_end<false>(lo), hi = wave_end<true>(hi);
-    if (lane == 0) sh_lo[wave] = lo, sh_hi[wave] = hi;
+    if (lane == 0) sh.lo[wave] = lo, sh.hi[wave] = hi;
     uint32_t all_open;
-    block_scan<WAVES>(open, sh[0], all_open);
-    lo = wave_end<false>(sh_lo[lane % WAVES]), hi = wave_end<true>(sh_hi[lane % WAVES]);
+    block_scan<WAVES>(open, sh.sums[0], all_open);
+    lo = wave_end<false>(sh.lo[lane % WAVES]), hi = wave_end<true>(sh.hi[lane % WAVES]);
 
     // Victims are the rows up to `limit` in the order of (key, slot). Where only their key is known, last, and how many rows have it and go, need, the
     // slot is looked for behind.
@@ -265,7 +281,7 @@ template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims
 #pragma unroll
                     for (int i = 0; i < kRun; ++i)
                         if (key[i] != kProtected && ((uint64_t)(key[i] ^ last) >> down) == 0) {
-                            const uint32_t to = atomicAdd(&n_few, 1u);
+                            const uint32_t to = atomicAdd(&sh.n_few, 1u);
                             if (to < kWave) few[to] = (unsigned long long)key[i] << 32 | (uint32_t)(j + i);
                         }
                 });
@@ -289,15 +305,15 @@ template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims
             uint32_t mine = 0, total;
 #pragma unroll
             for (int i = 0; i < kRun; ++i) mine += j + i < n && key[i] == last;
-            uint32_t rank = before + block_scan<WAVES>(mine, sh[1], total);
+            uint32_t rank = before + block_scan<WAVES>(mine, sh.sums[1], total);
             before += total;
 #pragma unroll
             for (int i = 0; i < kRun; ++i)
-                if (j + i < n && key[i] == last && ++rank == need) sh_slot = j + i;
-            if constexpr (!HELD) __syncthreads();  // sh is written again
+                if (j + i < n && key[i] == last && ++rank == need) sh.slot = j + i;
+            if constexpr (!ONCE) __syncthreads();
         });
         __syncthreads();
-        limit = (unsigned long long)last << 32 | sh_slot;
+        limit = (unsigned long long)last << 32 | sh.slot;
     }
 
     uint32_t holes = 0, movers = 0;
@@ -310,7 +326,7 @@ template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims
             flags |= (uint32_t)hole << i | (uint32_t)mover << (8 + i);
             both += (uint32_t)hole | (uint32_t)mover << 16;
         }
-        uint32_t at = block_scan<WAVES>(both, sh[2], total);
+        uint32_t at = block_scan<WAVES>(both, sh.sums[2], total);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             const uint32_t row = page < 0 ? ~0u : ((uint32_t)page << rows.pages.shift) + ((j + i) & (rows.pages.page() - 1));
@@ -320,7 +336,7 @@ template <int THREADS, bool HELD> __device__ __forceinline__ void select_victims
             at += (flags >> i & 1) | (flags >> (8 + i) & 1) << 16;
         }
         holes += total & 0xffff, movers += total >> 16;
-        if constexpr (!HELD) __syncthreads();
+        if constexpr (!ONCE) __syncthreads();
     });
     if (tid == 0) *counts = min(min(holes, movers), (uint32_t)gone);  // equal, unless masses change while they are read
 }
@@ -337,9 +353,12 @@ __global__ __launch_bounds__(THREADS) void paged_evict_select_kernel(const int32
         return;
     }
     uint2* list = moves + (size_t)blockIdx.x * goal.max_evict;
-    // fewer than kEvictThreads only where the table ends before
-    if (THREADS < kEvictThreads || rows.n <= kEvictThreads * kRun) select_victims<THREADS, true>(rows, gone, counts + blockIdx.x, list);
-    else select_victims<THREADS, false>(rows, gone, counts + blockIdx.x, list);
+    __shared__ SelectShared<THREADS> sh;
+    int32_t* count = counts + blockIdx.x;
+    if (THREADS < kEvictThreads || rows.n <= THREADS * kRun) select_victims<THREADS, 1, true>(rows, gone, count, list, sh);  // (fewer where the table ends before)
+    else if (rows.n <= 2 * THREADS * kRun) select_victims<THREADS, 2, true>(rows, gone, count, list, sh);
+    else if (rows.n <= 4 * THREADS * kRun) select_victims<THREADS, 4, true>(rows, gone, count, list, sh);
+    else select_victims<THREADS, 1, false>(rows, gone, count, list, sh);
 }
 
 // A row number of the list (page and row in it) in a pool of `heads` heads.
@@ -394,12 +413,13 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
     unsigned long long best = ~0ull;  // (key, slot)
     int page = -1;                    // of this thread's best
     for (int j = tid * kRun; j < n; j += kEvictThreads * kRun) {
-        uint32_t key[kRun];
-        const int id = rows.keys(j, key);
+        uint32_t key[1][kRun];
+        int id[1];
+        rows.keys<1>(j, 0, key, id);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const unsigned long long x = (unsigned long long)key[i] << 32 | (uint32_t)(j + i);
-            if (j + i < n && x < best) best = x, page = id;
+            const unsigned long long x = (unsigned long long)key[0][i] << 32 | (uint32_t)(j + i);
+            if (j + i < n && x < best) best = x, page = id[0];
         }
     }
     u32x4 row[HELD];

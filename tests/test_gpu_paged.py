@@ -370,6 +370,8 @@ EVICTS = [  # dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent
     ("f32", 64, 1, 1, 256, [70001], [30000], 65000, 1, 25),
     ("bf16", 64, 1, 1, 128, [32768], [20000], 12768, 3, 50),
     ("bf16", 64, 1, 1, 64, [8193], [8000], 1000, 1, 25),
+    ("bf16", 64, 1, 1, 16, [16385], [1000], 15385, 1, 25),
+    ("bf16", 64, 1, 1, 256, [32769], [32700], 100, 1, 25),
     ("bf16", 128, 1, 1, 32, [40009], [40008], 1, 1, 25),
 ]
 
