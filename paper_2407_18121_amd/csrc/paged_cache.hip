@@ -393,11 +393,62 @@ __global__ __launch_bounds__(256) void paged_evict_move_kernel(u32x4* k_pages, u
     }
 }
 
-// One row of every sequence, the step of a generation loop, in one launch: the workgroup that finds the least row fills its place. Only the last row can be
+// The least (key, slot) of those a thread has seen, and its page.
+struct Least {
+    unsigned long long of = ~0ull;
+    int page = -1;
+    __device__ __forceinline__ void look(const EvictRows& rows, int from, int step)
+    {
+        for (int j = from; j < rows.n; j += step) {
+            uint32_t key[1][kRun];
+            int id[1];
+            rows.keys<1>(j, 0, key, id);
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                const unsigned long long x = (unsigned long long)key[0][i] << 32 | (uint32_t)(j + i);
+                if (j + i < rows.n && x < of) of = x, page = id[0];
+            }
+        }
+    }
+    // That of the workgroup, for every thread. The shared words are written once.
+    __device__ __forceinline__ void of_all(unsigned long long* sh_of, int* sh_page)
+    {
+        const unsigned long long mine = of;
+        of = wave_least(of);
+        if (threadIdx.x % kWave == 0) sh_of[threadIdx.x / kWave] = of;
+        __syncthreads();
+        of = wave_least(sh_of[threadIdx.x % kEvictWaves]);
+        if (mine == of) *sh_page = page;  // one thread's: slots differ (several, where nobody has a row)
+        __syncthreads();
+        page = *sh_page;
+    }
+};
+
+// Long sequences, whose masses one compute unit is slow to read: the least row of each part, a workgroup a part, in a launch before (us of a call, one launch /
+// two: one sequence of 16300 rows 7.6 / 8.1, 24000 9.2 / 8.1, 131000 33 / 8.2; 16 of 16300 8.1 / 8.5, 24000 10.7 / 8.8).
+constexpr int kOneParts = 64, kOneAlone = 16384;  // slots up to which the workgroup that fills the hole looks through them all
+struct Candidate {
+    unsigned long long of;
+    int page, unused;
+};
+__global__ __launch_bounds__(kEvictThreads) void paged_evict_least_kernel(const int32_t* __restrict__ pos_pages, const float* __restrict__ mass_pages, Pages pages,
+                                                                          EvictGoal goal, int G, Candidate* __restrict__ candidates)
+{
+    __shared__ unsigned long long sh_of[kEvictWaves];
+    __shared__ int sh_page;
+    const EvictRows rows(pos_pages, mass_pages, pages, goal, G, blockIdx.y);
+    if (goal.victims(rows.b, rows.n) == 0) return;
+    Least least;
+    least.look(rows, (blockIdx.x * kEvictThreads + threadIdx.x) * kRun, gridDim.x * kEvictThreads * kRun);
+    least.of_all(sh_of, &sh_page);
+    if (threadIdx.x == 0) candidates[blockIdx.y * kOneParts + blockIdx.x] = {least.of, least.page, 0};
+}
+
+// One row of every sequence, the step of a generation loop: the workgroup that finds the least row fills its place. Only the last row can be
 // the one that moves, so it is fetched while the least one is sought; what is left of the chain is length, table, masses, the reduction and the store.
-template <int CH>
+template <int CH, bool PARTS>
 __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k_pages, u32x4* v_pages, int32_t* pos_pages, float* mass_pages, Pages pages,
-                                                                        EvictGoal goal, int Hkv, int G)
+                                                                        EvictGoal goal, int Hkv, int G, const Candidate* __restrict__ candidates, int parts)
 {
     constexpr int HELD = 3;  // chunks of a thread that are fetched early: 48 heads of 512 bytes
     __shared__ unsigned long long sh_best[kEvictWaves];
@@ -410,17 +461,14 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
     auto place = [&](int i, int id, int slot) {  // chunk i of the heads' K and V rows in a slot
         return (i / CH & 1 ? v_pages : k_pages) + pages.row(id, Hkv, head0 + i / (2 * CH), slot) * CH + i % CH;
     };
-    unsigned long long best = ~0ull;  // (key, slot)
-    int page = -1;                    // of this thread's best
-    for (int j = tid * kRun; j < n; j += kEvictThreads * kRun) {
-        uint32_t key[1][kRun];
-        int id[1];
-        rows.keys<1>(j, 0, key, id);
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            const unsigned long long x = (unsigned long long)key[0][i] << 32 | (uint32_t)(j + i);
-            if (j + i < n && x < best) best = x, page = id[0];
+    Least least;
+    if constexpr (PARTS) {
+        if (tid < parts) {
+            const Candidate c = candidates[blockIdx.x * kOneParts + tid];
+            least.of = c.of, least.page = c.page;
         }
+    } else {
+        least.look(rows, tid * kRun, kEvictThreads * kRun);
     }
     u32x4 row[HELD];
     float mass = 0.f;
@@ -432,14 +480,8 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
         mass = mass_pages[pages.row(from, G, rows.g, n - 1)];
         if (pos_pages) pos = pos_pages[pages.row(from, G, rows.g, n - 1)];
     }
-    const unsigned long long mine = best;
-    best = wave_least(best);
-    if (tid % kWave == 0) sh_best[tid / kWave] = best;
-    __syncthreads();
-    best = wave_least(sh_best[tid % kEvictWaves]);
-    if (mine == best) sh_page = page;  // one thread's: slots differ
-    __syncthreads();
-    const int hole = (int)(uint32_t)best, to = sh_page;
+    least.of_all(sh_best, &sh_page);
+    const int hole = (int)(uint32_t)least.of, to = least.page;
     if (hole == n - 1 || to < 0 || from < 0) return;
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
@@ -453,6 +495,7 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
 
 size_t paged_evict_ws(int B, int G, int max_evict)
 {
+    if (max_evict == 1) return (size_t)B * G * kOneParts * sizeof(Candidate);
     return (((size_t)B * G * 4 + 255) & ~(size_t)255) + (((size_t)B * G * max_evict * 8 + 255) & ~(size_t)255);
 }
 
@@ -465,12 +508,21 @@ int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float
     const EvictGoal goal{len_b, keep_b, seen_b, max_evict, protect_first, protect_recent};
     u32x4 *k = static_cast<u32x4*>(k_pages), *v = static_cast<u32x4*>(v_pages);
     if (max_evict == 1) {
-#define EC_ONE(CH_)                  \
-    if (row_bytes == CH_ * 16)       \
-        hipLaunchKernelGGL(paged_evict_one_kernel<CH_>, dim3(B * G), dim3(kEvictThreads), 0, stream, k, v, pos_pages, mass_pages, pages, goal, Hkv, G)
-        EC_ONE(8);
-        EC_ONE(16);
-        EC_ONE(32);
+        Candidate* candidates = static_cast<Candidate*>(ws);
+        const int slots = pages.slots(), parts = slots > kOneAlone ? std::min((slots + kEvictThreads * kRun - 1) / (kEvictThreads * kRun), kOneParts) : 0;
+        if (parts) {
+            hipLaunchKernelGGL(paged_evict_least_kernel, dim3(parts, B * G), dim3(kEvictThreads), 0, stream, pos_pages, mass_pages, pages, goal, G, candidates);
+            if (const int rc = status_from_hip(hipGetLastError())) return rc;
+        }
+#define EC_ONE(CH_, PARTS_)                           \
+    if (row_bytes == CH_ * 16 && (parts > 0) == PARTS_) \
+        hipLaunchKernelGGL((paged_evict_one_kernel<CH_, PARTS_>), dim3(B * G), dim3(kEvictThreads), 0, stream, k, v, pos_pages, mass_pages, pages, goal, Hkv, G, candidates, parts)
+        EC_ONE(8, false);
+        EC_ONE(16, false);
+        EC_ONE(32, false);
+        EC_ONE(8, true);
+        EC_ONE(16, true);
+        EC_ONE(32, true);
 #undef EC_ONE
         return status_from_hip(hipGetLastError());
     }

@@ -373,6 +373,7 @@ EVICTS = [  # dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent
     ("bf16", 64, 1, 1, 16, [16385], [1000], 15385, 1, 25),
     ("bf16", 64, 1, 1, 256, [32769], [32700], 100, 1, 25),
     ("bf16", 128, 1, 1, 32, [40009], [40008], 1, 1, 25),
+    ("bf16", 64, 2, 2, 256, [8900, 3, 0, 1, 8192], [8899, 1, 0, 1, 9000], 1, 1, 25),   # in tables of 70 pages
 ]
 
 
@@ -381,7 +382,7 @@ EVICTS = [  # dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent
 def test_evict(case, masses):
     dtype, D, Hkv, G, page, lens, keep, max_evict, first, recent = EVICTS[case]
     rng = np.random.default_rng(50 + case)
-    max_pages = max(-(-max(lens) // page) + 1, -(-max_evict // page))
+    max_pages = max(-(-max(lens) // page) + 1, -(-max_evict // page), 70 if max_evict == 1 and page == 256 else 0)
     pool = make(rng, dtype, len(lens), Hkv, G, D, page, max_pages, lens, junk=4.0) if max(lens) < 9000 else None
     if pool is None:  # a long one, quicker to make
         N = max_pages
