@@ -493,12 +493,17 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                 least = fminf(least, x);
                 p[t][r] = __builtin_amdgcn_exp2f(x);
             }
-        const bool small = __any(least < kSmallExponent && c16 < heads);
+        bool small = __any(least < kSmallExponent && c16 < heads);
         if (__builtin_expect(small, 0)) {
+            bool some = false;  // masked rows and scores of -inf, whose weight is 0 either way, are none of them
 #pragma unroll
             for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[t][r] = exp2f((s[t][r] - m) * of_diff);
+                for (int r = 0; r < 4; ++r) {
+                    p[t][r] = exp2f((s[t][r] - m) * of_diff);
+                    some |= p[t][r] > 0.f && p[t][r] < kSmall;
+                }
+            small = __any(some && c16 < heads);
         }
 #pragma unroll
         for (int t = 0; t < BLOCKS; ++t)
@@ -517,15 +522,28 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                 lo[e] = (__bf16)fmaxf(x - h, x * 0x1p-20f);
             };
             // x + V^T . P^T of 16 features, P one of its halves
-            auto multiply = [&](int i, const bf16xp& half, f32x4 x) __attribute__((always_inline)) {
+            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& half, f32x4 x) __attribute__((always_inline)) {
                 if constexpr (BLOCKS == 2)
-                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(vh[i][0], vh[i][1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
                 else
-                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vh[i][0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
             };
-            // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64
+            // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64. A row is in one of the two products
+            // and weighs 0 in the other, which an infinite V does not bear: V's infinities and NaN are taken out of both, with a weight of 1.
             bf16xp hi, lo;
             if (__builtin_expect(small, 0)) {
+#pragma unroll
+                for (int e = 0; e < PV; ++e) hi[e] = p[e / 4][e % 4] > 0.f ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+                for (int i = 0; i < OB; ++i) {
+                    bf16x4 unbounded[BLOCKS];
+#pragma unroll
+                    for (int t = 0; t < BLOCKS; ++t) {
+                        const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), is = (v & (short)0x7f80) == (short)0x7f80;
+                        unbounded[t] = __builtin_bit_cast(bf16x4, v & is), vh[i][t] = __builtin_bit_cast(bf16x4, v & ~is);
+                    }
+                    o[i] = multiply(unbounded, hi, o[i]);
+                }
 #pragma unroll
                 for (int e = 0; e < PV; ++e) {
                     float& x = p[e / 4][e % 4];
@@ -534,7 +552,7 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                 }
 #pragma unroll
                 for (int i = 0; i < OB; ++i) {
-                    const f32x4 x = multiply(i, lo, multiply(i, hi, f32x4{0.f, 0.f, 0.f, 0.f}));
+                    const f32x4 x = multiply(vh[i], lo, multiply(vh[i], hi, f32x4{0.f, 0.f, 0.f, 0.f}));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[i][r] = fmaf(x[r], 0x1p-64f, o[i][r]);
                 }
@@ -542,9 +560,9 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
 #pragma unroll
             for (int e = 0; e < PV; ++e) halves(p[e / 4][e % 4], e, hi, lo);
 #pragma unroll
-            for (int i = 0; i < OB; ++i) o[i] = multiply(i, hi, o[i]);
+            for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], hi, o[i]);
 #pragma unroll
-            for (int i = 0; i < OB; ++i) o[i] = multiply(i, lo, o[i]);
+            for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], lo, o[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4
