@@ -512,28 +512,34 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
         l += sum;
 
         if constexpr (T::kHalf) {
-            // a probability is the sum of two bf16 numbers, its upper half (cut, so that the rest is not negative) and the rest, together
-            // 2^-16 of it off; the rest of one that is not 0 is not 0 either, so that an infinite V stays infinite
+            // a probability enters as the sum of three bf16 numbers, its 24 bits cut into eights (what is left is not negative); none of those of one that
+            // is not 0 is 0, so that an infinite V stays infinite: 2^-24 and 2^-25 of it at least, less than its last bit. (Two numbers, 2^-16 off: B1 H32 640 rows
+            // 8.4 us, with three 8.5; B16 H32 870 rows 38.8, 39.2; two of them in one instruction of 32 rows, which their V has to be copied for: the same.)
             constexpr int PV = BLOCKS * 4;  // probabilities of a lane
             typedef __attribute__((ext_vector_type(PV))) __bf16 bf16xp;
-            auto halves = [](float x, int e, bf16xp& hi, bf16xp& lo) __attribute__((always_inline)) {
-                const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-                hi[e] = (__bf16)h;
-                lo[e] = (__bf16)fmaxf(x - h, x * 0x1p-20f);
+            struct Parts {
+                bf16xp of[3];
             };
-            // x + V^T . P^T of 16 features, P one of its halves
-            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& half, f32x4 x) __attribute__((always_inline)) {
+            auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+            auto split = [&](float x, int e, Parts& to) __attribute__((always_inline)) {
+                const float high = cut(x), rest = x - high, middle = cut(rest);
+                to.of[0][e] = (__bf16)high;
+                to.of[1][e] = (__bf16)fmaxf(middle, x * 0x1p-24f);
+                to.of[2][e] = (__bf16)fmaxf(rest - middle, x * 0x1p-25f);
+            };
+            // x + V^T . P^T of 16 features, P one of its parts
+            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& part, f32x4 x) __attribute__((always_inline)) {
                 if constexpr (BLOCKS == 2)
-                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), half, x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), part, x, 0, 0, 0);
                 else
-                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, half), x, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, part), x, 0, 0, 0);
             };
-            // weights whose halves would leave bf16's range, which count where V is large enough: apart, times 2^64. A row is in one of the two products
+            // weights whose parts would leave bf16's range, which count where V is large enough: apart, times 2^64. A row is in one of the two products
             // and weighs 0 in the other, which an infinite V does not bear: V's infinities and NaN are taken out of both, with a weight of 1.
-            bf16xp hi, lo;
+            Parts parts;
             if (__builtin_expect(small, 0)) {
 #pragma unroll
-                for (int e = 0; e < PV; ++e) hi[e] = p[e / 4][e % 4] > 0.f ? (__bf16)1.f : (__bf16)0.f;
+                for (int e = 0; e < PV; ++e) parts.of[0][e] = p[e / 4][e % 4] > 0.f ? (__bf16)1.f : (__bf16)0.f;
 #pragma unroll
                 for (int i = 0; i < OB; ++i) {
                     bf16x4 unbounded[BLOCKS];
@@ -542,27 +548,29 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                         const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), is = (v & (short)0x7f80) == (short)0x7f80;
                         unbounded[t] = __builtin_bit_cast(bf16x4, v & is), vh[i][t] = __builtin_bit_cast(bf16x4, v & ~is);
                     }
-                    o[i] = multiply(unbounded, hi, o[i]);
+                    o[i] = multiply(unbounded, parts.of[0], o[i]);
                 }
 #pragma unroll
                 for (int e = 0; e < PV; ++e) {
                     float& x = p[e / 4][e % 4];
-                    halves(x < kSmall ? x * 0x1p64f : 0.f, e, hi, lo);
+                    split(x < kSmall ? x * 0x1p64f : 0.f, e, parts);
                     x = x < kSmall ? 0.f : x;
                 }
 #pragma unroll
                 for (int i = 0; i < OB; ++i) {
-                    const f32x4 x = multiply(vh[i], lo, multiply(vh[i], hi, f32x4{0.f, 0.f, 0.f, 0.f}));
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) x = multiply(vh[i], parts.of[part], x);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[i][r] = fmaf(x[r], 0x1p-64f, o[i][r]);
                 }
             }
 #pragma unroll
-            for (int e = 0; e < PV; ++e) halves(p[e / 4][e % 4], e, hi, lo);
+            for (int e = 0; e < PV; ++e) split(p[e / 4][e % 4], e, parts);
 #pragma unroll
-            for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], hi, o[i]);
+            for (int part = 0; part < 3; ++part)
 #pragma unroll
-            for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], lo, o[i]);
+                for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], parts.of[part], o[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4

@@ -14,12 +14,12 @@ def step(pool, q, kn, vn, lens, new_pos, scale, dtype):
                  (terms + 8) U (S_j + max S)
       weight     an exponential of 4 U; rescaled where the maximum rises, once a tile at most, and once where partial results meet; the sum of the
                  weights: n additions at most, and the rescalings go with them; a division:  (n + 40) U
-      weighted V bf16: the weight in two parts, 2^-16 off, 2 n additions at most;  fp32: n additions
+      weighted V bf16: the weight in three parts, 2^-24 + 2^-25 < 2^-23 off, 3 n additions at most;  fp32: n additions
       mass       the mean over `heads`: as many additions and a division
     A mass is added to what was there (one rounding) and an output rounded to its type (half a step)."""
     B, H, D = q.shape
     g, heads = H // pool.Hkv, H // pool.G
-    parts, w_off = (2, 2.0 ** -16) if dtype == "bf16" else (1, 0.0)
+    parts, w_off = (3, 2 * U) if dtype == "bf16" else (1, 0.0)
     out, tol = np.zeros((B, H, D)), np.zeros((B, H, D))
     add, add_tol = np.zeros(pool.mass.shape), np.zeros(pool.mass.shape)
     for b in range(B):

@@ -1,4 +1,4 @@
-"""Infinite values in the attention over paged caches, where rows do not fill a tile and where they do."""
+"""Infinite values and the precision of weights in the attention over paged caches, where rows do not fill a tile and where they do."""
 import numpy as np
 import pytest
 import torch
@@ -69,3 +69,19 @@ def test_infinite_values_beside_small_weights(dtype, D, below, n):
     pool.v[p2, 0, o2, 6] = np.nan
     vn[0, 0, 8] = np.inf
     run(pool, dtype, [n], q, kn, vn, 2 * float(np.log(2)))
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 3])
+def test_weights_are_held_in_24_bits(D, n):
+    """Sums that nearly cancel show what a weight is off by: with weights of 16 bits about a hundredth of these heads is out of bounds. q has one element that
+    is not 0, so that the scores are nearly exact."""
+    H, rng = 2048, np.random.default_rng(7)
+    pool = make(rng, "bf16", 1, 1, 1, D, 16, 4, [n], junk=0.0)
+    q, kn, vn = np.zeros((1, H, D), np.float32), np.zeros((1, 1, D), np.float32), np.zeros((1, 1, D), np.float32)
+    q[0, :, 0] = quantize(rng.uniform(0.1, 1.0, H), "bf16")
+    pool.k[:], pool.v[:] = 0, 0
+    p, o = pool.at(0, 0)
+    pool.k[p, 0, o, 0], pool.v[p, 0, o] = -1.0, 1.0
+    # V of the new row: -w of the d-th head, so that its sum and its neighbours' are small
+    vn[0, 0] = quantize(-np.exp(-q[0, :D, 0].astype(np.float64)), "bf16")
+    run(pool, "bf16", [n], q, kn, vn, 1.0)
