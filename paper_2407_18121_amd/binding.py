@@ -423,7 +423,7 @@ def ec_decode_score_step_static(q, k_new, v_new, k_cache, v_cache, pos, freq, ca
     if freq.dim() != 3:
         raise ValueError("ec_decode_score_step_static: freq must be [B,G,cap]")
     ptrs, po, (B, H, G, D, cap) = _decode_args(q, k_new, v_new, k_cache, v_cache, pos, out, freq.shape[1],
-                                               "ec_decode_score_step_static", "ec_paged_store", "ec_paged_decode_step", "ec_paged_decode_score_step", "ec_paged_evict_min")
+                                               "ec_decode_score_step_static")
     rc = _call(load().ec_decode_score_step_static, *ptrs, _chk(freq, "freq", torch.float32, (B, G, cap)), B, H, G, D,
                cap, cache_len, new_pos, scale, dtype_code(k_cache), po, _stream())
     if check and rc != EC_OK:
