@@ -391,9 +391,11 @@ int ec_evict_min(void* k_cache, void* v_cache, int32_t* pos, float* freq, int B,
  *    GiB.  G is 1 or Hkv.  H query heads share Hkv key/value heads, H a multiple of Hkv; query head h reads key/value head h / (H / Hkv).
  *  - Everything that changes from token to token is read on the device, so the calls can be captured and replayed.
  *  - A table entry outside 0 .. n_pages-1 names no page (entries behind a sequence's last page are not read at all): rows there are
- *    not read, not written and weigh nothing.  Pages that a call only reads may be shared by sequences (a common prefix); a
- *    page that it writes (the new row's; for ec_paged_evict_min all pages of a sequence) must be one sequence's alone, else that
- *    page's contents are unspecified.  Nothing outside the pools is touched in any case.
+ *    not read, not written and weigh nothing.  Pages that a call only reads may be shared by sequences (a common prefix) or named
+ *    twice by one.  A page that it writes must be one sequence's alone, named once, else what it writes there is unspecified: all pages that
+ *    ec_paged_store fills; the new row's for the two steps, and for ec_paged_decode_score_step the masses of ALL pages of a sequence (K, V and
+ *    positions of the others are only read; what it adds to shared masses is lost in part); all pages of a sequence for
+ *    ec_paged_evict_min.  Nothing outside the pools is touched in any case.
  *  - k, v, q, out and the pools start on 16-byte boundaries (else EC_EUNSUPPORTED), ws on one too.
  */
 
@@ -438,7 +440,7 @@ int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, vo
  *     mass_j += p_j for rows j < L,   mass_L = p_L
  * where p is the mean of the step's softmax rows over all query heads (G == 1) or over the query heads of the key/value head
  * (G == Hkv), added in a fixed order.
- *   mass_pages     updated
+ *   mass_pages     updated in every page of a sequence, none of which may be shared then
  *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_DECODE_SCORE_STEP, B,H, max_pages * page, D,dt); zeros before its first use and
  *                  one call at a time, as there
  */

@@ -652,7 +652,7 @@ def ec_paged_decode_step(q, k_new, v_new, k_pages, v_pages, pos_pages, page_tabl
 
 def ec_paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale: float, out,
                                ws, check=True) -> int:
-    """ec_paged_decode_step that also adds the attention every row receives to mass_pages [N,G,page] f32."""
+    """ec_paged_decode_step that also adds the attention every row receives to mass_pages [N,G,page] f32 (no page may be in two sequences then)."""
     if _fast is not None:
         rc = _fast.paged_decode_score_step(q, k_new, v_new, k_pages, v_pages, pos_pages, mass_pages, page_table, cache_len_b, new_pos_b, scale, out,
                                            ws)
