@@ -460,7 +460,7 @@ int ec_paged_decode_score_step(const void* q, const void* k_new, const void* v_n
  * they held.  len_b and keep_b are not changed; pages behind slot m - 1 are the caller's to give away.
  *   pos_pages      may be NULL; protect_first and protect_recent must be 0 then
  *   seen_b         may be NULL when protect_recent is 0
- *   max_evict      1 .. max_pages * page: what no sequence loses more than; sizes the scratch
+ *   max_evict      1 .. max_pages * page: what no sequence loses more than; sizes the scratch, which also serves every smaller one
  *   ws             DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_EVICT_MIN, B,G, max_evict, D,dt)
  */
 int ec_paged_evict_min(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const int32_t* page_table,

@@ -493,10 +493,11 @@ __global__ __launch_bounds__(kEvictThreads) void paged_evict_one_kernel(u32x4* k
     }
 }
 
+// Enough for every smaller max_evict too: the candidates of one row take more than short lists.
 size_t paged_evict_ws(int B, int G, int max_evict)
 {
-    if (max_evict == 1) return (size_t)B * G * kOneParts * sizeof(Candidate);
-    return (((size_t)B * G * 4 + 255) & ~(size_t)255) + (((size_t)B * G * max_evict * 8 + 255) & ~(size_t)255);
+    const size_t lists = (((size_t)B * G * 4 + 255) & ~(size_t)255) + (((size_t)B * G * max_evict * 8 + 255) & ~(size_t)255);
+    return std::max(lists, (size_t)B * G * kOneParts * sizeof(Candidate));
 }
 
 int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const Pages& pages, const int32_t* len_b,
