@@ -8,16 +8,16 @@ namespace ec {
 // ------------------------------------------------------------------ store
 // A workgroup takes kStoreRows rows of a (sequence, head), all its loads in flight; that of the first head takes positions and masses along. Bound: memory,
 // at the rate of a plain copy (5.2 TB/s read and written at B16 H32 1024 .. 2048 rows; 4.97 without the non-temporal hints, 4.8 with 64 rows).
-constexpr int kStoreRows = 32;
+constexpr int kStoreRows = 32, kStoreGrid = 1 << 23;  // (a launch holds less than 2^32 threads in a dimension)
 template <int CH>  // 16-byte chunks of a row
 __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restrict__ k, const u32x4* __restrict__ v, const int32_t* __restrict__ pos,
                                                           const float* __restrict__ mass, Pages pages, const int32_t* __restrict__ start_b,
-                                                          const int32_t* __restrict__ n_rows_b, int Hkv, int G, int T, int src_rows,
+                                                          const int32_t* __restrict__ n_rows_b, int Hkv, int G, int base, int T, int src_rows,
                                                           u32x4* __restrict__ k_pages, u32x4* __restrict__ v_pages, int32_t* __restrict__ pos_pages,
                                                           float* __restrict__ mass_pages)
 {
     constexpr int ROWS = 256 / CH, EACH = kStoreRows / ROWS;  // rows of a pass, passes
-    const int b = blockIdx.z, head = blockIdx.y, r0 = blockIdx.x * kStoreRows;
+    const int b = blockIdx.z, head = blockIdx.y, r0 = base + blockIdx.x * kStoreRows;
     const int n = min(max(n_rows_b ? n_rows_b[b] : T, 0), T), start = start_b ? start_b[b] : 0;
     if (r0 >= n) return;
     auto page_at = [&](int r) {  // page of row r's slot, or -1
@@ -56,16 +56,20 @@ int paged_store_dispatch(const void* k, const void* v, const int32_t* pos, const
                          const int32_t* n_rows_b, int B, int Hkv, int G, int T, int src_rows, int row_bytes, void* k_pages, void* v_pages,
                          int32_t* pos_pages, float* mass_pages, hipStream_t stream)
 {
-    const dim3 grid((T + kStoreRows - 1) / kStoreRows, k ? Hkv : 1, B);
+    const int chunks = (T - 1) / kStoreRows + 1;
+    for (int chunk = 0; chunk < chunks; chunk += kStoreGrid) {  // (once, but for sources of more than 2^28 rows)
+        const dim3 grid(std::min(chunks - chunk, kStoreGrid), k ? Hkv : 1, B);
 #define EC_STORE(CH_)                                                                                                                     \
     if (row_bytes == CH_ * 16)                                                                                                            \
         hipLaunchKernelGGL(paged_store_kernel<CH_>, grid, dim3(256), 0, stream, (const u32x4*)k, (const u32x4*)v, pos, mass, pages, start_b, \
-                           n_rows_b, Hkv, G, T, src_rows, (u32x4*)k_pages, (u32x4*)v_pages, pos_pages, mass_pages)
-    EC_STORE(8);
-    EC_STORE(16);
-    EC_STORE(32);
+                           n_rows_b, Hkv, G, chunk * kStoreRows, T, src_rows, (u32x4*)k_pages, (u32x4*)v_pages, pos_pages, mass_pages)
+        EC_STORE(8);
+        EC_STORE(16);
+        EC_STORE(32);
 #undef EC_STORE
-    return status_from_hip(hipGetLastError());
+        if (const int rc = status_from_hip(hipGetLastError())) return rc;
+    }
+    return EC_OK;
 }
 
 // ------------------------------------------------------------------ eviction
