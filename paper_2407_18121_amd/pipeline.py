@@ -110,35 +110,60 @@ class PagedBatch:
         dt = ec.dtype_code(self.k_pages)
         self.ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, places, H, max_pages * page, D, dt, device)
         self.ws_one = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, places, G, 1, D, dt, device)
-        self.budget = None
+        self.budgets = {}  # by budget, for the batch's lifetime: a graph may hold them
+        self.changes = {}  # entries of the table that are not on the device yet, by their place in it
         self._upload()
 
+    def _send(self, x):
+        """A host tensor on the device, without waiting (torch keeps pinned memory until the copy out of it has ended)."""
+        return x.pin_memory().to(self.table.device, non_blocking=True) if self.table.is_cuda else x
+
     def _ints(self, x):
-        return torch.tensor(x, dtype=torch.int32, device=self.table.device)
+        return self._send(torch.tensor(x, dtype=torch.int32))
 
     def _upload(self):
-        self.numbers.copy_(self._ints([self.rows, [n + 1 for n in self.rows], self.seen, [n + 1 for n in self.seen]]))
+        x = torch.tensor([self.rows, [n + 1 for n in self.rows], self.seen, [n + 1 for n in self.seen]], dtype=torch.int32)
+        self.numbers.copy_(x.pin_memory() if self.table.is_cuda else x, non_blocking=True)
 
     def _budget(self, keep):
-        """`keep` for every place: the layers of a token share the tensor. A graph under capture gets one of its own, filled by its replays."""
-        if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
-            return torch.full_like(self.len_b, keep)
-        if self.budget is None or self.budget[0] != keep:
-            self.budget = (keep, torch.full_like(self.len_b, keep))
-        return self.budget[1]
+        """`keep` for every place: the layers of a token share the tensor, and so do graphs captured after a token with that budget. A graph captured
+        before one has a tensor of its own in every layer, filled by its replays."""
+        if keep not in self.budgets:
+            made = torch.full_like(self.len_b, keep)
+            if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
+                return made
+            self.budgets[keep] = made
+        return self.budgets[keep]
+
+    def _room(self, rows):
+        """Refuses, before anything is changed, what the free pages and a sequence's table do not hold: rows by place."""
+        for b, n in rows.items():
+            if -(-n // self.page) > self.max_pages:
+                raise ValueError(f"sequence {b}: {-(-n // self.page)} pages for {n} rows, but a sequence has {self.max_pages} at most")
+        more = {b: -(-n // self.page) - len(self.held[b]) for b, n in rows.items()}
+        if sum(max(n, 0) for n in more.values()) > len(self.free):
+            raise ValueError(f"{[n for n in more.values() if n > 0]} more pages for sequences {[b for b, n in more.items() if n > 0]}, but {len(self.free)} are free")
 
     def _hold(self, place, rows):
-        """Exactly the pages that `rows` rows need, taken from the free ones or given back to them."""
-        held, need = self.held[place], -(-rows // self.page)
-        if need > self.max_pages or need - len(held) > len(self.free):
-            raise ValueError(f"sequence {place}: {need} pages for {rows} rows, but {len(self.free)} are free and a sequence has {self.max_pages} at most")
-        if need == len(held):
-            return
+        """Exactly the pages that `rows` rows need, taken from the free ones or given back to them; _upload_table() sends what has changed."""
+        held, need, first = self.held[place], -(-rows // self.page), place * self.max_pages
         while len(held) < need:
             held.append(self.free.pop())
+            self.changes[first + len(held) - 1] = held[-1]
         while len(held) > need:
             self.free.append(held.pop())
-        self.table[place].copy_(self._ints(held + [-1] * (self.max_pages - need)))
+            self.changes[first + len(held)] = -1
+
+    def _upload_table(self):
+        if not self.changes:
+            return
+        n = len(self.changes)  # their places (64 bits), then their contents, in one copy
+        x = torch.empty(3 * n, dtype=torch.int32)
+        x[:2 * n].view(torch.int64).copy_(torch.tensor(list(self.changes)))
+        x[2 * n:] = torch.tensor(list(self.changes.values()), dtype=torch.int32)
+        x = self._send(x)
+        self.table.view(-1).index_copy_(0, x[:2 * n].view(torch.int64), x[2 * n:])
+        self.changes = {}
 
     def _places(self, places):
         """Places of the batch, each named once."""
@@ -155,18 +180,18 @@ class PagedBatch:
         for b in places:
             if self.rows[b] >= 0:
                 raise ValueError(f"place {b} holds a sequence")
-        need = [-(-n // self.page) for n in rows]
-        if sum(need) > len(self.free) or max(need, default=0) > self.max_pages:
-            raise ValueError(f"{need} pages for {list(rows)} rows, but {len(self.free)} are free and a sequence has {self.max_pages} at most")
+        self._room(dict(zip(places, rows)))
         for b, n, t in zip(places, rows, seen):
             self._hold(b, n)
             self.rows[b], self.seen[b] = n, t
+        self._upload_table()
         self._upload()
 
     def release(self, place):
         self._places([place])
         self._hold(place, 0)
         self.rows[place], self.seen[place] = -1, 0
+        self._upload_table()
         self._upload()
 
     def store(self, layer, places, k, v, pos, mass):
@@ -174,14 +199,17 @@ class PagedBatch:
         places = self._places(places)
         if any(self.rows[b] > k.shape[2] for b in places):
             raise ValueError(f"{k.shape[2]} rows for sequences of {[self.rows[b] for b in places]}")
-        ec.ec_paged_store(k, v, pos, mass, self.table[places], self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer],
-                          self.mass_pages[layer], None, self._ints([self.rows[b] for b in places]))
+        table = self.table.index_select(0, self._send(torch.tensor(places, dtype=torch.int64)))
+        ec.ec_paged_store(k, v, pos, mass, table, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], None,
+                          self._ints([self.rows[b] for b in places]))
 
     def begin(self):
         """Room for one more row of every sequence."""
-        for b, n in enumerate(self.rows):
-            if n >= 0:
-                self._hold(b, n + 1)
+        rows = {b: n + 1 for b, n in enumerate(self.rows) if n >= 0}
+        self._room(rows)
+        for b, n in rows.items():
+            self._hold(b, n)
+        self._upload_table()
 
     def decode(self, layer, q, k_new, v_new, scale, out):
         """One layer of a token: append and attend (places without a sequence get zeros).  Masses are left alone, so that new rows have none of
@@ -222,4 +250,5 @@ class PagedBatch:
             if n > keep:
                 self.rows[b] = keep
                 self._hold(b, keep)
+        self._upload_table()
         self._upload()
