@@ -4,11 +4,12 @@
     python -m paper_2407_18121_amd.tune merge    # ec_merge_compact on three anchor distributions
     python -m paper_2407_18121_amd.tune select   # ec_select_anchors
     python -m paper_2407_18121_amd.tune score    # ec_prefill_score
-    python -m paper_2407_18121_amd.tune paged    # attention, storing and eviction over pages
+    python -m paper_2407_18121_amd.tune paged    # attention, storing and eviction over pages, and a batch's tokens
 
 Every measurement replays one HIP graph that walks several distinct sets of buffers (so that nothing is served
 from a cache a real layer loop would not have), 100 ms of it before anything is timed, and reports microseconds per call by HIP
-events on the launch stream, the median of five runs.  Inputs are seeded random numbers: this tool times kernels, it checks nothing.
+events on the launch stream, the median of five runs.  (A batch's tokens are called one after the other from the host and timed by its clock.)
+Inputs are seeded random numbers: this tool times kernels, it checks nothing.
 """
 from __future__ import annotations
 
@@ -18,6 +19,7 @@ import time
 import torch
 
 from . import binding as ec
+from .pipeline import PagedBatch
 
 BF16 = torch.bfloat16
 
@@ -170,7 +172,7 @@ def tune_score():
         print(f"score {name}: {ms * 1e3:9.1f} us {3.0 * D * T * (T + 1) * B * H / (ms * 1e-3) / 1e12:7.1f} TFLOP/s", flush=True)
 
 
-def paged_timer(B, H, Hkv, D, rows, page, dtype=BF16, sets=8, G=1):
+def paged_timer(B, H, Hkv, D, rows, page, dtype=BF16, sets=32, G=1):
     """us per call of ec_paged_decode_step, of ec_paged_decode_score_step with the removal of one row, and of storing `rows` rows, over caches of
     `rows` rows in pages of any order; GB/s of the rows' bytes in the first and of both ways in the last."""
     per = rows // page + 1
@@ -178,12 +180,14 @@ def paged_timer(B, H, Hkv, D, rows, page, dtype=BF16, sets=8, G=1):
     k, v = (torch.randn(sets, n_pages, Hkv, page, D, device="cuda").to(dtype) for _ in range(2))
     table = torch.randperm(n_pages, device="cuda").to(torch.int32).view(B, per)
     pos, mass = torch.zeros(sets, n_pages, G, page, dtype=torch.int32, device="cuda"), torch.rand(sets, n_pages, G, page, device="cuda")
+    pos[:, table.long()] = torch.arange(per * page, dtype=torch.int32, device="cuda").view(per, 1, page)
     q, kn, vn = (torch.randn(B, h, D, device="cuda").to(dtype) for h in (H, Hkv, Hkv))
     out, n, one = torch.empty_like(q), torch.full((B,), rows, dtype=torch.int32, device="cuda"), torch.full((B,), rows + 1, dtype=torch.int32, device="cuda")
     dt = ec.dtype_code(q)
     ws = ec.new_workspace(ec.EC_FN_PAGED_DECODE_SCORE_STEP, B, H, per * page, D, dt)
     ws_one = ec.new_workspace(ec.EC_FN_PAGED_EVICT_MIN, B, G, 1, D, dt)
-    src, spos, smass = torch.randn(B, Hkv, rows, D, device="cuda").to(dtype), torch.zeros(B, G, rows, dtype=torch.int32, device="cuda"), torch.rand(B, G, rows, device="cuda")
+    src_k, src_v = (torch.randn(sets, B, Hkv, rows, D, device="cuda").to(dtype) for _ in range(2))
+    spos, smass = torch.zeros(sets, B, G, rows, dtype=torch.int32, device="cuda"), torch.rand(sets, B, G, rows, device="cuda")
 
     def step():
         for i in range(sets):
@@ -196,7 +200,7 @@ def paged_timer(B, H, Hkv, D, rows, page, dtype=BF16, sets=8, G=1):
 
     def store():
         for i in range(sets):
-            ec.ec_paged_store(src, src, spos, smass, table, k[i], v[i], pos[i], mass[i])
+            ec.ec_paged_store(src_k[i], src_v[i], spos[i], smass[i], table, k[i], v[i], pos[i], mass[i])
 
     us = [graph_time_ms(f) * 1e3 / sets for f in (step, scored, store)]
     rows_bytes = 2 * B * Hkv * D * k.element_size() * rows
@@ -224,17 +228,50 @@ def time_paged_evict(B, Hkv, D, rows, keep, page, sets=4, G=1):
     return (graph_time_ms(evict) - graph_time_ms(copies)) * 1e3 / sets
 
 
+def time_batch(places, layers, H, Hkv, D, rows, page, keep, tokens=100):
+    """us per token of a PagedBatch as a generation loop calls it, lengths from `rows` downwards, a row apart; keep 0: without masses."""
+    pages = -(-(rows + tokens + 20) // page)
+    batch = PagedBatch(layers, places, H, Hkv, D, page, places * pages, pages, BF16)
+    lens = [max(rows - b, 1) for b in range(places)]
+    batch.admit(range(places), lens, lens)
+    for pool in (batch.k_pages, batch.v_pages):
+        pool.normal_()
+    q, k = _randn(layers, places, H, D), _randn(layers, places, Hkv, D)
+    out = torch.empty_like(q)
+
+    def token():
+        batch.begin()
+        for i in range(layers):
+            if keep:
+                batch.decode_scored(i, q[i], k[i], k[i], 0.088, out[i], keep)
+            else:
+                batch.decode(i, q[i], k[i], k[i], 0.088, out[i])
+        batch.end(keep or None)
+
+    for _ in range(20):
+        token()
+    torch.cuda.synchronize()
+    start = time.perf_counter()
+    for _ in range(tokens):
+        token()
+    torch.cuda.synchronize()
+    return (time.perf_counter() - start) * 1e6 / tokens
+
+
 def tune_paged():
     print("shape: us of a step | its rows' TB/s | a step with masses and the removal of a row | storing the rows | TB/s read and written")
     for B, H, Hkv, D, rows, page, dtype in ((1, 4, 4, 64, 100, 16, torch.float32), (1, 32, 32, 128, 640, 16, BF16), (1, 32, 8, 128, 2048, 16, BF16),
                                             (8, 32, 8, 128, 1500, 16, BF16), (8, 32, 32, 128, 1000, 16, torch.float32), (16, 32, 32, 128, 870, 16, BF16),
                                             (16, 32, 32, 128, 870, 64, BF16), (8, 32, 32, 64, 1000, 16, BF16), (64, 32, 8, 128, 1000, 16, BF16),
                                             (1, 40, 8, 128, 131072, 64, BF16)):
-        us, gbps, copy = paged_timer(B, H, Hkv, D, rows, page, dtype, 8 if rows < 10000 else 2)
+        us, gbps, copy = paged_timer(B, H, Hkv, D, rows, page, dtype, 32 if rows < 10000 else 2)
         name = f"B{B} H{H}/{Hkv} D{D} {rows} rows, pages of {page}, {'bf16' if dtype == BF16 else 'fp32'}"
         print(f"{name}: {us[0]:8.2f} | {gbps / 1e3:5.2f} | {us[1]:8.2f} | {us[2]:8.2f} | {copy / 1e3:5.2f}", flush=True)
     for B, Hkv, rows, keep in ((1, 32, 640, 512), (8, 8, 3000, 1000), (16, 32, 8192, 820), (16, 32, 8192, 8000)):
         print(f"eviction B{B} Hkv{Hkv} D128 {rows} -> {keep} rows, pages of 16: {time_paged_evict(B, Hkv, 128, rows, keep, 16):8.2f} us", flush=True)
+    for places, layers, H, Hkv, rows in ((1, 32, 32, 32, 640), (16, 4, 32, 32, 870), (16, 32, 32, 32, 870), (64, 32, 32, 8, 400)):
+        plain, scored = (time_batch(places, layers, H, Hkv, 128, rows, 16, keep) for keep in (0, rows))
+        print(f"PagedBatch {places} places H{H}/{Hkv} D128 {rows} rows, {layers} layers: {plain:7.0f} us a token, with masses and the removal of a row {scored:7.0f}", flush=True)
 
 
 def main(argv):
