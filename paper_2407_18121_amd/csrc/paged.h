@@ -24,4 +24,18 @@ struct Pages {
     }
 };
 
+// Sum over the wave's lanes up to this one, of int or uint32_t.
+template <typename T> __device__ __forceinline__ T wave_scan(T x_)
+{
+    static_assert(sizeof(T) == 4);
+    int x = (int)x_;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next one (rows 1, 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
+    return (T)x;
+}
+
 }  // namespace ec

@@ -134,19 +134,6 @@ struct EvictRows {
     }
 };
 
-// Inclusive sum over the wave's lanes.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x_)
-{
-    int x = (int)x_;
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next one (rows 1, 3)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
-    return (uint32_t)x;
-}
-
 // The smallest, the largest over the wave's lanes.
 template <bool LARGEST> __device__ __forceinline__ uint32_t wave_end(uint32_t x)
 {
@@ -174,7 +161,7 @@ template <int WAVES> __device__ __forceinline__ uint32_t block_scan(uint32_t x, 
     const uint32_t in = wave_scan(x);
     if (lane == kWave - 1) sh[wave] = in;
     __syncthreads();
-    const uint32_t sums = wave_scan(lane < WAVES ? sh[lane] : 0);
+    const uint32_t sums = wave_scan(lane < WAVES ? sh[lane] : 0u);
     total = __builtin_amdgcn_readlane(sums, WAVES - 1);
     const uint32_t before = __builtin_amdgcn_readlane(sums, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
     return (wave ? before : 0) + in - x;

@@ -106,16 +106,6 @@ template <int DT, int D> struct PagedTile {
     static __device__ __forceinline__ int swz_v(int r) { return !kHalf ? 0 : CH >= 16 ? (r & 7) << 1 : (r >> 1 & 3) << 1; }
 };
 
-__device__ __forceinline__ int scan_wave(int x)  // sum over the lanes up to this one
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next one (rows 1, 3)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
-    return x;
-}
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
 
 // The maximum, the sum over the lanes that share a query head (l % 16); all four get it.
@@ -189,7 +179,7 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
     long long all = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
         n = rows(b0 + lane);
-        all += last_lane(scan_wave(rounds_of(b0 + lane, n)));
+        all += last_lane(wave_scan(rounds_of(b0 + lane, n)));
     }
     int most = (int)((all * pairs + kPagedSegments - 1) / kPagedSegments);
     // Sequences of different lengths that are cut into two or not at all leave some compute units with much and others with little: twice as many
@@ -199,13 +189,13 @@ template <int ROUND> __device__ __forceinline__ Segment find_segment(const int32
     if (B <= kWave && most >= 8 && B * pairs > kPagedSegments / 3 && B * pairs <= 2 * kPagedSegments &&
         wave_max((float)rounds_of(lane, n)) * B > 1.125f * all) {
         most = (int)((all * pairs + 2 * kPagedSegments - 1) / (2 * kPagedSegments));
-        while (last_lane(scan_wave(divided(rounds_of(lane, n) + most - 1, most))) * pairs > 2 * kPagedSegments) most += (most + 7) / 8;
+        while (last_lane(wave_scan(divided(rounds_of(lane, n) + most - 1, most))) * pairs > 2 * kPagedSegments) most += (most + 7) / 8;
     }
     int before = 0, cut = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
         if (B > kWave) n = rows(b0 + lane);
         const int rounds = rounds_of(b0 + lane, n), count = min(divided(rounds + most - 1, most), most_segments(rounds));
-        const int upto = scan_wave(count), cut_upto = scan_wave(count > 1 ? count : 0);
+        const int upto = wave_scan(count), cut_upto = wave_scan(count > 1 ? count : 0);
         const unsigned long long beyond = __ballot(id < before + upto * pairs);
         if (beyond) {
             const int at = __ffsll(beyond) - 1;
