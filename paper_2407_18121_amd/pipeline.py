@@ -114,6 +114,11 @@ class PagedBatch:
         self.changes = {}  # entries of the table that are not on the device yet, by their place in it
         self._upload()
 
+    def _eager(self, what):
+        """A replay would send the lengths and pages of the capture again, out of memory that holds something else by then."""
+        if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError(f"PagedBatch.{what}() cannot be captured: it sends what the host knows now (a token's graph holds its decode calls)")
+
     def _send(self, x):
         """A host tensor on the device, without waiting (torch keeps pinned memory until the copy out of it has ended)."""
         return x.pin_memory().to(self.table.device, non_blocking=True) if self.table.is_cuda else x
@@ -174,6 +179,7 @@ class PagedBatch:
 
     def admit(self, places, rows, seen):
         """Pages for sequences that start with `rows` rows of a prompt of `seen` tokens; store() brings the rows of every layer."""
+        self._eager("admit")
         places = self._places(places)
         if not len(places) == len(rows) == len(seen) or any(n < 0 for n in rows):
             raise ValueError(f"places {places}, rows {list(rows)} and seen {list(seen)} do not belong together")
@@ -188,6 +194,7 @@ class PagedBatch:
         self._upload()
 
     def release(self, place):
+        self._eager("release")
         self._places([place])
         self._hold(place, 0)
         self.rows[place], self.seen[place] = -1, 0
@@ -196,6 +203,7 @@ class PagedBatch:
 
     def store(self, layer, places, k, v, pos, mass):
         """Rows 0.. of k, v [len(places),Hkv,n,D], pos and mass [len(places),G,n] as the sequences' rows (their first rows[place] ones)."""
+        self._eager("store")
         places = self._places(places)
         if any(self.rows[b] > k.shape[2] for b in places):
             raise ValueError(f"{k.shape[2]} rows for sequences of {[self.rows[b] for b in places]}")
@@ -205,6 +213,7 @@ class PagedBatch:
 
     def begin(self):
         """Room for one more row of every sequence."""
+        self._eager("begin")
         rows = {b: n + 1 for b, n in enumerate(self.rows) if n >= 0}
         self._room(rows)
         for b, n in rows.items():
@@ -227,6 +236,7 @@ class PagedBatch:
 
     def end(self, keep: int | None = None):
         """Behind the last layer of a token; keep as in decode_scored, None after decode."""
+        self._eager("end")
         if any(n >= len(held) * self.page for n, held in zip(self.rows, self.held)):
             raise ValueError("a token ends, but begin() has not made room for its row")
         for b, n in enumerate(self.rows):
@@ -237,6 +247,7 @@ class PagedBatch:
 
     def shrink(self, keep: int):
         """Sequences of more than `keep` rows keep the heaviest, in every layer; the pages behind are free."""
+        self._eager("shrink")
         if keep < 0:
             raise ValueError(f"keep is {keep}")
         most = max(max(self.rows) - keep, 0)

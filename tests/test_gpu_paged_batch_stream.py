@@ -94,3 +94,25 @@ def test_layers_of_a_captured_token_share_the_budget():
     for _ in range(3):
         graph.replay()
         assert copy.eq(23).all() and batch._budget(12).eq(12).all()
+
+
+def test_what_the_host_sends_is_not_captured():
+    """Refused with everything as it was, and the graph of a token around it still works."""
+    batch = admitted()
+    inputs, out = made(1)
+    x = [x[0, 0] for x in inputs]
+    kv, pos = torch.zeros(1, HKV, 64, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 1, 64, dtype=torch.int32, device="cuda")
+    batch.begin()
+    batch.decode(0, *x, 0.125, out[0, 0])
+    state = lambda: (list(batch.rows), list(batch.seen), [list(h) for h in batch.held], list(batch.free), dict(batch.changes))  # noqa: E731
+    before, graph = state(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in (lambda: batch.admit([2], [3], [3]), lambda: batch.release(0), lambda: batch.store(0, [0], kv, kv, pos, pos.float()), batch.begin, batch.end,
+                     lambda: batch.shrink(3)):
+            with pytest.raises(RuntimeError, match="cannot be captured"):
+                call()
+        batch.decode(0, *x, 0.125, out[0, 1])
+    graph.replay()
+    assert state() == before and torch.equal(out[0, 0], out[0, 1])
+    batch.end()
+    assert batch.numbers[0].tolist() == [8, 10, -1, 31, 65]
