@@ -7,7 +7,7 @@ namespace ec {
 
 // ------------------------------------------------------------------ store
 // A workgroup takes kStoreRows rows of a (sequence, head), all its loads in flight; that of the first head takes positions and masses along. Bound: memory,
-// at the rate of a plain copy (5.2 TB/s read and written at B16 H32 1024 .. 2048 rows; 4.97 without the non-temporal hints, 4.8 with 64 rows).
+// at the rate of a plain copy (5.3 TB/s read and written at B16 H32 1024 .. 2048 rows; 4.97 without the non-temporal hints, 4.8 with 64 rows).
 constexpr int kStoreRows = 32, kStoreGrid = 1 << 23;  // (a launch holds less than 2^32 threads in a dimension)
 template <int CH>  // 16-byte chunks of a row
 __global__ __launch_bounds__(256) void paged_store_kernel(const u32x4* __restrict__ k, const u32x4* __restrict__ v, const int32_t* __restrict__ pos,

@@ -9,7 +9,7 @@
 // The segments' results meet by the rule of the softmax: with M the largest of their maxima m_i, out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
 //
 // Bound by the bytes of the rows, of which the counters see 1.002 .. 1.003 times what has to be read (a large copy on this card moves 5.0 .. 5.5 TB/s):
-//   bf16 D128 B16 H32/32 870 rows 39.0 us, 5.9 TB/s; one cache of 131071 rows, H40/8 89.3, 6.0; fp32 B8 H32/32 1000 rows 48.9, 5.4.
+//   bf16 D128 B16 H32/32 870 rows 39.6 us, 5.8 TB/s; one cache of 131071 rows, H40/8 89.2, 6.0; fp32 B8 H32/32 1000 rows 47.7, 5.5.
 // Short caches by a chain of latencies, 8 us of B1 H32/32 640 rows: lengths and pages 0.6, first rows 1.1, a tile 0.8 and 0.5 for each further one,
 // the waves' results 1.0, the ticket 0.5, the other segments' results 2.
 #include <algorithm>
