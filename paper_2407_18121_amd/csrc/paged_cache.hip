@@ -416,7 +416,8 @@ struct Least {
 };
 
 // Long sequences, whose masses one compute unit is slow to read: the least row of each part, a workgroup a part, in a launch before (us of a call, one launch /
-// two: one sequence of 16300 rows 7.6 / 8.1, 24000 9.2 / 8.1, 131000 33 / 8.2; 16 of 16300 8.1 / 8.5, 24000 10.7 / 8.8).
+// two: one sequence of 16300 rows 7.6 / 8.1, 24000 9.2 / 8.1, 131000 33 / 8.2; 16 of 16300 8.1 / 8.5, 24000 10.7 / 8.8). The host knows
+// the tables' room only: short sequences in long tables pay for the launch (640 rows 4.1 / 6.2, 16 of 640 4.5 / 6.9, one of 8000 5.2 / 7.2).
 constexpr int kOneParts = 64, kOneAlone = 16384;  // slots up to which the workgroup that fills the hole looks through them all
 struct Candidate {
     unsigned long long of;
