@@ -427,7 +427,8 @@ int ec_paged_store(const void* k, const void* v, const int32_t* pos, const float
  *                  use (calls leave at zero what has to be), this call's and ec_paged_decode_score_step's alone, of one call at a
  *                  time: calls that may overlap, on two streams or in two graphs, need one each
  * Products are formed on the matrix cores with fp32 accumulation, sums and the softmax in fp32 (bf16: a weight enters its product with V
- * as the sum of three bf16 numbers, its 24 bits).  A weight below fp32's range, 2^-149 of the largest, counts as 0.  Results are deterministic.
+ * as the sum of three bf16 numbers, its 24 bits).  A weight below the range of fp32, 2^-149 of the largest, is 0, and an infinite V with it NaN.
+ * Results are deterministic.
  */
 int ec_paged_decode_step(const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, int32_t* pos_pages,
                          const int32_t* page_table, const int32_t* cache_len_b, const int32_t* new_pos_b, int B, int H, int Hkv,
