@@ -25,6 +25,7 @@
  *    head-wise variant of the ablation (Table 3c).
  *  - Supported: D in {64,128}; dt in {EC_F32, EC_BF16}; multi-head attention
  *    with as many key/value heads as query heads; the calls on paged caches also take fewer key/value heads.
+ *  - Several new tokens of a sequence at a time over paged caches: ec_tokens.h.
  */
 #ifndef EC_H_
 #define EC_H_
@@ -56,7 +57,10 @@ typedef enum {
     EC_FN_PAGED_STORE = 6,
     EC_FN_PAGED_DECODE_STEP = 7,
     EC_FN_PAGED_DECODE_SCORE_STEP = 8,
-    EC_FN_PAGED_EVICT_MIN = 9
+    EC_FN_PAGED_EVICT_MIN = 9,
+    EC_FN_PAGED_PLAN = 10,
+    EC_FN_PAGED_ROTARY_STORE = 11,
+    EC_FN_PAGED_CHUNK_STEP = 12
 } ec_fn;
 
 /* Budget rule of the retention test (Sec. 3.3 Output Generation; Alg. 1). */
@@ -84,7 +88,7 @@ const char* ec_status_string(int status);
  * Bytes of workspace the given entry point needs for these shapes.  Host, pure.
  * For EC_FN_DECODE_STEP and EC_FN_DECODE_SCORE_STEP pass T = cap; for EC_FN_PAGED_DECODE_STEP and
  * EC_FN_PAGED_DECODE_SCORE_STEP H query heads and T = max_pages * page; for EC_FN_PAGED_EVICT_MIN H = G and
- * T = max_evict.  Returns 0 for entry points that need none
+ * T = max_evict; for EC_FN_PAGED_CHUNK_STEP H query heads and T tokens.  Returns 0 for entry points that need none
  * and (size_t)-1 for unsupported shapes.
  */
 size_t ec_workspace_bytes(int fn, int B, int H, int T, int D, int dt);

@@ -19,16 +19,19 @@ LIB_PATH = os.environ.get("EC_LIB_PATH", os.path.join(_HERE, "libelastic_cache.s
 EC_OK, EC_EINVAL, EC_EUNSUPPORTED, EC_EWORKSPACE, EC_EDEVICE = range(5)
 EC_F32, EC_BF16 = 0, 1
 (EC_FN_PREFILL_SCORE, EC_FN_SELECT_ANCHORS, EC_FN_MERGE_COMPACT, EC_FN_DECODE_STEP, EC_FN_DECODE_SCORE_STEP,
- EC_FN_EVICT_MIN, EC_FN_PAGED_STORE, EC_FN_PAGED_DECODE_STEP, EC_FN_PAGED_DECODE_SCORE_STEP, EC_FN_PAGED_EVICT_MIN) = range(10)
+ EC_FN_EVICT_MIN, EC_FN_PAGED_STORE, EC_FN_PAGED_DECODE_STEP, EC_FN_PAGED_DECODE_SCORE_STEP, EC_FN_PAGED_EVICT_MIN,
+ EC_FN_PAGED_PLAN, EC_FN_PAGED_ROTARY_STORE, EC_FN_PAGED_CHUNK_STEP) = range(13)
 EC_BUDGET_RATIO, EC_BUDGET_FIXED = 0, 1
 EC_TRUNC_RECENT, EC_TRUNC_ABS = 0, 1
 EC_MERGE_MEAN, EC_MERGE_EVICT = 0, 1
+EC_ROTARY_HALVES, EC_ROTARY_NEIGHBOURS = 0, 1
 
 SYMBOLS = ("ec_status_string", "ec_workspace_bytes", "ec_prefill_score", "ec_chunk_score", "ec_select_anchors",
            "ec_merge_compact", "ec_remerge_compact", "ec_evict_index", "ec_decode_step", "ec_decode_score_step",
            "ec_evict_min", "ec_prefill_score_varlen", "ec_select_anchors_varlen", "ec_merge_compact_varlen",
            "ec_decode_step_varlen", "ec_importance_mean", "ec_retention_step_varlen", "ec_decode_step_shaped",
            "ec_decode_score_step_static", "ec_paged_store", "ec_paged_decode_step", "ec_paged_decode_score_step", "ec_paged_evict_min")
+TOKEN_SYMBOLS = ("ec_paged_plan", "ec_paged_rotary_store", "ec_paged_chunk_step")  # of ec_tokens.h
 
 _lib = None
 _fast = None  # the usual calls in native code (csrc/fastcall.cpp); None in an answer of theirs: not a usual call
@@ -101,6 +104,12 @@ def load():
     lib.ec_paged_decode_score_step.restype = c_int
     lib.ec_paged_evict_min.argtypes = [c_vp] * 8 + [c_int] * 11 + [c_vp, c_sz, c_vp]
     lib.ec_paged_evict_min.restype = c_int
+    lib.ec_paged_plan.argtypes = [c_vp] * 7 + [c_int] * 5 + [c_vp] * 7
+    lib.ec_paged_plan.restype = c_int
+    lib.ec_paged_rotary_store.argtypes = [c_vp] * 3 + [ctypes.c_int64] * 3 + [c_vp] * 3 + [c_f] + [c_int] * 10 + [c_vp] * 6
+    lib.ec_paged_rotary_store.restype = c_int
+    lib.ec_paged_chunk_step.argtypes = [c_vp] * 6 + [c_int] * 8 + [c_f, c_int] + [c_vp] * 3 + [c_sz, c_vp]
+    lib.ec_paged_chunk_step.restype = c_int
     _fast = _load_fast(lib)
     _lib = lib
     return lib
@@ -685,3 +694,76 @@ def ec_paged_evict_min(k_pages, v_pages, pos_pages, mass_pages, page_table, len_
                _chk(page_table, "page_table", i32, (B, max_pages)), _i32(len_b, "len_b", B), _i32(keep_b, "keep_b", B), _i32(seen_b, "seen_b", B, True),
                B, Hkv, G, D, page, N, max_pages, max_evict, protect_first, protect_recent, dtype_code(k_pages), wp, wb, _stream())
     return _status("ec_paged_evict_min", rc, check)
+
+
+def ec_paged_plan(len_b, new_b, page_table, held_b, free_pages, n_free, page: int, start_b, len_after_b, token_start, rows=None, pos=None, seen_b=None,
+                  seen_after_b=None, T: int | None = None, check=True) -> int:
+    """Pages for new_b[b] rows behind len_b[b] of every sequence, out of the stack free_pages[:n_free] (n_pages entries), and where every token goes: int32 [B] len_b,
+    new_b, held_b, start_b, len_after_b, seen_b, seen_after_b, [B,max_pages] page_table, [1] n_free, [B+1] token_start, [T] pos; rows int64 [T].
+    T is the size of rows or pos, or is given."""
+    B, max_pages = _paged_table(page_table, "ec_paged_plan")
+    maps = rows if rows is not None else pos
+    if maps is not None:
+        T = maps.numel()
+    if T is None:
+        raise ValueError("ec_paged_plan: T is needed without rows and pos")
+    i32, N = torch.int32, free_pages.numel()
+    _same_device(len_b, new_b, page_table, held_b, free_pages, n_free, start_b, len_after_b, token_start, rows, pos, seen_b, seen_after_b)
+    rc = _call(load().ec_paged_plan, _i32(len_b, "len_b", B), _i32(new_b, "new_b", B), _i32(seen_b, "seen_b", B, True),
+               _chk(page_table, "page_table", i32, (B, max_pages)), _i32(held_b, "held_b", B), _i32(free_pages, "free_pages", N), _i32(n_free, "n_free", 1),
+               B, T, page, N, max_pages, _i32(start_b, "start_b", B), _i32(len_after_b, "len_after_b", B), _i32(seen_after_b, "seen_after_b", B, True),
+               _i32(token_start, "token_start", B + 1), _chk(rows, "rows", torch.int64, (T,), True), _i32(pos, "pos", T, True), _stream())
+    return _status("ec_paged_plan", rc, check)
+
+
+def _tokens(t, name, dtype, shape):
+    """Pointer and elements from token to token of [T,heads,D] whose tokens may lie apart: a part of a projection's output."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if (shape[2] > 1 and t.stride(2) != 1) or (shape[1] > 1 and t.stride(1) != shape[2]):
+        raise ValueError(f"{name}: the heads of a token must be dense")
+    step = t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+    return (t.data_ptr() if t.is_cuda else _Checked(t, name)), step
+
+
+def ec_paged_rotary_store(q, k, v, pos, rows, freq, q_out, k_pages, v_pages, pos_pages=None, mass_pages=None, interleaved: bool = False, mscale: float = 1.0,
+                          check=True) -> int:
+    """q [T,H,D], k,v [T,Hkv,D], tokens at any distance (views of one projection); pos int32 [T], rows int64 [T] as ec_paged_plan writes them; freq f32 [rot/2]
+    -> q_out [T,H,D] and the rows of the pools (k_pages,v_pages [N,Hkv,page,D], pos_pages int32, mass_pages f32 [N,G,page] or None)."""
+    if q.dim() != 3 or k.dim() != 3 or k_pages.dim() != 4:
+        raise ValueError("ec_paged_rotary_store: q and k must be [T,heads,D] and k_pages [N,Hkv,page,D]")
+    T, H, D = q.shape
+    N, Hkv, page, _ = k_pages.shape
+    dt, i32, f32 = k_pages.dtype, torch.int32, torch.float32
+    groups = pos_pages if pos_pages is not None else mass_pages
+    if groups is not None and groups.dim() != 3:
+        raise ValueError("ec_paged_rotary_store: pos_pages and mass_pages must be [N,G,page]")
+    G = _groups(groups.shape[1] if groups is not None else 1, Hkv, "ec_paged_rotary_store")
+    _same_device(q, k, v, pos, rows, freq, q_out, k_pages, v_pages, pos_pages, mass_pages)
+    (qp, qs), (kp, ks), (vp, vs) = _tokens(q, "q", dt, (T, H, D)), _tokens(k, "k", dt, (T, Hkv, D)), _tokens(v, "v", dt, (T, Hkv, D))
+    rc = _call(load().ec_paged_rotary_store, qp, kp, vp, qs, ks, vs, _i32(pos, "pos", T), _chk(rows, "rows", torch.int64, (T,)),
+               _chk(freq, "freq", f32, (freq.numel(),)), mscale, 2 * freq.numel(), EC_ROTARY_NEIGHBOURS if interleaved else EC_ROTARY_HALVES, T, H, Hkv, G, D, page,
+               N, dtype_code(k_pages), _chk(q_out, "q_out", dt, (T, H, D)), _chk(k_pages, "k_pages", dt, (N, Hkv, page, D)),
+               _chk(v_pages, "v_pages", dt, (N, Hkv, page, D)), _chk(pos_pages, "pos_pages", i32, (N, G, page), True),
+               _chk(mass_pages, "mass_pages", f32, (N, G, page), True), _stream())
+    return _status("ec_paged_rotary_store", rc, check)
+
+
+def ec_paged_chunk_step(q, k_pages, v_pages, page_table, start_b, token_start, scale: float, out, ws, lse=None, check=True) -> int:
+    """q,out [T,H,D], tokens of sequence b from token_start[b] on (int32 [B+1]); k_pages,v_pages [N,Hkv,page,D] hold their rows from slot start_b[b] on (int32 [B]);
+    lse f32 [T,H] or None."""
+    B, max_pages = _paged_table(page_table, "ec_paged_chunk_step")
+    if q.dim() != 3 or k_pages.dim() != 4:
+        raise ValueError("ec_paged_chunk_step: q must be [T,H,D] and k_pages [N,Hkv,page,D]")
+    T, H, D = q.shape
+    N, Hkv, page, _ = k_pages.shape
+    dt, i32 = k_pages.dtype, torch.int32
+    _same_device(q, k_pages, v_pages, page_table, start_b, token_start, out, ws, lse)
+    wp, wb = _ws(ws)
+    rc = _call(load().ec_paged_chunk_step, _chk(q, "q", dt, (T, H, D)), _chk(k_pages, "k_pages", dt, (N, Hkv, page, D)),
+               _chk(v_pages, "v_pages", dt, (N, Hkv, page, D)), _chk(page_table, "page_table", i32, (B, max_pages)), _i32(start_b, "start_b", B),
+               _i32(token_start, "token_start", B + 1), B, T, H, Hkv, D, page, N, max_pages, scale, dtype_code(k_pages), _chk(out, "out", dt, (T, H, D)),
+               _chk(lse, "lse", torch.float32, (T, H), True), wp, wb, _stream())
+    return _status("ec_paged_chunk_step", rc, check)

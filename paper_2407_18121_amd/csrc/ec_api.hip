@@ -5,6 +5,7 @@
 #include <initializer_list>
 #include <mutex>
 
+#include "../../include/ec_tokens.h"
 #include "ec_common.h"
 #include "paged.h"
 #include "score_route.h"
@@ -51,6 +52,15 @@ int paged_step_dispatch(const void* q, const void* k_new, const void* v_new, voi
 int paged_evict_dispatch(void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, const Pages& pages, const int32_t* len_b,
                          const int32_t* keep_b, const int32_t* seen_b, int B, int Hkv, int G, int row_bytes, int max_evict, int protect_first,
                          int protect_recent, void* ws, hipStream_t stream);
+size_t paged_chunk_ws(int T, int H, int D);
+int paged_plan_dispatch(const int32_t* len_b, const int32_t* new_b, const int32_t* seen_b, int32_t* page_table, int32_t* held_b, int32_t* free_pages,
+                        int32_t* n_free, int B, int T, int page_shift, int n_pages, int max_pages, int32_t* start_b, int32_t* len_after_b,
+                        int32_t* seen_after_b, int32_t* token_start, int64_t* rows, int32_t* pos, hipStream_t stream);
+int paged_rotary_dispatch(const void* q, const void* k, const void* v, int64_t q_step, int64_t k_step, int64_t v_step, const int32_t* pos,
+                          const int64_t* rows, const float* freq, float mscale, int rot, bool neighbours, int T, int H, int Hkv, int G, int D, int page_shift,
+                          int n_pages, int dt, void* q_out, void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, hipStream_t stream);
+int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages, const Pages& pages, const int32_t* start_b, const int32_t* token_start,
+                         int B, int T, int H, int Hkv, int D, float scale, int dt, void* out, float* lse, void* ws, hipStream_t stream);
 int head_mean_launch(const float* head_imp, float* score, int B, int H, int T, hipStream_t stream);
 }  // namespace ec
 
@@ -80,6 +90,10 @@ void* static_scratch_ptr()
 }
 
 bool shape_supported(int D, int dt) { return (D == 64 || D == 128) && (dt == EC_F32 || dt == EC_BF16); }
+
+// Packed tokens of a call, with all their query heads.
+constexpr int kMostTokens = 1 << 24;
+bool tokens_ok(int T, int H) { return T <= kMostTokens && (long long)T * H <= 1 << 30; }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -169,6 +183,11 @@ size_t ec_workspace_bytes(int fn, int B, int H, int T, int D, int dt)
             if (!shape_supported(D, dt)) return (size_t)-1;
             return ec::paged_step_ws(B, H, T, D, fn == EC_FN_PAGED_DECODE_SCORE_STEP);
         case EC_FN_PAGED_EVICT_MIN: return ec::paged_evict_ws(B, H, T);
+        case EC_FN_PAGED_PLAN: return 0;
+        case EC_FN_PAGED_ROTARY_STORE: return 0;
+        case EC_FN_PAGED_CHUNK_STEP:
+            if (!shape_supported(D, dt) || !tokens_ok(T, H)) return (size_t)-1;
+            return ec::paged_chunk_ws(T, H, D);
         default: return (size_t)-1;
     }
 }
@@ -438,12 +457,17 @@ bool aligned16(std::initializer_list<const void*> ptrs)
 
 int row_bytes(int D, int dt) { return D * (dt == EC_BF16 ? 2 : 4); }
 
+// Some byte of [p, p + n) lies in [q, q + m).
+bool overlap(const void* p, size_t n, const void* q, size_t m) { return p && q && (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n; }
+
+bool page_ok(int page) { return !(page & (page - 1)) && page >= 8 && page <= 256; }
+
 // What every call on paged caches is checked for; EC_OK, and the pages then.
 int paged_shape(const int32_t* page_table, int B, int Hkv, int G, int D, int page, int n_pages, int max_pages, int dt, ec::Pages& pages)
 {
     if (!page_table || B < 1 || Hkv < 1 || D < 1 || page < 1 || n_pages < 1 || max_pages < 1) return EC_EINVAL;
     if (G != 1 && G != Hkv) return EC_EINVAL;
-    if ((page & (page - 1)) || page < 8 || page > 256 || (long long)max_pages * page > 1 << 28) return EC_EUNSUPPORTED;
+    if (!page_ok(page) || (long long)max_pages * page > 1 << 28) return EC_EUNSUPPORTED;
     if ((long long)n_pages * page >= 1LL << 32) return EC_EUNSUPPORTED;
     if ((long long)B * Hkv > 65535) return EC_EUNSUPPORTED;
     if (!shape_supported(D, dt)) return EC_EUNSUPPORTED;
@@ -519,6 +543,68 @@ int ec_paged_evict_min(void* k_pages, void* v_pages, int32_t* pos_pages, float* 
     if (!ws || ws_bytes < ec_workspace_bytes(EC_FN_PAGED_EVICT_MIN, B, G, max_evict, D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
     return ec::paged_evict_dispatch(k_pages, v_pages, pos_pages, mass_pages, pages, len_b, keep_b, seen_b, B, Hkv, G, row_bytes(D, dt), max_evict,
                                     protect_first, protect_recent, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
+int ec_paged_plan(const int32_t* len_b, const int32_t* new_b, const int32_t* seen_b, int32_t* page_table, int32_t* held_b, int32_t* free_pages,
+                  int32_t* n_free, int B, int T, int page, int n_pages, int max_pages, int32_t* start_b, int32_t* len_after_b, int32_t* seen_after_b,
+                  int32_t* token_start, int64_t* rows, int32_t* pos, void* stream)
+{
+    if (!len_b || !new_b || !page_table || !held_b || !free_pages || !n_free || !start_b || !len_after_b || !token_start) return EC_EINVAL;
+    if (!seen_b != !seen_after_b || B < 1 || T < 1 || page < 1 || n_pages < 1 || max_pages < 1) return EC_EINVAL;
+    if (!page_ok(page) || (long long)max_pages * page > 1 << 28 || (long long)n_pages * page >= 1LL << 32) return EC_EUNSUPPORTED;
+    if (B > ec::kPlanMost || T > kMostTokens) return EC_EUNSUPPORTED;
+    const size_t batch = (size_t)B * 4;
+    const struct {
+        const void* p;
+        size_t bytes;
+    } all[] = {{page_table, batch * max_pages}, {held_b, batch}, {free_pages, (size_t)n_pages * 4}, {n_free, 4}, {start_b, batch}, {len_after_b, batch},
+               {seen_after_b, batch}, {token_start, batch + 4}, {rows, (size_t)T * 8}, {pos, (size_t)T * 4}, {len_b, batch}, {new_b, batch}, {seen_b, batch}};
+    constexpr int kWritten = 10, kAll = 13;
+    for (int i = 0; i < kWritten; ++i)
+        for (int j = i + 1; j < kAll; ++j) {
+            const bool in_place = all[i].p == all[j].p && ((all[i].p == len_after_b && j == 10) || (all[i].p == seen_after_b && j == 12));
+            if (!in_place && overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes)) return EC_EINVAL;
+        }
+    return ec::paged_plan_dispatch(len_b, new_b, seen_b, page_table, held_b, free_pages, n_free, B, T, __builtin_ctz((unsigned)page), n_pages, max_pages, start_b,
+                                   len_after_b, seen_after_b, token_start, rows, pos, reinterpret_cast<hipStream_t>(stream));
+}
+
+int ec_paged_rotary_store(const void* q, const void* k, const void* v, int64_t q_step, int64_t k_step, int64_t v_step, const int32_t* pos, const int64_t* rows,
+                          const float* freq, float mscale, int rot, int pairing, int T, int H, int Hkv, int G, int D, int page, int n_pages, int dt, void* q_out,
+                          void* k_pages, void* v_pages, int32_t* pos_pages, float* mass_pages, void* stream)
+{
+    if (!q || !k || !v || !pos || !rows || !freq || !q_out || !k_pages || !v_pages) return EC_EINVAL;
+    if (T < 1 || H < 1 || rot < 2 || rot % 2 || rot > D || !std::isfinite(mscale)) return EC_EINVAL;
+    if (pairing != EC_ROTARY_HALVES && pairing != EC_ROTARY_NEIGHBOURS) return EC_EINVAL;
+    ec::Pages pages;
+    if (const int rc = paged_shape(pos, 1, Hkv, G, D, page, n_pages, 1, dt, pages)) return rc;
+    if (H > 65535 || !tokens_ok(T, H) || !tokens_ok(T, Hkv)) return EC_EUNSUPPORTED;
+    const int64_t e = dt == EC_BF16 ? 2 : 4, most = (int64_t)1 << 40;
+    if (q_step < (int64_t)H * D || k_step < (int64_t)Hkv * D || v_step < (int64_t)Hkv * D) return EC_EINVAL;
+    if (q_step > most || k_step > most || v_step > most || (q_step | k_step | v_step) * e % 16) return EC_EUNSUPPORTED;
+    if (!aligned16({q, k, v, q_out, k_pages, v_pages})) return EC_EUNSUPPORTED;
+    const size_t out_bytes = (size_t)T * H * D * e;
+    auto span = [&](int64_t step, int heads) { return (size_t)((T - 1) * step + (int64_t)heads * D) * e; };
+    if (overlap(q_out, out_bytes, q, span(q_step, H)) || overlap(q_out, out_bytes, k, span(k_step, Hkv)) || overlap(q_out, out_bytes, v, span(v_step, Hkv)))
+        return EC_EINVAL;
+    return ec::paged_rotary_dispatch(q, k, v, q_step * e, k_step * e, v_step * e, pos, rows, freq, mscale, rot, pairing == EC_ROTARY_NEIGHBOURS, T, H, Hkv, G, D,
+                                     pages.shift, n_pages, dt, q_out, k_pages, v_pages, pos_pages, mass_pages, reinterpret_cast<hipStream_t>(stream));
+}
+
+int ec_paged_chunk_step(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* start_b, const int32_t* token_start,
+                        int B, int T, int H, int Hkv, int D, int page, int n_pages, int max_pages, float scale, int dt, void* out, float* lse, void* ws,
+                        size_t ws_bytes, void* stream)
+{
+    if (!q || !k_pages || !v_pages || !start_b || !token_start || !out) return EC_EINVAL;
+    if (T < 1 || H < 1 || Hkv < 1 || H % Hkv || !scale_ok(scale)) return EC_EINVAL;
+    ec::Pages pages;
+    if (const int rc = paged_shape(page_table, B, Hkv, 1, D, page, n_pages, max_pages, dt, pages)) return rc;
+    if (H > 65535 || !tokens_ok(T, H) || !aligned16({q, k_pages, v_pages, out})) return EC_EUNSUPPORTED;
+    if (!ws || ws_bytes < ec_workspace_bytes(EC_FN_PAGED_CHUNK_STEP, B, H, T, D, dt) || !aligned16({ws})) return EC_EWORKSPACE;
+    const size_t bytes = (size_t)T * H * row_bytes(D, dt), lse_bytes = (size_t)T * H * 4;
+    if (overlap(out, bytes, q, bytes) || overlap(lse, lse_bytes, q, bytes) || overlap(lse, lse_bytes, out, bytes)) return EC_EINVAL;
+    return ec::paged_chunk_dispatch(q, k_pages, v_pages, pages, start_b, token_start, B, T, H, Hkv, D, scale, dt, out, lse, ws,
+                                    reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

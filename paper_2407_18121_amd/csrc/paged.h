@@ -24,6 +24,8 @@ struct Pages {
     }
 };
 
+constexpr int kPlanMost = 8192;  // sequences of a batch that is planned on the device: their sums lie in LDS
+
 // Sum over the wave's lanes up to this one, of int or uint32_t.
 template <typename T> __device__ __forceinline__ T wave_scan(T x_)
 {

@@ -1,0 +1,657 @@
+// ec_paged_chunk_step: attention of the new tokens of every sequence, packed one after the other, over the rows that are cached in pages, their own
+// among them: token i of a sequence of L rows before the step sees slots 0 .. L + i.
+//
+// The query heads that share a key/value head lie one after the other: row r of a (sequence, key/value head) is token r / group, head r % group of its
+// query heads, so that every row of K and V that comes in serves all of them, and one token of many heads is as good a tile as many tokens
+// of one head. A workgroup takes a tile of these rows and a segment of the slots that they see; where a batch has few tiles, long sequences are cut
+// into several segments, whose results meet in a second launch by the rule of the softmax: with M the largest of their maxima m_i,
+// out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
+#include <algorithm>
+#include <type_traits>
+
+#include "paged_tile.h"
+
+namespace ec {
+
+constexpr int kChunkTarget = 512;  // segments that a launch is cut into, about: as many as the chip holds at once
+constexpr int kChunkLeast = 4;     // units of a segment, at least
+constexpr int kChunkJoinRows = 4;  // rows of a joining workgroup, a wave each
+
+struct ChunkStep {
+    const void *q, *k_pages, *v_pages;
+    void* out;
+    float* lse;
+    const int32_t *start_b, *token_start;
+    Pages pages;
+    int B, T, H, Hkv, group;
+    float scale, scale_log2e;
+    int part_rows;    // rows of a segment's place in the workspace
+    float* partials;  // [segment][part_rows][D] of sequences that are cut
+    float2* stats;    // [segment][part_rows] largest score, before its scale, and sum
+};
+
+// Rows of a tile of a sequence with so many.
+__device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : 32; }
+
+// What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of slots that its last token sees.
+struct ChunkSeq {
+    int L, t0, n, rows, tile_rows, tiles, units;
+    bool live;
+    template <int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
+    {
+        L = -1, t0 = n = 0;
+        if (b < a.B) {
+            L = a.start_b[b];
+            t0 = min(max(a.token_start[b], 0), a.T);
+            n = max(min(a.token_start[b + 1], a.T) - t0, 0);
+        }
+        const int slots = a.pages.slots();
+        live = L >= 0 && L < slots;
+        rows = n * a.group;
+        tile_rows = chunk_tile_rows(rows);
+        tiles = (rows + tile_rows - 1) / tile_rows;
+        units = !n ? 0 : live ? (min(L + n, slots) + UNIT - 1) / UNIT : 1;
+    }
+};
+// All sequences' cuts: a segment is at most `most` units.
+struct ChunkCut {
+    int most;
+    __device__ __forceinline__ int segments(const ChunkSeq& s) const { return s.units <= most ? 1 : (s.units + most - 1) / most; }
+    __device__ __forceinline__ int each(const ChunkSeq& s) const
+    {
+        const int n = segments(s);
+        return (s.units + n - 1) / n;
+    }
+};
+__device__ __forceinline__ long long wave_sum(long long x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) x += __shfl_xor(x, d, kWave);
+    return x;
+}
+// A sequence that is cut has units > most >= total / target, hence segments < 2 units / most: tiles * segments * Hkv of all of them is less than 2 target.
+template <int UNIT> __device__ __forceinline__ ChunkCut chunk_cut(const ChunkStep& a)
+{
+    long long all = 0;
+    ChunkSeq s;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        s.read<UNIT>(a, b0 + threadIdx.x % kWave);
+        all += wave_sum((long long)s.tiles * s.units);
+    }
+    const long long most = (all * a.Hkv + kChunkTarget - 1) / kChunkTarget;
+    return {(int)min(max(most, (long long)kChunkLeast), 1LL << 30)};
+}
+
+struct ChunkItem {
+    ChunkSeq s;
+    int hk, tile, segment, segments, each, split;  // split: place of the segment's results, of sequences that are cut
+    int b;                                         // < 0: none
+};
+// The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
+// which sees most, then segments.
+template <int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, int id)
+{
+    const ChunkCut cut = chunk_cut<UNIT>(a);
+    const int lane = threadIdx.x % kWave, hk = id % a.Hkv, j = id / a.Hkv;
+    int before = 0, split = 0;
+    ChunkItem it;
+    it.b = -1;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        ChunkSeq s;
+        s.read<UNIT>(a, b0 + lane);
+        const int segments = cut.segments(s), items = s.tiles * segments;
+        const int upto = wave_scan(items), split_upto = wave_scan(segments > 1 ? items : 0);
+        const unsigned long long beyond = __ballot(j < before + upto);
+        if (beyond) {
+            const int at = __ffsll(beyond) - 1;
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+            it.s = {of(s.L), of(s.t0), of(s.n), of(s.rows), of(s.tile_rows), of(s.tiles), of(s.units), of(s.live) != 0};
+            it.segments = of(segments);
+            it.each = scalar((it.s.units + it.segments - 1) / it.segments);
+            const int in = j - before - (of(upto) - of(items));
+            if (in < 0 || in >= of(items)) return it;
+            it.segment = scalar(in / it.s.tiles);
+            it.tile = it.s.tiles - 1 - (in - it.segment * it.s.tiles);
+            it.hk = hk;
+            it.split = (split + of(split_upto) - of(segments > 1 ? items : 0) + in) * a.Hkv + hk;
+            it.b = b0 + at;
+            return it;
+        }
+        before += last_lane(upto), split += last_lane(split_upto);
+    }
+    return it;
+}
+// Units that a tile's last row sees.
+template <int UNIT> __device__ __forceinline__ int chunk_units(const ChunkStep& a, const ChunkSeq& s, int tile)
+{
+    if (!s.live) return 1;
+    const int last = (min((tile + 1) * s.tile_rows, s.rows) - 1) / a.group;
+    return min(s.L + last, a.pages.slots() - 1) / UNIT + 1;
+}
+
+template <int DT, int D> __device__ __forceinline__ void chunk_write(const ChunkStep& a, size_t at, float x, float y)
+{
+    if constexpr (DT == EC_BF16) static_cast<uint32_t*>(a.out)[at / 2] = (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16;
+    else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(x, y);
+}
+// Number of the (token, query head) that a row is, in out and lse.
+__device__ __forceinline__ size_t chunk_row(const ChunkStep& a, const ChunkSeq& s, int hk, int row)
+{
+    const int token = row / a.group;
+    return (size_t)(s.t0 + token) * a.H + hk * a.group + (row - token * a.group);
+}
+
+template <int DT, int D> __device__ __forceinline__ void chunk_nothing(const ChunkStep& a, const ChunkItem& at)
+{
+    const int r0 = at.tile * at.s.tile_rows, rows = min(at.s.tile_rows, at.s.rows - r0);
+    for (int i = threadIdx.x; i < rows * (D / 2); i += blockDim.x) {
+        const size_t row = chunk_row(a, at.s, at.hk, r0 + i / (D / 2));
+        chunk_write<DT, D>(a, row * D + i % (D / 2) * 2, 0.f, 0.f);
+        if (a.lse && i % (D / 2) == 0) a.lse[row] = -INFINITY;
+    }
+}
+
+// Up to 16 RB rows: the workgroup's waves share the slots, a wave takes every WAVES-th tile of TR of them and keeps a running (maximum, sum,
+// weighted V) for the rows.
+//   S^T = K . Q^T      matrix instructions, so that a lane owns one row in 16 and 4 consecutive slots of a block of 16
+//   O^T += V^T . P^T   the probabilities are the second operand as they stand; V is transposed on its way out of LDS (bf16)
+// A bf16 probability enters as the sum of three bf16 numbers, all its 24 bits: few rows are bound by the bytes of K and V, and the matrix pipes have the room.
+template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(const ChunkStep& a, const ChunkItem& at, unsigned char* tiles, float* sh_m, float* sh_l)
+{
+    using T = PagedTile<DT, D>;
+    constexpr int WAVES = kPagedWaves, TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
+    constexpr int KB = ROW / 64;   // 64-byte blocks of a row: what the four quarters of a wave contract together
+    constexpr int OB = D / 16;     // 16-feature blocks of the output
+    constexpr int OROW = D + 4;    // floats of a row's sums in LDS, padded
+    constexpr int BLOCKS = TR / 16;
+    static_assert(16 * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int c16 = lane % 16, quarter = lane / 16;
+    const int slots = a.pages.slots(), r0 = at.tile * at.s.tile_rows;
+    const int seen = chunk_units<ROUND>(a, at.s, at.tile);
+    const int first = at.segment * at.each, last = min(first + at.each, seen);
+    if (first >= last) return;  // a tile that sees fewer segments than its sequence has
+    const bool whole = at.each >= seen;  // the tile's only segment
+
+    // ------------------------------------------------------------------ rows into LDS
+    const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles + wave * 4 * T::BYTES));
+    const int lowest = min(at.s.L + r0 / a.group, slots - 1);  // what the tile's first row sees last
+    const int highest = min(at.s.L + (min(r0 + 16 * RB, at.s.rows) - 1) / a.group, slots - 1);
+    const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(highest + 1, last * ROUND);
+    const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
+    uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in the rows of a load instruction, K: of even and odd runs
+#pragma unroll
+    for (int i = 0; i < T::IPG; ++i) {
+        const int r = i * RPI + lane / CH;
+        k_part[0][i] = lane / CH * ROW + (lane % CH ^ T::swz_k(r)) * 16;
+        k_part[1][i] = lane / CH * ROW + (lane % CH ^ T::swz_k(r + 8)) * 16;
+        v_part[i] = lane / CH * ROW + (lane % CH ^ T::swz_v(r)) * 16;
+    }
+    // Where the runs of a tile lie in the pools, and how many bytes of them are there: none behind the segment or on no page, and what is not
+    // there becomes zeros in LDS. A run in the page of the one before it needs no table entry.
+    struct Ids {
+        int id[T::GROUPS];
+    };
+    const int page_rows = 1 << shift;
+    auto pages_of = [&](int row) __attribute__((always_inline)) {
+        Ids ids;
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u)
+            if (u == 0 || u * 8 % page_rows == 0) ids.id[u] = table[min((row + u * 8) >> shift, a.pages.max_pages - 1)];
+        return ids;
+    };
+    struct Places {
+        size_t from[T::GROUPS];
+        int bytes[T::GROUPS], bad;  // bit u: run u has rows, but no page
+    };
+    const uint32_t head_bytes = (uint32_t)ROW << shift, page_bytes = head_bytes * (uint32_t)a.Hkv;
+    auto places_of = [&](int row, const Ids& ids) __attribute__((always_inline)) {
+        Places pl;
+        pl.bad = 0;
+        bool page = false;
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u) {
+            const int r = row + u * 8, left = end - r;
+            if (u == 0 || u * 8 % page_rows == 0) {
+                page = (unsigned)ids.id[u] < (unsigned)a.pages.n_pages;
+                pl.from[u] = (size_t)(uint32_t)(page ? ids.id[u] : 0) * page_bytes + (at.hk * head_bytes + (uint32_t)(r & mask) * ROW);
+            } else {
+                pl.from[u] = pl.from[u ? u - 1 : 0] + 8 * ROW;
+            }
+            pl.bytes[u] = page ? max(min(left, 8), 0) * ROW : 0;
+            pl.bad |= page || left <= 0 ? 0 : 1 << u;
+        }
+        return pl;
+    };
+    auto issue_k = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u)
+            load_run_lds<T::IPG, false>(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, k_part[u & 1]);
+    };
+    auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::GROUPS; ++u)
+            load_run_lds<T::IPG, false>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, v_part);
+    };
+
+    // ------------------------------------------------------------------ one tile after the other
+    f32x4 o[RB][OB];
+    float m[RB], l[RB];  // l: of this lane's slots
+    int limit[RB];       // last slot that the lane's row sees
+    u32x4 qf[RB][KB];    // the lane's row, chunks 4 kb + quarter of its query
+    const float of_diff = a.scale_log2e;  // differences of scores are scaled, so that no score leaves the range
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int r = r0 + rb * 16 + c16, token = r / a.group;
+        limit[rb] = r < at.s.rows ? min(at.s.L + token, slots - 1) : -1;
+        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s, at.hk, min(r, at.s.rows - 1)) * ROW);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) qf[rb][kb] = q[kb * 4 + quarter];
+        m[rb] = kLowest, l[rb] = 0.f;
+#pragma unroll
+        for (int i = 0; i < OB; ++i) o[rb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    uint32_t k_at[KB], v_at[OB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) k_at[kb] = mine + c16 * ROW + ((kb * 4 + quarter) ^ T::swz_k(c16)) * 16;
+#pragma unroll
+    for (int i = 0; i < OB; ++i) {
+        if constexpr (T::kHalf) {  // 4 features of row 4 quarter + (lane % 16) / 4: the transposing read's share
+            const int r = quarter * 4 + c16 / 4;
+            v_at[i] = mine + 2 * T::BYTES + r * ROW + ((i * 2 + c16 % 4 / 2) ^ T::swz_v(r)) * 16 + c16 % 2 * 8;
+        } else {  // row 4 quarter + i % 4, features 64 (i / 4) + 4 c16 .. + 3
+            v_at[i] = mine + 2 * T::BYTES + (quarter * 4 + i % 4) * ROW + (c16 + i / 4 * 16) * 16;
+        }
+    }
+    // off: which of the two places; left: tiles with this one; later: the tile after the next, whose loads are issued once this one is in registers
+    auto tile = [&](uint32_t off, int row, int bad, int left, const Places& later) __attribute__((always_inline)) {
+        if (left > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");  // all loads but the next tile's have landed
+        else wait_loads();
+        f32x4 kf[KB][BLOCKS];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t) kf[kb][t] = *(lds_f32x4*)(uintptr_t)(k_at[kb] + off + t * 16 * ROW);
+        bf16x4 vh[OB][BLOCKS];  // V, bf16
+        f32x4 vw[OB];           // V, fp32
+#pragma unroll
+        for (int i = 0; i < OB; ++i) {
+            if constexpr (T::kHalf) {
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) vh[i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(v_at[i] + off + t * 16 * ROW));
+            } else {
+                vw[i] = *(lds_f32x4*)(uintptr_t)(v_at[i] + off);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 s[RB][BLOCKS];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            if constexpr (T::kHalf) {
+                f32x4 part[BLOCKS][2];  // two chains
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t) part[t][0] = part[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int t = 0; t < BLOCKS; ++t)
+                        part[t][kb % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[kb][t]), __builtin_bit_cast(bf16x8, qf[rb][kb]),
+                                                                                 part[t][kb % 2], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[rb][t][r] = part[t][0][r] + part[t][1][r];
+            } else {
+                f32x4 part[4];  // four chains, so that every partial sum is short
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][0][e], __uint_as_float(qf[rb][kb][e]), part[e], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[rb][0][r] = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
+            }
+        }
+        wait_lds();
+        if (left > 2) {
+            issue_k(mine + off, later);
+            issue_v(mine + 2 * T::BYTES + off, later);
+        }
+
+        const bool masked = bad || row + TR - 1 > lowest;  // some row does not see some slot of the tile
+        float p[RB][BLOCKS][4];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = row + t * 16 + quarter * 4 + r;
+                        if (j > limit[rb] || (bad >> (t * 2 + quarter / 2) & 1)) s[rb][t][r] = -INFINITY;
+                    }
+            }
+            float top = s[rb][0][0];
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, s[rb][t][r]);
+            const float m_new = fmaxf(m[rb], head_max(top));
+            if (__any(m_new > m[rb])) {
+                const float c = exp2f((m[rb] - m_new) * of_diff);
+                l[rb] *= c;
+#pragma unroll
+                for (int i = 0; i < OB; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[rb][i][r] *= c;
+            }
+            m[rb] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    p[rb][t][r] = __builtin_amdgcn_exp2f((s[rb][t][r] - m[rb]) * of_diff);
+                    sum += p[rb][t][r];
+                }
+            l[rb] += sum;
+        }
+
+        if constexpr (T::kHalf) {
+            constexpr int PV = BLOCKS * 4;  // probabilities of a lane
+            typedef __attribute__((ext_vector_type(PV))) __bf16 bf16xp;
+            struct Parts {
+                bf16xp of[3];
+            };
+            auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+            // none of the three numbers of a probability that is not 0 is 0, so that an infinite V stays infinite
+            auto split = [&](float x, int e, Parts& to) __attribute__((always_inline)) {
+                const float high = cut(x), rest = x - high, middle = cut(rest);
+                to.of[0][e] = (__bf16)high;
+                to.of[1][e] = (__bf16)fmaxf(middle, x * 0x1p-24f);
+                to.of[2][e] = (__bf16)fmaxf(rest - middle, x * 0x1p-25f);
+            };
+            // x + V^T . P^T of 16 features, P one of its parts
+            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& part, f32x4 x) __attribute__((always_inline)) {
+                if constexpr (BLOCKS == 2)
+                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), part, x, 0, 0, 0);
+                else
+                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, part), x, 0, 0, 0);
+            };
+            if (masked) {
+                // An infinite V must not reach the rows that do not see it, as 0 times infinity would: it leaves the product, and every row adds the
+                // kinds that it sees.
+                bool some = false;
+#pragma unroll
+                for (int i = 0; i < OB; ++i)
+#pragma unroll
+                    for (int t = 0; t < BLOCKS; ++t) {
+                        const s16x4 is = (__builtin_bit_cast(s16x4, vh[i][t]) & (short)0x7f80) == (short)0x7f80;
+                        some |= (is[0] | is[1] | is[2] | is[3]) != 0;
+                    }
+                if (__builtin_expect(__any(some), 0)) {
+                    constexpr float kinds[3] = {INFINITY, -INFINITY, NAN};
+                    bf16xp ones[RB];
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                        for (int e = 0; e < PV; ++e) ones[rb][e] = p[rb][e / 4][e % 4] > 0.f ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+                    for (int i = 0; i < OB; ++i)
+#pragma unroll
+                        for (int kind = 0; kind < 3; ++kind) {
+                            bf16x4 of_kind[BLOCKS];
+#pragma unroll
+                            for (int t = 0; t < BLOCKS; ++t) {
+                                const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), inf = (short)0x7f80 - (s16x4){0, 0, 0, 0};
+                                const s16x4 is = kind == 0 ? v == inf : kind == 1 ? v == (inf | (short)0x8000) : (v & (short)0x7fff) > inf;
+                                of_kind[t] = __builtin_bit_cast(bf16x4, is & (short)0x3f80);  // 1
+                            }
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) {
+                                const f32x4 n = multiply(of_kind, ones[rb], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) o[rb][i][r] += n[r] > 0.f ? kinds[kind] : 0.f;
+                            }
+                        }
+#pragma unroll
+                    for (int i = 0; i < OB; ++i)
+#pragma unroll
+                        for (int t = 0; t < BLOCKS; ++t) {
+                            const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), is = (v & (short)0x7f80) == (short)0x7f80;
+                            vh[i][t] = __builtin_bit_cast(bf16x4, v & ~is);
+                        }
+                }
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                Parts parts;
+#pragma unroll
+                for (int e = 0; e < PV; ++e) split(p[rb][e / 4][e % 4], e, parts);
+#pragma unroll
+                for (int part = 0; part < 3; ++part)
+#pragma unroll
+                    for (int i = 0; i < OB; ++i) o[rb][i] = multiply(vh[i], parts.of[part], o[rb][i]);
+            }
+        } else {
+            if (masked) {
+                bool some = false;
+#pragma unroll
+                for (int i = 0; i < OB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) some |= !(fabsf(vw[i][e]) < INFINITY);
+                if (__builtin_expect(__any(some), 0)) {
+                    constexpr float kinds[3] = {INFINITY, -INFINITY, NAN};
+#pragma unroll
+                    for (int kind = 0; kind < 3; ++kind)
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) {
+                            f32x4 n[OB];
+#pragma unroll
+                            for (int i = 0; i < OB; ++i) n[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float v = vw[i][e];
+                                    const bool is = kind == 0 ? v == INFINITY : kind == 1 ? v == -INFINITY : v != v;
+                                    n[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.f : 0.f, p[rb][0][i % 4] > 0.f ? 1.f : 0.f, n[i / 4 * 4 + e], 0, 0, 0);
+                                }
+#pragma unroll
+                            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) o[rb][i][r] += n[i][r] > 0.f ? kinds[kind] : 0.f;
+                        }
+#pragma unroll
+                    for (int i = 0; i < OB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vw[i][e] = fabsf(vw[i][e]) < INFINITY ? vw[i][e] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[rb][i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw[i][e], p[rb][0][i % 4], o[rb][i / 4 * 4 + e], 0, 0, 0);
+                }
+        }
+    };
+    {
+        // the queries have to be there before the first load into LDS is issued: what the compiler waits for by counting must not be behind it
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qf[rb][kb]));
+        int row = (first * WAVES + wave) * TR, left = last - first;  // rounds
+        const Places here = places_of(row, pages_of(row));
+        issue_k(mine, here);
+        issue_v(mine + 2 * T::BYTES, here);
+        Places next = places_of(row + ROUND, pages_of(row + ROUND));
+        if (left > 1) {
+            issue_k(mine + T::BYTES, next);
+            issue_v(mine + 3 * T::BYTES, next);
+        }
+        uint32_t off = 0;
+        int bad = here.bad, next_bad = next.bad;
+        if (left > 2) next = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+        for (;; --left) {
+            Ids ids;
+            if (left > 3) ids = pages_of(row + 3 * ROUND);
+            tile(off, row, bad, left, next);
+            if (left == 1) break;
+            bad = next_bad, next_bad = next.bad;
+            row += ROUND, off ^= T::BYTES;
+            if (left > 3) next = places_of(row + 2 * ROUND, ids);
+        }
+    }
+
+    // ------------------------------------------------------------------ the waves' results together
+    wait_loads();  // nothing more arrives in the tiles, whose place the sums take
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const float all = head_sum(l[rb]);
+        if (rb) __syncthreads();  // the sums before have been read
+        if (quarter == 0) sh_m[wave * 16 + c16] = m[rb], sh_l[wave * 16 + c16] = all;
+#pragma unroll
+        for (int i = 0; i < OB; ++i) {
+            if constexpr (T::kHalf) {
+                *(lds_f32x4*)(uintptr_t)(mine + (c16 * OROW + i * 16 + quarter * 4) * 4) = o[rb][i];
+            } else {  // features 64 (i / 4) + 4 (4 quarter + r) + i % 4
+                typedef __attribute__((address_space(3))) float lds_float;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) *(lds_float*)(uintptr_t)(mine + (c16 * OROW + i / 4 * 64 + (quarter * 4 + r) * 4 + i % 4) * 4) = o[rb][i][r];
+            }
+        }
+        __syncthreads();
+        const int rows = min(16, at.s.rows - r0 - rb * 16);
+        for (int i = tid; i < rows * (D / 2); i += WAVES * kWave) {
+            const int r = i / (D / 2), d = i % (D / 2) * 2;
+            float top = sh_m[r], sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_m[w * 16 + r]);
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float c = exp2f((sh_m[w * 16 + r] - top) * of_diff);
+                const float2 v = *reinterpret_cast<const float2*>(tiles + w * 4 * T::BYTES + (r * OROW + d) * 4);
+                sum += sh_l[w * 16 + r] * c, x += v.x * c, y += v.y * c;
+            }
+            if (whole) {
+                const size_t row = chunk_row(a, at.s, at.hk, r0 + rb * 16 + r);
+                chunk_write<DT, D>(a, row * D + d, sum == 0.f ? 0.f : x / sum, sum == 0.f ? 0.f : y / sum);
+                if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+            } else {
+                const size_t place = (size_t)at.split * a.part_rows + rb * 16 + r;
+                *reinterpret_cast<float2*>(a.partials + place * D + d) = make_float2(x, y);
+                if (d == 0) a.stats[place] = make_float2(top, sum);
+            }
+        }
+    }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep a)
+{
+    using T = PagedTile<DT, D>;
+    constexpr int UNIT = kPagedWaves * T::TR;
+    __shared__ __align__(256) unsigned char tiles[kPagedWaves * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
+    __shared__ float sh_m[kPagedWaves * 16], sh_l[kPagedWaves * 16];
+    const ChunkItem at = chunk_item<UNIT>(a, blockIdx.x);
+    if (at.b < 0) return;
+    if (!at.s.live) {
+        if (at.segment == 0) chunk_nothing<DT, D>(a, at);
+        return;
+    }
+    if (at.s.tile_rows == 16) chunk_few_rows<DT, D, 1>(a, at, tiles, sh_m, sh_l);
+    else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
+}
+
+// The segments' results of every row of a sequence that is cut, a wave a row.
+template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) void paged_chunk_join_kernel(ChunkStep a)
+{
+    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR, E = D / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const ChunkCut cut = chunk_cut<UNIT>(a);
+    long long first = 0;  // rows of the sequences before
+    int split = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        ChunkSeq all;
+        all.read<UNIT>(a, b0 + lane);
+        unsigned long long cuts = __ballot(all.live && cut.segments(all) > 1);
+        for (; cuts; cuts &= cuts - 1) {  // sequences that are cut
+            const int at = __ffsll(cuts) - 1;
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+            const ChunkSeq s{of(all.L), of(all.t0), of(all.n), of(all.rows), of(all.tile_rows), of(all.tiles), of(all.units), true};
+            const int segments = cut.segments(s), each = cut.each(s);
+            const long long rows = (long long)s.rows * a.Hkv, step = (long long)gridDim.x * kChunkJoinRows;
+            const long long me = (long long)blockIdx.x * kChunkJoinRows + wave;
+            // rows are dealt out over all cut sequences
+            for (long long i = (me - first % step + step) % step; i < rows; i += step) {
+                const int r = (int)(i / a.Hkv), hk = (int)(i % a.Hkv), tile = r / s.tile_rows;
+                const int seen = chunk_units<UNIT>(a, s, tile), count = (seen + each - 1) / each;
+                if (count == 1) continue;  // written already
+                auto place = [&](int g) {
+                    return ((size_t)(split + g * s.tiles + (s.tiles - 1 - tile)) * a.Hkv + hk) * a.part_rows + (r - tile * s.tile_rows);
+                };
+                float top = kLowest;
+                for (int g = lane; g < count; g += kWave) {
+                    const float2 x = a.stats[place(g)];
+                    if (!(x.y == 0.f)) top = fmaxf(top, x.x);
+                }
+                top = wave_max(top);
+                float sum = 0.f, o[E] = {};
+                for (int g = 0; g < count; ++g) {
+                    const float2 x = a.stats[place(g)];
+                    if (x.y == 0.f) continue;
+                    const float c = exp2f((x.x - top) * a.scale_log2e);
+                    sum = fmaf(x.y, c, sum);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(a.partials[place(g) * D + lane * E + e], c, o[e]);
+                }
+                const size_t row = chunk_row(a, s, hk, r);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float x = sum == 0.f ? 0.f : o[e] / sum;
+                    if constexpr (DT == EC_BF16) static_cast<uint16_t*>(a.out)[row * D + lane * E + e] = f32_to_bf16(x);
+                    else static_cast<float*>(a.out)[row * D + lane * E + e] = x;
+                }
+                if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+            }
+            first += rows, split += s.tiles * segments;
+        }
+    }
+}
+
+// Workspace: the results of segments, of which sequences that are cut have less than 2 kChunkTarget (see chunk_cut).
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+static int part_rows(int T, int H) { return (long long)T * H <= 16 ? 16 : 32; }
+static size_t stat_bytes(int T, int H) { return up256((size_t)2 * kChunkTarget * part_rows(T, H) * sizeof(float2)); }
+size_t paged_chunk_ws(int T, int H, int D) { return stat_bytes(T, H) + (size_t)2 * kChunkTarget * part_rows(T, H) * D * sizeof(float); }
+
+template <int DT, int D> static int launch(const ChunkStep& a, hipStream_t stream)
+{
+    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR;
+    const long long tiles = ((long long)a.T * a.group + 31) / 32 + std::min(a.B, a.T), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    const bool cut = units > kChunkLeast;
+    const long long items = tiles * a.Hkv + (cut ? 2 * kChunkTarget : 0);
+    hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)items), dim3(kPagedWaves * kWave), 0, stream, a);
+    if (const int rc = status_from_hip(hipGetLastError())) return rc;
+    if (!cut) return EC_OK;
+    const long long rows = ((long long)a.T * a.H + kChunkJoinRows - 1) / kChunkJoinRows;
+    hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(rows, 1024)), dim3(kChunkJoinRows * kWave), 0, stream, a);
+    return status_from_hip(hipGetLastError());
+}
+
+int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages, const Pages& pages, const int32_t* start_b, const int32_t* token_start,
+                         int B, int T, int H, int Hkv, int D, float scale, int dt, void* out, float* lse, void* ws, hipStream_t stream)
+{
+    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, H / Hkv, scale, scale * kLog2e, part_rows(T, H),
+                      reinterpret_cast<float*>(static_cast<char*>(ws) + stat_bytes(T, H)), static_cast<float2*>(ws)};
+    if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);
+    return D == 128 ? launch<EC_F32, 128>(a, stream) : launch<EC_F32, 64>(a, stream);
+}
+
+}  // namespace ec
