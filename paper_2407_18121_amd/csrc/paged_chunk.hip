@@ -31,13 +31,13 @@ struct ChunkStep {
 };
 
 // Rows of a tile of a sequence with so many.
-__device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : 32; }
+template <int DT> __device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 || DT == EC_F32 ? 32 : 128; }
 
 // What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of slots that its last token sees.
 struct ChunkSeq {
     int L, t0, n, rows, tile_rows, tiles, units;
     bool live;
-    template <int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
+    template <int DT, int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
     {
         L = -1, t0 = n = 0;
         if (b < a.B) {
@@ -48,7 +48,7 @@ struct ChunkSeq {
         const int slots = a.pages.slots();
         live = L >= 0 && L < slots;
         rows = n * a.group;
-        tile_rows = chunk_tile_rows(rows);
+        tile_rows = chunk_tile_rows<DT>(rows);
         tiles = (rows + tile_rows - 1) / tile_rows;
         units = !n ? 0 : live ? (min(L + n, slots) + UNIT - 1) / UNIT : 1;
     }
@@ -70,57 +70,18 @@ __device__ __forceinline__ long long wave_sum(long long x)
     return x;
 }
 // A sequence that is cut has units > most >= total / target, hence segments < 2 units / most: tiles * segments * Hkv of all of them is less than 2 target.
-template <int UNIT> __device__ __forceinline__ ChunkCut chunk_cut(const ChunkStep& a)
+template <int DT, int UNIT> __device__ __forceinline__ ChunkCut chunk_cut(const ChunkStep& a)
 {
     long long all = 0;
     ChunkSeq s;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        s.read<UNIT>(a, b0 + threadIdx.x % kWave);
+        s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
         all += wave_sum((long long)s.tiles * s.units);
     }
     const long long most = (all * a.Hkv + kChunkTarget - 1) / kChunkTarget;
     return {(int)min(max(most, (long long)kChunkLeast), 1LL << 30)};
 }
 
-struct ChunkItem {
-    ChunkSeq s;
-    int hk, tile, segment, segments, each, split;  // split: place of the segment's results, of sequences that are cut
-    int b;                                         // < 0: none
-};
-// The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
-// which sees most, then segments.
-template <int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, int id)
-{
-    const ChunkCut cut = chunk_cut<UNIT>(a);
-    const int lane = threadIdx.x % kWave, hk = id % a.Hkv, j = id / a.Hkv;
-    int before = 0, split = 0;
-    ChunkItem it;
-    it.b = -1;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        ChunkSeq s;
-        s.read<UNIT>(a, b0 + lane);
-        const int segments = cut.segments(s), items = s.tiles * segments;
-        const int upto = wave_scan(items), split_upto = wave_scan(segments > 1 ? items : 0);
-        const unsigned long long beyond = __ballot(j < before + upto);
-        if (beyond) {
-            const int at = __ffsll(beyond) - 1;
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-            it.s = {of(s.L), of(s.t0), of(s.n), of(s.rows), of(s.tile_rows), of(s.tiles), of(s.units), of(s.live) != 0};
-            it.segments = of(segments);
-            it.each = scalar((it.s.units + it.segments - 1) / it.segments);
-            const int in = j - before - (of(upto) - of(items));
-            if (in < 0 || in >= of(items)) return it;
-            it.segment = scalar(in / it.s.tiles);
-            it.tile = it.s.tiles - 1 - (in - it.segment * it.s.tiles);
-            it.hk = hk;
-            it.split = (split + of(split_upto) - of(segments > 1 ? items : 0) + in) * a.Hkv + hk;
-            it.b = b0 + at;
-            return it;
-        }
-        before += last_lane(upto), split += last_lane(split_upto);
-    }
-    return it;
-}
 // Units that a tile's last row sees.
 template <int UNIT> __device__ __forceinline__ int chunk_units(const ChunkStep& a, const ChunkSeq& s, int tile)
 {
@@ -129,6 +90,50 @@ template <int UNIT> __device__ __forceinline__ int chunk_units(const ChunkStep& 
     return min(s.L + last, a.pages.slots() - 1) / UNIT + 1;
 }
 
+
+struct ChunkItem {
+    ChunkSeq s;
+    int hk, segment, each;  // units of a segment
+    int r0, r1, seen;       // rows of the tile, units that its last row sees
+    size_t place;           // of the segment's results in the workspace, of sequences that are cut
+    int b;                  // < 0: none
+};
+// The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
+// which sees most, then segments.
+template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, int id)
+{
+    const ChunkCut cut = chunk_cut<DT, UNIT>(a);
+    const int lane = threadIdx.x % kWave, hk = id % a.Hkv, j = id / a.Hkv;
+    int before = 0, split = 0;
+    ChunkItem it;
+    it.b = -1;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        ChunkSeq s;
+        s.read<DT, UNIT>(a, b0 + lane);
+        const int segments = cut.segments(s), items = s.tiles * segments;
+        const int upto = wave_scan(items), split_upto = wave_scan(segments > 1 ? items : 0);
+        const unsigned long long beyond = __ballot(j < before + upto);
+        if (beyond) {
+            const int at = __ffsll(beyond) - 1;
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+            it.s = {of(s.L), of(s.t0), of(s.n), of(s.rows), of(s.tile_rows), of(s.tiles), of(s.units), of(s.live) != 0};
+            const int n = of(segments);
+            it.each = scalar((it.s.units + n - 1) / n);
+            const int in = j - before - (of(upto) - of(items));
+            if (in < 0 || in >= of(items)) return it;
+            it.segment = scalar(in / it.s.tiles);
+            const int tile = it.s.tiles - 1 - (in - it.segment * it.s.tiles);
+            it.r0 = tile * it.s.tile_rows, it.r1 = min(it.r0 + it.s.tile_rows, it.s.rows);
+            it.seen = scalar(chunk_units<UNIT>(a, it.s, tile));
+            it.hk = hk;
+            it.place = ((size_t)(split + of(split_upto) - of(segments > 1 ? items : 0) + in) * a.Hkv + hk) * a.part_rows;
+            it.b = b0 + at;
+            return it;
+        }
+        before += last_lane(upto), split += last_lane(split_upto);
+    }
+    return it;
+}
 template <int DT, int D> __device__ __forceinline__ void chunk_write(const ChunkStep& a, size_t at, float x, float y)
 {
     if constexpr (DT == EC_BF16) static_cast<uint32_t*>(a.out)[at / 2] = (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16;
@@ -143,7 +148,7 @@ __device__ __forceinline__ size_t chunk_row(const ChunkStep& a, const ChunkSeq& 
 
 template <int DT, int D> __device__ __forceinline__ void chunk_nothing(const ChunkStep& a, const ChunkItem& at)
 {
-    const int r0 = at.tile * at.s.tile_rows, rows = min(at.s.tile_rows, at.s.rows - r0);
+    const int r0 = at.r0, rows = at.r1 - r0;
     for (int i = threadIdx.x; i < rows * (D / 2); i += blockDim.x) {
         const size_t row = chunk_row(a, at.s, at.hk, r0 + i / (D / 2));
         chunk_write<DT, D>(a, row * D + i % (D / 2) * 2, 0.f, 0.f);
@@ -167,16 +172,15 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
     static_assert(16 * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c16 = lane % 16, quarter = lane / 16;
-    const int slots = a.pages.slots(), r0 = at.tile * at.s.tile_rows;
-    const int seen = chunk_units<ROUND>(a, at.s, at.tile);
-    const int first = at.segment * at.each, last = min(first + at.each, seen);
+    const int slots = a.pages.slots(), r0 = at.r0;
+    const int first = at.segment * at.each, last = min(first + at.each, at.seen);
     if (first >= last) return;  // a tile that sees fewer segments than its sequence has
-    const bool whole = at.each >= seen;  // the tile's only segment
+    const bool whole = at.each >= at.seen;  // the tile's only segment
 
     // ------------------------------------------------------------------ rows into LDS
     const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles + wave * 4 * T::BYTES));
     const int lowest = min(at.s.L + r0 / a.group, slots - 1);  // what the tile's first row sees last
-    const int highest = min(at.s.L + (min(r0 + 16 * RB, at.s.rows) - 1) / a.group, slots - 1);
+    const int highest = min(at.s.L + (min(r0 + 16 * RB, at.r1) - 1) / a.group, slots - 1);
     const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(highest + 1, last * ROUND);
     const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
     uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in the rows of a load instruction, K: of even and odd runs
@@ -243,8 +247,8 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int r = r0 + rb * 16 + c16, token = r / a.group;
-        limit[rb] = r < at.s.rows ? min(at.s.L + token, slots - 1) : -1;
-        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s, at.hk, min(r, at.s.rows - 1)) * ROW);
+        limit[rb] = r < at.r1 ? min(at.s.L + token, slots - 1) : -1;
+        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s, at.hk, min(r, at.r1 - 1)) * ROW);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) qf[rb][kb] = q[kb * 4 + quarter];
         m[rb] = kLowest, l[rb] = 0.f;
@@ -527,7 +531,7 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
             }
         }
         __syncthreads();
-        const int rows = min(16, at.s.rows - r0 - rb * 16);
+        const int rows = min(16, at.r1 - r0 - rb * 16);
         for (int i = tid; i < rows * (D / 2); i += WAVES * kWave) {
             const int r = i / (D / 2), d = i % (D / 2) * 2;
             float top = sh_m[r], sum = 0.f, x = 0.f, y = 0.f;
@@ -544,13 +548,17 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
                 chunk_write<DT, D>(a, row * D + d, sum == 0.f ? 0.f : x / sum, sum == 0.f ? 0.f : y / sum);
                 if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
             } else {
-                const size_t place = (size_t)at.split * a.part_rows + rb * 16 + r;
+                const size_t place = at.place + rb * 16 + r;
                 *reinterpret_cast<float2*>(a.partials + place * D + d) = make_float2(x, y);
                 if (d == 0) a.stats[place] = make_float2(top, sum);
             }
         }
     }
 }
+
+}  // namespace ec
+#include "paged_chunk_many.h"
+namespace ec {
 
 template <int DT, int D>
 __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep a)
@@ -559,11 +567,24 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
     constexpr int UNIT = kPagedWaves * T::TR;
     __shared__ __align__(256) unsigned char tiles[kPagedWaves * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
     __shared__ float sh_m[kPagedWaves * 16], sh_l[kPagedWaves * 16];
-    const ChunkItem at = chunk_item<UNIT>(a, blockIdx.x);
+    const ChunkItem at = chunk_item<DT, UNIT>(a, blockIdx.x);
     if (at.b < 0) return;
     if (!at.s.live) {
         if (at.segment == 0) chunk_nothing<DT, D>(a, at);
         return;
+    }
+    if constexpr (DT == EC_BF16) {
+        static_assert(sizeof(tiles) >= 4 * kManySlots * D * 2 && UNIT % kManySlots == 0);
+        if (at.s.tile_rows == kManyRows) {
+            if (chunk_many_rows<D>(a, at, tiles, UNIT)) return;
+            ChunkItem part = at;
+            for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
+                part.r1 = min(part.r0 + 16, at.r1);
+                chunk_few_rows<DT, D, 1>(a, part, tiles, sh_m, sh_l);
+                __syncthreads();
+            }
+            return;
+        }
     }
     if (at.s.tile_rows == 16) chunk_few_rows<DT, D, 1>(a, at, tiles, sh_m, sh_l);
     else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
@@ -574,12 +595,12 @@ template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) voi
 {
     constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR, E = D / kWave;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const ChunkCut cut = chunk_cut<UNIT>(a);
+    const ChunkCut cut = chunk_cut<DT, UNIT>(a);
     long long first = 0;  // rows of the sequences before
     int split = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         ChunkSeq all;
-        all.read<UNIT>(a, b0 + lane);
+        all.read<DT, UNIT>(a, b0 + lane);
         unsigned long long cuts = __ballot(all.live && cut.segments(all) > 1);
         for (; cuts; cuts &= cuts - 1) {  // sequences that are cut
             const int at = __ffsll(cuts) - 1;
@@ -627,14 +648,15 @@ template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) voi
 
 // Workspace: the results of segments, of which sequences that are cut have less than 2 kChunkTarget (see chunk_cut).
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-static int part_rows(int T, int H) { return (long long)T * H <= 16 ? 16 : 32; }
+static int part_rows(int T, int H) { return (int)std::min<long long>(((long long)T * H + 15) / 16 * 16, 128); }
 static size_t stat_bytes(int T, int H) { return up256((size_t)2 * kChunkTarget * part_rows(T, H) * sizeof(float2)); }
 size_t paged_chunk_ws(int T, int H, int D) { return stat_bytes(T, H) + (size_t)2 * kChunkTarget * part_rows(T, H) * D * sizeof(float); }
 
 template <int DT, int D> static int launch(const ChunkStep& a, hipStream_t stream)
 {
     constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR;
-    const long long tiles = ((long long)a.T * a.group + 31) / 32 + std::min(a.B, a.T), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    constexpr int kRows = DT == EC_F32 ? 32 : 128;
+    const long long tiles = ((long long)a.T * a.group + kRows - 1) / kRows + std::min(a.B, a.T), units = (a.pages.slots() + UNIT - 1) / UNIT;
     const bool cut = units > kChunkLeast;
     const long long items = tiles * a.Hkv + (cut ? 2 * kChunkTarget : 0);
     hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)items), dim3(kPagedWaves * kWave), 0, stream, a);
