@@ -13,9 +13,10 @@
 
 namespace ec {
 
-constexpr int kChunkTarget = 512;  // segments that a launch is cut into, about: as many as the chip holds at once
-constexpr int kChunkLeast = 4;     // units of a segment, at least
-constexpr int kChunkJoinRows = 4;  // rows of a joining workgroup, a wave each
+constexpr int kChunkPlaces = 512;              // workgroups that the chip holds at once
+constexpr int kChunkParts = 4 * kChunkPlaces;  // segments whose results the workspace holds, at most
+constexpr int kChunkTiles = 128;               // tiles from which on segments may take several rounds
+constexpr int kChunkJoinRows = 4;              // rows of a joining workgroup, a wave each
 
 struct ChunkStep {
     const void *q, *k_pages, *v_pages;
@@ -24,18 +25,22 @@ struct ChunkStep {
     const int32_t *start_b, *token_start;
     Pages pages;
     int B, T, H, Hkv, group;
+    uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
+    int rounds;
     float scale, scale_log2e;
     int part_rows;    // rows of a segment's place in the workspace
     float* partials;  // [segment][part_rows][D] of sequences that are cut
     float2* stats;    // [segment][part_rows] largest score, before its scale, and sum
 };
 
+__device__ __forceinline__ int token_of(const ChunkStep& a, int row) { return (int)(__umulhi((uint32_t)row << 2, a.group_mul) >> a.group_shift); }
+
 // Rows of a tile of a sequence with so many.
 template <int DT> __device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 || DT == EC_F32 ? 32 : 128; }
 
-// What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of slots that its last token sees.
+// What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of UNIT slots that its last token sees.
 struct ChunkSeq {
-    int L, t0, n, rows, tile_rows, tiles, units;
+    int L, t0, n, rows, tile_rows, tiles, units, first_units;  // first_units: that the first tile sees
     bool live;
     template <int DT, int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
     {
@@ -49,44 +54,77 @@ struct ChunkSeq {
         live = L >= 0 && L < slots;
         rows = n * a.group;
         tile_rows = chunk_tile_rows<DT>(rows);
-        tiles = (rows + tile_rows - 1) / tile_rows;
+        tiles = (rows + tile_rows - 1) >> (tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : 7);
         units = !n ? 0 : live ? (min(L + n, slots) + UNIT - 1) / UNIT : 1;
+        first_units = !n ? 0 : live ? min(L + token_of(a, min(tile_rows, rows) - 1), slots - 1) / UNIT + 1 : 1;
     }
 };
-// All sequences' cuts: a segment is at most `most` units.
-struct ChunkCut {
-    int most;
-    __device__ __forceinline__ int segments(const ChunkSeq& s) const { return s.units <= most ? 1 : (s.units + most - 1) / most; }
-    __device__ __forceinline__ int each(const ChunkSeq& s) const
-    {
-        const int n = segments(s);
-        return (s.units + n - 1) / n;
-    }
-};
+// Sum over the wave, of numbers below 2^54.
 __device__ __forceinline__ long long wave_sum(long long x)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) x += __shfl_xor(x, d, kWave);
-    return x;
+    const int low = last_lane(wave_scan((int)(x & 0x3ffff))), middle = last_lane(wave_scan((int)(x >> 18 & 0x3ffff))), high = last_lane(wave_scan((int)(x >> 36)));
+    return ((long long)high << 36) + ((long long)middle << 18) + low;
 }
-// A sequence that is cut has units > most >= total / target, hence segments < 2 units / most: tiles * segments * Hkv of all of them is less than 2 target.
-template <int DT, int UNIT> __device__ __forceinline__ ChunkCut chunk_cut(const ChunkStep& a)
+// How a sequence's tiles are cut: from the last tile on `whole` of them not at all, the others into `segments` of `each` units (those that see less into fewer).
+struct ChunkCut {
+    int whole, segments, each;
+    __device__ __forceinline__ int items(const ChunkSeq& s) const { return whole + (s.tiles - whole) * segments; }
+    __device__ __forceinline__ int parts(const ChunkSeq& s) const { return (s.tiles - whole) * segments; }
+};
+// What all of them are cut by: the units that are a place's share of the whole batch, and the rounds that segments may take.
+struct ChunkShare {
+    int units, rounds;
+    // Units of a segment, at least: as many as its results, written and read again, take the time of.
+    static __device__ __forceinline__ int least(const ChunkSeq& s) { return s.tile_rows == 128 ? 16 : 4; }
+    // A tile of U units, against a share of A:
+    //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
+    //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
+    //   else        whole: the last tiles to start are short beside the rest
+    // These are r tiles U / A segments of a sequence, or 2 tiles U / A: within what the workspace holds, as chunk_share sees to it.
+    __device__ __forceinline__ ChunkCut of(const ChunkSeq& s) const
+    {
+        const int U = s.units, A = max(units, least(s));
+        auto cut = [&](int whole, int n) { return ChunkCut{whole, n, divided(U + n - 1, n)}; };
+        if (U > A) {
+            int n = divided(U, A), time = divided(U + n - 1, n);
+            if (rounds > 1 && U < 4 * A) {
+                for (int r = 2; r <= rounds; ++r) {
+                    const int m = divided(r * U, A), t = r * divided(U + m - 1, m) + (r - 1) * least(s);
+                    if (t < time) time = t, n = m;
+                }
+            }
+            if (n > 1) return cut(0, n);
+        } else if (rounds > 1 && U > 0 && A < 4 * U) {
+            const int k = divided(A, U), rest = A - k * U;
+            if (rest >= least(s) && rest * 8 >= A && (long long)s.tiles * rest >= A) {
+                const int n = divided(U, rest);
+                if (n > 1) return cut((int)((long long)s.tiles * k * U / A), n);
+            }
+        }
+        return {s.tiles, 1, U};
+    }
+};
+template <int DT, int UNIT> __device__ __forceinline__ ChunkShare chunk_share(const ChunkStep& a)
 {
-    long long all = 0;
+    long long all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
     ChunkSeq s;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
-        all += wave_sum((long long)s.tiles * s.units);
+        if (a.rounds > 1) all += wave_sum((long long)s.tiles * (s.units + s.first_units));
+        most += wave_sum((long long)s.tiles * s.units);
     }
-    const long long most = (all * a.Hkv + kChunkTarget - 1) / kChunkTarget;
-    return {(int)min(max(most, (long long)kChunkLeast), 1LL << 30)};
+    all *= a.Hkv, most *= a.Hkv;
+    // one round: most / share <= kChunkPlaces parts; several: rounds * most / share and 2 most / share <= kChunkParts, as most <= all
+    const long long share = a.rounds > 1 ? (all + 2 * kChunkPlaces - 1) / (2 * kChunkPlaces) : (most + kChunkPlaces - 1) / kChunkPlaces;
+    const int units = (int)min(max(share, 1LL), 1LL << 22);
+    return {units, a.rounds > 1 ? (int)min(4LL, kChunkParts * (long long)units / max(most, 1LL)) : 1};
 }
 
 // Units that a tile's last row sees.
 template <int UNIT> __device__ __forceinline__ int chunk_units(const ChunkStep& a, const ChunkSeq& s, int tile)
 {
     if (!s.live) return 1;
-    const int last = (min((tile + 1) * s.tile_rows, s.rows) - 1) / a.group;
+    const int last = token_of(a, min((tile + 1) * s.tile_rows, s.rows) - 1);
     return min(s.L + last, a.pages.slots() - 1) / UNIT + 1;
 }
 
@@ -102,35 +140,40 @@ struct ChunkItem {
 // which sees most, then segments.
 template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, int id)
 {
-    const ChunkCut cut = chunk_cut<DT, UNIT>(a);
+    const ChunkShare share = chunk_share<DT, UNIT>(a);
     const int lane = threadIdx.x % kWave, hk = id % a.Hkv, j = id / a.Hkv;
-    int before = 0, split = 0;
+    int before = 0, parts_before = 0;
     ChunkItem it;
     it.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         ChunkSeq s;
         s.read<DT, UNIT>(a, b0 + lane);
-        const int segments = cut.segments(s), items = s.tiles * segments;
-        const int upto = wave_scan(items), split_upto = wave_scan(segments > 1 ? items : 0);
+        const ChunkCut cut = share.of(s);
+        const int items = cut.items(s), parts = cut.parts(s);
+        const int upto = wave_scan(items), parts_upto = wave_scan(parts);
         const unsigned long long beyond = __ballot(j < before + upto);
         if (beyond) {
             const int at = __ffsll(beyond) - 1;
             auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-            it.s = {of(s.L), of(s.t0), of(s.n), of(s.rows), of(s.tile_rows), of(s.tiles), of(s.units), of(s.live) != 0};
-            const int n = of(segments);
-            it.each = scalar((it.s.units + n - 1) / n);
-            const int in = j - before - (of(upto) - of(items));
+            it.s = {of(s.L), of(s.t0), of(s.n), of(s.rows), of(s.tile_rows), of(s.tiles), of(s.units), of(s.first_units), of(s.live) != 0};
+            const int in = j - before - (of(upto) - of(items)), whole = of(cut.whole), part = in - whole;
             if (in < 0 || in >= of(items)) return it;
-            it.segment = scalar(in / it.s.tiles);
-            const int tile = it.s.tiles - 1 - (in - it.segment * it.s.tiles);
+            int tile = in;  // from the last one on
+            it.segment = 0, it.each = it.s.units;
+            if (part >= 0) {
+                const int tiles = it.s.tiles - whole;
+                it.segment = scalar(divided(part, tiles)), it.each = of(cut.each);
+                tile = whole + part - it.segment * tiles;
+            }
+            tile = it.s.tiles - 1 - tile;
             it.r0 = tile * it.s.tile_rows, it.r1 = min(it.r0 + it.s.tile_rows, it.s.rows);
             it.seen = scalar(chunk_units<UNIT>(a, it.s, tile));
             it.hk = hk;
-            it.place = ((size_t)(split + of(split_upto) - of(segments > 1 ? items : 0) + in) * a.Hkv + hk) * a.part_rows;
+            it.place = ((size_t)(parts_before + of(parts_upto) - of(parts) + max(part, 0)) * a.Hkv + hk) * a.part_rows;
             it.b = b0 + at;
             return it;
         }
-        before += last_lane(upto), split += last_lane(split_upto);
+        before += last_lane(upto), parts_before += last_lane(parts_upto);
     }
     return it;
 }
@@ -142,7 +185,7 @@ template <int DT, int D> __device__ __forceinline__ void chunk_write(const Chunk
 // Number of the (token, query head) that a row is, in out and lse.
 __device__ __forceinline__ size_t chunk_row(const ChunkStep& a, const ChunkSeq& s, int hk, int row)
 {
-    const int token = row / a.group;
+    const int token = token_of(a, row);
     return (size_t)(s.t0 + token) * a.H + hk * a.group + (row - token * a.group);
 }
 
@@ -179,8 +222,8 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
 
     // ------------------------------------------------------------------ rows into LDS
     const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_address(tiles + wave * 4 * T::BYTES));
-    const int lowest = min(at.s.L + r0 / a.group, slots - 1);  // what the tile's first row sees last
-    const int highest = min(at.s.L + (min(r0 + 16 * RB, at.r1) - 1) / a.group, slots - 1);
+    const int lowest = min(at.s.L + token_of(a, r0), slots - 1);  // what the tile's first row sees last
+    const int highest = min(at.s.L + token_of(a, min(r0 + 16 * RB, at.r1) - 1), slots - 1);
     const int shift = a.pages.shift, mask = (1 << shift) - 1, end = min(highest + 1, last * ROUND);
     const const_i32* table = (const const_i32*)(uintptr_t)(a.pages.table + (size_t)at.b * a.pages.max_pages);
     uint32_t k_part[2][T::IPG], v_part[T::IPG];  // a lane's place in the rows of a load instruction, K: of even and odd runs
@@ -246,8 +289,8 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
     const float of_diff = a.scale_log2e;  // differences of scores are scaled, so that no score leaves the range
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int r = r0 + rb * 16 + c16, token = r / a.group;
-        limit[rb] = r < at.r1 ? min(at.s.L + token, slots - 1) : -1;
+        const int r = r0 + rb * 16 + c16;
+        limit[rb] = r < at.r1 ? min(at.s.L + token_of(a, r), slots - 1) : -1;
         const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s, at.hk, min(r, at.r1 - 1)) * ROW);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) qf[rb][kb] = q[kb * 4 + quarter];
@@ -590,47 +633,62 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
     else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
 }
 
-// The segments' results of every row of a sequence that is cut, a wave a row.
+// The segments' results of every row of tiles that are cut, a wave a row. Bound by latency: the statistics, a lane a segment, then the sums, eight segments' in
+// flight.
 template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) void paged_chunk_join_kernel(ChunkStep a)
 {
-    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR, E = D / kWave;
+    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR, E = D / kWave, AHEAD = 8;
+    typedef __attribute__((ext_vector_type(E))) float of_row;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const ChunkCut cut = chunk_cut<DT, UNIT>(a);
-    long long first = 0;  // rows of the sequences before
-    int split = 0;
+    const ChunkShare share = chunk_share<DT, UNIT>(a);
+    const int step = gridDim.x * kChunkJoinRows;
+    int me = blockIdx.x * kChunkJoinRows + wave;  // rows are dealt out over all sequences that are cut; me: of the present one
+    int parts = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         ChunkSeq all;
         all.read<DT, UNIT>(a, b0 + lane);
-        unsigned long long cuts = __ballot(all.live && cut.segments(all) > 1);
-        for (; cuts; cuts &= cuts - 1) {  // sequences that are cut
-            const int at = __ffsll(cuts) - 1;
+        const ChunkCut cuts = share.of(all);
+        for (unsigned long long todo = __ballot(cuts.segments > 1); todo; todo &= todo - 1) {
+            const int at = __ffsll(todo) - 1;
             auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-            const ChunkSeq s{of(all.L), of(all.t0), of(all.n), of(all.rows), of(all.tile_rows), of(all.tiles), of(all.units), true};
-            const int segments = cut.segments(s), each = cut.each(s);
-            const long long rows = (long long)s.rows * a.Hkv, step = (long long)gridDim.x * kChunkJoinRows;
-            const long long me = (long long)blockIdx.x * kChunkJoinRows + wave;
-            // rows are dealt out over all cut sequences
-            for (long long i = (me - first % step + step) % step; i < rows; i += step) {
-                const int r = (int)(i / a.Hkv), hk = (int)(i % a.Hkv), tile = r / s.tile_rows;
-                const int seen = chunk_units<UNIT>(a, s, tile), count = (seen + each - 1) / each;
+            const ChunkSeq s{of(all.L), of(all.t0), of(all.n), of(all.rows), of(all.tile_rows), of(all.tiles), of(all.units), of(all.first_units), true};
+            const ChunkCut cut{of(cuts.whole), of(cuts.segments), of(cuts.each)};
+            const int tiles = s.tiles - cut.whole;  // the first ones
+            const int heads = min(tiles * s.tile_rows, s.rows);  // rows of a key/value head
+            for (; me < heads * a.Hkv; me += step) {
+                const int hk = me / heads, r = me - hk * heads, tile = r / s.tile_rows;
+                const int seen = chunk_units<UNIT>(a, s, tile), count = (seen + cut.each - 1) / cut.each;
                 if (count == 1) continue;  // written already
-                auto place = [&](int g) {
-                    return ((size_t)(split + g * s.tiles + (s.tiles - 1 - tile)) * a.Hkv + hk) * a.part_rows + (r - tile * s.tile_rows);
-                };
+                const int between = tiles * a.Hkv * a.part_rows;  // rows from a segment to the next
+                const size_t first = ((size_t)(parts + tiles - 1 - tile) * a.Hkv + hk) * a.part_rows + (r - tile * s.tile_rows);
                 float top = kLowest;
                 for (int g = lane; g < count; g += kWave) {
-                    const float2 x = a.stats[place(g)];
-                    if (!(x.y == 0.f)) top = fmaxf(top, x.x);
+                    const float2 x = a.stats[first + (size_t)g * between];
+                    if (!(x.y == 0.f)) top = fmaxf(top, x.x);  // (NaN counts)
                 }
                 top = wave_max(top);
-                float sum = 0.f, o[E] = {};
-                for (int g = 0; g < count; ++g) {
-                    const float2 x = a.stats[place(g)];
-                    if (x.y == 0.f) continue;
-                    const float c = exp2f((x.x - top) * a.scale_log2e);
-                    sum = fmaf(x.y, c, sum);
+                float sum = 0.f;
+                of_row o = {};
+                for (int g0 = 0; g0 < count; g0 += kWave) {
+                    float2 x = make_float2(0.f, 0.f);
+                    if (g0 + lane < count) x = a.stats[first + (size_t)(g0 + lane) * between];
+                    const float weight = x.y == 0.f ? 0.f : exp2f((x.x - top) * a.scale_log2e);
+                    const float share_of = x.y == 0.f ? 0.f : x.y * weight;
+                    for (int g = g0; g < min(g0 + kWave, count); g += AHEAD) {
+                        of_row v[AHEAD];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = fmaf(a.partials[place(g) * D + lane * E + e], c, o[e]);
+                        for (int u = 0; u < AHEAD; ++u)
+                            v[u] = *reinterpret_cast<const of_row*>(a.partials + (first + (size_t)min(g + u, count - 1) * between) * D + lane * E);
+#pragma unroll
+                        for (int u = 0; u < AHEAD; ++u) {
+                            if (g + u >= count) continue;
+                            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), g + u - g0));
+                            sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share_of), g + u - g0));
+                            // a segment of which the row sees nothing has sums of 0
+#pragma unroll
+                            for (int e = 0; e < E; ++e) o[e] = fmaf(v[u][e], w, o[e]);
+                        }
+                    }
                 }
                 const size_t row = chunk_row(a, s, hk, r);
 #pragma unroll
@@ -641,36 +699,44 @@ template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) voi
                 }
                 if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
             }
-            first += rows, split += s.tiles * segments;
+            me -= heads * a.Hkv, parts += cut.parts(s);
         }
     }
 }
 
-// Workspace: the results of segments, of which sequences that are cut have less than 2 kChunkTarget (see chunk_cut).
+// Workspace: the results of the segments of tiles that are cut (see ChunkShare).
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 static int part_rows(int T, int H) { return (int)std::min<long long>(((long long)T * H + 15) / 16 * 16, 128); }
-static size_t stat_bytes(int T, int H) { return up256((size_t)2 * kChunkTarget * part_rows(T, H) * sizeof(float2)); }
-size_t paged_chunk_ws(int T, int H, int D) { return stat_bytes(T, H) + (size_t)2 * kChunkTarget * part_rows(T, H) * D * sizeof(float); }
+// Tiles of all key/value heads that a call can have, and segments whose results its workspace holds: of any number of sequences and of key/value heads.
+static long long most_tiles(long long T, long long group, long long Hkv, long long B, int rows) { return ((T * group + rows - 1) / rows + std::min(B, T)) * Hkv; }
+static int most_parts(int T, int H) { return (long long)T * H + most_tiles(T, H, 1, 0, 32) + H >= kChunkTiles ? kChunkParts : kChunkPlaces; }
+static size_t stat_bytes(int T, int H) { return up256((size_t)most_parts(T, H) * part_rows(T, H) * sizeof(float2)); }
+size_t paged_chunk_ws(int T, int H, int D) { return stat_bytes(T, H) + (size_t)most_parts(T, H) * part_rows(T, H) * D * sizeof(float); }
 
-template <int DT, int D> static int launch(const ChunkStep& a, hipStream_t stream)
+template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
 {
     constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR;
-    constexpr int kRows = DT == EC_F32 ? 32 : 128;
-    const long long tiles = ((long long)a.T * a.group + kRows - 1) / kRows + std::min(a.B, a.T), units = (a.pages.slots() + UNIT - 1) / UNIT;
-    const bool cut = units > kChunkLeast;
-    const long long items = tiles * a.Hkv + (cut ? 2 * kChunkTarget : 0);
+    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    a.rounds = tiles >= kChunkTiles ? 4 : 1;
+    const bool cut = units > 4;  // (fewer make no two segments)
+    // as many workgroups as there can be items; those without one leave at once
+    const long long items = tiles + (cut ? a.rounds > 1 ? kChunkParts : kChunkPlaces : 0);
     hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)items), dim3(kPagedWaves * kWave), 0, stream, a);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     if (!cut) return EC_OK;
     const long long rows = ((long long)a.T * a.H + kChunkJoinRows - 1) / kChunkJoinRows;
-    hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(rows, 1024)), dim3(kChunkJoinRows * kWave), 0, stream, a);
+    hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(rows, 2048)), dim3(kChunkJoinRows * kWave), 0, stream, a);
     return status_from_hip(hipGetLastError());
 }
 
 int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages, const Pages& pages, const int32_t* start_b, const int32_t* token_start,
                          int B, int T, int H, int Hkv, int D, float scale, int dt, void* out, float* lse, void* ws, hipStream_t stream)
 {
-    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, H / Hkv, scale, scale * kLog2e, part_rows(T, H),
+    const uint32_t group = H / Hkv;
+    uint32_t shift = 0;
+    while (1u << shift < group) ++shift;
+    const uint32_t mul = (uint32_t)(((1ULL << (30 + shift)) + group - 1) / group);
+    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul, shift, 1, scale, scale * kLog2e, part_rows(T, H),
                       reinterpret_cast<float*>(static_cast<char*>(ws) + stat_bytes(T, H)), static_cast<float2*>(ws)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);
     return D == 128 ? launch<EC_F32, 128>(a, stream) : launch<EC_F32, 64>(a, stream);

@@ -45,7 +45,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     const int group = a.group, L = at.s.L;
 
     // tiles of the workgroup, and up to what this wave's rows see
-    auto sees = [&](int row) { return min(L + min(row, at.s.rows - 1) / group, slots - 1); };  // last slot
+    auto sees = [&](int row) { return min(L + token_of(a, min(row, at.s.rows - 1)), slots - 1); };  // last slot
     const int highest = scalar(sees(at.r0 + kManyRows - 1));
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
     if (first >= last) return true;  // a tile that sees fewer segments than its sequence has
@@ -99,11 +99,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     {
         int ids = ids_of(t0);
         asm volatile("" : "+v"(ids));
-        const int token0 = scalar(min(rw, at.s.rows - 1) / group);
+        const int token0 = scalar(token_of(a, min(rw, at.s.rows - 1)));
         const u32x4 q_rsrc = tile_rsrc(static_cast<const char*>(a.q) + (size_t)(at.s.t0 + token0) * a.H * ROW, 0xfffffff0u);
 #pragma unroll
         for (int j = 0; j < 32 / RPI; ++j) {
-            const int i = j * RPI + lane / CH, row = min(rw + i, at.s.rows - 1), token = row / group;
+            const int i = j * RPI + lane / CH, row = min(rw + i, at.s.rows - 1), token = token_of(a, row);
             const uint32_t from = ((uint32_t)(token - token0) * a.H + at.hk * group + (row - token * group)) * ROW + (lane % CH ^ ManySwizzleK<D>::at(i)) * 16;
             load_lds_16(q_rsrc, q_at + (j * RPI < 16 ? 0 : TILE - 16 * ROW) + j * RPI * ROW, from);
         }
@@ -152,6 +152,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         const int n0 = t * kManySlots;
         const bool some = bad || n0 + kManySlots - 1 > lowest;
         if (some) {
+            asm volatile("");  // a branch, not 64 instructions in every tile
             const int upto = limit - n0 - h * 8;
 #pragma unroll
             for (int nb = 0; nb < 2; ++nb)
@@ -285,10 +286,8 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     wait_lds();  // their place is free
 #pragma unroll
     for (int j = 0; j < NI; ++j) move_v(V0, pl1, j);
-    if (n_iter > 1) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) move_k(K1, pl2, j);
-    }
+    for (int j = 0; j < NI; ++j) move_k(K1, pl2, j);
     pl1 = pl2;
     pl2 = places_of(t0 + 2, ids3);
     meet();
@@ -319,16 +318,12 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
             pl1 = pl2, pl2 = places_of(t0 + i + 2, ids);
         }
         ids = ids_of(t0 + i + 3);
-        const bool more = i + 2 < n_iter;
         phase_a(std::true_type{}, s, sn, k_next, [&](int f) __attribute__((always_inline)) {
             constexpr int EVERY = NA / (2 * NI);
             static_assert(EVERY >= 1, "a phase has room for its loads");
             if (f < NA && f % EVERY == 0) {
-                if (f / EVERY < NI) {
-                    if (more) move_k(k_old, pl2, f / EVERY);
-                } else {
-                    move_v(v_next, pl1, f / EVERY - NI);
-                }
+                if (f / EVERY < NI) move_k(k_old, pl2, f / EVERY);  // (behind the last tile nothing is fetched)
+                else move_v(v_next, pl1, f / EVERY - NI);
             }
         });
         const bool was = hidden;
