@@ -75,7 +75,7 @@ struct ChunkCut {
 struct ChunkShare {
     int units, rounds;
     // Units of a segment, at least: as many as its results, written and read again, take the time of.
-    static __device__ __forceinline__ int least(const ChunkSeq& s) { return s.tile_rows == 128 ? 16 : 4; }
+    static __device__ __forceinline__ int least(const ChunkSeq& s) { return max(min(s.rows, s.tile_rows) / 8, 4); }
     // A tile of U units, against a share of A:
     //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
     //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
@@ -138,10 +138,9 @@ struct ChunkItem {
 };
 // The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
 // which sees most, then segments.
-template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, int id)
+template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare& share, int id)
 {
-    const ChunkShare share = chunk_share<DT, UNIT>(a);
-    const int lane = threadIdx.x % kWave, hk = id % a.Hkv, j = id / a.Hkv;
+    const int lane = anew(threadIdx.x) & (kWave - 1), hk = id % a.Hkv, j = id / a.Hkv;
     int before = 0, parts_before = 0;
     ChunkItem it;
     it.b = -1;
@@ -213,7 +212,7 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
     constexpr int OROW = D + 4;    // floats of a row's sums in LDS, padded
     constexpr int BLOCKS = TR / 16;
     static_assert(16 * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int tid = anew(threadIdx.x) & (WAVES * kWave - 1), lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c16 = lane % 16, quarter = lane / 16;
     const int slots = a.pages.slots(), r0 = at.r0;
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
@@ -273,12 +272,12 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
     auto issue_k = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::GROUPS; ++u)
-            load_run_lds<T::IPG, false>(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, k_part[u & 1]);
+            load_run_lds<T::IPG, T::kHalf>(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, k_part[u & 1]);
     };
     auto issue_v = [&](uint32_t lds, const Places& pl) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::GROUPS; ++u)
-            load_run_lds<T::IPG, false>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, v_part);
+            load_run_lds<T::IPG, T::kHalf>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, v_part);
     };
 
     // ------------------------------------------------------------------ one tile after the other
@@ -610,27 +609,35 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
     constexpr int UNIT = kPagedWaves * T::TR;
     __shared__ __align__(256) unsigned char tiles[kPagedWaves * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
     __shared__ float sh_m[kPagedWaves * 16], sh_l[kPagedWaves * 16];
-    const ChunkItem at = chunk_item<DT, UNIT>(a, blockIdx.x);
-    if (at.b < 0) return;
-    if (!at.s.live) {
-        if (at.segment == 0) chunk_nothing<DT, D>(a, at);
-        return;
-    }
-    if constexpr (DT == EC_BF16) {
-        static_assert(sizeof(tiles) >= 4 * kManySlots * D * 2 && UNIT % kManySlots == 0);
-        if (at.s.tile_rows == kManyRows) {
-            if (chunk_many_rows<D>(a, at, tiles, UNIT)) return;
-            ChunkItem part = at;
-            for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
-                part.r1 = min(part.r0 + 16, at.r1);
-                chunk_few_rows<DT, D, 1>(a, part, tiles, sh_m, sh_l);
-                __syncthreads();
-            }
+    __shared__ int flags[kPagedWaves];
+    const ChunkShare share = chunk_share<DT, UNIT>(a);
+    auto take = [&](const ChunkItem& at) __attribute__((always_inline)) {
+        if (!at.s.live) {
+            chunk_nothing<DT, D>(a, at);
             return;
         }
+        if constexpr (DT == EC_BF16) {
+            static_assert(sizeof(tiles) >= 4 * kManySlots * D * 2 && UNIT % kManySlots == 0);
+            if (at.s.tile_rows == kManyRows) {
+                if (chunk_many_rows<D>(a, at, tiles, flags, UNIT)) return;
+                ChunkItem part = at;
+                for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
+                    part.r1 = min(part.r0 + 16, at.r1);
+                    chunk_few_rows<DT, D, 1>(a, part, tiles, sh_m, sh_l);
+                    __syncthreads();
+                }
+                return;
+            }
+        }
+        if (at.s.tile_rows == 16) chunk_few_rows<DT, D, 1>(a, at, tiles, sh_m, sh_l);
+        else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
+    };
+    for (int id = blockIdx.x;; id += gridDim.x) {
+        const ChunkItem at = chunk_item<DT, UNIT>(a, share, id);
+        if (at.b < 0) return;
+        take(at);
+        __syncthreads();  // the tiles have been read
     }
-    if (at.s.tile_rows == 16) chunk_few_rows<DT, D, 1>(a, at, tiles, sh_m, sh_l);
-    else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
 }
 
 // The segments' results of every row of tiles that are cut, a wave a row. Bound by latency: the statistics, a lane a segment, then the sums, eight segments' in
@@ -719,9 +726,9 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128), units = (a.pages.slots() + UNIT - 1) / UNIT;
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
     const bool cut = units > 4;  // (fewer make no two segments)
-    // as many workgroups as there can be items; those without one leave at once
-    const long long items = tiles + (cut ? a.rounds > 1 ? kChunkParts : kChunkPlaces : 0);
-    hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)items), dim3(kPagedWaves * kWave), 0, stream, a);
+    // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
+    const long long groups = cut ? std::max<long long>(tiles, kChunkPlaces) : tiles;
+    hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)groups), dim3(kPagedWaves * kWave), 0, stream, a);
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     if (!cut) return EC_OK;
     const long long rows = ((long long)a.T * a.H + kChunkJoinRows - 1) / kChunkJoinRows;

@@ -28,7 +28,7 @@ template <int D> struct ManySwizzleV {  // four rows at the same 64 bytes (a tra
 };
 
 // False, and nothing written: rows of V that are not finite are seen by some of the rows only.
-template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, unsigned char* tiles, int unit)
+template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, unsigned char* tiles, int* flags, int unit)
 {
     constexpr int ROW = D * 2, CH = ROW / 16, RPI = kWave / CH;  // bytes and chunks of a row, rows of a load instruction
     constexpr int KB = D / 16;    // contraction blocks of Q.K
@@ -37,9 +37,9 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     constexpr int NP = 4 * DB;    // of phase B: (16-slot block, db)
     constexpr int EV = 32 / NA;   // elements turned into probabilities per matrix instruction of phase A
     constexpr int TILE = kManySlots * ROW;
-    constexpr int RUNS = 2, IPR = 8 / RPI, NI = RUNS * IPR;  // a wave moves 16 rows of a tile: two runs of 8, each in one page
+    constexpr int RUNS = 2, IPR = 8 / RPI;  // a wave moves 16 rows of a tile: two runs of 8, each in one page
     constexpr int K0 = 0, K1 = TILE, V0 = 2 * TILE, V1 = 3 * TILE;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int tid = anew(threadIdx.x) & (kPagedWaves * kWave - 1), lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int c32 = lane % 32, h = lane / 32;
     const int slots = a.pages.slots(), rw = at.r0 + wave * 32;  // first row of the workgroup, of this wave
     const int group = a.group, L = at.s.L;
@@ -52,7 +52,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     const bool whole = at.each >= at.seen;
     const int t0 = first * (unit / kManySlots), t1 = min(last * (unit / kManySlots), highest / kManySlots + 1), n_iter = t1 - t0;
     const int end = min(highest + 1, t1 * kManySlots);  // rows behind it arrive as zeros
-    const int lowest = scalar(sees(rw)), limit = sees(rw + c32);
+    const int lowest = scalar(sees(rw));
     const int count = rw < at.s.rows ? max(min(scalar(sees(rw + 31)) / kManySlots + 1, t1) - t0, 0) : 0;
 
     // ------------------------------------------------------------------ rows into LDS
@@ -60,13 +60,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     const int shift = a.pages.shift, mask = (1 << shift) - 1;
     const uint32_t head_bytes = (uint32_t)ROW << shift, page_bytes = head_bytes * (uint32_t)a.Hkv;
     const int32_t* table = a.pages.table + (size_t)at.b * a.pages.max_pages;
-    uint32_t k_part[NI], v_part[IPR];  // a lane's place in its run
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-        const int r = j * RPI + lane / CH;
-        k_part[j] = r % 8 * ROW + (lane % CH ^ ManySwizzleK<D>::at(r)) * 16;
-        if (j < IPR) v_part[j] = r % 8 * ROW + (lane % CH ^ ManySwizzleV<D>::at(r)) * 16;
-    }
+    // A lane's place in the first run that its wave moves; a load instruction further is RPI rows further. K's swizzle turns over with the row number, whose
+    // bits that change from instruction to instruction are others than those that change from lane to lane.
+    const uint32_t k_part = lane / CH * ROW + (lane % CH ^ ManySwizzleK<D>::at(lane / CH)) * 16;
+    const uint32_t v_part = lane / CH * ROW + (lane % CH ^ ManySwizzleV<D>::at(lane / CH)) * 16;
+    constexpr int KTURN = (D == 128 ? RPI : RPI / 2) * 16;  // bytes that a chunk's place turns over by
     // entries of a tile's eight runs, one in each of the first eight lanes; what lies behind the table is no slot of anybody
     auto ids_of = [&](int t) __attribute__((always_inline)) { return table[min((t * kManySlots + lane % 8 * 8) >> shift, a.pages.max_pages - 1)]; };
     struct Places {
@@ -87,11 +85,18 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         }
         return pl;
     };
-    auto move_k = [&](int to, const Places& pl, int j) __attribute__((always_inline)) {
-        load_lds_16(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[j / IPR], pl.bytes[j / IPR]), base + to + (wave * 16 + j * RPI) * ROW, k_part[j]);
+    // run u of the wave's share
+    auto move_k = [&](int to, const Places& pl, int u) __attribute__((always_inline)) {
+        uint32_t from[IPR];
+#pragma unroll
+        for (int j = 0; j < IPR; ++j) from[j] = k_part ^ (u * IPR + j) * KTURN;
+        load_run_lds<IPR, false>(tile_rsrc(static_cast<const char*>(a.k_pages) + pl.from[u], pl.bytes[u]), base + to + (wave * 16 + u * 8) * ROW, from);
     };
-    auto move_v = [&](int to, const Places& pl, int j) __attribute__((always_inline)) {
-        load_lds_16(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[j / IPR], pl.bytes[j / IPR]), base + to + (wave * 16 + j * RPI) * ROW, v_part[j % IPR]);
+    auto move_v = [&](int to, const Places& pl, int u) __attribute__((always_inline)) {
+        uint32_t from[IPR];
+#pragma unroll
+        for (int j = 0; j < IPR; ++j) from[j] = v_part;
+        load_run_lds<IPR, false>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), base + to + (wave * 16 + u * 8) * ROW, from);
     };
 
     // A wave's 32 rows of queries travel through the place of its own share of the V tiles, 16 rows each
@@ -109,17 +114,18 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         }
         const Places pl = places_of(t0, ids);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) move_k(K0, pl, j);
+        for (int u = 0; u < RUNS; ++u) move_k(K0, pl, u);
     }
     int ids1 = ids_of(t0), ids2 = ids_of(t0 + 1), ids3 = ids_of(t0 + 2);
     // A operand of S^T: row i of a 32-slot block is slot swap23(i) (bits 2 and 3 of i exchanged), so that registers 8G .. 8G+7 of a lane hold the 8
     // consecutive slots 16G + 8h .. +7: the P fragment of a P.V instruction is a run of registers.
     const int krow = (c32 & ~12) | ((c32 & 4) << 1) | ((c32 & 8) >> 1);
-    uint32_t k_at[KB];  // byte address of this lane's 16 bytes of contraction block kb in tile K0
+    uint32_t k_at[KB / 4];  // byte address of this lane's 16 bytes of contraction blocks 4 i and, turned over, 4 i + 1 .. 3 in tile K0
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) k_at[kb] = one_register(base + krow * ROW + ((2 * kb + h) ^ ManySwizzleK<D>::at(krow)) * 16);
+    for (int i = 0; i < KB / 4; ++i) k_at[i] = one_register(base + krow * ROW + ((8 * i + h) ^ ManySwizzleK<D>::at(krow)) * 16);
     auto k_frag = [&](int kt, int f) __attribute__((always_inline)) {  // f = 2 kb + 32-slot block
-        return *(lds_bf16x8*)(uintptr_t)(k_at[f / 2] + kt + f % 2 * 32 * ROW);
+        const uint32_t from = k_at[f / 8] ^ f / 2 % 4 * 32;
+        return *(lds_bf16x8*)(uintptr_t)(from + kt + f % 2 * 32 * ROW);
     };
     uint32_t v_at[DB];  // of the transposing read: 4 features of one slot
 #pragma unroll
@@ -152,13 +158,13 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         const int n0 = t * kManySlots;
         const bool some = bad || n0 + kManySlots - 1 > lowest;
         if (some) {
-            asm volatile("");  // a branch, not 64 instructions in every tile
-            const int upto = limit - n0 - h * 8;
+            const int l = anew(lane);  // (a branch, not 64 instructions in every tile, and no register between tiles)
+            const int upto = sees(rw + l % 32) - n0 - l / 32 * 8;
 #pragma unroll
             for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (nb * 32 + (r / 8) * 16 + (r % 8) > upto || (bad >> (nb * 4 + r / 8 * 2 + h) & 1)) s[nb][r] = -INFINITY;
+                    if (nb * 32 + (r / 8) * 16 + (r % 8) > upto || (bad >> (nb * 4 + r / 8 * 2 + l / 32) & 1)) s[nb][r] = -INFINITY;
         }
         return some;
     };
@@ -285,9 +291,9 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         qf[kb] = *(lds_bf16x8*)(uintptr_t)(q_at + c32 / 16 * TILE + c32 % 16 * ROW + ((2 * kb + h) ^ ManySwizzleK<D>::at(c32)) * 16);
     wait_lds();  // their place is free
 #pragma unroll
-    for (int j = 0; j < NI; ++j) move_v(V0, pl1, j);
+    for (int u = 0; u < RUNS; ++u) move_v(V0, pl1, u);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) move_k(K1, pl2, j);
+    for (int u = 0; u < RUNS; ++u) move_k(K1, pl2, u);
     pl1 = pl2;
     pl2 = places_of(t0 + 2, ids3);
     meet();
@@ -319,11 +325,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         }
         ids = ids_of(t0 + i + 3);
         phase_a(std::true_type{}, s, sn, k_next, [&](int f) __attribute__((always_inline)) {
-            constexpr int EVERY = NA / (2 * NI);
+            constexpr int EVERY = NA / (2 * RUNS);
             static_assert(EVERY >= 1, "a phase has room for its loads");
             if (f < NA && f % EVERY == 0) {
-                if (f / EVERY < NI) move_k(k_old, pl2, f / EVERY);  // (behind the last tile nothing is fetched)
-                else move_v(v_next, pl1, f / EVERY - NI);
+                if (f / EVERY < RUNS) move_k(k_old, pl2, f / EVERY);  // (behind the last tile nothing is fetched)
+                else move_v(v_next, pl1, f / EVERY - RUNS);
             }
         });
         const bool was = hidden;
@@ -352,11 +358,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         const bool even = i % 2 == 0;
         if (i + 2 < n_iter) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j) move_k(even ? K0 : K1, pl2, j);
+            for (int u = 0; u < RUNS; ++u) move_k(even ? K0 : K1, pl2, u);
         }
         if (i + 1 < n_iter) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j) move_v(even ? V1 : V0, pl1, j);
+            for (int u = 0; u < RUNS; ++u) move_v(even ? V1 : V0, pl1, u);
         }
         if (work) {
             if (odd) {
@@ -368,7 +374,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
             phase_b(std::false_type{}, sB, even ? V0 : V1);
         }
     }
-    if (__syncthreads_or(unbounded)) return false;
+    const bool mine = __any(unbounded);
+    if (lane == 0) flags[wave] = mine;
+    __syncthreads();
+    static_assert(kPagedWaves == 4);
+    if (flags[0] | flags[1] | flags[2] | flags[3]) return false;
     if (rw >= at.s.rows) return true;
 
     const int el = anew(lane), ec = el % 32, eh = el / 32;  // lane, row and half of the way out
