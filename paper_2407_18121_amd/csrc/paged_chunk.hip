@@ -13,10 +13,19 @@
 
 namespace ec {
 
-constexpr int kChunkPlaces = 512;              // workgroups that the chip holds at once
-constexpr int kChunkParts = 4 * kChunkPlaces;  // segments whose results the workspace holds, at most
-constexpr int kChunkTiles = 128;               // tiles from which on segments may take several rounds
-constexpr int kChunkJoinRows = 4;              // rows of a joining workgroup, a wave each
+// Waves of a workgroup: four, of which a compute unit holds two workgroups, or eight where a batch has no more tiles than the chip has compute units. A wave
+// alone on its SIMD issues half as much as two do.
+constexpr int kFewWaves = 4, kManyWaves = 8;
+template <int WAVES> constexpr int kChunkPlaces = 2 * kFewWaves * kComputeUnits / WAVES;  // workgroups that the chip holds at once
+constexpr int kChunkParts = 4 * kChunkPlaces<kFewWaves>;  // segments whose results the workspace holds, at most
+constexpr int kChunkTiles = 128;                          // tiles from which on segments may take several rounds
+constexpr int kJoinWaves = 4, kJoinGroups = 8;            // waves of a joining workgroup, and workgroups that share a tile's rows
+
+// A tile whose segments' results are joined: rows r0 .. r1-1, `count` segments, those of the first from row `place` of the workspace on, `between` rows from
+// one to the next.
+struct CutTile {
+    int place, between, count, r0, r1, t0, hk, unused;
+};
 
 struct ChunkStep {
     const void *q, *k_pages, *v_pages;
@@ -27,11 +36,31 @@ struct ChunkStep {
     int B, T, H, Hkv, group;
     uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
     int rounds;
+    bool cut;         // whether tiles may be cut
     float scale, scale_log2e;
+    int* cut_tiles;   // tiles that are cut, which paged_chunk_join_kernel goes over
+    CutTile* records;
     int part_rows;    // rows of a segment's place in the workspace
     float* partials;  // [segment][part_rows][D] of sequences that are cut
     float2* stats;    // [segment][part_rows] largest score, before its scale, and sum
 };
+
+// The lane, found out anew: as with the arguments, nothing is kept for it.
+__device__ __forceinline__ int lane_anew() { return anew((int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0))) & (kWave - 1); }
+
+// The launch's arguments, read anew: what a workgroup needs only at its start or its end takes no registers in between.
+__device__ __forceinline__ ChunkStep chunk_args()
+{
+    typedef __attribute__((address_space(4))) const uint32_t const_u32;
+    struct Words {
+        uint32_t of[sizeof(ChunkStep) / 4];
+    } words;
+    const const_u32* from = (const const_u32*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(from));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(ChunkStep) / 4); ++i) words.of[i] = from[i];
+    return __builtin_bit_cast(ChunkStep, words);
+}
 
 __device__ __forceinline__ int token_of(const ChunkStep& a, int row) { return (int)(__umulhi((uint32_t)row << 2, a.group_mul) >> a.group_shift); }
 
@@ -72,10 +101,10 @@ struct ChunkCut {
     __device__ __forceinline__ int parts(const ChunkSeq& s) const { return (s.tiles - whole) * segments; }
 };
 // What all of them are cut by: the units that are a place's share of the whole batch, and the rounds that segments may take.
-struct ChunkShare {
+template <int UNIT> struct ChunkShare {
     int units, rounds;
     // Units of a segment, at least: as many as its results, written and read again, take the time of.
-    static __device__ __forceinline__ int least(const ChunkSeq& s) { return max(min(s.rows, s.tile_rows) / 8, 4); }
+    static __device__ __forceinline__ int least(const ChunkSeq& s) { return max(min(s.rows, s.tile_rows) * 8, 256) / UNIT; }
     // A tile of U units, against a share of A:
     //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
     //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
@@ -104,20 +133,20 @@ struct ChunkShare {
         return {s.tiles, 1, U};
     }
 };
-template <int DT, int UNIT> __device__ __forceinline__ ChunkShare chunk_share(const ChunkStep& a)
+// s: of this lane's sequence afterwards, if there are no more than lanes
+template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
     long long all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
-    ChunkSeq s;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
         if (a.rounds > 1) all += wave_sum((long long)s.tiles * (s.units + s.first_units));
         most += wave_sum((long long)s.tiles * s.units);
     }
     all *= a.Hkv, most *= a.Hkv;
-    // one round: most / share <= kChunkPlaces parts; several: rounds * most / share and 2 most / share <= kChunkParts, as most <= all
-    const long long share = a.rounds > 1 ? (all + 2 * kChunkPlaces - 1) / (2 * kChunkPlaces) : (most + kChunkPlaces - 1) / kChunkPlaces;
+    // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
+    const long long share = a.rounds > 1 ? (all + 2 * PLACES - 1) / (2 * PLACES) : (most + PLACES - 1) / PLACES;
     const int units = (int)min(max(share, 1LL), 1LL << 22);
-    return {units, a.rounds > 1 ? (int)min(4LL, kChunkParts * (long long)units / max(most, 1LL)) : 1};
+    return {units, a.rounds > 1 ? (int)min(4LL, 4 * PLACES * (long long)units / max(most, 1LL)) : 1};
 }
 
 // Units that a tile's last row sees.
@@ -133,23 +162,22 @@ struct ChunkItem {
     ChunkSeq s;
     int hk, segment, each;  // units of a segment
     int r0, r1, seen;       // rows of the tile, units that its last row sees
-    size_t place;           // of the segment's results in the workspace, of sequences that are cut
+    size_t place;           // row of the segment's results in the workspace, of sequences that are cut
     int b;                  // < 0: none
 };
 // The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
-// which sees most, then segments.
-template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare& share, int id)
+// which sees most, then segments. s: as chunk_share leaves it.
+template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
 {
-    const int lane = anew(threadIdx.x) & (kWave - 1), hk = id % a.Hkv, j = id / a.Hkv;
-    int before = 0, parts_before = 0;
+    const int lane = lane_anew(), hk = id % a.Hkv, j = id / a.Hkv;
+    int before = 0, parts_before = 0, cut_before = 0;
     ChunkItem it;
     it.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        ChunkSeq s;
-        s.read<DT, UNIT>(a, b0 + lane);
+        if (a.B > kWave) s.read<DT, UNIT>(a, b0 + lane);
         const ChunkCut cut = share.of(s);
-        const int items = cut.items(s), parts = cut.parts(s);
-        const int upto = wave_scan(items), parts_upto = wave_scan(parts);
+        const int items = cut.items(s), parts = cut.parts(s), cut_tiles = cut.segments > 1 ? s.tiles - cut.whole : 0;
+        const int upto = wave_scan(items), parts_upto = wave_scan(parts), cut_upto = wave_scan(cut_tiles);
         const unsigned long long beyond = __ballot(j < before + upto);
         if (beyond) {
             const int at = __ffsll(beyond) - 1;
@@ -159,40 +187,55 @@ template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(cons
             if (in < 0 || in >= of(items)) return it;
             int tile = in;  // from the last one on
             it.segment = 0, it.each = it.s.units;
+            const int tiles = it.s.tiles - whole;
             if (part >= 0) {
-                const int tiles = it.s.tiles - whole;
                 it.segment = scalar(divided(part, tiles)), it.each = of(cut.each);
                 tile = whole + part - it.segment * tiles;
             }
+            const int nth = tile - whole;
             tile = it.s.tiles - 1 - tile;
             it.r0 = tile * it.s.tile_rows, it.r1 = min(it.r0 + it.s.tile_rows, it.s.rows);
             it.seen = scalar(chunk_units<UNIT>(a, it.s, tile));
             it.hk = hk;
             it.place = ((size_t)(parts_before + of(parts_upto) - of(parts) + max(part, 0)) * a.Hkv + hk) * a.part_rows;
             it.b = b0 + at;
+            if (part >= 0 && it.segment == 0 && wave == 0 && lane == 0)
+                a.records[(cut_before + of(cut_upto) - of(cut_tiles) + nth) * a.Hkv + hk] = {(int)it.place, tiles * a.Hkv * a.part_rows,
+                                                                                            scalar(divided(it.seen + it.each - 1, it.each)), it.r0, it.r1, it.s.t0, hk, 0};
             return it;
         }
-        before += last_lane(upto), parts_before += last_lane(parts_upto);
+        before += last_lane(upto), parts_before += last_lane(parts_upto), cut_before += last_lane(cut_upto);
     }
     return it;
 }
+template <int DT, int UNIT> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s)
+{
+    int n = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        if (a.B > kWave) s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
+        const ChunkCut cut = share.of(s);
+        n += last_lane(wave_scan(cut.segments > 1 ? s.tiles - cut.whole : 0));
+    }
+    if (threadIdx.x == 0) *a.cut_tiles = n * a.Hkv;
+}
+
 template <int DT, int D> __device__ __forceinline__ void chunk_write(const ChunkStep& a, size_t at, float x, float y)
 {
     if constexpr (DT == EC_BF16) static_cast<uint32_t*>(a.out)[at / 2] = (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16;
     else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(x, y);
 }
 // Number of the (token, query head) that a row is, in out and lse.
-__device__ __forceinline__ size_t chunk_row(const ChunkStep& a, const ChunkSeq& s, int hk, int row)
+__device__ __forceinline__ size_t chunk_row(const ChunkStep& a, int t0, int hk, int row)
 {
     const int token = token_of(a, row);
-    return (size_t)(s.t0 + token) * a.H + hk * a.group + (row - token * a.group);
+    return (size_t)(t0 + token) * a.H + hk * a.group + (row - token * a.group);
 }
 
-template <int DT, int D> __device__ __forceinline__ void chunk_nothing(const ChunkStep& a, const ChunkItem& at)
+template <int DT, int D, int WAVES> __device__ __forceinline__ void chunk_nothing(const ChunkStep& a, const ChunkItem& at, int wave)
 {
     const int r0 = at.r0, rows = at.r1 - r0;
-    for (int i = threadIdx.x; i < rows * (D / 2); i += blockDim.x) {
-        const size_t row = chunk_row(a, at.s, at.hk, r0 + i / (D / 2));
+    for (int i = wave * kWave + lane_anew(); i < rows * (D / 2); i += WAVES * kWave) {
+        const size_t row = chunk_row(a, at.s.t0, at.hk, r0 + i / (D / 2));
         chunk_write<DT, D>(a, row * D + i % (D / 2) * 2, 0.f, 0.f);
         if (a.lse && i % (D / 2) == 0) a.lse[row] = -INFINITY;
     }
@@ -203,16 +246,16 @@ template <int DT, int D> __device__ __forceinline__ void chunk_nothing(const Chu
 //   S^T = K . Q^T      matrix instructions, so that a lane owns one row in 16 and 4 consecutive slots of a block of 16
 //   O^T += V^T . P^T   the probabilities are the second operand as they stand; V is transposed on its way out of LDS (bf16)
 // A bf16 probability enters as the sum of three bf16 numbers, all its 24 bits: few rows are bound by the bytes of K and V, and the matrix pipes have the room.
-template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(const ChunkStep& a, const ChunkItem& at, unsigned char* tiles, float* sh_m, float* sh_l)
+template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chunk_few_rows(const ChunkStep& a, const ChunkItem& at, int wave, unsigned char* tiles, float* sh_m, float* sh_l)
 {
     using T = PagedTile<DT, D>;
-    constexpr int WAVES = kPagedWaves, TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
+    constexpr int TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
     constexpr int KB = ROW / 64;   // 64-byte blocks of a row: what the four quarters of a wave contract together
     constexpr int OB = D / 16;     // 16-feature blocks of the output
     constexpr int OROW = D + 4;    // floats of a row's sums in LDS, padded
     constexpr int BLOCKS = TR / 16;
     static_assert(16 * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
-    const int tid = anew(threadIdx.x) & (WAVES * kWave - 1), lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lane = lane_anew(), tid = wave * kWave + lane;
     const int c16 = lane % 16, quarter = lane / 16;
     const int slots = a.pages.slots(), r0 = at.r0;
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
@@ -290,7 +333,7 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
     for (int rb = 0; rb < RB; ++rb) {
         const int r = r0 + rb * 16 + c16;
         limit[rb] = r < at.r1 ? min(at.s.L + token_of(a, r), slots - 1) : -1;
-        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s, at.hk, min(r, at.r1 - 1)) * ROW);
+        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + chunk_row(a, at.s.t0, at.hk, min(r, at.r1 - 1)) * ROW);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) qf[rb][kb] = q[kb * 4 + quarter];
         m[rb] = kLowest, l[rb] = 0.f;
@@ -557,6 +600,7 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
 
     // ------------------------------------------------------------------ the waves' results together
     wait_loads();  // nothing more arrives in the tiles, whose place the sums take
+    const ChunkStep e = chunk_args();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const float all = head_sum(l[rb]);
@@ -586,13 +630,13 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
                 sum += sh_l[w * 16 + r] * c, x += v.x * c, y += v.y * c;
             }
             if (whole) {
-                const size_t row = chunk_row(a, at.s, at.hk, r0 + rb * 16 + r);
-                chunk_write<DT, D>(a, row * D + d, sum == 0.f ? 0.f : x / sum, sum == 0.f ? 0.f : y / sum);
-                if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+                const size_t row = chunk_row(e, at.s.t0, at.hk, r0 + rb * 16 + r);
+                chunk_write<DT, D>(e, row * D + d, sum == 0.f ? 0.f : x / sum, sum == 0.f ? 0.f : y / sum);
+                if (e.lse && d == 0) e.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, e.scale, logf(sum));
             } else {
                 const size_t place = at.place + rb * 16 + r;
-                *reinterpret_cast<float2*>(a.partials + place * D + d) = make_float2(x, y);
-                if (d == 0) a.stats[place] = make_float2(top, sum);
+                *reinterpret_cast<float2*>(e.partials + place * D + d) = make_float2(x, y);
+                if (d == 0) e.stats[place] = make_float2(top, sum);
             }
         }
     }
@@ -602,111 +646,99 @@ template <int DT, int D, int RB> __device__ __forceinline__ void chunk_few_rows(
 #include "paged_chunk_many.h"
 namespace ec {
 
-template <int DT, int D>
-__global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep a)
+template <int DT, int D, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep first)
 {
     using T = PagedTile<DT, D>;
-    constexpr int UNIT = kPagedWaves * T::TR;
-    __shared__ __align__(256) unsigned char tiles[kPagedWaves * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
-    __shared__ float sh_m[kPagedWaves * 16], sh_l[kPagedWaves * 16];
-    __shared__ int flags[kPagedWaves];
-    const ChunkShare share = chunk_share<DT, UNIT>(a);
-    auto take = [&](const ChunkItem& at) __attribute__((always_inline)) {
+    constexpr int UNIT = WAVES * T::TR;
+    __shared__ __align__(256) unsigned char tiles[WAVES * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
+    __shared__ float sh_m[WAVES * 32], sh_l[WAVES * 32];
+    __shared__ int flags[WAVES];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    ChunkSeq s;
+    const auto share = chunk_share<DT, UNIT, kChunkPlaces<WAVES>>(first, s);
+    if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<DT, UNIT>(first, share, s);
+    auto take = [&](const ChunkStep& a, const ChunkItem& at) __attribute__((always_inline)) {
         if (!at.s.live) {
-            chunk_nothing<DT, D>(a, at);
+            chunk_nothing<DT, D, WAVES>(a, at, wave);
             return;
         }
         if constexpr (DT == EC_BF16) {
-            static_assert(sizeof(tiles) >= 4 * kManySlots * D * 2 && UNIT % kManySlots == 0);
+            static_assert(sizeof(tiles) >= WAVES * kManySlots * D * 2 && UNIT % kManySlots == 0);
             if (at.s.tile_rows == kManyRows) {
-                if (chunk_many_rows<D>(a, at, tiles, flags, UNIT)) return;
+                if (chunk_many_rows<D, WAVES>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT)) return;
                 ChunkItem part = at;
                 for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
                     part.r1 = min(part.r0 + 16, at.r1);
-                    chunk_few_rows<DT, D, 1>(a, part, tiles, sh_m, sh_l);
+                    chunk_few_rows<DT, D, WAVES, 1>(a, part, wave, tiles, sh_m, sh_l);
                     __syncthreads();
                 }
                 return;
             }
         }
-        if (at.s.tile_rows == 16) chunk_few_rows<DT, D, 1>(a, at, tiles, sh_m, sh_l);
-        else chunk_few_rows<DT, D, 2>(a, at, tiles, sh_m, sh_l);
+        if (at.s.tile_rows == 16) chunk_few_rows<DT, D, WAVES, 1>(a, at, wave, tiles, sh_m, sh_l);
+        else chunk_few_rows<DT, D, WAVES, 2>(a, at, wave, tiles, sh_m, sh_l);
     };
     for (int id = blockIdx.x;; id += gridDim.x) {
-        const ChunkItem at = chunk_item<DT, UNIT>(a, share, id);
+        const ChunkStep a = chunk_args();
+        if (id != blockIdx.x && a.B <= kWave) s.read<DT, UNIT>(a, lane_anew());
+        const ChunkItem at = chunk_item<DT, UNIT>(a, share, s, id, wave);
         if (at.b < 0) return;
-        take(at);
+        take(a, at);
         __syncthreads();  // the tiles have been read
     }
 }
 
-// The segments' results of every row of tiles that are cut, a wave a row. Bound by latency: the statistics, a lane a segment, then the sums, eight segments' in
-// flight.
-template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) void paged_chunk_join_kernel(ChunkStep a)
+// The segments' results of every row of tiles that are cut, a wave a row. Bound by latency: the tile, the statistics, a lane a segment, then the sums, eight
+// segments' in flight.
+template <int DT, int D> __global__ __launch_bounds__(kJoinWaves* kWave) void paged_chunk_join_kernel(ChunkStep a)
 {
-    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR, E = D / kWave, AHEAD = 8;
+    constexpr int E = D / kWave, AHEAD = 8;
     typedef __attribute__((ext_vector_type(E))) float of_row;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const ChunkShare share = chunk_share<DT, UNIT>(a);
-    const int step = gridDim.x * kChunkJoinRows;
-    int me = blockIdx.x * kChunkJoinRows + wave;  // rows are dealt out over all sequences that are cut; me: of the present one
-    int parts = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        ChunkSeq all;
-        all.read<DT, UNIT>(a, b0 + lane);
-        const ChunkCut cuts = share.of(all);
-        for (unsigned long long todo = __ballot(cuts.segments > 1); todo; todo &= todo - 1) {
-            const int at = __ffsll(todo) - 1;
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-            const ChunkSeq s{of(all.L), of(all.t0), of(all.n), of(all.rows), of(all.tile_rows), of(all.tiles), of(all.units), of(all.first_units), true};
-            const ChunkCut cut{of(cuts.whole), of(cuts.segments), of(cuts.each)};
-            const int tiles = s.tiles - cut.whole;  // the first ones
-            const int heads = min(tiles * s.tile_rows, s.rows);  // rows of a key/value head
-            for (; me < heads * a.Hkv; me += step) {
-                const int hk = me / heads, r = me - hk * heads, tile = r / s.tile_rows;
-                const int seen = chunk_units<UNIT>(a, s, tile), count = (seen + cut.each - 1) / cut.each;
-                if (count == 1) continue;  // written already
-                const int between = tiles * a.Hkv * a.part_rows;  // rows from a segment to the next
-                const size_t first = ((size_t)(parts + tiles - 1 - tile) * a.Hkv + hk) * a.part_rows + (r - tile * s.tile_rows);
-                float top = kLowest;
-                for (int g = lane; g < count; g += kWave) {
-                    const float2 x = a.stats[first + (size_t)g * between];
-                    if (!(x.y == 0.f)) top = fmaxf(top, x.x);  // (NaN counts)
-                }
-                top = wave_max(top);
-                float sum = 0.f;
-                of_row o = {};
-                for (int g0 = 0; g0 < count; g0 += kWave) {
-                    float2 x = make_float2(0.f, 0.f);
-                    if (g0 + lane < count) x = a.stats[first + (size_t)(g0 + lane) * between];
-                    const float weight = x.y == 0.f ? 0.f : exp2f((x.x - top) * a.scale_log2e);
-                    const float share_of = x.y == 0.f ? 0.f : x.y * weight;
-                    for (int g = g0; g < min(g0 + kWave, count); g += AHEAD) {
-                        of_row v[AHEAD];
+    const int all = *a.cut_tiles * kJoinGroups;
+    for (int i = blockIdx.x; i < all; i += gridDim.x) {
+        const CutTile tile = a.records[i / kJoinGroups];
+        if (tile.count == 1) continue;  // written already
+        for (int r = tile.r0 + i % kJoinGroups * kJoinWaves + wave; r < tile.r1; r += kJoinGroups * kJoinWaves) {
+            const int first = tile.place + (r - tile.r0);
+            float top = kLowest;
+            for (int g = lane; g < tile.count; g += kWave) {
+                const float2 x = a.stats[first + g * tile.between];
+                if (!(x.y == 0.f)) top = fmaxf(top, x.x);  // (NaN counts)
+            }
+            top = wave_max(top);
+            float sum = 0.f;
+            of_row o = {};
+            for (int g0 = 0; g0 < tile.count; g0 += kWave) {
+                float2 x = make_float2(0.f, 0.f);
+                if (g0 + lane < tile.count) x = a.stats[first + (g0 + lane) * tile.between];
+                const float weight = x.y == 0.f ? 0.f : exp2f((x.x - top) * a.scale_log2e);
+                const float share = x.y == 0.f ? 0.f : x.y * weight;
+                for (int g = g0; g < min(g0 + kWave, tile.count); g += AHEAD) {
+                    of_row v[AHEAD];
 #pragma unroll
-                        for (int u = 0; u < AHEAD; ++u)
-                            v[u] = *reinterpret_cast<const of_row*>(a.partials + (first + (size_t)min(g + u, count - 1) * between) * D + lane * E);
+                    for (int u = 0; u < AHEAD; ++u)
+                        v[u] = *reinterpret_cast<const of_row*>(a.partials + (size_t)(first + min(g + u, tile.count - 1) * tile.between) * D + lane * E);
 #pragma unroll
-                        for (int u = 0; u < AHEAD; ++u) {
-                            if (g + u >= count) continue;
-                            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), g + u - g0));
-                            sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share_of), g + u - g0));
-                            // a segment of which the row sees nothing has sums of 0
+                    for (int u = 0; u < AHEAD; ++u) {
+                        if (g + u >= tile.count) continue;
+                        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), g + u - g0));
+                        sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), g + u - g0));
+                        // a segment of which the row sees nothing has sums of 0
 #pragma unroll
-                            for (int e = 0; e < E; ++e) o[e] = fmaf(v[u][e], w, o[e]);
-                        }
+                        for (int e = 0; e < E; ++e) o[e] = fmaf(v[u][e], w, o[e]);
                     }
                 }
-                const size_t row = chunk_row(a, s, hk, r);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float x = sum == 0.f ? 0.f : o[e] / sum;
-                    if constexpr (DT == EC_BF16) static_cast<uint16_t*>(a.out)[row * D + lane * E + e] = f32_to_bf16(x);
-                    else static_cast<float*>(a.out)[row * D + lane * E + e] = x;
-                }
-                if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
             }
-            me -= heads * a.Hkv, parts += cut.parts(s);
+            const size_t row = chunk_row(a, tile.t0, tile.hk, r);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = sum == 0.f ? 0.f : o[e] / sum;
+                if constexpr (DT == EC_BF16) static_cast<uint16_t*>(a.out)[row * D + lane * E + e] = f32_to_bf16(x);
+                else static_cast<float*>(a.out)[row * D + lane * E + e] = x;
+            }
+            if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
         }
     }
 }
@@ -715,24 +747,37 @@ template <int DT, int D> __global__ __launch_bounds__(kChunkJoinRows* kWave) voi
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 static int part_rows(int T, int H) { return (int)std::min<long long>(((long long)T * H + 15) / 16 * 16, 128); }
 // Tiles of all key/value heads that a call can have, and segments whose results its workspace holds: of any number of sequences and of key/value heads.
-static long long most_tiles(long long T, long long group, long long Hkv, long long B, int rows) { return ((T * group + rows - 1) / rows + std::min(B, T)) * Hkv; }
-static int most_parts(int T, int H) { return (long long)T * H + most_tiles(T, H, 1, 0, 32) + H >= kChunkTiles ? kChunkParts : kChunkPlaces; }
-static size_t stat_bytes(int T, int H) { return up256((size_t)most_parts(T, H) * part_rows(T, H) * sizeof(float2)); }
-size_t paged_chunk_ws(int T, int H, int D) { return stat_bytes(T, H) + (size_t)most_parts(T, H) * part_rows(T, H) * D * sizeof(float); }
+static long long most_tiles(long long T, long long group, long long Hkv, long long B, int rows) { return (T * group + std::min(B, T) * (rows - 1)) / rows * Hkv; }
+static int most_parts(int T, int H) { return most_tiles(T, 1, H, T, 32) >= kChunkTiles ? kChunkParts : kChunkPlaces<kFewWaves>; }
+struct ChunkPlaces {  // where things lie in a workspace
+    size_t records, stats, partials, end;
+    ChunkPlaces(int T, int H, int D)
+    {
+        const size_t parts = most_parts(T, H), rows = parts * part_rows(T, H);
+        records = 256, stats = records + up256(parts * sizeof(CutTile)), partials = stats + up256(rows * sizeof(float2));
+        end = partials + rows * D * sizeof(float);
+    }
+};
+size_t paged_chunk_ws(int T, int H, int D) { return ChunkPlaces(T, H, D).end; }
 
 template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
 {
-    constexpr int UNIT = kPagedWaves * PagedTile<DT, D>::TR;
-    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
+    constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
-    const bool cut = units > 4;  // (fewer make no two segments)
+    a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (fewer units make no two segments)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
-    const long long groups = cut ? std::max<long long>(tiles, kChunkPlaces) : tiles;
-    hipLaunchKernelGGL((paged_chunk_kernel<DT, D>), dim3((unsigned)groups), dim3(kPagedWaves * kWave), 0, stream, a);
+    auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };
+    if (DT == EC_BF16 && tiles <= kComputeUnits) {
+        if constexpr (DT == EC_BF16)
+            hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kManyWaves>), groups(kChunkPlaces<kManyWaves>), dim3(kManyWaves * kWave), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kFewWaves>), groups(kChunkPlaces<kFewWaves>), dim3(kFewWaves * kWave), 0, stream, a);
+    }
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
-    if (!cut) return EC_OK;
-    const long long rows = ((long long)a.T * a.H + kChunkJoinRows - 1) / kChunkJoinRows;
-    hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(rows, 2048)), dim3(kChunkJoinRows * kWave), 0, stream, a);
+    if (!a.cut) return EC_OK;
+    const long long joins = std::min<long long>(tiles, most_parts(a.T, a.H)) * kJoinGroups;
+    hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(joins, 2048)), dim3(kJoinWaves * kWave), 0, stream, a);
     return status_from_hip(hipGetLastError());
 }
 
@@ -743,8 +788,11 @@ int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages
     uint32_t shift = 0;
     while (1u << shift < group) ++shift;
     const uint32_t mul = (uint32_t)(((1ULL << (30 + shift)) + group - 1) / group);
-    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul, shift, 1, scale, scale * kLog2e, part_rows(T, H),
-                      reinterpret_cast<float*>(static_cast<char*>(ws) + stat_bytes(T, H)), static_cast<float2*>(ws)};
+    const ChunkPlaces at(T, H, D);
+    char* const w = static_cast<char*>(ws);
+    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul, shift, 1, false, scale, scale * kLog2e,
+                      reinterpret_cast<int*>(w), reinterpret_cast<CutTile*>(w + at.records), part_rows(T, H), reinterpret_cast<float*>(w + at.partials),
+                      reinterpret_cast<float2*>(w + at.stats)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);
     return D == 128 ? launch<EC_F32, 128>(a, stream) : launch<EC_F32, 64>(a, stream);
 }

@@ -27,9 +27,12 @@ template <int D> struct ManySwizzleV {  // four rows at the same 64 bytes (a tra
     static __device__ __forceinline__ int at(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// False, and nothing written: rows of V that are not finite are seen by some of the rows only.
-template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, unsigned char* tiles, int* flags, int unit)
+// False, and nothing written: something has come out that is no number.
+// sh_m, sh_l: a float a thread of four waves.
+template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, int wave_wg, unsigned char* tiles, float* sh_m,
+                                                                            float* sh_l, int* flags, int unit)
 {
+    constexpr int QW = 4, KS = WAVES / QW;  // waves that share the rows, and groups of them that take turns at the tiles
     constexpr int ROW = D * 2, CH = ROW / 16, RPI = kWave / CH;  // bytes and chunks of a row, rows of a load instruction
     constexpr int KB = D / 16;    // contraction blocks of Q.K
     constexpr int DB = D / 32;    // 32-row blocks of O^T
@@ -39,7 +42,8 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     constexpr int TILE = kManySlots * ROW;
     constexpr int RUNS = 2, IPR = 8 / RPI;  // a wave moves 16 rows of a tile: two runs of 8, each in one page
     constexpr int K0 = 0, K1 = TILE, V0 = 2 * TILE, V1 = 3 * TILE;
-    const int tid = anew(threadIdx.x) & (kPagedWaves * kWave - 1), lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lane = lane_anew();
+    const int grp = wave_wg / QW, wave = wave_wg % QW;
     const int c32 = lane % 32, h = lane / 32;
     const int slots = a.pages.slots(), rw = at.r0 + wave * 32;  // first row of the workgroup, of this wave
     const int group = a.group, L = at.s.L;
@@ -50,13 +54,14 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
     if (first >= last) return true;  // a tile that sees fewer segments than its sequence has
     const bool whole = at.each >= at.seen;
-    const int t0 = first * (unit / kManySlots), t1 = min(last * (unit / kManySlots), highest / kManySlots + 1), n_iter = t1 - t0;
+    const int t0 = first * (unit / kManySlots), t1 = min(last * (unit / kManySlots), highest / kManySlots + 1), n_iter = (t1 - t0 + KS - 1) / KS;
+    auto nth = [&](int i) { return t0 + i * KS + grp; };  // the group's i-th tile
     const int end = min(highest + 1, t1 * kManySlots);  // rows behind it arrive as zeros
     const int lowest = scalar(sees(rw));
-    const int count = rw < at.s.rows ? max(min(scalar(sees(rw + 31)) / kManySlots + 1, t1) - t0, 0) : 0;
+    const int count = rw < at.s.rows ? max(min(scalar(sees(rw + 31)) / kManySlots + 1, t1) - t0 - grp + KS - 1, 0) / KS : 0;
 
     // ------------------------------------------------------------------ rows into LDS
-    const uint32_t base = lds_address(tiles);
+    const uint32_t base = lds_address(tiles) + grp * 4 * TILE;
     const int shift = a.pages.shift, mask = (1 << shift) - 1;
     const uint32_t head_bytes = (uint32_t)ROW << shift, page_bytes = head_bytes * (uint32_t)a.Hkv;
     const int32_t* table = a.pages.table + (size_t)at.b * a.pages.max_pages;
@@ -102,7 +107,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     // A wave's 32 rows of queries travel through the place of its own share of the V tiles, 16 rows each
     const uint32_t q_at = base + V0 + wave * (16 * ROW);
     {
-        int ids = ids_of(t0);
+        int ids = ids_of(nth(0));
         asm volatile("" : "+v"(ids));
         const int token0 = scalar(token_of(a, min(rw, at.s.rows - 1)));
         const u32x4 q_rsrc = tile_rsrc(static_cast<const char*>(a.q) + (size_t)(at.s.t0 + token0) * a.H * ROW, 0xfffffff0u);
@@ -112,11 +117,11 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
             const uint32_t from = ((uint32_t)(token - token0) * a.H + at.hk * group + (row - token * group)) * ROW + (lane % CH ^ ManySwizzleK<D>::at(i)) * 16;
             load_lds_16(q_rsrc, q_at + (j * RPI < 16 ? 0 : TILE - 16 * ROW) + j * RPI * ROW, from);
         }
-        const Places pl = places_of(t0, ids);
+        const Places pl = places_of(nth(0), ids);
 #pragma unroll
         for (int u = 0; u < RUNS; ++u) move_k(K0, pl, u);
     }
-    int ids1 = ids_of(t0), ids2 = ids_of(t0 + 1), ids3 = ids_of(t0 + 2);
+    int ids1 = ids_of(nth(0)), ids2 = ids_of(nth(1)), ids3 = ids_of(nth(2));
     // A operand of S^T: row i of a 32-slot block is slot swap23(i) (bits 2 and 3 of i exchanged), so that registers 8G .. 8G+7 of a lane hold the 8
     // consecutive slots 16G + 8h .. +7: the P fragment of a P.V instruction is a run of registers.
     const int krow = (c32 & ~12) | ((c32 & 4) << 1) | ((c32 & 8) >> 1);
@@ -153,11 +158,10 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     f32x16 sA[2], sB[2];
     bf16x8 pf[4];
 
-    // scores of slots that the row does not see; true if there may be some (the same for the whole wave)
+    // scores of slots that the row does not see
     auto hide = [&](f32x16 (&s)[2], int t, uint32_t bad) __attribute__((always_inline)) {
         const int n0 = t * kManySlots;
-        const bool some = bad || n0 + kManySlots - 1 > lowest;
-        if (some) {
+        if (bad || n0 + kManySlots - 1 > lowest) {
             const int l = anew(lane);  // (a branch, not 64 instructions in every tile, and no register between tiles)
             const int upto = sees(rw + l % 32) - n0 - l / 32 * 8;
 #pragma unroll
@@ -166,7 +170,6 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
                 for (int r = 0; r < 16; ++r)
                     if (nb * 32 + (r / 8) * 16 + (r % 8) > upto || (bad >> (nb * 4 + r / 8 * 2 + l / 32) & 1)) s[nb][r] = -INFINITY;
         }
-        return some;
     };
     auto raise_max = [&](float mx) __attribute__((always_inline)) {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
@@ -270,21 +273,9 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         }
         if constexpr (next.value) raise_max(fmaxf(mx[0], mx[1]));
     };
-    // An infinite V must not reach the rows that do not see it, as 0 times infinity would: the tiles of which some row does not see all slots are
-    // looked through, and where there is one the rows are left to chunk_few_rows.
-    bool unbounded = false;
-    auto look = [&](int vt) __attribute__((always_inline)) {
-#pragma unroll
-        for (int g = 0; g < NP; ++g) {
-            const u32x4 v = __builtin_bit_cast(u32x4, v_frag(vt, g));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) unbounded |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-        }
-    };
-
     wait_loads();  // this wave's queries and its share of the first K tile
     asm volatile("" : "+v"(ids1), "+v"(ids2), "+v"(ids3));
-    Places pl1 = places_of(t0, ids1), pl2 = places_of(t0 + 1, ids2);  // of the next V tile and the next K tile but one
+    Places pl1 = places_of(nth(0), ids1), pl2 = places_of(nth(1), ids2);  // of the next V tile and the next K tile but one
     const uint32_t bad = pl1.bad;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -295,9 +286,8 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
 #pragma unroll
     for (int u = 0; u < RUNS; ++u) move_k(K1, pl2, u);
     pl1 = pl2;
-    pl2 = places_of(t0 + 2, ids3);
+    pl2 = places_of(nth(2), ids3);
     meet();
-    bool hidden = false;  // of the tile in s
     if (count > 0) {  // scores of the first tile
         bf16x8 ka[NA];
 #pragma unroll
@@ -308,7 +298,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
             for (int r = 0; r < 16; ++r) sA[nb][r] = 0.f;
 #pragma unroll
         for (int f = 0; f < NA; ++f) sA[f % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[f], qf[f / 2], sA[f % 2], 0, 0, 0);
-        hidden = hide(sA, t0, bad);
+        hide(sA, nth(0), bad);
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(fmaxf(mx, sA[0][r]), sA[1][r]);
@@ -316,14 +306,16 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
     }
     // One tile with a successor: K of tile i + 1 and V of tile i have landed; K of tile i + 2 goes where K of tile i was, V of tile i + 1 where V of tile
     // i - 1 was, both read for the last time before the barrier.
+    // With scalar loads on their way (what the arguments are read by) the compiler could not tell LDS reads apart by their number: there are none from here on.
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     int ids = 0;
     auto body = [&](int i, f32x16 (&s)[2], f32x16 (&sn)[2], int k_old, int k_next, int v_cur, int v_next) __attribute__((always_inline)) {
         tile_barrier();
         if (i > 0) {
             asm volatile("" : "+v"(ids));
-            pl1 = pl2, pl2 = places_of(t0 + i + 2, ids);
+            pl1 = pl2, pl2 = places_of(nth(i + 2), ids);
         }
-        ids = ids_of(t0 + i + 3);
+        ids = ids_of(nth(i + 3));
         phase_a(std::true_type{}, s, sn, k_next, [&](int f) __attribute__((always_inline)) {
             constexpr int EVERY = NA / (2 * RUNS);
             static_assert(EVERY >= 1, "a phase has room for its loads");
@@ -332,9 +324,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
                 else move_v(v_next, pl1, f / EVERY - RUNS);
             }
         });
-        const bool was = hidden;
-        hidden = hide(sn, t0 + i + 1, pl1.bad);
-        if (was) look(v_cur);
+        hide(sn, nth(i + 1), pl1.bad);
         phase_b(std::true_type{}, sn, v_cur);
     };
     int i = 0;
@@ -352,9 +342,9 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
         tile_barrier();
         if (i > 0) {
             asm volatile("" : "+v"(ids));
-            pl1 = pl2, pl2 = places_of(t0 + i + 2, ids);
+            pl1 = pl2, pl2 = places_of(nth(i + 2), ids);
         }
-        ids = ids_of(t0 + i + 3);
+        ids = ids_of(nth(i + 3));
         const bool even = i % 2 == 0;
         if (i + 2 < n_iter) {
 #pragma unroll
@@ -370,24 +360,56 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
                 for (int nb = 0; nb < 2; ++nb) sA[nb] = sB[nb];
             }
             phase_a(std::false_type{}, sA, sB, K0, [](int) {});
-            if (hidden) look(even ? V0 : V1);
             phase_b(std::false_type{}, sB, even ? V0 : V1);
         }
     }
-    const bool mine = __any(unbounded);
-    if (lane == 0) flags[wave] = mine;
+    // An infinite V has reached the rows that do not see it too, as 0 times infinity. Where anything has come out that is no number the rows are left to
+    // chunk_few_rows, which takes care of it.
+    float zero = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = fmaf(o[db][r], 0.f, zero);
+    const bool mine = __any(!(zero == 0.f));
+    if (lane == 0) flags[wave_wg] = mine;
     __syncthreads();
-    static_assert(kPagedWaves == 4);
-    if (flags[0] | flags[1] | flags[2] | flags[3]) return false;
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) any |= flags[w];
+    if (any) return false;
+    if constexpr (KS == 2) {
+        // the second group hands its sums over through its tiles; word j of thread t lies at j * THREADS + t: consecutive lanes, consecutive words
+        constexpr int THREADS = QW * kWave;
+        static_assert(THREADS * DB * 16 * 4 <= 4 * TILE);
+        float* sums = reinterpret_cast<float*>(tiles + 4 * TILE);
+        const int t = wave * kWave + lane;
+        if (grp == 1) {
+            sh_m[t] = m, sh_l[t] = l;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sums[(db * 16 + r) * THREADS + t] = o[db][r];
+        }
+        __syncthreads();
+        if (grp == 1) return true;
+        const float m1 = sh_m[t], top = fmaxf(m, m1), f0 = __builtin_amdgcn_exp2f((m - top) * c), f1 = __builtin_amdgcn_exp2f((m1 - top) * c);
+        l = l * f0 + sh_l[t] * f1;
+        m = top;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[db][r] = o[db][r] * f0 + sums[(db * 16 + r) * THREADS + t] * f1;
+    }
     if (rw >= at.s.rows) return true;
 
+    const ChunkStep e = chunk_args();
     const int el = anew(lane), ec = el % 32, eh = el / 32;  // lane, row and half of the way out
     const float sum = l + __shfl_xor(l, 32, kWave);
     const int row = rw + ec;
     if (!whole) {
         const size_t place = at.place + wave * 32 + ec;
         if (row < at.s.rows) {
-            if (eh == 0) a.stats[place] = make_float2(m, sum);
+            if (eh == 0) e.stats[place] = make_float2(m, sum);
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -395,12 +417,12 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
                     f32x4 y;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) y[t] = o[db][g * 4 + t];
-                    *reinterpret_cast<f32x4*>(a.partials + place * D + db * 32 + g * 8 + eh * 4) = y;
+                    *reinterpret_cast<f32x4*>(e.partials + place * D + db * 32 + g * 8 + eh * 4) = y;
                 }
         }
         return true;
     }
-    if (a.lse && eh == 0 && row < at.s.rows) a.lse[chunk_row(a, at.s, at.hk, row)] = sum == 0.f ? -INFINITY : fmaf(m, a.scale, logf(sum));
+    if (e.lse && eh == 0 && row < at.s.rows) e.lse[chunk_row(e, at.s.t0, at.hk, row)] = sum == 0.f ? -INFINITY : fmaf(m, e.scale, logf(sum));
     // The accumulators hold 8-byte pieces of 32 rows per register pair. Half a row at a time they are turned through this wave's share of tile K1 (every
     // wave has read K for the last time), so that a store instruction writes whole stretches of a row.
     constexpr int HC = D / 16;        // 16-byte chunks in half a row
@@ -424,7 +446,7 @@ template <int D> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep
             const int r = j * RPS + el / HC;
             const u32x4 y = __builtin_bit_cast(u32x4, *(lds_bf16x8*)(uintptr_t)(stage + place(r, el % HC)));
             if (rw + r < at.s.rows)
-                *reinterpret_cast<u32x4*>(static_cast<char*>(a.out) + chunk_row(a, at.s, at.hk, rw + r) * ROW + half * (ROW / 2) + el % HC * 16) = y;
+                *reinterpret_cast<u32x4*>(static_cast<char*>(e.out) + chunk_row(e, at.s.t0, at.hk, rw + r) * ROW + half * (ROW / 2) + el % HC * 16) = y;
         }
     }
     return true;
