@@ -125,9 +125,9 @@ template <int UNIT> struct ChunkShare {
             if (n > 1) return cut(0, n);
         } else if (rounds > 1 && U > 0 && A < 4 * U) {
             const int k = divided(A, U), rest = A - k * U;
-            if (rest >= least(s) && rest * 8 >= A && (long long)s.tiles * rest >= A) {
+            if (rest >= least(s) && rest * 8 >= A && (long long)s.tiles * rest >= A && (long long)s.tiles * k * U < 1 << 24) {
                 const int n = divided(U, rest);
-                if (n > 1) return cut((int)((long long)s.tiles * k * U / A), n);
+                if (n > 1) return cut(divided(s.tiles * k * U, A), n);
             }
         }
         return {s.tiles, 1, U};
@@ -146,7 +146,8 @@ template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UN
     // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
     const long long share = a.rounds > 1 ? (all + 2 * PLACES - 1) / (2 * PLACES) : (most + PLACES - 1) / PLACES;
     const int units = (int)min(max(share, 1LL), 1LL << 22);
-    return {units, a.rounds > 1 ? (int)min(4LL, 4 * PLACES * (long long)units / max(most, 1LL)) : 1};
+    const long long held = 4LL * PLACES * units;
+    return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
 }
 
 // Units that a tile's last row sees.
@@ -169,7 +170,7 @@ struct ChunkItem {
 // which sees most, then segments. s: as chunk_share leaves it.
 template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
 {
-    const int lane = lane_anew(), hk = id % a.Hkv, j = id / a.Hkv;
+    const int lane = lane_anew(), j = scalar(id < 1 << 24 ? divided(id, a.Hkv) : id / a.Hkv), hk = id - j * a.Hkv;
     int before = 0, parts_before = 0, cut_before = 0;
     ChunkItem it;
     it.b = -1;
@@ -252,9 +253,7 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
     constexpr int TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
     constexpr int KB = ROW / 64;   // 64-byte blocks of a row: what the four quarters of a wave contract together
     constexpr int OB = D / 16;     // 16-feature blocks of the output
-    constexpr int OROW = D + 4;    // floats of a row's sums in LDS, padded
     constexpr int BLOCKS = TR / 16;
-    static_assert(16 * OROW * 4 <= 4 * T::BYTES, "a wave's sums fit into its tiles");
     const int lane = lane_anew(), tid = wave * kWave + lane;
     const int c16 = lane % 16, quarter = lane / 16;
     const int slots = a.pages.slots(), r0 = at.r0;
@@ -322,6 +321,12 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
         for (int u = 0; u < T::GROUPS; ++u)
             load_run_lds<T::IPG, T::kHalf>(tile_rsrc(static_cast<const char*>(a.v_pages) + pl.from[u], pl.bytes[u]), lds + u * 8 * ROW, v_part);
     };
+
+    int row = (first * WAVES + wave) * TR, left = last - first;  // rounds
+    const Ids at_once = pages_of(row), ahead = pages_of(row + ROUND);
+    const Places here = places_of(row, at_once);
+    issue_k(mine, here);
+    issue_v(mine + 2 * T::BYTES, here);
 
     // ------------------------------------------------------------------ one tile after the other
     f32x4 o[RB][OB];
@@ -570,16 +575,12 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
         }
     };
     {
-        // the queries have to be there before the first load into LDS is issued: what the compiler waits for by counting must not be behind it
+        // (what the compiler waits for by counting, the queries, comes between loads that it does not count: it waits for those before, too)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qf[rb][kb]));
-        int row = (first * WAVES + wave) * TR, left = last - first;  // rounds
-        const Places here = places_of(row, pages_of(row));
-        issue_k(mine, here);
-        issue_v(mine + 2 * T::BYTES, here);
-        Places next = places_of(row + ROUND, pages_of(row + ROUND));
+        Places next = places_of(row + ROUND, ahead);
         if (left > 1) {
             issue_k(mine + T::BYTES, next);
             issue_v(mine + 3 * T::BYTES, next);
@@ -599,45 +600,53 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
     }
 
     // ------------------------------------------------------------------ the waves' results together
+    // Row r of a wave's sums lies in its tiles at r * D, the 16-byte chunk c of it at place c ^ r, so that the lanes of a row block meet all banks alike.
     wait_loads();  // nothing more arrives in the tiles, whose place the sums take
     const ChunkStep e = chunk_args();
+    constexpr int ROWS = 16 * RB, CHUNKS = D / 4;
+    static_assert(ROWS * D * 4 <= 4 * T::BYTES && CHUNKS >= 16);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const float all = head_sum(l[rb]);
-        if (rb) __syncthreads();  // the sums before have been read
-        if (quarter == 0) sh_m[wave * 16 + c16] = m[rb], sh_l[wave * 16 + c16] = all;
+        if (quarter == 0) sh_m[wave * ROWS + rb * 16 + c16] = m[rb], sh_l[wave * ROWS + rb * 16 + c16] = all;
 #pragma unroll
         for (int i = 0; i < OB; ++i) {
             if constexpr (T::kHalf) {
-                *(lds_f32x4*)(uintptr_t)(mine + (c16 * OROW + i * 16 + quarter * 4) * 4) = o[rb][i];
+                *(lds_f32x4*)(uintptr_t)(mine + (rb * 16 + c16) * (D * 4) + ((i * 4 + quarter) ^ c16) * 16) = o[rb][i];
             } else {  // features 64 (i / 4) + 4 (4 quarter + r) + i % 4
                 typedef __attribute__((address_space(3))) float lds_float;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) *(lds_float*)(uintptr_t)(mine + (c16 * OROW + i / 4 * 64 + (quarter * 4 + r) * 4 + i % 4) * 4) = o[rb][i][r];
+                for (int r = 0; r < 4; ++r) *(lds_float*)(uintptr_t)(mine + (rb * 16 + c16) * (D * 4) + ((i / 4 * 16 + quarter * 4 + r) ^ c16) * 16 + i % 4 * 4) = o[rb][i][r];
             }
         }
-        __syncthreads();
-        const int rows = min(16, at.r1 - r0 - rb * 16);
-        for (int i = tid; i < rows * (D / 2); i += WAVES * kWave) {
-            const int r = i / (D / 2), d = i % (D / 2) * 2;
-            float top = sh_m[r], sum = 0.f, x = 0.f, y = 0.f;
+    }
+    __syncthreads();
+    const int rows = min(ROWS, at.r1 - r0);
+    for (int i = tid; i < rows * CHUNKS; i += WAVES * kWave) {
+        const int r = i / CHUNKS, chunk = i % CHUNKS;
+        float mw[WAVES], top = kLowest, sum = 0.f;
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_m[w * 16 + r]);
+        for (int w = 0; w < WAVES; ++w) mw[w] = sh_m[w * ROWS + r];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float c = exp2f((sh_m[w * 16 + r] - top) * of_diff);
-                const float2 v = *reinterpret_cast<const float2*>(tiles + w * 4 * T::BYTES + (r * OROW + d) * 4);
-                sum += sh_l[w * 16 + r] * c, x += v.x * c, y += v.y * c;
-            }
-            if (whole) {
-                const size_t row = chunk_row(e, at.s.t0, at.hk, r0 + rb * 16 + r);
-                chunk_write<DT, D>(e, row * D + d, sum == 0.f ? 0.f : x / sum, sum == 0.f ? 0.f : y / sum);
-                if (e.lse && d == 0) e.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, e.scale, logf(sum));
-            } else {
-                const size_t place = at.place + rb * 16 + r;
-                *reinterpret_cast<float2*>(e.partials + place * D + d) = make_float2(x, y);
-                if (d == 0) e.stats[place] = make_float2(top, sum);
-            }
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, mw[w]);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float c = __builtin_amdgcn_exp2f((mw[w] - top) * of_diff);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(tiles + w * 4 * T::BYTES + r * (D * 4) + (chunk ^ (r & 15)) * 16);
+            sum = fmaf(sh_l[w * ROWS + r], c, sum);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = fmaf(v[k], c, x[k]);
+        }
+        if (whole) {
+            const size_t row = chunk_row(e, at.s.t0, at.hk, r0 + r), to = row * D + chunk * 4;
+            const bool none = sum == 0.f;
+            chunk_write<DT, D>(e, to, none ? 0.f : x[0] / sum, none ? 0.f : x[1] / sum);
+            chunk_write<DT, D>(e, to + 2, none ? 0.f : x[2] / sum, none ? 0.f : x[3] / sum);
+            if (e.lse && chunk == 0) e.lse[row] = none ? -INFINITY : fmaf(top, e.scale, logf(sum));
+        } else {
+            *reinterpret_cast<f32x4*>(e.partials + (at.place + r) * D + chunk * 4) = x;
+            if (chunk == 0) e.stats[at.place + r] = make_float2(top, sum);
         }
     }
 }
