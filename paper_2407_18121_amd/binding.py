@@ -38,6 +38,7 @@ _fast = None  # the usual calls in native code (csrc/fastcall.cpp); None in an a
 _FAST = ("prefill_score", "prefill_score_varlen", "chunk_score", "select_anchors", "merge_compact", "remerge_compact",
          "decode_step", "decode_step_varlen", "decode_score_step", "evict_min")  # in the order of its table
 _FAST_PAGED = ("paged_store", "paged_decode_step", "paged_decode_score_step", "paged_evict_min")  # and of its second one
+_FAST_TOKENS = ("paged_plan", "paged_rotary_store", "paged_chunk_step")  # and of its third
 
 
 class EcError(RuntimeError):
@@ -131,6 +132,7 @@ def _load_fast(lib):
             _fastcall.bind(_raw_stream, _device,
                            tuple(ctypes.cast(getattr(lib, "ec_" + n), ctypes.c_void_p).value for n in _FAST))
             _fastcall.bind_paged(tuple(ctypes.cast(getattr(lib, "ec_" + n), ctypes.c_void_p).value for n in _FAST_PAGED))
+            _fastcall.bind_tokens(tuple(ctypes.cast(getattr(lib, "ec_" + n), ctypes.c_void_p).value for n in _FAST_TOKENS))
             return _fastcall
         why = f"it was built for torch {built_for}"
     warnings.warn(f"the native half of the binding is not used, calls take 4 to 10 us longer: {why}", RuntimeWarning, stacklevel=3)
@@ -701,6 +703,10 @@ def ec_paged_plan(len_b, new_b, page_table, held_b, free_pages, n_free, page: in
     """Pages for new_b[b] rows behind len_b[b] of every sequence, out of the stack free_pages[:n_free] (n_pages entries), and where every token goes: int32 [B] len_b,
     new_b, held_b, start_b, len_after_b, seen_b, seen_after_b, [B,max_pages] page_table, [1] n_free, [B+1] token_start, [T] pos; rows int64 [T].
     T is the size of rows or pos, or is given."""
+    if _fast is not None:
+        rc = _fast.paged_plan(len_b, new_b, page_table, held_b, free_pages, n_free, page, start_b, len_after_b, token_start, rows, pos, seen_b, seen_after_b, T)
+        if rc is not None:
+            return _status("ec_paged_plan", rc, check)
     B, max_pages = _paged_table(page_table, "ec_paged_plan")
     maps = rows if rows is not None else pos
     if maps is not None:
@@ -732,6 +738,10 @@ def ec_paged_rotary_store(q, k, v, pos, rows, freq, q_out, k_pages, v_pages, pos
                           check=True) -> int:
     """q [T,H,D], k,v [T,Hkv,D], tokens at any distance (views of one projection); pos int32 [T], rows int64 [T] as ec_paged_plan writes them; freq f32 [rot/2]
     -> q_out [T,H,D] and the rows of the pools (k_pages,v_pages [N,Hkv,page,D], pos_pages int32, mass_pages f32 [N,G,page] or None)."""
+    if _fast is not None:
+        rc = _fast.paged_rotary_store(q, k, v, pos, rows, freq, q_out, k_pages, v_pages, pos_pages, mass_pages, interleaved, mscale)
+        if rc is not None:
+            return _status("ec_paged_rotary_store", rc, check)
     if q.dim() != 3 or k.dim() != 3 or k_pages.dim() != 4:
         raise ValueError("ec_paged_rotary_store: q and k must be [T,heads,D] and k_pages [N,Hkv,page,D]")
     T, H, D = q.shape
@@ -754,6 +764,10 @@ def ec_paged_rotary_store(q, k, v, pos, rows, freq, q_out, k_pages, v_pages, pos
 def ec_paged_chunk_step(q, k_pages, v_pages, page_table, start_b, token_start, scale: float, out, ws, lse=None, check=True) -> int:
     """q,out [T,H,D], tokens of sequence b from token_start[b] on (int32 [B+1]); k_pages,v_pages [N,Hkv,page,D] hold their rows from slot start_b[b] on (int32 [B]);
     lse f32 [T,H] or None."""
+    if _fast is not None:
+        rc = _fast.paged_chunk_step(q, k_pages, v_pages, page_table, start_b, token_start, scale, out, ws, lse)
+        if rc is not None:
+            return _status("ec_paged_chunk_step", rc, check)
     B, max_pages = _paged_table(page_table, "ec_paged_chunk_step")
     if q.dim() != 3 or k_pages.dim() != 4:
         raise ValueError("ec_paged_chunk_step: q must be [T,H,D] and k_pages [N,Hkv,page,D]")

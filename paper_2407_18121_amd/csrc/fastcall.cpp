@@ -43,6 +43,14 @@ struct PagedFunctions {  // of the calls on paged caches
     int (*evict_min)(void*, void*, int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, const int32_t*, int, int, int, int, int, int, int, int,
                      int, int, int, void*, size_t, void*);
 } paged;
+struct TokenFunctions {  // of those on several new tokens at a time
+    int (*plan)(const int32_t*, const int32_t*, const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int, int, int, int, int, int32_t*, int32_t*,
+                int32_t*, int32_t*, int64_t*, int32_t*, void*);
+    int (*rotary_store)(const void*, const void*, const void*, int64_t, int64_t, int64_t, const int32_t*, const int64_t*, const float*, float, int, int, int,
+                        int, int, int, int, int, int, int, void*, void*, void*, int32_t*, float*, void*);
+    int (*chunk_step)(const void*, const void*, const void*, const int32_t*, const int32_t*, const int32_t*, int, int, int, int, int, int, int, int, float,
+                      int, void*, float*, void*, size_t, void*);
+} tokens;
 PyObject *raw_stream, *current_device;  // of torch: the current stream's handle, the current device's number
 
 struct Unusual {};  // thrown for whatever binding.py has to look at
@@ -463,6 +471,80 @@ PyObject* paged_evict_min(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+// ------------------------------------------------------------------ several new tokens at a time
+// len_b new_b page_table held_b free_pages n_free page start_b len_after_b token_start rows pos seen_b seen_after_b T
+PyObject* paged_plan(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<15>(args, n, [](PyObject* const* a) {
+        const Here here;
+        const at::Tensor &table = required(a[2], 2), *rows = tensor(a[10]), *pos = tensor(a[11]), *free = tensor(a[4]);
+        if (!free) throw Unusual{};
+        const int64_t B = table.size(0), max_pages = table.size(1), N = free->numel(), T = rows ? rows->numel() : pos ? pos->numel() : integer(a[14]);
+        return [=, len = here.counters(a[0], B), fresh = here.counters(a[1], B), tp = here.fits<int32_t>(&table, at::kInt, {B, max_pages}),
+                held = here.counters(a[3], B), fp = here.counters(a[4], N), n_free = here.counters(a[5], 1), page = integer(a[6]),
+                start = here.counters(a[7], B), after = here.counters(a[8], B), first = here.counters(a[9], B + 1),
+                rp = here.fits<int64_t>(rows, at::kLong, {T}, true), pp = here.counters(a[11], T, true), seen = here.counters(a[12], B, true),
+                seen_after = here.counters(a[13], B, true), iB = size(B), iT = size(T), iN = size(N), im = size(max_pages), s = here.stream] {
+            return tokens.plan(len, fresh, seen, tp, held, fp, n_free, iB, iT, page, iN, im, start, after, seen_after, first, rp, pp, s);
+        };
+    });
+}
+
+// A tensor [T,heads,D] whose tokens may lie apart.
+struct Tokens {
+    void* p;
+    int64_t step;
+    Tokens(const Here& here, PyObject* o, at::ScalarType type, int64_t T, int64_t heads, int64_t D)
+    {
+        const at::Tensor& t = required(o, 3);
+        if (t.scalar_type() != type || t.size(0) != T || t.size(1) != heads || t.size(2) != D || (D > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != D) ||
+            !t.is_cuda() || t.device().index() != here.device)
+            throw Unusual{};
+        p = t.data_ptr(), step = T > 1 ? t.stride(0) : heads * D;
+    }
+};
+
+// q k v pos rows freq q_out k_pages v_pages pos_pages mass_pages interleaved mscale
+PyObject* paged_rotary_store(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<13>(args, n, [](PyObject* const* a) {
+        const Here here;
+        const at::Tensor &q_ = required(a[0], 3), &k_ = required(a[7], 4), *freq = tensor(a[5]);
+        if (!freq || !PyBool_Check(a[11])) throw Unusual{};
+        PyObject* grouped = a[9] != Py_None ? a[9] : a[10];
+        const int64_t T = q_.size(0), H = q_.size(1), D = q_.size(2), N = k_.size(0), Hkv = k_.size(1), page = k_.size(2), half = freq->numel();
+        const int64_t G = groups(grouped != Py_None ? required(grouped, 3).size(1) : 1, Hkv);
+        const auto dt = k_.scalar_type();
+        return [=, q = Tokens(here, a[0], dt, T, H, D), k = Tokens(here, a[1], dt, T, Hkv, D), v = Tokens(here, a[2], dt, T, Hkv, D),
+                pos = here.counters(a[3], T), rows = here.fits<int64_t>(a[4], at::kLong, {T}), fp = here.fits<float>(freq, at::kFloat, {half}),
+                out = here.fits(a[6], dt, {T, H, D}), kp = here.fits(&k_, dt, {N, Hkv, page, D}), vp = here.fits(a[8], dt, {N, Hkv, page, D}),
+                pp = here.fits<int32_t>(a[9], at::kInt, {N, G, page}, true), mp = here.fits<float>(a[10], at::kFloat, {N, G, page}, true),
+                pairing = a[11] == Py_True ? 1 : 0, mscale = number(a[12]), code = type_code(k_), iT = size(T), iH = size(H), ik = size(Hkv), iG = size(G),
+                iD = size(D), ip = size(page), iN = size(N), rot = size(2 * half), s = here.stream] {
+            return tokens.rotary_store(q.p, k.p, v.p, q.step, k.step, v.step, pos, rows, fp, mscale, rot, pairing, iT, iH, ik, iG, iD, ip, iN, code, out, kp,
+                                       vp, pp, mp, s);
+        };
+    });
+}
+
+// q k_pages v_pages page_table start_b token_start scale out ws lse
+PyObject* paged_chunk_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return entry<10>(args, n, [](PyObject* const* a) {
+        const Here here;
+        const at::Tensor &q = required(a[0], 3), &k = required(a[1], 4), &table = required(a[3], 2);
+        const int64_t T = q.size(0), H = q.size(1), D = q.size(2), N = k.size(0), Hkv = k.size(1), page = k.size(2), B = table.size(0), max_pages = table.size(1);
+        const auto dt = k.scalar_type();
+        return [=, ws = here.workspace(a[8]), qp = here.fits(&q, dt, {T, H, D}), kp = here.fits(&k, dt, {N, Hkv, page, D}),
+                vp = here.fits(a[2], dt, {N, Hkv, page, D}), tp = here.fits<int32_t>(&table, at::kInt, {B, max_pages}), start = here.counters(a[4], B),
+                first = here.counters(a[5], B + 1), scale = number(a[6]), out = here.fits(a[7], dt, {T, H, D}),
+                lse = here.fits<float>(a[9], at::kFloat, {T, H}, true), code = type_code(k), iB = size(B), iT = size(T), iH = size(H), ik = size(Hkv),
+                iD = size(D), ip = size(page), iN = size(N), im = size(max_pages), s = here.stream] {
+            return tokens.chunk_step(qp, kp, vp, tp, start, first, iB, iT, iH, ik, iD, ip, iN, im, scale, code, out, lse, ws.p, ws.bytes, s);
+        };
+    });
+}
+
 template <typename F> bool take_addresses(PyObject* addresses, F& to)
 {
     constexpr Py_ssize_t kCount = sizeof(F) / sizeof(void*);
@@ -486,6 +568,14 @@ PyObject* bind_paged(PyObject*, PyObject* args)
     Py_RETURN_NONE;
 }
 
+// bind_tokens(addresses in the order of TokenFunctions), after bind
+PyObject* bind_tokens(PyObject*, PyObject* args)
+{
+    PyObject* addresses;
+    if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses) || !take_addresses(addresses, tokens)) return nullptr;
+    Py_RETURN_NONE;
+}
+
 // bind(raw_stream, current_device, addresses in the order of Functions)
 PyObject* bind(PyObject*, PyObject* args)
 {
@@ -501,8 +591,10 @@ PyObject* bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {EC_FAST(prefill_score),   EC_FAST(prefill_score_varlen), EC_FAST(chunk_score),       EC_FAST(select_anchors),
                          EC_FAST(merge_compact),   EC_FAST(remerge_compact),      EC_FAST(decode_step),       EC_FAST(decode_step_varlen),
                          EC_FAST(decode_score_step), EC_FAST(evict_min),          EC_FAST(paged_store),       EC_FAST(paged_decode_step),
-                         EC_FAST(paged_decode_score_step), EC_FAST(paged_evict_min), {"bind", bind, METH_VARARGS, nullptr},
-                         {"bind_paged", bind_paged, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         EC_FAST(paged_decode_score_step), EC_FAST(paged_evict_min), EC_FAST(paged_plan),
+                         EC_FAST(paged_rotary_store), EC_FAST(paged_chunk_step), {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_paged", bind_paged, METH_VARARGS, nullptr}, {"bind_tokens", bind_tokens, METH_VARARGS, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
