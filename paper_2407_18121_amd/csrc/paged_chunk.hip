@@ -16,8 +16,9 @@ namespace ec {
 // Waves of a workgroup: four, of which a compute unit holds two workgroups, or eight where a batch has no more tiles than the chip has compute units. A wave
 // alone on its SIMD issues half as much as two do.
 constexpr int kFewWaves = 4, kManyWaves = 8;
-template <int WAVES> constexpr int kChunkPlaces = 2 * kFewWaves * kComputeUnits / WAVES;  // workgroups that the chip holds at once
-constexpr int kChunkParts = 4 * kChunkPlaces<kFewWaves>;  // segments whose results the workspace holds, at most
+// Workgroups that the chip holds at once
+template <int DT, int D, int WAVES> constexpr int kChunkPlaces = WAVES == kFewWaves ? PagedTile<DT, D>::kResident * kComputeUnits : kComputeUnits;
+constexpr int kMostPlaces = 2 * kComputeUnits, kChunkParts = 4 * kMostPlaces;  // kChunkParts: segments whose results the workspace holds, at most
 constexpr int kChunkTiles = 128;                          // tiles from which on segments may take several rounds
 constexpr int kJoinWaves = 4, kJoinGroups = 8;            // waves of a joining workgroup, and workgroups that share a tile's rows
 
@@ -665,7 +666,7 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
     __shared__ int flags[WAVES];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     ChunkSeq s;
-    const auto share = chunk_share<DT, UNIT, kChunkPlaces<WAVES>>(first, s);
+    const auto share = chunk_share<DT, UNIT, kChunkPlaces<DT, D, WAVES>>(first, s);
     if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<DT, UNIT>(first, share, s);
     auto take = [&](const ChunkStep& a, const ChunkItem& at) __attribute__((always_inline)) {
         if (!at.s.live) {
@@ -757,7 +758,7 @@ static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 static int part_rows(int T, int H) { return (int)std::min<long long>(((long long)T * H + 15) / 16 * 16, 128); }
 // Tiles of all key/value heads that a call can have, and segments whose results its workspace holds: of any number of sequences and of key/value heads.
 static long long most_tiles(long long T, long long group, long long Hkv, long long B, int rows) { return (T * group + std::min(B, T) * (rows - 1)) / rows * Hkv; }
-static int most_parts(int T, int H) { return most_tiles(T, 1, H, T, 32) >= kChunkTiles ? kChunkParts : kChunkPlaces<kFewWaves>; }
+static int most_parts(int T, int H) { return most_tiles(T, 1, H, T, 32) >= kChunkTiles ? kChunkParts : kMostPlaces; }
 struct ChunkPlaces {  // where things lie in a workspace
     size_t records, stats, partials, end;
     ChunkPlaces(int T, int H, int D)
@@ -779,9 +780,9 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };
     if (DT == EC_BF16 && tiles <= kComputeUnits) {
         if constexpr (DT == EC_BF16)
-            hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kManyWaves>), groups(kChunkPlaces<kManyWaves>), dim3(kManyWaves * kWave), 0, stream, a);
+            hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kManyWaves>), groups(kChunkPlaces<DT, D, kManyWaves>), dim3(kManyWaves * kWave), 0, stream, a);
     } else {
-        hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kFewWaves>), groups(kChunkPlaces<kFewWaves>), dim3(kFewWaves * kWave), 0, stream, a);
+        hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kFewWaves>), groups(kChunkPlaces<DT, D, kFewWaves>), dim3(kFewWaves * kWave), 0, stream, a);
     }
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     if (!a.cut) return EC_OK;
