@@ -37,7 +37,7 @@ struct ChunkStep {
     int B, T, H, Hkv, group;
     uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
     int rounds;
-    bool cut;         // whether tiles may be cut
+    bool cut;         // whether tiles may be cut and the second launch follows
     float scale, scale_log2e;
     int* cut_tiles;   // tiles that are cut, which paged_chunk_join_kernel goes over
     CutTile* records;
@@ -137,6 +137,10 @@ template <int UNIT> struct ChunkShare {
 // s: of this lane's sequence afterwards, if there are no more than lanes
 template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
+    if (!a.cut) {  // a share that no tile exceeds
+        if (a.B <= kWave) s.read<DT, UNIT>(a, threadIdx.x % kWave);
+        return {1 << 22, 1};
+    }
     long long all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
@@ -775,7 +779,7 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
     constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
-    a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (fewer units make no two segments)
+    a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (the second launch takes longer than shorter sequences)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
     auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };
     if (DT == EC_BF16 && tiles <= kComputeUnits) {

@@ -66,6 +66,15 @@ def test_lengths(dtype, D, L, n):
     run(make(rng, dtype, 2, D, 16, [L + n]), dtype, 4, [L], [n], pad=2)
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("rows", [257, 281, 384, 449, 500, 512, 513, 530])
+def test_lengths_where_cutting_begins(dtype, D, rows):
+    """Whether a table is long enough for tiles to be cut is the host's to say, how they are cut the device's."""
+    rng = np.random.default_rng(rows)
+    for news in ([1], [9], [60], [150], [2, 60, 1]):
+        run(make(rng, dtype, 3, D, 16, [rows] * len(news), spare=0), dtype, 6, [rows - n for n in news], news)
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
 @pytest.mark.parametrize("H,Hkv", [(1, 1), (3, 3), (3, 1), (10, 2), (14, 2), (16, 1), (33, 1), (32, 4), (64, 1)])
 def test_query_groups(dtype, D, H, Hkv):
