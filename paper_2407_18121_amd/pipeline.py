@@ -7,8 +7,13 @@ extend():   ec_chunk_score -> ec_select_anchors -> ec_remerge_compact      (a la
 
 PagedBatch holds the compressed caches of sequences that come and go in pages of one pool per layer:
 admit() / store() -> begin() -> decode() or decode_scored() in every layer -> end(), shrink() when memory runs short, release()
+
+PagedTokens does so for steps of any number of new tokens a sequence, with pages given out on the device and positions by rotation:
+admit() -> begin() -> attend() in every layer, release()
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
@@ -263,3 +268,98 @@ class PagedBatch:
                 self._hold(b, keep)
         self._upload_table()
         self._upload()
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, kind: str = "linear", trained: int = 4096, low: float = 1.0, high: float = 32.0,
+                       device="cuda"):
+    """(freq f32 [rot/2], mscale) for ec_paged_rotary_store: base^(-2i/rot) radians a position, stretched for contexts `factor` times as long as the `trained` one:
+      linear  every frequency divided by the factor
+      base    the base raised, so that the slowest pair is divided by the factor and the fastest stays: base * factor^(rot/(rot-2))
+      parts   pairs that turn more than `high` times over the trained context stay, those that turn less than `low` times are divided by the factor, those
+              between in proportion; mscale = 0.1 ln(factor) + 1"""
+    if rot < 2 or rot % 2 or factor < 1.0 or kind not in ("linear", "base", "parts"):
+        raise ValueError(f"rot {rot} must be even, the factor {factor} at least 1, the kind {kind!r} one of linear, base, parts")
+    if kind == "base" and factor > 1.0:
+        if rot == 2:
+            raise ValueError("a raised base needs more than one pair")
+        base = base * factor ** (rot / (rot - 2))
+    freq = torch.tensor(base, dtype=torch.float64) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    mscale = 1.0
+    if kind == "linear":
+        freq = freq / factor
+    elif kind == "parts":
+        kept = ((freq * trained / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        freq = freq * kept + freq / factor * (1.0 - kept)
+        mscale = 0.1 * math.log(factor) + 1.0
+    return freq.float().to(device), mscale
+
+
+class PagedTokens:
+    """The caches of up to `places` sequences in pages for steps of any number of new tokens a sequence, up to `tokens` in all: chunks of prompts, drafted tokens and
+    single ones side by side. Lengths, the page table and the free pages live on the device, and begin() and attend() send nothing from the host and read nothing
+    back, so that a step can be captured and replayed with other numbers of tokens.
+
+        batch.admit([0, 1])                                  # two new sequences
+        batch.new_b.copy_(new)                               # int32 [places]: tokens of each sequence in this step
+        batch.begin()                                        # pages, rows and positions for them
+        for i in range(n_layers):
+            batch.attend(i, q[i], k[i], v[i], scale, out[i]) # [tokens,H or Hkv,D] packed, sequence after sequence (batch.token_start)
+
+    A sequence that the free pages do not hold keeps what it has: its tokens get zeros, len_b and seen_b do not grow, start_b is -1.
+    Compressed prompts come in as rows: admit(places, rows, seen), begin() without tokens for them, store() in every layer.
+    New rows' masses are 0 (what adds to masses is ec_paged_decode_score_step)."""
+
+    def __init__(self, layers, places, tokens, H, Hkv, D, page, n_pages, max_pages, dtype: torch.dtype, freq, mscale=1.0, interleaved=False, G=1, device="cuda"):
+        self.page, self.mscale, self.interleaved = page, mscale, interleaved
+        self.k_pages, self.v_pages = (torch.zeros((layers, n_pages, Hkv, page, D), dtype=dtype, device=device) for _ in range(2))
+        self.pos_pages = torch.zeros((layers, n_pages, G, page), dtype=torch.int32, device=device)
+        self.mass_pages = torch.zeros((layers, n_pages, G, page), dtype=torch.float32, device=device)
+        ints = lambda *s, fill=0: torch.full(s, fill, dtype=torch.int32, device=device)  # noqa: E731
+        self.table, self.held = ints(places, max_pages, fill=-1), ints(places)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        self.n_free = ints(1, fill=n_pages)
+        self.len_b, self.seen_b, self.new_b = ints(places, fill=-1), ints(places), ints(places)  # rows (-1: no sequence), tokens seen, tokens of the next step
+        self.start_b, self.token_start = ints(places, fill=-1), ints(places + 1)
+        self.rows, self.pos = torch.full((tokens,), -1, dtype=torch.int64, device=device), ints(tokens)
+        self.freq = freq
+        self.turned = torch.zeros((tokens, H, D), dtype=dtype, device=device)
+        self.ws = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, places, H, tokens, D, ec.dtype_code(self.k_pages), device)
+
+    def _set(self, places, rows, seen):
+        if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("PagedTokens: sequences come and go outside a capture (a step's graph holds begin() and attend())")
+        places = list(places)
+        if len(set(places)) != len(places) or any(not 0 <= b < self.table.shape[0] for b in places):
+            raise ValueError(f"{places} are not different places of 0 .. {self.table.shape[0] - 1}")
+        at = torch.tensor(places, dtype=torch.int64).to(self.table.device)
+        for x, values in ((self.len_b, rows), (self.seen_b, seen)):
+            x.index_copy_(0, at, torch.tensor(values, dtype=torch.int32).to(x.device))
+
+    def admit(self, places, rows=None, seen=None):
+        """Sequences that start with `rows` rows of prompts of `seen` tokens, none by default; a place's earlier sequence is gone. Their pages come with begin()."""
+        places = list(places)
+        rows, seen = (list(x) if x is not None else [0] * len(places) for x in (rows, seen))
+        if not len(places) == len(rows) == len(seen) or any(n < 0 for n in rows):
+            raise ValueError(f"places {places}, rows {rows} and seen {seen} do not belong together")
+        self._set(places, rows, seen)
+
+    def release(self, places):
+        """Sequences that are over; their pages are free with the next begin()."""
+        places = list(places)
+        self._set(places, [-1] * len(places), [0] * len(places))
+
+    def begin(self):
+        """Pages, rows and positions for new_b more tokens of every sequence."""
+        ec.ec_paged_plan(self.len_b, self.new_b, self.table, self.held, self.free_pages, self.n_free, self.page, self.start_b, self.len_b, self.token_start,
+                         self.rows, self.pos, seen_b=self.seen_b, seen_after_b=self.seen_b)
+
+    def store(self, layer, places, k, v, pos, mass, n_rows_b=None):
+        """Rows 0.. of k, v [len(places),Hkv,n,D], pos and mass [len(places),G,n] as the first rows of the sequences (n_rows_b int32 of each, all by default)."""
+        table = self.table.index_select(0, torch.tensor(list(places), dtype=torch.int64).to(self.table.device))
+        ec.ec_paged_store(k, v, pos, mass, table, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], None, n_rows_b)
+
+    def attend(self, layer, q, k, v, scale, out, lse=None):
+        """One layer of the step that begin() has planned: q, out [tokens,H,D], k, v [tokens,Hkv,D] (q, k and v may be parts of one projection's output)."""
+        ec.ec_paged_rotary_store(q, k, v, self.pos, self.rows, self.freq, self.turned, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer],
+                                 self.mass_pages[layer], interleaved=self.interleaved, mscale=self.mscale)
+        ec.ec_paged_chunk_step(self.turned, self.k_pages[layer], self.v_pages[layer], self.table, self.start_b, self.token_start, scale, out, self.ws, lse=lse)

@@ -3,10 +3,12 @@ import ctypes
 import os
 import re
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2407_18121_amd import binding as ec
+from paper_2407_18121_amd.pipeline import rotary_frequencies
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 at = lambda n: ctypes.c_void_p(n << 32)  # noqa: E731  far apart, never dereferenced: validation fails first
@@ -139,3 +141,29 @@ def test_python_refusals_of_layout():
                 ec.ec_paged_rotary_store(**dict(good, **{p: bad}))
     with pytest.raises(ValueError, match="T is needed"):
         ec.ec_paged_plan(**dict(_calls()["ec_paged_plan"], rows=None, pos=None))
+
+
+@pytest.mark.parametrize("rot", [2, 22, 64, 128])
+def test_frequencies(rot):
+    """The three ways to stretch a context, pair by pair; an fp32 number is half a step off."""
+    i = np.arange(rot // 2)
+    plain = 10000.0 ** (-2.0 * i / rot)
+    near = lambda got, want: np.all(np.abs(got[0].numpy() - want) <= np.abs(want) * 2.0 ** -24 * 1.0001)  # noqa: E731
+    f = lambda *a, **k: rotary_frequencies(rot, *a, **k, device="cpu")  # noqa: E731
+    assert near(f(), plain) and f()[1] == 1.0 and f()[0].dtype == torch.float32
+    assert near(f(500000.0), 500000.0 ** (-2.0 * i / rot))
+    assert near(f(factor=8.0), plain / 8)
+    if rot > 2:
+        raised = f(factor=8.0, kind="base")
+        assert near(raised, (10000.0 * 8.0 ** (rot / (rot - 2))) ** (-2.0 * i / rot)) and raised[1] == 1.0
+        assert raised[0][0] == 1.0 and abs(float(raised[0][-1]) * 8 / plain[-1] - 1) < 1e-6
+    got, mscale = f(factor=8.0, kind="parts", trained=2048)
+    turns = plain * 2048 / (2 * np.pi)
+    want = [w if t > 32 else w / 8 if t < 1 else w * (t - 1) / 31 + w / 8 * (32 - t) / 31 for w, t in zip(plain, turns)]
+    assert np.all(np.abs(got.numpy() - want) <= np.abs(want) * 2.0 ** -23) and abs(mscale - (0.1 * np.log(8) + 1)) < 1e-15
+
+
+def test_frequency_refusals():
+    for bad in (dict(rot=3), dict(rot=0), dict(rot=64, factor=0.5), dict(rot=64, kind="other"), dict(rot=2, kind="base", factor=2.0)):
+        with pytest.raises(ValueError):
+            rotary_frequencies(**bad, device="cpu")
