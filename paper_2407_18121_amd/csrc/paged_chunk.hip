@@ -36,7 +36,9 @@ struct ChunkStep {
     Pages pages;
     int B, T, H, Hkv, group;
     uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
+    uint32_t heads_mul, heads_shift;  // x / Hkv, as above
     int rounds;
+    bool small;       // the units of all tiles have 29 bits
     bool cut;         // whether tiles may be cut and the second launch follows
     float scale, scale_log2e;
     int* cut_tiles;   // tiles that are cut, which paged_chunk_join_kernel goes over
@@ -62,6 +64,10 @@ __device__ __forceinline__ ChunkStep chunk_args()
     for (int i = 0; i < (int)(sizeof(ChunkStep) / 4); ++i) words.of[i] = from[i];
     return __builtin_bit_cast(ChunkStep, words);
 }
+
+// x / by, not more and for x < 2^20 not less: a smaller reciprocal, and half a step further from where it changes. In fewer instructions than divided().
+__device__ __forceinline__ float low_rcp(int by) { return __builtin_amdgcn_rcpf((float)by) * (1.f - 0x1p-21f); }
+__device__ __forceinline__ int about(int x, float low) { return (int)(((float)x + 0.5f) * low); }
 
 __device__ __forceinline__ int token_of(const ChunkStep& a, int row) { return (int)(__umulhi((uint32_t)row << 2, a.group_mul) >> a.group_shift); }
 
@@ -98,14 +104,12 @@ __device__ __forceinline__ long long wave_sum(long long x)
 // How a sequence's tiles are cut: from the last tile on `whole` of them not at all, the others into `segments` of `each` units (those that see less into fewer).
 struct ChunkCut {
     int whole, segments, each;
-    __device__ __forceinline__ int items(const ChunkSeq& s) const { return whole + (s.tiles - whole) * segments; }
-    __device__ __forceinline__ int parts(const ChunkSeq& s) const { return (s.tiles - whole) * segments; }
 };
 // What all of them are cut by: the units that are a place's share of the whole batch, and the rounds that segments may take.
 template <int UNIT> struct ChunkShare {
     int units, rounds;
-    // Units of a segment, at least: as many as its results, written and read again, take the time of.
-    static __device__ __forceinline__ int least(const ChunkSeq& s) { return max(min(s.rows, s.tile_rows) * 8, 256) / UNIT; }
+    // Units of a segment, at least: as many as its results, written and read again, take the time of, or half as many where workgroups would have nothing to do
+    __device__ __forceinline__ int least(const ChunkSeq& s) const { return max(min(s.rows, s.tile_rows) * (rounds > 1 ? 8 : 4), 256) / UNIT; }
     // A tile of U units, against a share of A:
     //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
     //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
@@ -113,27 +117,38 @@ template <int UNIT> struct ChunkShare {
     // These are r tiles U / A segments of a sequence, or 2 tiles U / A: within what the workspace holds, as chunk_share sees to it.
     __device__ __forceinline__ ChunkCut of(const ChunkSeq& s) const
     {
-        const int U = s.units, A = max(units, least(s));
-        auto cut = [&](int whole, int n) { return ChunkCut{whole, n, divided(U + n - 1, n)}; };
+        const int U = s.units, floor = least(s), A = max(units, floor);
+        const float low = low_rcp(A);
+        int n = 1, whole = 0;
         if (U > A) {
-            int n = divided(U, A), time = divided(U + n - 1, n);
+            n = about(U, low);
             if (rounds > 1 && U < 4 * A) {
-                for (int r = 2; r <= rounds; ++r) {
-                    const int m = divided(r * U, A), t = r * divided(U + m - 1, m) + (r - 1) * least(s);
-                    if (t < time) time = t, n = m;
+                int time = about(U + n - 1, low_rcp(n));
+#pragma unroll
+                for (int r = 2; r <= 4; ++r) {
+                    const int m = about(r * U, low), t = r * about(U + m - 1, low_rcp(m)) + (r - 1) * floor;
+                    if (r <= rounds && t < time) time = t, n = m;
                 }
             }
-            if (n > 1) return cut(0, n);
         } else if (rounds > 1 && U > 0 && A < 4 * U) {
             const int k = divided(A, U), rest = A - k * U;
-            if (rest >= least(s) && rest * 8 >= A && (long long)s.tiles * rest >= A && (long long)s.tiles * k * U < 1 << 24) {
-                const int n = divided(U, rest);
-                if (n > 1) return cut(divided(s.tiles * k * U, A), n);
+            if (rest >= floor && rest * 8 >= A && (long long)s.tiles * rest >= A && (long long)s.tiles * k * U < 1 << 24) {
+                n = divided(U, rest);
+                whole = divided(s.tiles * k * U, A);
             }
         }
-        return {s.tiles, 1, U};
+        if (n <= 1) return {s.tiles, 1, U};
+        return {whole, n, divided(U + n - 1, n)};
     }
 };
+template <int UNIT, int PLACES, class N> __device__ __forceinline__ ChunkShare<UNIT> chunk_share_of(const ChunkStep& a, N all, N most)
+{
+    // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
+    const N share = a.rounds > 1 ? (all + (2 * PLACES - 1)) / (2 * PLACES) : (most + (PLACES - 1)) / PLACES;
+    const int units = (int)min(max(share, (N)1), (N)(1 << 22));
+    const N held = (N)4 * PLACES * units;
+    return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
+}
 // s: of this lane's sequence afterwards, if there are no more than lanes
 template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
@@ -141,18 +156,22 @@ template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UN
         if (a.B <= kWave) s.read<DT, UNIT>(a, threadIdx.x % kWave);
         return {1 << 22, 1};
     }
-    long long all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
+    if (a.small) {
+        uint32_t all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
+            const int units = wave_scan(s.tiles * s.units), both = wave_scan(s.tiles * (s.units + s.first_units));
+            most += last_lane(units), all += last_lane(both);
+        }
+        return chunk_share_of<UNIT, PLACES>(a, all * a.Hkv, most * a.Hkv);
+    }
+    unsigned long long all = 0, most = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
-        if (a.rounds > 1) all += wave_sum((long long)s.tiles * (s.units + s.first_units));
+        all += wave_sum((long long)s.tiles * (s.units + s.first_units));
         most += wave_sum((long long)s.tiles * s.units);
     }
-    all *= a.Hkv, most *= a.Hkv;
-    // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
-    const long long share = a.rounds > 1 ? (all + 2 * PLACES - 1) / (2 * PLACES) : (most + PLACES - 1) / PLACES;
-    const int units = (int)min(max(share, 1LL), 1LL << 22);
-    const long long held = 4LL * PLACES * units;
-    return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
+    return chunk_share_of<UNIT, PLACES>(a, all * a.Hkv, most * a.Hkv);
 }
 
 // Units that a tile's last row sees.
@@ -175,15 +194,15 @@ struct ChunkItem {
 // which sees most, then segments. s: as chunk_share leaves it.
 template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
 {
-    const int lane = lane_anew(), j = scalar(id < 1 << 24 ? divided(id, a.Hkv) : id / a.Hkv), hk = id - j * a.Hkv;
-    int before = 0, parts_before = 0, cut_before = 0;
+    const int lane = lane_anew(), j = (int)(__umulhi((uint32_t)id << 2, a.heads_mul) >> a.heads_shift), hk = id - j * a.Hkv;
+    int before = 0, parts_before = 0;  // parts: and cut tiles in the high half, both at most kChunkParts
     ChunkItem it;
     it.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         if (a.B > kWave) s.read<DT, UNIT>(a, b0 + lane);
         const ChunkCut cut = share.of(s);
-        const int items = cut.items(s), parts = cut.parts(s), cut_tiles = cut.segments > 1 ? s.tiles - cut.whole : 0;
-        const int upto = wave_scan(items), parts_upto = wave_scan(parts), cut_upto = wave_scan(cut_tiles);
+        const int cut_tiles = s.tiles - cut.whole, items = s.tiles + cut_tiles * (cut.segments - 1), parts = cut_tiles * cut.segments + (cut_tiles << 16);
+        const int upto = wave_scan(items), parts_upto = wave_scan(parts);
         const unsigned long long beyond = __ballot(j < before + upto);
         if (beyond) {
             const int at = __ffsll(beyond) - 1;
@@ -203,14 +222,15 @@ template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(cons
             it.r0 = tile * it.s.tile_rows, it.r1 = min(it.r0 + it.s.tile_rows, it.s.rows);
             it.seen = scalar(chunk_units<UNIT>(a, it.s, tile));
             it.hk = hk;
-            it.place = ((size_t)(parts_before + of(parts_upto) - of(parts) + max(part, 0)) * a.Hkv + hk) * a.part_rows;
+            const int parts_of = parts_before + of(parts_upto) - of(parts);
+            it.place = ((size_t)((parts_of & 0xffff) + max(part, 0)) * a.Hkv + hk) * a.part_rows;
             it.b = b0 + at;
             if (part >= 0 && it.segment == 0 && wave == 0 && lane == 0)
-                a.records[(cut_before + of(cut_upto) - of(cut_tiles) + nth) * a.Hkv + hk] = {(int)it.place, tiles * a.Hkv * a.part_rows,
+                a.records[((parts_of >> 16) + nth) * a.Hkv + hk] = {(int)it.place, tiles * a.Hkv * a.part_rows,
                                                                                             scalar(divided(it.seen + it.each - 1, it.each)), it.r0, it.r1, it.s.t0, hk, 0};
             return it;
         }
-        before += last_lane(upto), parts_before += last_lane(parts_upto), cut_before += last_lane(cut_upto);
+        before += last_lane(upto), parts_before += last_lane(parts_upto);
     }
     return it;
 }
@@ -219,8 +239,7 @@ template <int DT, int UNIT> __device__ __forceinline__ void count_cut_tiles(cons
     int n = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         if (a.B > kWave) s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
-        const ChunkCut cut = share.of(s);
-        n += last_lane(wave_scan(cut.segments > 1 ? s.tiles - cut.whole : 0));
+        n += last_lane(wave_scan(s.tiles - share.of(s).whole));
     }
     if (threadIdx.x == 0) *a.cut_tiles = n * a.Hkv;
 }
@@ -668,11 +687,11 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
     __shared__ __align__(256) unsigned char tiles[WAVES * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
     __shared__ float sh_m[WAVES * 32], sh_l[WAVES * 32];
     __shared__ int flags[WAVES];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     ChunkSeq s;
     const auto share = chunk_share<DT, UNIT, kChunkPlaces<DT, D, WAVES>>(first, s);
     if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<DT, UNIT>(first, share, s);
-    auto take = [&](const ChunkStep& a, const ChunkItem& at) __attribute__((always_inline)) {
+    auto take = [&](const ChunkStep& a, const ChunkItem& at, int wave) __attribute__((always_inline)) {
         if (!at.s.live) {
             chunk_nothing<DT, D, WAVES>(a, at, wave);
             return;
@@ -695,10 +714,12 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
     };
     for (int id = blockIdx.x;; id += gridDim.x) {
         const ChunkStep a = chunk_args();
+        int wave = first_wave;  // (what follows from it is not kept from item to item)
+        asm volatile("" : "+s"(wave));
         if (id != blockIdx.x && a.B <= kWave) s.read<DT, UNIT>(a, lane_anew());
         const ChunkItem at = chunk_item<DT, UNIT>(a, share, s, id, wave);
         if (at.b < 0) return;
-        take(a, at);
+        take(a, at, wave);
         __syncthreads();  // the tiles have been read
     }
 }
@@ -779,6 +800,7 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
     constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
+    a.small = tiles * 2 * ((a.pages.slots() + UNIT - 1) / UNIT) < 1 << 29;
     a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (the second launch takes longer than shorter sequences)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
     auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };
@@ -799,12 +821,16 @@ int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages
                          int B, int T, int H, int Hkv, int D, float scale, int dt, void* out, float* lse, void* ws, hipStream_t stream)
 {
     const uint32_t group = H / Hkv;
-    uint32_t shift = 0;
-    while (1u << shift < group) ++shift;
-    const uint32_t mul = (uint32_t)(((1ULL << (30 + shift)) + group - 1) / group);
+    auto shift_of = [](uint32_t by) {
+        uint32_t shift = 0;
+        while (1u << shift < by) ++shift;
+        return shift;
+    };
+    auto mul_of = [&](uint32_t by) { return (uint32_t)(((1ULL << (30 + shift_of(by))) + by - 1) / by); };
     const ChunkPlaces at(T, H, D);
     char* const w = static_cast<char*>(ws);
-    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul, shift, 1, false, scale, scale * kLog2e,
+    const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul_of(group), shift_of(group),
+                      mul_of(Hkv), shift_of(Hkv), 1, false, false, scale, scale * kLog2e,
                       reinterpret_cast<int*>(w), reinterpret_cast<CutTile*>(w + at.records), part_rows(T, H), reinterpret_cast<float*>(w + at.partials),
                       reinterpret_cast<float2*>(w + at.stats)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);
