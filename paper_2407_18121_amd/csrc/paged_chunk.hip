@@ -724,57 +724,109 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
     }
 }
 
-// The segments' results of every row of tiles that are cut, a wave a row. Bound by latency: the tile, the statistics, a lane a segment, then the sums, eight
-// segments' in flight.
-template <int DT, int D> __global__ __launch_bounds__(kJoinWaves* kWave) void paged_chunk_join_kernel(ChunkStep a)
+// Results of N segments at most, D / 4 lanes a row, all of them on their way at once.
+template <int DT, int D, int N> __device__ __forceinline__ void join_few(const ChunkStep& a, const CutTile& tile, int row, int step)
+{
+    constexpr int LANES = D / 4, ROWS = kWave / LANES;
+    const int lane = threadIdx.x % kWave, chunk = lane % LANES;
+    for (int r = tile.r0 + row * ROWS + lane / LANES; r < tile.r1; r += step * ROWS) {
+        const int first = tile.place + (r - tile.r0);
+        float2 x[N];
+        f32x4 v[N], o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < N; ++g) {
+            const size_t at = first + min(g, tile.count - 1) * tile.between;
+            x[g] = a.stats[at], v[g] = *reinterpret_cast<const f32x4*>(a.partials + at * D + chunk * 4);
+        }
+        float top = kLowest, sum = 0.f;
+#pragma unroll
+        for (int g = 0; g < N; ++g)
+            if (!(x[g].y == 0.f)) top = fmaxf(top, x[g].x);  // (NaN counts)
+#pragma unroll
+        for (int g = 0; g < N; ++g) {
+            const float weight = g >= tile.count || x[g].y == 0.f ? 0.f : exp2f((x[g].x - top) * a.scale_log2e);
+            if (g < tile.count && !(x[g].y == 0.f)) {  // a segment of which the row sees nothing has sums of 0
+                sum = fmaf(x[g].y, weight, sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(v[g][e], weight, o[e]);
+            }
+        }
+        const size_t at = chunk_row(a, tile.t0, tile.hk, r);
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = sum == 0.f ? 0.f : o[e] / sum;
+        if constexpr (DT == EC_BF16) {
+            const uint32_t w0 = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16, w1 = (uint32_t)f32_to_bf16(y[2]) | (uint32_t)f32_to_bf16(y[3]) << 16;
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * D + chunk * 4) = make_uint2(w0, w1);
+        } else {
+            *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at * D + chunk * 4) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+        if (a.lse && chunk == 0) a.lse[at] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+    }
+}
+
+// Results of any number of segments, a wave a row: a lane a segment for the statistics, then the sums, eight segments' in flight.
+template <int DT, int D> __device__ __forceinline__ void join_many(const ChunkStep& a, const CutTile& tile, int row, int step)
 {
     constexpr int E = D / kWave, AHEAD = 8;
     typedef __attribute__((ext_vector_type(E))) float of_row;
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int all = *a.cut_tiles * kJoinGroups;
-    for (int i = blockIdx.x; i < all; i += gridDim.x) {
-        const CutTile tile = a.records[i / kJoinGroups];
-        if (tile.count == 1) continue;  // written already
-        for (int r = tile.r0 + i % kJoinGroups * kJoinWaves + wave; r < tile.r1; r += kJoinGroups * kJoinWaves) {
-            const int first = tile.place + (r - tile.r0);
-            float top = kLowest;
-            for (int g = lane; g < tile.count; g += kWave) {
-                const float2 x = a.stats[first + g * tile.between];
-                if (!(x.y == 0.f)) top = fmaxf(top, x.x);  // (NaN counts)
-            }
-            top = wave_max(top);
-            float sum = 0.f;
-            of_row o = {};
-            for (int g0 = 0; g0 < tile.count; g0 += kWave) {
-                float2 x = make_float2(0.f, 0.f);
-                if (g0 + lane < tile.count) x = a.stats[first + (g0 + lane) * tile.between];
-                const float weight = x.y == 0.f ? 0.f : exp2f((x.x - top) * a.scale_log2e);
-                const float share = x.y == 0.f ? 0.f : x.y * weight;
-                for (int g = g0; g < min(g0 + kWave, tile.count); g += AHEAD) {
-                    of_row v[AHEAD];
+    const int lane = threadIdx.x % kWave;
+    for (int r = tile.r0 + row; r < tile.r1; r += step) {
+        const int first = tile.place + (r - tile.r0);
+        float top = kLowest;
+        for (int g = lane; g < tile.count; g += kWave) {
+            const float2 x = a.stats[first + g * tile.between];
+            if (!(x.y == 0.f)) top = fmaxf(top, x.x);  // (NaN counts)
+        }
+        top = wave_max(top);
+        float sum = 0.f;
+        of_row o = {};
+        for (int g0 = 0; g0 < tile.count; g0 += kWave) {
+            float2 x = make_float2(0.f, 0.f);
+            if (g0 + lane < tile.count) x = a.stats[first + (g0 + lane) * tile.between];
+            const float weight = x.y == 0.f ? 0.f : exp2f((x.x - top) * a.scale_log2e);
+            const float share = x.y == 0.f ? 0.f : x.y * weight;
+            for (int g = g0; g < min(g0 + kWave, tile.count); g += AHEAD) {
+                of_row v[AHEAD];
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u)
-                        v[u] = *reinterpret_cast<const of_row*>(a.partials + (size_t)(first + min(g + u, tile.count - 1) * tile.between) * D + lane * E);
+                for (int u = 0; u < AHEAD; ++u)
+                    v[u] = *reinterpret_cast<const of_row*>(a.partials + (size_t)(first + min(g + u, tile.count - 1) * tile.between) * D + lane * E);
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) {
-                        if (g + u >= tile.count) continue;
-                        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), g + u - g0));
-                        sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), g + u - g0));
-                        // a segment of which the row sees nothing has sums of 0
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (g + u >= tile.count) continue;
+                    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), g + u - g0));
+                    sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), g + u - g0));
+                    // a segment of which the row sees nothing has sums of 0
 #pragma unroll
-                        for (int e = 0; e < E; ++e) o[e] = fmaf(v[u][e], w, o[e]);
-                    }
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(v[u][e], w, o[e]);
                 }
             }
-            const size_t row = chunk_row(a, tile.t0, tile.hk, r);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = sum == 0.f ? 0.f : o[e] / sum;
-                if constexpr (DT == EC_BF16) static_cast<uint16_t*>(a.out)[row * D + lane * E + e] = f32_to_bf16(x);
-                else static_cast<float*>(a.out)[row * D + lane * E + e] = x;
-            }
-            if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
         }
+        const size_t at = chunk_row(a, tile.t0, tile.hk, r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = sum == 0.f ? 0.f : o[e] / sum;
+            if constexpr (DT == EC_BF16) static_cast<uint16_t*>(a.out)[at * D + lane * E + e] = f32_to_bf16(x);
+            else static_cast<float*>(a.out)[at * D + lane * E + e] = x;
+        }
+        if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+    }
+}
+
+// The segments' results of every row of tiles that are cut. Bound by latency: the tile, the statistics and the sums.
+template <int DT, int D> __global__ __launch_bounds__(kJoinWaves* kWave) void paged_chunk_join_kernel(ChunkStep a)
+{
+    constexpr int step = kJoinGroups * kJoinWaves;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    int i = blockIdx.x;
+    CutTile tile = a.records[i / kJoinGroups];  // (of nothing where there are fewer tiles)
+    for (const int all = *a.cut_tiles * kJoinGroups; i < all;) {
+        const int row = i % kJoinGroups * kJoinWaves + wave;
+        if (tile.count > 8) join_many<DT, D>(a, tile, row, step);
+        else if (tile.count > 4) join_few<DT, D, 8>(a, tile, row, step);
+        else if (tile.count > 1) join_few<DT, D, 4>(a, tile, row, step);  // (one: written already)
+        i += gridDim.x;
+        if (i < all) tile = a.records[i / kJoinGroups];
     }
 }
 

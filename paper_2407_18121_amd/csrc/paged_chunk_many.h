@@ -407,18 +407,27 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
     const float sum = l + __shfl_xor(l, 32, kWave);
     const int row = rw + ec;
     if (!whole) {
-        const size_t place = at.place + wave * 32 + ec;
-        if (row < at.s.rows) {
-            if (eh == 0) e.stats[place] = make_float2(m, sum);
+        // The accumulators hold 16-byte pieces of 32 rows: turned through this wave's quarter of the tiles, which nobody reads any more, so that a store
+        // instruction writes a stretch of 1 KB (two segments each of 128 tiles of 128 rows 38.5 -> 30.2 us with the join).
+        constexpr int CHUNKS = D / 4, RPS = kWave / CHUNKS;  // 16-byte chunks of a row, rows per store instruction
+        static_assert(32 * D * 4 <= TILE);
+        const uint32_t stage = base + wave * TILE;
+        const size_t place = at.place + wave * 32;
+        if (eh == 0 && row < at.s.rows) e.stats[place + ec] = make_float2(m, sum);
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    f32x4 y;
+            for (int g = 0; g < 4; ++g) {
+                f32x4 y;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) y[t] = o[db][g * 4 + t];
-                    *reinterpret_cast<f32x4*>(e.partials + place * D + db * 32 + g * 8 + eh * 4) = y;
-                }
+                for (int t = 0; t < 4; ++t) y[t] = o[db][g * 4 + t];
+                *(lds_f32x4*)(uintptr_t)(stage + ec * (D * 4) + ((db * 8 + g * 2 + eh) ^ (ec & 7)) * 16) = y;
+            }
+#pragma unroll
+        for (int j = 0; j < 32 / RPS; ++j) {
+            const int r = j * RPS + el / CHUNKS;
+            const f32x4 y = *(lds_f32x4*)(uintptr_t)(stage + r * (D * 4) + ((el % CHUNKS) ^ (r & 7)) * 16);
+            if (rw + r < at.s.rows) *reinterpret_cast<f32x4*>(e.partials + (place + r) * D + el % CHUNKS * 4) = y;
         }
         return true;
     }
