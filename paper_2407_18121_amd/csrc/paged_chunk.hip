@@ -271,7 +271,9 @@ template <int DT, int D, int WAVES> __device__ __forceinline__ void chunk_nothin
 //   S^T = K . Q^T      matrix instructions, so that a lane owns one row in 16 and 4 consecutive slots of a block of 16
 //   O^T += V^T . P^T   the probabilities are the second operand as they stand; V is transposed on its way out of LDS (bf16)
 // A bf16 probability enters as the sum of three bf16 numbers, all its 24 bits: few rows are bound by the bytes of K and V, and the matrix pipes have the room.
-template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chunk_few_rows(const ChunkStep& a, const ChunkItem& at, int wave, unsigned char* tiles, float* sh_m, float* sh_l)
+// False: something has come out that is no number, with two blocks of fp32 rows, which leave the care for infinite V to single ones.
+template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkItem& at, int wave, unsigned char* tiles, float* sh_m, float* sh_l,
+                                                                                          int* flags)
 {
     using T = PagedTile<DT, D>;
     constexpr int TR = T::TR, ROW = T::kRowBytes, CH = T::CH, RPI = T::RPI, NI = T::NI, ROUND = WAVES * TR;
@@ -282,7 +284,7 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
     const int c16 = lane % 16, quarter = lane / 16;
     const int slots = a.pages.slots(), r0 = at.r0;
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
-    if (first >= last) return;  // a tile that sees fewer segments than its sequence has
+    if (first >= last) return true;  // a tile that sees fewer segments than its sequence has
     const bool whole = at.each >= at.seen;  // the tile's only segment
 
     // ------------------------------------------------------------------ rows into LDS
@@ -605,21 +607,147 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qf[rb][kb]));
         Places next = places_of(row + ROUND, ahead);
-        if (left > 1) {
-            issue_k(mine + T::BYTES, next);
-            issue_v(mine + 3 * T::BYTES, next);
-        }
         uint32_t off = 0;
         int bad = here.bad, next_bad = next.bad;
-        if (left > 2) next = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
-        for (;; --left) {
-            Ids ids;
-            if (left > 3) ids = pages_of(row + 3 * ROUND);
-            tile(off, row, bad, left, next);
-            if (left == 1) break;
-            bad = next_bad, next_bad = next.bad;
-            row += ROUND, off ^= T::BYTES;
-            if (left > 3) next = places_of(row + 2 * ROUND, ids);
+        if constexpr (!T::kHalf && RB == 2) {
+            // Two blocks of rows, fp32: the matrix pipe is the bound, and a wave is alone on its SIMD, of which it issues an instruction every eighth cycle, four
+            // while a matrix instruction lasts. What a block's softmax takes is issued between the matrix instructions of the other block, the scores' or
+            // the weighted sum's, loads between those of the first scores:
+            //   S of block 0, loads of the tile after the next | S of block 1, softmax of block 0 | O of block 0, softmax of block 1 | O of block 1
+            // with K of the next tile on its way out of LDS beside O, V beside S of block 0. 6900 cycles a tile of 16 slots, of which the matrix pipe works
+            // 4096, where one block after the other took 7500 (1024 first tokens of 32 heads 143 -> 133 us); what is left is mostly instructions that
+            // do not fit beside matrix instructions. (Raising the maximum in steps of 2^8, places in eight parts: no faster.)
+            constexpr int N = KB * 4, STAGES = 9;  // matrix instructions of a block's scores; of its sums there are as many
+            static_assert(N == OB * 4 && T::GROUPS == 2);
+            f32x4 kf[KB], vw[OB], part[2][4], s[2], x[2];
+            float correction[2];
+            int beyond[2];  // the first of the lane's four slots that its row does not see
+            auto read_k = [&](uint32_t off) __attribute__((always_inline)) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) kf[kb] = *(lds_f32x4*)(uintptr_t)(k_at[kb] + off);
+            };
+            auto score = [&](int rb, int n) __attribute__((always_inline)) {
+                part[rb][n % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[n / 4][n % 4], __uint_as_float(qf[rb][n / 4][n % 4]),
+                                                                      n < 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[rb][n % 4], 0, 0, 0);
+            };
+            auto weighted = [&](int rb, int n) __attribute__((always_inline)) {
+                const int i = n / 4, e = n % 4;
+                o[rb][i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vw[i][e], x[rb][i % 4], o[rb][i / 4 * 4 + e], 0, 0, 0);
+            };
+            auto softmax = [&](int rb, int stage) __attribute__((always_inline)) {
+                if (stage == 0) s[rb] = (part[rb][0] + part[rb][1]) + (part[rb][2] + part[rb][3]);
+                if (stage == 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[rb][r] = r < beyond[rb] ? s[rb][r] : -INFINITY;
+                }
+                if (stage == 2) x[rb][0] = fmaxf(fmaxf(s[rb][0], s[rb][1]), fmaxf(s[rb][2], s[rb][3]));
+                if (stage == 3) x[rb][0] = head_max(x[rb][0]);
+                if (stage == 4) {
+                    const float top = fmaxf(m[rb], x[rb][0]);
+                    correction[rb] = m[rb] == top ? 0.f : m[rb] - top;
+                    m[rb] = top;
+                }
+                if (stage == 5) correction[rb] = __builtin_amdgcn_exp2f(correction[rb] * of_diff);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (stage == 6) x[rb][r] = (s[rb][r] - m[rb]) * of_diff;
+                    if (stage == 7) x[rb][r] = __builtin_amdgcn_exp2f(x[rb][r]);
+                }
+                if (stage == 8) {
+                    l[rb] = fmaf(l[rb], correction[rb], (x[rb][0] + x[rb][1]) + (x[rb][2] + x[rb][3]));
+                    asm volatile("" : "+v"(x[rb]), "+v"(l[rb]), "+v"(correction[rb]));  // (here, not where they are used)
+                }
+            };
+            // the stages of a block's softmax that belong to matrix instruction n of N, from the third on
+            auto beside = [&](int rb, int n) __attribute__((always_inline)) {
+                constexpr int ROOM = N - 3;
+#pragma unroll
+                for (int i = 0; i < STAGES; ++i)
+                    if (n >= 2 && i >= (n - 2) * STAGES / ROOM && i < (n - 1) * STAGES / ROOM) softmax(rb, i);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            // with 512 registers a wave the sums stay in those that only matrix instructions reach, but for the times when they are rescaled
+            auto keep = [&](int rb) __attribute__((always_inline)) {
+                if constexpr (T::kResident == 1) {
+#pragma unroll
+                    for (int i = 0; i < OB; ++i) asm volatile("" : "+a"(o[rb][i]));
+                }
+            };
+            auto rescale = [&](int rb) __attribute__((always_inline)) {
+                if (__any(correction[rb] != 1.f)) {
+                    keep(rb);
+#pragma unroll
+                    for (int i = 0; i < OB; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[rb][i][r] *= correction[rb];
+                    keep(rb);
+                }
+                keep(rb);
+            };
+            // (behind the segment nothing is fetched: loads of no bytes, not a branch around them)
+            issue_k(mine + T::BYTES, next);
+            issue_v(mine + 3 * T::BYTES, next);
+            next_bad = next.bad;
+            next = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+            read_k(0);
+            keep(0), keep(1);
+            for (;; --left) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");  // all loads but the next tile's have landed
+#pragma unroll
+                for (int i = 0; i < OB; ++i) vw[i] = *(lds_f32x4*)(uintptr_t)(v_at[i] + off);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    score(0, n);
+                    if (n == N / 2) wait_lds();  // V is in registers
+                    if (n % (N / 8) == N / 8 - 1 && n >= N / 2) {
+                        const int u = (n - N / 2) / (N / 8);
+                        if (u < 2) load_run_lds<T::IPG, T::kHalf>(tile_rsrc(static_cast<const char*>(a.k_pages) + next.from[u % 2], next.bytes[u % 2]), mine + off + u % 2 * 8 * ROW, k_part[u % 2]);
+                        else load_run_lds<T::IPG, T::kHalf>(tile_rsrc(static_cast<const char*>(a.v_pages) + next.from[u % 2], next.bytes[u % 2]), mine + 2 * T::BYTES + off + u % 2 * 8 * ROW, v_part);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) beyond[rb] = (bad >> (quarter / 2) & 1 ? -1 : limit[rb]) + 1 - row - quarter * 4;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    score(1, n);
+                    beside(0, n);
+                }
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NI) : "memory");  // all up to the next tile's K
+                read_k(off ^ T::BYTES);
+                const Ids ids = pages_of(row + 3 * ROUND);
+                rescale(0);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    weighted(0, n);
+                    beside(1, n);
+                }
+                rescale(1);
+                bad = next_bad, next_bad = next.bad;
+#pragma unroll
+                for (int n = 0; n < N; ++n) weighted(1, n);
+                next = places_of(row + 3 * ROUND, ids);
+                keep(0), keep(1);
+                if (left == 1) break;
+                row += ROUND, off ^= T::BYTES;
+            }
+        } else {
+            if (left > 1) {
+                issue_k(mine + T::BYTES, next);
+                issue_v(mine + 3 * T::BYTES, next);
+            }
+            if (left > 2) next = places_of(row + 2 * ROUND, pages_of(row + 2 * ROUND));
+            for (;; --left) {
+                Ids ids;
+                if (left > 3) ids = pages_of(row + 3 * ROUND);
+                tile(off, row, bad, left, next);
+                if (left == 1) break;
+                bad = next_bad, next_bad = next.bad;
+                row += ROUND, off ^= T::BYTES;
+                if (left > 3) next = places_of(row + 2 * ROUND, ids);
+            }
         }
     }
 
@@ -646,6 +774,7 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
     }
     __syncthreads();
     const int rows = min(ROWS, at.r1 - r0);
+    float zero = 0.f;
     for (int i = tid; i < rows * CHUNKS; i += WAVES * kWave) {
         const int r = i / CHUNKS, chunk = i % CHUNKS;
         float mw[WAVES], top = kLowest, sum = 0.f;
@@ -662,6 +791,10 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[k] = fmaf(v[k], c, x[k]);
         }
+        if constexpr (!T::kHalf && RB == 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) zero = fmaf(x[k], 0.f, zero);
+        }
         if (whole) {
             const size_t row = chunk_row(e, at.s.t0, at.hk, r0 + r), to = row * D + chunk * 4;
             const bool none = sum == 0.f;
@@ -673,6 +806,16 @@ template <int DT, int D, int WAVES, int RB> __device__ __forceinline__ void chun
             if (chunk == 0) e.stats[at.place + r] = make_float2(top, sum);
         }
     }
+    if constexpr (!T::kHalf && RB == 2) {
+        const bool mine = __any(!(zero == 0.f));
+        if (lane_anew() == 0) flags[wave] = mine;
+        __syncthreads();
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) any |= flags[w];
+        return !any;
+    }
+    return true;
 }
 
 }  // namespace ec
@@ -696,21 +839,28 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
             chunk_nothing<DT, D, WAVES>(a, at, wave);
             return;
         }
+        auto by_16 = [&] {
+            ChunkItem part = at;
+            for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
+                part.r1 = min(part.r0 + 16, at.r1);
+                chunk_few_rows<DT, D, WAVES, 1>(a, part, wave, tiles, sh_m, sh_l, flags);
+                __syncthreads();
+            }
+        };
         if constexpr (DT == EC_BF16) {
             static_assert(sizeof(tiles) >= WAVES * kManySlots * D * 2 && UNIT % kManySlots == 0);
             if (at.s.tile_rows == kManyRows) {
                 if (chunk_many_rows<D, WAVES>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT)) return;
-                ChunkItem part = at;
-                for (; part.r0 < at.r1; part.r0 += 16, part.place += 16) {
-                    part.r1 = min(part.r0 + 16, at.r1);
-                    chunk_few_rows<DT, D, WAVES, 1>(a, part, wave, tiles, sh_m, sh_l);
-                    __syncthreads();
-                }
+                by_16();
                 return;
             }
         }
-        if (at.s.tile_rows == 16) chunk_few_rows<DT, D, WAVES, 1>(a, at, wave, tiles, sh_m, sh_l);
-        else chunk_few_rows<DT, D, WAVES, 2>(a, at, wave, tiles, sh_m, sh_l);
+        if constexpr (DT == EC_BF16) {
+            if (at.s.tile_rows == 16) chunk_few_rows<DT, D, WAVES, 1>(a, at, wave, tiles, sh_m, sh_l, flags);
+            else chunk_few_rows<DT, D, WAVES, 2>(a, at, wave, tiles, sh_m, sh_l, flags);
+        } else {
+            if (at.s.tile_rows == 16 || !chunk_few_rows<DT, D, WAVES, 2>(a, at, wave, tiles, sh_m, sh_l, flags)) by_16();
+        }
     };
     for (int id = blockIdx.x;; id += gridDim.x) {
         const ChunkStep a = chunk_args();
