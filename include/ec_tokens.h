@@ -12,14 +12,15 @@ extern "C" {
 #endif
 
 /*
- * Three calls: pages and slots for the tokens (once for all layers), then in every layer their queries and keys turned by their positions and stored, and their attention. Tokens are
- * packed: those of sequence b are token_start[b] .. token_start[b+1] - 1 of T, sequence after sequence; tokens behind the last sequence's are padding.
+ * Three calls: pages and slots for the tokens (once for all layers), then in every layer their queries and keys turned by their positions and stored, and
+ * their attention.  Tokens are packed: those of sequence b are token_start[b] .. token_start[b+1] - 1 of T, sequence after sequence; tokens behind the
+ * last sequence's are padding.
  */
 
 /*
- * Pages for new rows, on the device: page table, a stack of free pages, and where every new token goes.  With L = len_b[b] the rows of sequence b that stay (below
- * 0: the place holds no sequence, and all its pages are given back), n = max(new_b[b], 0) its new tokens, h = held_b[b] the pages that it holds, entries 0 .. h-1
- * of its row of the table:
+ * Pages for new rows, on the device: page table, a stack of free pages, and where every new token goes.  With L = len_b[b] the rows of sequence b that
+ * stay (below 0: the place holds no sequence, and all its pages are given back), n = max(new_b[b], 0) its new tokens, h = held_b[b] the pages that it
+ * holds, entries 0 .. h-1 of its row of the table:
  *   1. a sequence fits if L >= 0, its tokens end at or before T and ceil((L + n) / page) <= max_pages.  It wants ceil((L + n) / page) pages, one that
  *      does not fit ceil(L / page) and none beyond those it holds
  *   2. pages beyond what a sequence wants are given back: sequence after sequence, each from its last entry down, onto the stack; their entries become -1
@@ -72,16 +73,18 @@ int ec_paged_rotary_store(const void* q, const void* k, const void* v, int64_t q
 /*
  * Attention of the new tokens over paged caches that hold their rows already.  For token i of sequence b, L = start_b[b]:
  *     out = softmax_j(scale * <q, k_j>) . v_j,   lse = log sum_j exp(scale * <q, k_j>)   over slots j = 0 .. L + i
- * of the query head's key/value head.  Slots behind the table's last and on no page weigh nothing.  A token that sees no row, or only scores of -inf, gets zeros
- * and an lse of -inf; so do all tokens of a place whose L is outside 0 .. max_pages * page - 1.  Rows of out and lse behind the last sequence's tokens
- * are left as they are.
+ * of the query head's key/value head.  Slots behind the table's last and on no page weigh nothing.  A token that sees no row, or only scores of -inf,
+ * gets zeros and an lse of -inf; so do all tokens of a place whose L is outside 0 .. max_pages * page - 1.  Rows of out and lse behind the last
+ * sequence's tokens are left as they are.
  *   q,out           DEVICE [T,H,D] dt; out must not overlap q (EC_EINVAL)
  *   lse             DEVICE [T,H] float, written; may be NULL; must not overlap q or out (EC_EINVAL)
  *   start_b         DEVICE [B] int32, token_start DEVICE [B+1] int32 (taken as 0 .. T; what overlaps or falls is unspecified)
  *   ws              DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_CHUNK_STEP, B,H,T,D,dt), of one call at a time
- * Requires T <= 2^24, T * H <= 2^30.  Products are formed on the matrix cores with fp32 accumulation, sums and the softmax in fp32.  A weight
- * below the range of normal fp32 numbers, 2^-126 of the largest, is 0.  An infinite or NaN row of V reaches the tokens that see it, and no others.
- * Results are deterministic.
+ * Requires T <= 2^24, T * H <= 2^30.  Products are formed on the matrix cores with fp32 accumulation, sums and the softmax in fp32.  Where a sequence of bf16
+ * brings more than 32 tokens times query heads of a key/value head, its weights enter the product with V rounded to bf16 (their sum does not); with
+ * fewer, and in fp32, they enter with all 24 bits.  A weight below the range of normal fp32 numbers, 2^-126 of the largest, is 0.  An infinite or NaN row
+ * of V reaches the tokens that see it, and no others.  ws needs no contents.  Results are deterministic: a row's sum is formed in an order that depends on
+ * the lengths of the whole batch and on T, not on time.
  */
 int ec_paged_chunk_step(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* start_b,
                         const int32_t* token_start, int B, int T, int H, int Hkv, int D, int page, int n_pages, int max_pages, float scale,

@@ -7,6 +7,11 @@
 // The probabilities' sum is that of the fp32 numbers; rounding them to bf16, half a step off each, is what keeps the product at one matrix instruction where
 // few rows, which are bound by memory, take three: with many rows the matrix pipes are the bound.
 //
+// A tile takes two workgroups of a compute unit 3300 cycles of 2048 in the matrix pipe (D128; the pipes of a busy unit work 61 % of the time in 2.55 ms over
+// 65000 rows, H40/8, 2048 tokens: 1.09 PFLOP/s), what remains being the exponentials and the instructions between; a lone workgroup takes 3100. Where a
+// batch has fewer tiles than the chip has compute units, a workgroup has eight waves, two groups of four that take turns at the tiles, each with tiles of
+// its own in LDS: 4100 cycles a pair (512 tokens behind 768 rows, H32: 41.2 -> 30.9 us).
+//
 // Operands (lane l, half h = l / 32):  A (32 x 16): lane holds A[l % 32][8h .. 8h+7]    B (16 x 32): B[8h .. 8h+7][l % 32]
 //                                      C (32 x 32): C[8g + 4h + t][l % 32] in register 4g + t, g,t in 0..3
 #pragma once

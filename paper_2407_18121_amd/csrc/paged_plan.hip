@@ -5,7 +5,8 @@
 // say everything: of the new tokens (where b's tokens lie), of the pages given back (where they go on the stack), of the pages asked for
 // (which of the stack's are b's, and whether there are enough). The sums are formed by one workgroup, a thread a sequence; what follows from them
 // -- a page given, a page taken, a token -- is looked up by its number in the sums, so that long and short sequences cost the same.
-// Bound by latency: a chain of loads, sums and stores, each behind a barrier.
+// Bound by latency: a chain of loads, sums and stores, each behind a barrier (16 sequences of a token each 4.1 us; 256 sequences with 16100 tokens 9 us, and
+// 3 for the tokens' launch).
 #include "paged.h"
 
 namespace ec {
