@@ -42,7 +42,7 @@ struct ChunkStep {
     uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
     uint32_t heads_mul, heads_shift;  // x / Hkv, as above
     int rounds;
-    bool small;       // the units of all tiles have 29 bits
+    bool small;       // the units of all tiles have 29 bits, whatever token_start holds
     bool cut;         // whether tiles may be cut and the second launch follows
     float scale, scale_log2e;
     int* cut_tiles;   // tiles that are cut, which paged_chunk_join_kernel goes over
@@ -151,7 +151,7 @@ template <int UNIT, int PLACES, class N> __device__ __forceinline__ ChunkShare<U
 {
     // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
     const N share = a.rounds > 1 ? (all + (2 * PLACES - 1)) / (2 * PLACES) : (most + (PLACES - 1)) / PLACES;
-    const int units = (int)min(max(share, (N)1), (N)(1 << 22));
+    const int units = (int)min(max(share, (N)1), (N)((1 << 24) - 1));  // (from four times the units of the longest table on nothing is cut)
     const N held = (N)4 * PLACES * units;
     return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
 }
@@ -1008,7 +1008,8 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
     constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
-    a.small = tiles * 2 * ((a.pages.slots() + UNIT - 1) / UNIT) < 1 << 29;
+    const long long seq_tiles = most_tiles(a.T, a.group, a.Hkv, 1, DT == EC_F32 ? 32 : 128), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    a.small = a.B < 1 << 20 && seq_tiles < 1 << 20 && seq_tiles * a.B * 2 * units < 1 << 29;
     a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (the second launch takes longer than shorter sequences)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
     auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };

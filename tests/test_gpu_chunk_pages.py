@@ -254,3 +254,26 @@ def test_replays_and_streams():
         for s, L, starts in todo:
             want, tol, _, _ = ref.chunk(s["pool"], s["q"], L, starts, 0.1, "bf16")
             assert (np.abs(to_host(s["out"]) - want) <= tol)[:starts[-1]].all()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("T,slots", [(40, 4096), (300, 1024)])
+def test_tokens_that_overlap_stay_inside(dtype, D, T, slots):
+    """What tokens of several sequences get is not specified, but nothing beside out, lse and the workspace's bytes is written, however many tiles that makes."""
+    B, H, Hkv, page = 96, 4, 2, 32
+    rng = np.random.default_rng(T)
+    pool = make(rng, dtype, Hkv, D, page, [slots])
+    code = ec.EC_BF16 if dtype == "bf16" else ec.EC_F32
+    i = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    size = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, B, H, T, D, code).numel()
+    ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+    out = torch.full((T + 8, H, D), 5.5, dtype=torch_dtype(dtype), device="cuda")
+    lse = torch.full((T + 8, H), 6.5, device="cuda")
+    q = to_dev(quantize(rng.standard_normal((T, H, D)), dtype), dtype)
+    k, v = to_dev(pool.k, dtype), to_dev(pool.v, dtype)
+    table = i(np.repeat(pool.table[:1], B, 0))
+    for starts in ([0, T] * (B // 2) + [0], [2 ** 31 - 1, -5] * (B // 2) + [T], list(rng.integers(-T, 2 * T, B + 1))):
+        for start in ([slots - T] * B, list(rng.integers(-2, slots + 2, B)), [2 ** 31 - 1] * B):
+            assert ec.ec_paged_chunk_step(q, k, v, table, i(start), i(starts), 0.1, out[:T], ws[:size], lse[:T]) == ec.EC_OK
+            torch.cuda.synchronize()
+            assert (ws[size:] == 77).all() and (out[T:] == 5.5).all() and (lse[T:] == 6.5).all()
