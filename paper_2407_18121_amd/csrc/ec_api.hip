@@ -579,7 +579,7 @@ int ec_paged_rotary_store(const void* q, const void* k, const void* v, int64_t q
     ec::Pages pages;
     if (const int rc = paged_shape(pos, 1, Hkv, G, D, page, n_pages, 1, dt, pages)) return rc;
     if (H > 65535 || !tokens_ok(T, H) || !tokens_ok(T, Hkv)) return EC_EUNSUPPORTED;
-    const int64_t e = dt == EC_BF16 ? 2 : 4, most = (int64_t)1 << 40;
+    const int64_t e = dt == EC_BF16 ? 2 : 4, most = (int64_t)1 << 36;
     if (q_step < (int64_t)H * D || k_step < (int64_t)Hkv * D || v_step < (int64_t)Hkv * D) return EC_EINVAL;
     if (q_step > most || k_step > most || v_step > most || (q_step | k_step | v_step) * e % 16) return EC_EUNSUPPORTED;
     if (!aligned16({q, k, v, q_out, k_pages, v_pages})) return EC_EUNSUPPORTED;

@@ -305,8 +305,9 @@ class PagedTokens:
         for i in range(n_layers):
             batch.attend(i, q[i], k[i], v[i], scale, out[i]) # [tokens,H or Hkv,D] packed, sequence after sequence (batch.token_start)
 
-    A sequence that the free pages do not hold keeps what it has: its tokens get zeros, len_b and seen_b do not grow, start_b is -1.
-    Compressed prompts come in as rows: admit(places, rows, seen), begin() without tokens for them, store() in every layer.
+    A sequence that the free pages do not hold, or whose tokens end behind the last of `tokens`, keeps what it has: its tokens get zeros, len_b and seen_b do not
+    grow, start_b is -1. Rows of out behind the last sequence's tokens are left as they are.
+    Compressed prompts come in as rows: admit(places, rows, seen), begin() without tokens for them, store() in every layer where start_b has the rows.
     New rows' masses are 0 (what adds to masses is ec_paged_decode_score_step)."""
 
     def __init__(self, layers, places, tokens, H, Hkv, D, page, n_pages, max_pages, dtype: torch.dtype, freq, mscale=1.0, interleaved=False, G=1, device="cuda"):
