@@ -78,13 +78,13 @@ __device__ __forceinline__ int token_of(const ChunkStep& a, int row) { return (i
 // Rows of a tile of a sequence with so many: as few as hold them where the bytes of K and V are the bound, so that few matrix instructions are spent on rows
 // that are not there; 128 share what comes in where they are many, in bf16 (32 rows of fp32 take four times as long in the matrix pipe as K and V
 // take to come in from the L2).
-template <int DT> __device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 || DT == EC_F32 ? 32 : 128; }
+template <int MANY> __device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : MANY; }
 
 // What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of UNIT slots that its last token sees.
 struct ChunkSeq {
     int L, t0, n, rows, tile_rows, tiles, units, first_units;  // first_units: that the first tile sees
     bool live;
-    template <int DT, int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
+    template <int MANY, int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
     {
         L = -1, t0 = n = 0;
         if (b < a.B) {
@@ -95,8 +95,8 @@ struct ChunkSeq {
         const int slots = a.pages.slots();
         live = L >= 0 && L < slots;
         rows = n * a.group;
-        tile_rows = chunk_tile_rows<DT>(rows);
-        tiles = (rows + tile_rows - 1) >> (tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : 7);
+        tile_rows = chunk_tile_rows<MANY>(rows);
+        tiles = (rows + tile_rows - 1) >> (tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : MANY == 64 ? 6 : 7);
         units = !n ? 0 : live ? (min(L + n, slots) + UNIT - 1) / UNIT : 1;
         first_units = !n ? 0 : live ? min(L + token_of(a, min(tile_rows, rows) - 1), slots - 1) / UNIT + 1 : 1;
     }
@@ -156,16 +156,16 @@ template <int UNIT, int PLACES, class N> __device__ __forceinline__ ChunkShare<U
     return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
 }
 // s: of this lane's sequence afterwards, if there are no more than lanes
-template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
+template <int MANY, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
     if (!a.cut) {  // a share that no tile exceeds
-        if (a.B <= kWave) s.read<DT, UNIT>(a, threadIdx.x % kWave);
+        if (a.B <= kWave) s.read<MANY, UNIT>(a, threadIdx.x % kWave);
         return {1 << 22, 1};
     }
     if (a.small) {
         uint32_t all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
-            s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
+            s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
             const int units = wave_scan(s.tiles * s.units), both = wave_scan(s.tiles * (s.units + s.first_units));
             most += last_lane(units), all += last_lane(both);
         }
@@ -173,7 +173,7 @@ template <int DT, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UN
     }
     unsigned long long all = 0, most = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
+        s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
         all += wave_sum((long long)s.tiles * (s.units + s.first_units));
         most += wave_sum((long long)s.tiles * s.units);
     }
@@ -198,14 +198,14 @@ struct ChunkItem {
 };
 // The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
 // which sees most, then segments. s: as chunk_share leaves it.
-template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
+template <int MANY, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
 {
     const int lane = lane_anew(), j = (int)(__umulhi((uint32_t)id << 2, a.heads_mul) >> a.heads_shift), hk = id - j * a.Hkv;
     int before = 0, parts_before = 0;  // parts: and cut tiles in the high half, both at most kChunkParts
     ChunkItem it;
     it.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        if (a.B > kWave) s.read<DT, UNIT>(a, b0 + lane);
+        if (a.B > kWave) s.read<MANY, UNIT>(a, b0 + lane);
         const ChunkCut cut = share.of(s);
         const int cut_tiles = s.tiles - cut.whole, items = s.tiles + cut_tiles * (cut.segments - 1), parts = cut_tiles * cut.segments + (cut_tiles << 16);
         const int upto = wave_scan(items), parts_upto = wave_scan(parts);
@@ -240,11 +240,11 @@ template <int DT, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(cons
     }
     return it;
 }
-template <int DT, int UNIT> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s)
+template <int MANY, int UNIT> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s)
 {
     int n = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        if (a.B > kWave) s.read<DT, UNIT>(a, b0 + threadIdx.x % kWave);
+        if (a.B > kWave) s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
         n += last_lane(wave_scan(s.tiles - share.of(s).whole));
     }
     if (threadIdx.x == 0) *a.cut_tiles = n * a.Hkv;
@@ -828,18 +828,20 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
 #include "paged_chunk_many.h"
 namespace ec {
 
-template <int DT, int D, int WAVES>
+// MANY: rows of a tile of a sequence with more than 32
+template <int DT, int D, int WAVES, int MANY>
 __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep first)
 {
     using T = PagedTile<DT, D>;
     constexpr int UNIT = WAVES * T::TR;
     __shared__ __align__(256) unsigned char tiles[WAVES * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
-    __shared__ float sh_m[WAVES * 32], sh_l[WAVES * 32];
+    constexpr int SUMS = MANY == 64 ? 6 * kWave : WAVES * 32;  // (64 rows: three parts of two waves)
+    __shared__ float sh_m[SUMS], sh_l[SUMS];
     __shared__ int flags[WAVES];
     const int first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     ChunkSeq s;
-    const auto share = chunk_share<DT, UNIT, kChunkPlaces<DT, D, WAVES>>(first, s);
-    if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<DT, UNIT>(first, share, s);
+    const auto share = chunk_share<MANY, UNIT, kChunkPlaces<DT, D, WAVES>>(first, s);
+    if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<MANY, UNIT>(first, share, s);
     auto take = [&](const ChunkStep& a, const ChunkItem& at, int wave) __attribute__((always_inline)) {
         if (!at.s.live) {
             chunk_nothing<DT, D, WAVES>(a, at, wave);
@@ -855,8 +857,8 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
         };
         if constexpr (DT == EC_BF16) {
             static_assert(sizeof(tiles) >= WAVES * kManySlots * D * 2 && UNIT % kManySlots == 0);
-            if (at.s.tile_rows == kManyRows) {
-                if (chunk_many_rows<D, WAVES>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT)) return;
+            if (at.s.tile_rows > 32) {
+                if (chunk_many_rows<D, WAVES, MANY / 32>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT)) return;
                 by_16();
                 return;
             }
@@ -872,8 +874,8 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
         const ChunkStep a = chunk_args();
         int wave = first_wave;  // (what follows from it is not kept from item to item)
         asm volatile("" : "+s"(wave));
-        if (id != blockIdx.x && a.B <= kWave) s.read<DT, UNIT>(a, lane_anew());
-        const ChunkItem at = chunk_item<DT, UNIT>(a, share, s, id, wave);
+        if (id != blockIdx.x && a.B <= kWave) s.read<MANY, UNIT>(a, lane_anew());
+        const ChunkItem at = chunk_item<MANY, UNIT>(a, share, s, id, wave);
         if (at.b < 0) return;
         take(a, at, wave);
         __syncthreads();  // the tiles have been read
@@ -1003,21 +1005,38 @@ struct ChunkPlaces {  // where things lie in a workspace
 };
 size_t paged_chunk_ws(int T, int H, int D) { return ChunkPlaces(T, H, D).end; }
 
+// Rows of a tile of a sequence of bf16 with more than 32: 128, or 64 where neither tiles of 128 nor their segments (`least` units each) give all compute units
+// something to do. 512 tokens behind 768 rows of 32 heads 26.7 us instead of 30.2, 100 tokens behind 3000 rows H32/8 24.9 instead of 27.4; where segments
+// do, 128 rows read K and V half as often: 32 tokens behind 65000 rows H40/8 83 us instead of 89, 8 sequences of 2900 rows 28.2 instead of 30.4.
+static int many_rows(long long tiles, int slots)
+{
+    const long long segments = std::max(1, slots / (128 * (tiles >= kChunkTiles ? 8 : 4)));
+    return tiles <= kComputeUnits / 2 && tiles * segments < kComputeUnits ? 64 : 128;
+}
+
 template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
 {
-    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
     constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
+    const int rows = DT == EC_F32 ? 32 : many_rows(most_tiles(a.T, a.group, a.Hkv, a.B, 128), a.pages.slots());
+    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, rows);
     a.rounds = tiles >= kChunkTiles ? 4 : 1;
-    const long long seq_tiles = most_tiles(a.T, a.group, a.Hkv, 1, DT == EC_F32 ? 32 : 128), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    const long long seq_tiles = most_tiles(a.T, a.group, a.Hkv, 1, rows), units = (a.pages.slots() + UNIT - 1) / UNIT;
     a.small = a.B < 1 << 20 && seq_tiles < 1 << 20 && seq_tiles * a.B * 2 * units < 1 << 29;
-    a.cut = (a.pages.slots() + UNIT - 1) / UNIT > 4;  // (the second launch takes longer than shorter sequences)
+    a.cut = units > 4;  // (the second launch takes longer than shorter sequences)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
-    auto groups = [&](int places) { return dim3((unsigned)(a.cut ? std::max<long long>(tiles, places) : tiles)); };
-    if (DT == EC_BF16 && tiles <= kComputeUnits) {
-        if constexpr (DT == EC_BF16)
-            hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kManyWaves>), groups(kChunkPlaces<DT, D, kManyWaves>), dim3(kManyWaves * kWave), 0, stream, a);
+    auto go = [&](auto waves, auto many) {
+        constexpr int W = decltype(waves)::value;
+        const long long groups = a.cut ? std::max<long long>(tiles, kChunkPlaces<DT, D, W>) : tiles;
+        hipLaunchKernelGGL((paged_chunk_kernel<DT, D, W, decltype(many)::value>), dim3((unsigned)groups), dim3(W * kWave), 0, stream, a);
+    };
+    using Few = std::integral_constant<int, kFewWaves>;
+    if constexpr (DT == EC_F32) {
+        go(Few{}, std::integral_constant<int, 32>{});
     } else {
-        hipLaunchKernelGGL((paged_chunk_kernel<DT, D, kFewWaves>), groups(kChunkPlaces<DT, D, kFewWaves>), dim3(kFewWaves * kWave), 0, stream, a);
+        using Many = std::integral_constant<int, kManyWaves>;
+        if (rows == 64) go(Many{}, std::integral_constant<int, 64>{});
+        else if (tiles <= kComputeUnits) go(Many{}, std::integral_constant<int, 128>{});
+        else go(Few{}, std::integral_constant<int, 128>{});
     }
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     if (!a.cut) return EC_OK;

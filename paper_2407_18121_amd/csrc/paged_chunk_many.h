@@ -1,6 +1,6 @@
-// Attention of up to 128 rows (tokens times query heads of a key/value head) of a sequence over its pages, bf16: included by paged_chunk.hip.
+// Attention of up to 128 or 64 rows (tokens times query heads of a key/value head) of a sequence over its pages, bf16: included by paged_chunk.hip.
 //
-// Four waves, 32 rows each; tiles of 64 slots, K and V in two places each, straight from their pages into LDS. The score tile is computed transposed,
+// Four waves, 32 rows each (of 64 rows: two pairs, which take half of a tile's slots each); tiles of 64 slots, K and V in two places each, straight from their pages into LDS. The score tile is computed transposed,
 // S^T = K . Q^T, with 32x32x16 instructions, so that a lane owns one row and 16 slots of a block of 32; rounded to bf16 the probabilities are
 // the second operand of O^T += V^T . P^T as they stand, V transposed on its way out of LDS. Two phases a tile, each with vector work beside matrix work:
 //   A  probabilities of tile i beside the scores of tile i + 1       B  O^T += V^T . P^T of tile i beside the row maximum of tile i + 1
@@ -10,7 +10,8 @@
 // A tile takes two workgroups of a compute unit 3300 cycles of 2048 in the matrix pipe (D128; the pipes of a busy unit work 61 % of the time in 2.55 ms over
 // 65000 rows, H40/8, 2048 tokens: 1.09 PFLOP/s), what remains being the exponentials and the instructions between; a lone workgroup takes 3100. Where a
 // batch has fewer tiles than the chip has compute units, a workgroup has eight waves, two groups of four that take turns at the tiles, each with tiles of
-// its own in LDS: 4100 cycles a pair (512 tokens behind 768 rows, H32: 41.2 -> 30.9 us).
+// its own in LDS: 4100 cycles a pair (512 tokens behind 768 rows, H32: 41.2 -> 30.9 us); where it has less than half as many, and segments do not make up for
+// it, tiles of 64 rows (see many_rows). The sums of a row's parts meet in LDS at the end.
 //
 // Operands (lane l, half h = l / 32):  A (32 x 16): lane holds A[l % 32][8h .. 8h+7]    B (16 x 32): B[8h .. 8h+7][l % 32]
 //                                      C (32 x 32): C[8g + 4h + t][l % 32] in register 4g + t, g,t in 0..3
@@ -20,7 +21,6 @@ namespace ec {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
-constexpr int kManyRows = 128;   // of a workgroup
 constexpr int kManySlots = 64;   // of a tile
 constexpr int kManyAhead = 4;    // LDS fragments requested ahead of the matrix pipe
 
@@ -34,28 +34,32 @@ template <int D> struct ManySwizzleV {  // four rows at the same 64 bytes (a tra
 
 // False, and nothing written: something has come out that is no number.
 // sh_m, sh_l: a float a thread of four waves.
-template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, int wave_wg, unsigned char* tiles, float* sh_m,
-                                                                            float* sh_l, int* flags, int unit)
+template <int D, int WAVES, int QW>
+__device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkItem& at, int wave_wg, unsigned char* tiles, float* sh_m, float* sh_l, int* flags, int unit)
 {
-    constexpr int QW = 4, KS = WAVES / QW;  // waves that share the rows, and groups of them that take turns at the tiles
+    constexpr int KS = WAVES / 4;  // groups of four waves that take turns at the tiles
+    constexpr int SH = 4 / QW;     // of a group QW waves share the rows, 32 each, and SH the slots of a tile
+    constexpr int NB = 2 / SH;     // 32-slot blocks of a wave's share
+    constexpr int PARTS = KS * SH;  // sums of every row in a workgroup
     constexpr int ROW = D * 2, CH = ROW / 16, RPI = kWave / CH;  // bytes and chunks of a row, rows of a load instruction
     constexpr int KB = D / 16;    // contraction blocks of Q.K
     constexpr int DB = D / 32;    // 32-row blocks of O^T
-    constexpr int NA = 2 * KB;    // matrix instructions of phase A: (kb, 32-slot block)
-    constexpr int NP = 4 * DB;    // of phase B: (16-slot block, db)
-    constexpr int EV = 32 / NA;   // elements turned into probabilities per matrix instruction of phase A
+    constexpr int NA = NB * KB;      // matrix instructions of phase A: (kb, 32-slot block)
+    constexpr int NP = 2 * NB * DB;  // of phase B: (16-slot block, db)
+    constexpr int EV = 16 * NB / NA;  // elements turned into probabilities per matrix instruction of phase A
     constexpr int TILE = kManySlots * ROW;
     constexpr int RUNS = 2, IPR = 8 / RPI;  // a wave moves 16 rows of a tile: two runs of 8, each in one page
     constexpr int K0 = 0, K1 = TILE, V0 = 2 * TILE, V1 = 3 * TILE;
     const int lane = lane_anew();
-    const int grp = wave_wg / QW, wave = wave_wg % QW;
+    const int grp = wave_wg / 4, wave = wave_wg % 4, part = grp * SH + wave / QW, rwave = wave % QW;
+    const int in_tile = wave / QW * (32 * NB);  // slot of the tile where the wave's share starts
     const int c32 = lane % 32, h = lane / 32;
-    const int slots = a.pages.slots(), rw = at.r0 + wave * 32;  // first row of the workgroup, of this wave
+    const int slots = a.pages.slots(), rw = at.r0 + rwave * 32;  // first row of the workgroup, of this wave
     const int group = a.group, L = at.s.L;
 
     // tiles of the workgroup, and up to what this wave's rows see
     auto sees = [&](int row) { return min(L + token_of(a, min(row, at.s.rows - 1)), slots - 1); };  // last slot
-    const int highest = scalar(sees(at.r0 + kManyRows - 1));
+    const int highest = scalar(sees(at.r0 + QW * 32 - 1));
     const int first = at.segment * at.each, last = min(first + at.each, at.seen);
     if (first >= last) return true;  // a tile that sees fewer segments than its sequence has
     const bool whole = at.each >= at.seen;
@@ -132,16 +136,16 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
     const int krow = (c32 & ~12) | ((c32 & 4) << 1) | ((c32 & 8) >> 1);
     uint32_t k_at[KB / 4];  // byte address of this lane's 16 bytes of contraction blocks 4 i and, turned over, 4 i + 1 .. 3 in tile K0
 #pragma unroll
-    for (int i = 0; i < KB / 4; ++i) k_at[i] = one_register(base + krow * ROW + ((8 * i + h) ^ ManySwizzleK<D>::at(krow)) * 16);
-    auto k_frag = [&](int kt, int f) __attribute__((always_inline)) {  // f = 2 kb + 32-slot block
-        const uint32_t from = k_at[f / 8] ^ f / 2 % 4 * 32;
-        return *(lds_bf16x8*)(uintptr_t)(from + kt + f % 2 * 32 * ROW);
+    for (int i = 0; i < KB / 4; ++i) k_at[i] = one_register(base + (in_tile + krow) * ROW + ((8 * i + h) ^ ManySwizzleK<D>::at(krow)) * 16);
+    auto k_frag = [&](int kt, int f) __attribute__((always_inline)) {  // f = NB kb + 32-slot block
+        const uint32_t from = k_at[f / NB / 4] ^ f / NB % 4 * 32;
+        return *(lds_bf16x8*)(uintptr_t)(from + kt + f % NB * 32 * ROW);
     };
     uint32_t v_at[DB];  // of the transposing read: 4 features of one slot
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
         const int row = h * 8 + (lane % 16) / 4, chunk = db * 4 + (lane / 16) % 2 * 2 + lane % 4 / 2;
-        v_at[db] = one_register(base + row * ROW + (chunk ^ ManySwizzleV<D>::at(row)) * 16 + lane % 2 * 8);
+        v_at[db] = one_register(base + (in_tile + row) * ROW + (chunk ^ ManySwizzleV<D>::at(row)) * 16 + lane % 2 * 8);
     }
     auto v_frag = [&](int vt, int g) __attribute__((always_inline)) {  // g = DB * (16-slot block) + db
         const uint32_t src = v_at[g % DB] + vt + g / DB * 16 * ROW;
@@ -160,17 +164,18 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
     // scaled to it); l: this half-wave's share of the row sum
     const float c = a.scale_log2e;
     float m = kLowest, l = 0.f;
-    f32x16 sA[2], sB[2];
-    bf16x8 pf[4];
+    f32x16 sA[NB], sB[NB];
+    bf16x8 pf[2 * NB];
 
     // scores of slots that the row does not see
-    auto hide = [&](f32x16 (&s)[2], int t, uint32_t bad) __attribute__((always_inline)) {
-        const int n0 = t * kManySlots;
-        if (bad || n0 + kManySlots - 1 > lowest) {
+    auto hide = [&](f32x16 (&s)[NB], int t, uint32_t bad) __attribute__((always_inline)) {
+        const int n0 = t * kManySlots + in_tile;
+        bad >>= in_tile / 8;
+        if (bad || n0 + 32 * NB - 1 > lowest) {
             const int l = anew(lane);  // (a branch, not 64 instructions in every tile, and no register between tiles)
             const int upto = sees(rw + l % 32) - n0 - l / 32 * 8;
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (nb * 32 + (r / 8) * 16 + (r % 8) > upto || (bad >> (nb * 4 + r / 8 * 2 + l / 32) & 1)) s[nb][r] = -INFINITY;
@@ -190,9 +195,9 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
                 for (int r = 0; r < 16; ++r) o[db][r] *= corr;
         }
     };
-    auto pin = [&](bf16x8 (&p)[4]) __attribute__((always_inline)) {
+    auto pin = [&](bf16x8 (&p)[2 * NB]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
+        for (int kk = 0; kk < 2 * NB; ++kk) {
             u32x4 w = __builtin_bit_cast(u32x4, p[kk]);
             asm volatile("" : "+v"(w));
             p[kk] = __builtin_bit_cast(bf16x8, w);
@@ -200,14 +205,14 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
     };
     // Phase A: probabilities of the tile in s (into pf and the row sum) beside sn = K.Q^T of the next one; extra(f) is issued behind the f-th matrix
     // instruction.
-    auto phase_a = [&](auto next, f32x16 (&s)[2], f32x16 (&sn)[2], int kt, auto&& extra) __attribute__((always_inline)) {
+    auto phase_a = [&](auto next, f32x16 (&s)[NB], f32x16 (&sn)[NB], int kt, auto&& extra) __attribute__((always_inline)) {
         __builtin_amdgcn_s_setprio(1);  // of the SIMD's two waves the one with the vector work issues first
         bf16x8 ka[NA];
         if constexpr (next.value) {
 #pragma unroll
             for (int f = 0; f < kManyAhead; ++f) ka[f] = k_frag(kt, f);
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sn[nb][r] = 0.f;
             __builtin_amdgcn_sched_barrier(0);
@@ -215,7 +220,7 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
         float minus = -m * c;
         if (__builtin_expect(__any(!(fabsf(minus) < 3e38f)), 0)) {  // a maximum whose product with the scale has left the range: differences first
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[nb][r] -= m;
             minus = 0.f;
@@ -225,7 +230,7 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
         for (int f = 0; f < NA + 2; ++f) {
             if constexpr (next.value)
                 if (f < NA) {
-                    sn[f % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[f], qf[f / 2], sn[f % 2], 0, 0, 0);
+                    sn[f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[f], qf[f / NB], sn[f % NB], 0, 0, 0);
                     if (f + kManyAhead < NA) ka[f + kManyAhead] = k_frag(kt, f + kManyAhead);
                 }
             extra(f);
@@ -255,14 +260,14 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
         pin(pf);  // sum and probabilities are formed here, beside the matrix instructions, not where they are used
     };
     // Phase B: O^T += V^T.P^T of the tile in pf beside the row maximum of the scores in sn.
-    auto phase_b = [&](auto next, f32x16 (&sn)[2], int vt) __attribute__((always_inline)) {
+    auto phase_b = [&](auto next, f32x16 (&sn)[NB], int vt) __attribute__((always_inline)) {
         __builtin_amdgcn_s_setprio(0);
         float mx[2] = {-INFINITY, -INFINITY};
         bf16x8 va[NP];
 #pragma unroll
         for (int g = 0; g < kManyAhead; ++g) va[g] = v_frag(vt, g);
         __builtin_amdgcn_sched_barrier(0);
-        constexpr int MV = 32 / NP;
+        constexpr int MV = 16 * NB / NP;
 #pragma unroll
         for (int g = 0; g < NP; ++g) {
             o[g % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[g], pf[g / DB], o[g % DB], 0, 0, 0);
@@ -298,15 +303,17 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
 #pragma unroll
         for (int f = 0; f < NA; ++f) ka[f] = k_frag(K0, f);
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sA[nb][r] = 0.f;
 #pragma unroll
-        for (int f = 0; f < NA; ++f) sA[f % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[f], qf[f / 2], sA[f % 2], 0, 0, 0);
+        for (int f = 0; f < NA; ++f) sA[f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[f], qf[f / NB], sA[f % NB], 0, 0, 0);
         hide(sA, nth(0), bad);
         float mx = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(fmaxf(mx, sA[0][r]), sA[1][r]);
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sA[nb][r]);
         raise_max(mx);
     }
     // One tile with a successor: K of tile i + 1 and V of tile i have landed; K of tile i + 2 goes where K of tile i was, V of tile i + 1 where V of tile
@@ -314,7 +321,7 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
     // With scalar loads on their way (what the arguments are read by) the compiler could not tell LDS reads apart by their number: there are none from here on.
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     int ids = 0;
-    auto body = [&](int i, f32x16 (&s)[2], f32x16 (&sn)[2], int k_old, int k_next, int v_cur, int v_next) __attribute__((always_inline)) {
+    auto body = [&](int i, f32x16 (&s)[NB], f32x16 (&sn)[NB], int k_old, int k_next, int v_cur, int v_next) __attribute__((always_inline)) {
         tile_barrier();
         if (i > 0) {
             asm volatile("" : "+v"(ids));
@@ -362,7 +369,7 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
         if (work) {
             if (odd) {
 #pragma unroll
-                for (int nb = 0; nb < 2; ++nb) sA[nb] = sB[nb];
+                for (int nb = 0; nb < NB; ++nb) sA[nb] = sB[nb];
             }
             phase_a(std::false_type{}, sA, sB, K0, [](int) {});
             phase_b(std::false_type{}, sB, even ? V0 : V1);
@@ -382,28 +389,43 @@ template <int D, int WAVES> __device__ __forceinline__ bool chunk_many_rows(cons
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) any |= flags[w];
     if (any) return false;
-    if constexpr (KS == 2) {
-        // the second group hands its sums over through its tiles; word j of thread t lies at j * THREADS + t: consecutive lanes, consecutive words
-        constexpr int THREADS = QW * kWave;
-        static_assert(THREADS * DB * 16 * 4 <= 4 * TILE);
-        float* sums = reinterpret_cast<float*>(tiles + 4 * TILE);
-        const int t = wave * kWave + lane;
-        if (grp == 1) {
-            sh_m[t] = m, sh_l[t] = l;
+    if constexpr (PARTS > 1) {
+        // All parts of a row but the first hand their sums over through the tiles, at their end: the start is where the results leave through. Word j of lane t
+        // lies at j * 64 + t: consecutive lanes, consecutive words.
+        constexpr int WORDS = DB * 16 * kWave;
+        static_assert((PARTS - 1) * QW * WORDS * 4 + QW * TILE <= KS * 4 * TILE);
+        float* sums = reinterpret_cast<float*>(tiles + KS * 4 * TILE) - (PARTS - 1) * QW * WORDS;
+        auto of_part = [&](int p) { return ((p - 1) * QW + rwave); };
+        if (part) {
+            const int at = of_part(part);
+            sh_m[at * kWave + lane] = m, sh_l[at * kWave + lane] = l;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sums[(db * 16 + r) * THREADS + t] = o[db][r];
+                for (int r = 0; r < 16; ++r) sums[at * WORDS + (db * 16 + r) * kWave + lane] = o[db][r];
         }
         __syncthreads();
-        if (grp == 1) return true;
-        const float m1 = sh_m[t], top = fmaxf(m, m1), f0 = __builtin_amdgcn_exp2f((m - top) * c), f1 = __builtin_amdgcn_exp2f((m1 - top) * c);
-        l = l * f0 + sh_l[t] * f1;
-        m = top;
+        if (part) return true;
+        float top = m;
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p) top = fmaxf(top, sh_m[of_part(p) * kWave + lane]);
+        const float f0 = __builtin_amdgcn_exp2f((m - top) * c);
+        l *= f0;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[db][r] = o[db][r] * f0 + sums[(db * 16 + r) * THREADS + t] * f1;
+            for (int r = 0; r < 16; ++r) o[db][r] *= f0;
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p) {
+            const int at = of_part(p);
+            const float f = __builtin_amdgcn_exp2f((sh_m[at * kWave + lane] - top) * c);
+            l = fmaf(sh_l[at * kWave + lane], f, l);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[db][r] = fmaf(sums[at * WORDS + (db * 16 + r) * kWave + lane], f, o[db][r]);
+        }
+        m = top;
     }
     if (rw >= at.s.rows) return true;
 

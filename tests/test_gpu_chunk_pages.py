@@ -75,6 +75,15 @@ def test_lengths_where_cutting_begins(dtype, D, rows):
         run(make(rng, dtype, 3, D, 16, [rows] * len(news), spare=0), dtype, 6, [rows - n for n in news], news)
 
 
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("Hkv", [4, 32, 64])
+@pytest.mark.parametrize("L,news", [([0], [600]), ([700, 33], [90, 470]), ([511], [577])])
+def test_few_and_many_tiles(D, Hkv, L, news):
+    """Batches with fewer tiles than half the compute units, fewer than all of them, and more: three ways to share rows and slots among a workgroup's waves."""
+    rng = np.random.default_rng(Hkv + len(L))
+    run(make(rng, "bf16", Hkv, D, 32, [a + b for a, b in zip(L, news)]), "bf16", Hkv, L, news, pad=1)
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
 @pytest.mark.parametrize("H,Hkv", [(1, 1), (3, 3), (3, 1), (10, 2), (14, 2), (16, 1), (33, 1), (32, 4), (64, 1)])
 def test_query_groups(dtype, D, H, Hkv):
