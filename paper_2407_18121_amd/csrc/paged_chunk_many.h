@@ -377,12 +377,12 @@ __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkI
     }
     // An infinite V has reached the rows that do not see it too, as 0 times infinity. Where anything has come out that is no number the rows are left to
     // chunk_few_rows, which takes care of it.
-    float zero = 0.f;
+    float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) zero = fmaf(o[db][r], 0.f, zero);
-    const bool mine = __any(!(zero == 0.f));
+        for (int r = 0; r < 16; ++r) zero[r % 4] = fmaf(o[db][r], 0.f, zero[r % 4]);
+    const bool mine = __any(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f));
     if (lane == 0) flags[wave_wg] = mine;
     __syncthreads();
     int any = 0;
@@ -390,11 +390,11 @@ __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkI
     for (int w = 0; w < WAVES; ++w) any |= flags[w];
     if (any) return false;
     if constexpr (PARTS > 1) {
-        // All parts of a row but the first hand their sums over through the tiles, at their end: the start is where the results leave through. Word j of lane t
-        // lies at j * 64 + t: consecutive lanes, consecutive words.
-        constexpr int WORDS = DB * 16 * kWave;
-        static_assert((PARTS - 1) * QW * WORDS * 4 + QW * TILE <= KS * 4 * TILE);
-        float* sums = reinterpret_cast<float*>(tiles + KS * 4 * TILE) - (PARTS - 1) * QW * WORDS;
+        // All parts of a row but the first hand their sums over through the tiles, at their end: the start is where the results leave through. Four words j of
+        // lane t lie at 16 (j * 64 + t): consecutive lanes, consecutive addresses.
+        constexpr int WORDS = DB * 4 * kWave;  // of 16 bytes
+        static_assert((PARTS - 1) * QW * WORDS * 16 + QW * TILE <= KS * 4 * TILE);
+        f32x4* sums = reinterpret_cast<f32x4*>(tiles + KS * 4 * TILE) - (PARTS - 1) * QW * WORDS;
         auto of_part = [&](int p) { return ((p - 1) * QW + rwave); };
         if (part) {
             const int at = of_part(part);
@@ -402,7 +402,7 @@ __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkI
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sums[at * WORDS + (db * 16 + r) * kWave + lane] = o[db][r];
+                for (int g = 0; g < 4; ++g) sums[at * WORDS + (db * 4 + g) * kWave + lane] = f32x4{o[db][g * 4], o[db][g * 4 + 1], o[db][g * 4 + 2], o[db][g * 4 + 3]};
         }
         __syncthreads();
         if (part) return true;
@@ -423,7 +423,11 @@ __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkI
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[db][r] = fmaf(sums[at * WORDS + (db * 16 + r) * kWave + lane], f, o[db][r]);
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 y = sums[at * WORDS + (db * 4 + g) * kWave + lane];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) o[db][g * 4 + t] = fmaf(y[t], f, o[db][g * 4 + t]);
+                }
         }
         m = top;
     }
