@@ -286,3 +286,42 @@ def test_tokens_that_overlap_stay_inside(dtype, D, T, slots):
             assert ec.ec_paged_chunk_step(q, k, v, table, i(start), i(starts), 0.1, out[:T], ws[:size], lse[:T]) == ec.EC_OK
             torch.cuda.synchronize()
             assert (ws[size:] == 77).all() and (out[T:] == 5.5).all() and (lse[T:] == 6.5).all()
+
+
+@pytest.mark.parametrize("dtype,D,H", [("bf16", 128, 1), ("bf16", 64, 40), ("f32", 64, 1)])
+def test_the_longest_cache(dtype, D, H):
+    """2^28 slots, the most there are, all on one page: every row of it counts equally often, so that the output is that of the page alone. A lane adds up to 2^28 / (256
+    segments, 4 waves, 16 slots) = 16384 times 1 to 4 numbers of its own: within 2^16 roundings."""
+    page, rng = 256, np.random.default_rng(4)
+    pool = make(rng, dtype, 1, D, page, [page], spare=0)
+    q = quantize(rng.standard_normal((1, H, D)), dtype)
+    pool.table = np.zeros((1, 1), np.int32)
+    want, tol, lse, lse_tol = ref.chunk(pool, q, [page - 1], [0, 1], D ** -0.5, dtype)
+    i = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    out, got_lse = torch.empty(1, H, D, dtype=torch_dtype(dtype), device="cuda"), torch.empty(1, H, device="cuda")
+    ws = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, 1, H, 1, D, ec.EC_BF16 if dtype == "bf16" else ec.EC_F32)
+    table = torch.zeros((1, 2 ** 28 // page), dtype=torch.int32, device="cuda")
+    ec.ec_paged_chunk_step(to_dev(q, dtype), to_dev(pool.k, dtype), to_dev(pool.v, dtype), table, i([2 ** 28 - 1]), i([0, 1]), D ** -0.5, out, ws, got_lse)
+    more = 2.0 ** 16 * ref.U
+    w = np.abs(pool.v).max()
+    assert (np.abs(to_host(out) - want) <= tol + 2 * more * w).all()
+    assert (np.abs(to_host(got_lse) - (lse + 20 * np.log(2))) <= lse_tol + more + 64 * ref.U).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wide_tables(dtype):
+    """A table with room for 2^28 slots gives what one that just holds the sequences does, bit for bit."""
+    H, D, page, L, n = 16, 128, 256, 1500, 2048
+    rng = np.random.default_rng(8)
+    pool = make(rng, dtype, H, D, page, [L + n])
+    q = to_dev(quantize(rng.standard_normal((n, H, D)), dtype), dtype)
+    k, v = to_dev(pool.k, dtype), to_dev(pool.v, dtype)
+    i = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    wide = torch.full((1, 2 ** 28 // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :pool.table.shape[1]] = i(pool.table)
+    ws = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, 1, H, n, D, ec.EC_BF16 if dtype == "bf16" else ec.EC_F32)
+    out = []
+    for table in (i(pool.table), wide):
+        out.append(torch.empty_like(q))
+        ec.ec_paged_chunk_step(q, k, v, table, i([L]), i([0, n]), D ** -0.5, out[-1], ws)
+    assert torch.equal(out[0], out[1]) and not torch.isnan(out[0]).any()
