@@ -112,12 +112,15 @@ struct ChunkCut {
     int whole, segments, each;
 };
 // What all of them are cut by: the units that are a place's share of the whole batch, and the rounds that segments may take.
-template <int UNIT> struct ChunkShare {
-    int units, rounds;
+// ONE: whether a launch can have one round only, which four waves of bf16 never have.
+template <int UNIT, bool ONE> struct ChunkShare {
+    int units, rounds;  // rounds 0: one, in which segments of at most `units` find places
     // Units of a segment, at least: as many as its results, written and read again, take the time of (with 4 instead of 8 slots a row 2048 first tokens of 32
     // heads 110 us instead of 64), or half as many where workgroups would have nothing to do (8 drafts of 32 tokens over 2900 rows 33.4 us instead of 41.3,
     // with 6 36.3)
     __device__ __forceinline__ int least(const ChunkSeq& s) const { return max(min(s.rows, s.tile_rows) * (rounds > 1 ? 8 : 4), 256) / UNIT; }
+    // Segments of a tile of U units of at most `units` each, but no less than `floor`.
+    __device__ __forceinline__ int segments(int U, int floor) const { return max(min(about(U + units - 1, low_rcp(units)), about(U, low_rcp(floor))), 1); }
     // A tile of U units, against a share of A:
     //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
     //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
@@ -128,7 +131,9 @@ template <int UNIT> struct ChunkShare {
         const int U = s.units, floor = least(s), A = max(units, floor);
         const float low = low_rcp(A);
         int n = 1, whole = 0;
-        if (U > A) {
+        if (ONE && !rounds) {
+            n = segments(U, floor);
+        } else if (U > A) {
             n = about(U, low);
             if (rounds > 1 && U < 4 * A) {
                 int time = about(U + n - 1, low_rcp(n));
@@ -149,7 +154,7 @@ template <int UNIT> struct ChunkShare {
         return {whole, n, divided(U + n - 1, n)};
     }
 };
-template <int UNIT, int PLACES, class N> __device__ __forceinline__ ChunkShare<UNIT> chunk_share_of(const ChunkStep& a, N all, N most)
+template <int UNIT, bool ONE, int PLACES, class N> __device__ __forceinline__ ChunkShare<UNIT, ONE> chunk_share_of(const ChunkStep& a, N all, N most)
 {
     // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
     const N share = a.rounds > 1 ? (all + (2 * PLACES - 1)) / (2 * PLACES) : (most + (PLACES - 1)) / PLACES;
@@ -158,7 +163,7 @@ template <int UNIT, int PLACES, class N> __device__ __forceinline__ ChunkShare<U
     return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
 }
 // s: of this lane's sequence afterwards, if there are no more than lanes
-template <int MANY, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<UNIT> chunk_share(const ChunkStep& a, ChunkSeq& s)
+template <int MANY, int UNIT, bool ONE, int PLACES> __device__ __forceinline__ ChunkShare<UNIT, ONE> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
     if (!a.cut) {  // a share that no tile exceeds
         if (a.B <= kWave) s.read<MANY, UNIT>(a, threadIdx.x % kWave);
@@ -171,7 +176,14 @@ template <int MANY, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<
             const int units = wave_scan(s.tiles * s.units), both = wave_scan(s.tiles * (s.units + s.first_units));
             most += last_lane(units), all += last_lane(both);
         }
-        return chunk_share_of<UNIT, PLACES>(a, all * a.Hkv, most * a.Hkv);
+        const auto share = chunk_share_of<UNIT, ONE, PLACES>(a, all * a.Hkv, most * a.Hkv);
+        if (ONE && a.rounds == 1 && a.B <= kWave) {  // the least units by which all segments find places at once, if a few more than the share do
+            for (int more = 0; more < 4; ++more) {
+                const ChunkShare<UNIT, ONE> finer = {share.units + more, 0};
+                if (last_lane(wave_scan(s.tiles * finer.segments(s.units, finer.least(s)))) * a.Hkv <= PLACES) return finer;
+            }
+        }
+        return share;
     }
     unsigned long long all = 0, most = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
@@ -179,7 +191,7 @@ template <int MANY, int UNIT, int PLACES> __device__ __forceinline__ ChunkShare<
         all += wave_sum((long long)s.tiles * (s.units + s.first_units));
         most += wave_sum((long long)s.tiles * s.units);
     }
-    return chunk_share_of<UNIT, PLACES>(a, all * a.Hkv, most * a.Hkv);
+    return chunk_share_of<UNIT, ONE, PLACES>(a, all * a.Hkv, most * a.Hkv);
 }
 
 // Units that a tile's last row sees.
@@ -200,7 +212,7 @@ struct ChunkItem {
 };
 // The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
 // which sees most, then segments. s: as chunk_share leaves it.
-template <int MANY, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s, int id, int wave)
+template <int MANY, int UNIT, bool ONE> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT, ONE>& share, ChunkSeq& s, int id, int wave)
 {
     const int lane = lane_anew(), j = (int)(__umulhi((uint32_t)id << 2, a.heads_mul) >> a.heads_shift), hk = id - j * a.Hkv;
     int before = 0, parts_before = 0;  // parts: and cut tiles in the high half, both at most kChunkParts
@@ -242,7 +254,7 @@ template <int MANY, int UNIT> __device__ __forceinline__ ChunkItem chunk_item(co
     }
     return it;
 }
-template <int MANY, int UNIT> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT>& share, ChunkSeq& s)
+template <int MANY, int UNIT, bool ONE> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT, ONE>& share, ChunkSeq& s)
 {
     int n = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
@@ -842,7 +854,7 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
     __shared__ int flags[WAVES];
     const int first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     ChunkSeq s;
-    const auto share = chunk_share<MANY, UNIT, kChunkPlaces<DT, D, WAVES>>(first, s);
+    const auto share = chunk_share<MANY, UNIT, (DT == EC_F32 || WAVES == kManyWaves), kChunkPlaces<DT, D, WAVES>>(first, s);
     if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<MANY, UNIT>(first, share, s);
     auto take = [&](const ChunkStep& a, const ChunkItem& at, int wave) __attribute__((always_inline)) {
         if (!at.s.live) {
