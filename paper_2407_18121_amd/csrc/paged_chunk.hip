@@ -7,7 +7,7 @@
 // into several segments, whose results meet in a second launch by the rule of the softmax: with M the largest of their maxima m_i,
 // out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
 //
-// Few rows are bound by the bytes of K and V (8 sequences of up to 2900 rows H32/8 D128 bf16 with 5 tokens each: 58 MB, 22.8 us, of which 8 before the first
+// Few rows are bound by the bytes of K and V (8 sequences of up to 2900 rows H32/8 D128 bf16 with 5 tokens each: 58 MB, 21.9 us, of which 8 before the first
 // load, between the last and the output and in the second launch; 8 of 1000 rows H32 fp32 with one: 262 MB, 49 us, 5.4 TB/s), many rows by the matrix pipes (2048
 // tokens behind 65000 rows H40/8: 2.55 ms, 1.09 PFLOP/s; fp32, 1024 first tokens of 32 heads: 133 us, 65 TFLOP/s).
 #include <algorithm>
