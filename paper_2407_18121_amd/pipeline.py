@@ -307,7 +307,8 @@ class PagedTokens:
 
     A sequence that the free pages do not hold, or whose tokens end behind the last of `tokens`, keeps what it has: its tokens get zeros, len_b and seen_b do not
     grow, start_b is -1. Rows of out behind the last sequence's tokens are left as they are.
-    Compressed prompts come in as rows: admit(places, rows, seen), begin() without tokens for them, store() in every layer where start_b has the rows.
+    Compressed prompts come in as rows: admit(places, rows, seen), which takes their pages or is refused, then store() in every layer before the first step that has
+    tokens for them (until then the pages hold what others left there).
     New rows' masses are 0 (what adds to masses is ec_paged_decode_score_step)."""
 
     def __init__(self, layers, places, tokens, H, Hkv, D, page, n_pages, max_pages, dtype: torch.dtype, freq, mscale=1.0, interleaved=False, G=1, device="cuda"):
@@ -322,6 +323,7 @@ class PagedTokens:
         self.len_b, self.seen_b, self.new_b = ints(places, fill=-1), ints(places), ints(places)  # rows (-1: no sequence), tokens seen, tokens of the next step
         self.start_b, self.token_start = ints(places, fill=-1), ints(places + 1)
         self.rows, self.pos = torch.full((tokens,), -1, dtype=torch.int64, device=device), ints(tokens)
+        self.prompts = set()  # places that were admitted with rows
         self.freq = freq
         self.turned = torch.zeros((tokens, H, D), dtype=dtype, device=device)
         self.ws = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, places, H, tokens, D, ec.dtype_code(self.k_pages), device)
@@ -332,20 +334,32 @@ class PagedTokens:
         places = list(places)
         if len(set(places)) != len(places) or any(not 0 <= b < self.table.shape[0] for b in places):
             raise ValueError(f"{places} are not different places of 0 .. {self.table.shape[0] - 1}")
+        self.prompts.difference_update(places)
         at = torch.tensor(places, dtype=torch.int64).to(self.table.device)
         for x, values in ((self.len_b, rows), (self.seen_b, seen)):
             x.index_copy_(0, at, torch.tensor(values, dtype=torch.int32).to(x.device))
 
     def admit(self, places, rows=None, seen=None):
-        """Sequences that start with `rows` rows of prompts of `seen` tokens, none by default; a place's earlier sequence is gone. Their pages come with begin()."""
+        """Sequences that start with `rows` rows of prompts of `seen` tokens, none by default; a place's earlier sequence is gone. Rows get their pages here, and where
+        the free ones (those of places released before among them) or a table do not hold them all, the places are left free. Pages of tokens come with begin()."""
         places = list(places)
         rows, seen = (list(x) if x is not None else [0] * len(places) for x in (rows, seen))
         if not len(places) == len(rows) == len(seen) or any(n < 0 for n in rows):
             raise ValueError(f"places {places}, rows {rows} and seen {seen} do not belong together")
         self._set(places, rows, seen)
+        if not any(rows):
+            return
+        start, nothing, first = torch.empty_like(self.len_b), torch.zeros_like(self.new_b), torch.empty_like(self.token_start)
+        ec.ec_paged_plan(self.len_b, nothing, self.table, self.held, self.free_pages, self.n_free, self.page, start, self.len_b, first, T=1)
+        start = start.tolist()
+        refused = [b for b in places if start[b] < 0]
+        if refused:
+            self._set(places, [-1] * len(places), [0] * len(places))
+            raise ValueError(f"{[n for b, n in zip(places, rows) if b in refused]} rows for places {refused}: too few free pages, or more rows than a table holds")
+        self.prompts.update(b for b, n in zip(places, rows) if n)
 
     def release(self, places):
-        """Sequences that are over; their pages are free with the next begin()."""
+        """Sequences that are over; their pages are free with the next begin() or the next rows that admit() takes in."""
         places = list(places)
         self._set(places, [-1] * len(places), [0] * len(places))
 
@@ -356,7 +370,10 @@ class PagedTokens:
 
     def store(self, layer, places, k, v, pos, mass, n_rows_b=None):
         """Rows 0.. of k, v [len(places),Hkv,n,D], pos and mass [len(places),G,n] as the first rows of the sequences (n_rows_b int32 of each, all by default)."""
-        table = self.table.index_select(0, torch.tensor(list(places), dtype=torch.int64).to(self.table.device))
+        places = list(places)
+        if not self.prompts.issuperset(places):
+            raise ValueError(f"places {[b for b in places if b not in self.prompts]} were not admitted with rows")
+        table = self.table.index_select(0, torch.tensor(places, dtype=torch.int64).to(self.table.device))
         ec.ec_paged_store(k, v, pos, mass, table, self.k_pages[layer], self.v_pages[layer], self.pos_pages[layer], self.mass_pages[layer], None, n_rows_b)
 
     def attend(self, layer, q, k, v, scale, out, lse=None):
