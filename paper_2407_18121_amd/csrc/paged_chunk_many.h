@@ -217,8 +217,10 @@ __device__ __forceinline__ bool chunk_many_rows(const ChunkStep& a, const ChunkI
                 for (int r = 0; r < 16; ++r) sn[nb][r] = 0.f;
             __builtin_amdgcn_sched_barrier(0);
         }
+        // s c - m c in one step is off by the rounding of m c, 2^-24 |m c|: where that counts (from 2^32 on it would take all weights out of the range),
+        // differences first, as everywhere else
         float minus = -m * c;
-        if (__builtin_expect(__any(!(fabsf(minus) < 3e38f)), 0)) {  // a maximum whose product with the scale has left the range: differences first
+        if (__builtin_expect(__any(!(fabsf(minus) < 0x1p13f)), 0)) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
