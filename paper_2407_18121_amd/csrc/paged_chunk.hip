@@ -500,26 +500,8 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
         }
 
         if constexpr (T::kHalf) {
-            constexpr int PV = BLOCKS * 4;  // probabilities of a lane
-            typedef __attribute__((ext_vector_type(PV))) __bf16 bf16xp;
-            struct Parts {
-                bf16xp of[3];
-            };
-            auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
-            // none of the three numbers of a probability that is not 0 is 0, so that an infinite V stays infinite
-            auto split = [&](float x, int e, Parts& to) __attribute__((always_inline)) {
-                const float high = cut(x), rest = x - high, middle = cut(rest);
-                to.of[0][e] = (__bf16)high;
-                to.of[1][e] = (__bf16)fmaxf(middle, x * 0x1p-24f);
-                to.of[2][e] = (__bf16)fmaxf(rest - middle, x * 0x1p-25f);
-            };
-            // x + V^T . P^T of 16 features, P one of its parts
-            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& part, f32x4 x) __attribute__((always_inline)) {
-                if constexpr (BLOCKS == 2)
-                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), part, x, 0, 0, 0);
-                else
-                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, part), x, 0, 0, 0);
-            };
+            using Parts = WeightParts<BLOCKS>;
+            constexpr int PV = Parts::N;
             if (masked) {
                 // An infinite V must not reach the rows that do not see it, as 0 times infinity would: it leaves the product, and every row adds the
                 // kinds that it sees.
@@ -533,7 +515,7 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
                     }
                 if (__builtin_expect(__any(some), 0)) {
                     constexpr float kinds[3] = {INFINITY, -INFINITY, NAN};
-                    bf16xp ones[RB];
+                    typename Parts::bf16xn ones[RB];
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -551,7 +533,7 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
                             }
 #pragma unroll
                             for (int rb = 0; rb < RB; ++rb) {
-                                const f32x4 n = multiply(of_kind, ones[rb], f32x4{0.f, 0.f, 0.f, 0.f});
+                                const f32x4 n = Parts::multiply(of_kind, ones[rb], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) o[rb][i][r] += n[r] > 0.f ? kinds[kind] : 0.f;
                             }
@@ -569,11 +551,11 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
             for (int rb = 0; rb < RB; ++rb) {
                 Parts parts;
 #pragma unroll
-                for (int e = 0; e < PV; ++e) split(p[rb][e / 4][e % 4], e, parts);
+                for (int e = 0; e < PV; ++e) parts.set(e, p[rb][e / 4][e % 4]);
 #pragma unroll
                 for (int part = 0; part < 3; ++part)
 #pragma unroll
-                    for (int i = 0; i < OB; ++i) o[rb][i] = multiply(vh[i], parts.of[part], o[rb][i]);
+                    for (int i = 0; i < OB; ++i) o[rb][i] = Parts::multiply(vh[i], parts.of[part], o[rb][i]);
             }
         } else {
             if (masked) {

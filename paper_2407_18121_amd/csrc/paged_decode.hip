@@ -25,7 +25,6 @@ constexpr int kWholeRounds = 3;       // a pair of so many rounds is not cut: 60
 constexpr int kLengths = 1024;        // of a batch that are held in LDS
 constexpr int kMostSegments = 256;   // of a pair, whose weights have to fit into LDS when they are joined
 constexpr int kHeadBlock = 16;       // query heads of a pair, at most
-constexpr float kSmallExponent = -100.f, kSmall = 0x1p-100f;  // probabilities below it are looked at apart
 
 // The scale in base-2 units, log2(e) * scale. fp32: q takes all of it. bf16: q takes the power of two, 2^exponent, that leaves 1 .. 2 for the
 // differences of scores, so that no sum leaves the range that the score itself stays in.
@@ -430,28 +429,10 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
         l += sum;
 
         if constexpr (T::kHalf) {
-            // a probability enters as the sum of three bf16 numbers, its 24 bits cut into eights (what is left is not negative); none of those of one that
-            // is not 0 is 0, so that an infinite V stays infinite: 2^-24 and 2^-25 of it at least, less than its last bit. (Two numbers, 2^-16 off: B1 H32 640 rows
-            // 8.4 us, with three 8.5; B16 H32 870 rows 38.8, 39.2; two of them in one instruction of 32 rows, which their V has to be copied for: the same.)
-            constexpr int PV = BLOCKS * 4;  // probabilities of a lane
-            typedef __attribute__((ext_vector_type(PV))) __bf16 bf16xp;
-            struct Parts {
-                bf16xp of[3];
-            };
-            auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
-            auto split = [&](float x, int e, Parts& to) __attribute__((always_inline)) {
-                const float high = cut(x), rest = x - high, middle = cut(rest);
-                to.of[0][e] = (__bf16)high;
-                to.of[1][e] = (__bf16)fmaxf(middle, x * 0x1p-24f);
-                to.of[2][e] = (__bf16)fmaxf(rest - middle, x * 0x1p-25f);
-            };
-            // x + V^T . P^T of 16 features, P one of its parts
-            auto multiply = [](const bf16x4(&v)[BLOCKS], const bf16xp& part, f32x4 x) __attribute__((always_inline)) {
-                if constexpr (BLOCKS == 2)
-                    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), part, x, 0, 0, 0);
-                else
-                    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, part), x, 0, 0, 0);
-            };
+            // a probability enters as the sum of three bf16 numbers. (Two numbers, 2^-16 off: B1 H32 640 rows 8.4 us, with three 8.5; B16 H32 870 rows 38.8,
+            // 39.2; two of them in one instruction of 32 rows, which their V has to be copied for: the same.)
+            using Parts = WeightParts<BLOCKS>;
+            constexpr int PV = Parts::N;
             // weights whose parts would leave bf16's range, which count where V is large enough: apart, times 2^64. A row is in one of the two products
             // and weighs 0 in the other, which an infinite V does not bear: V's infinities and NaN are taken out of both, with a weight of 1.
             Parts parts;
@@ -466,29 +447,29 @@ __global__ __launch_bounds__(kPagedWaves* kWave, (PagedTile<DT, D>::kResident)) 
                         const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), is = (v & (short)0x7f80) == (short)0x7f80;
                         unbounded[t] = __builtin_bit_cast(bf16x4, v & is), vh[i][t] = __builtin_bit_cast(bf16x4, v & ~is);
                     }
-                    o[i] = multiply(unbounded, parts.of[0], o[i]);
+                    o[i] = Parts::multiply(unbounded, parts.of[0], o[i]);
                 }
 #pragma unroll
                 for (int e = 0; e < PV; ++e) {
                     float& x = p[e / 4][e % 4];
-                    split(x < kSmall ? x * 0x1p64f : 0.f, e, parts);
+                    parts.set(e, x < kSmall ? x * 0x1p64f : 0.f);
                     x = x < kSmall ? 0.f : x;
                 }
 #pragma unroll
                 for (int i = 0; i < OB; ++i) {
                     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int part = 0; part < 3; ++part) x = multiply(vh[i], parts.of[part], x);
+                    for (int part = 0; part < 3; ++part) x = Parts::multiply(vh[i], parts.of[part], x);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[i][r] = fmaf(x[r], 0x1p-64f, o[i][r]);
                 }
             }
 #pragma unroll
-            for (int e = 0; e < PV; ++e) split(p[e / 4][e % 4], e, parts);
+            for (int e = 0; e < PV; ++e) parts.set(e, p[e / 4][e % 4]);
 #pragma unroll
             for (int part = 0; part < 3; ++part)
 #pragma unroll
-                for (int i = 0; i < OB; ++i) o[i] = multiply(vh[i], parts.of[part], o[i]);
+                for (int i = 0; i < OB; ++i) o[i] = Parts::multiply(vh[i], parts.of[part], o[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < OB; ++i) {  // block i / 4 of 64 features, rows 4 quarter + i % 4

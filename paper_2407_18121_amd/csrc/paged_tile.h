@@ -80,6 +80,32 @@ __device__ __forceinline__ float head_sum(float x)
     return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
+constexpr float kSmallExponent = -100.f, kSmall = 0x1p-100f;  // probabilities below it are looked at apart
+
+// Probabilities of a lane, 4 of every block of 16 rows, as sums of three bf16 numbers each, their 24 bits cut into eights (what is left is not negative); none
+// of those of one of kSmall and more is 0, so that an infinite V stays infinite: 2^-24 and 2^-25 of it at least, less than its last bit.
+template <int BLOCKS> struct WeightParts {
+    static constexpr int N = BLOCKS * 4;
+    typedef __attribute__((ext_vector_type(N))) __bf16 bf16xn;
+    bf16xn of[3];
+    __device__ __forceinline__ void set(int e, float x)
+    {
+        auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+        const float high = cut(x), rest = x - high, middle = cut(rest);
+        of[0][e] = (__bf16)high;
+        of[1][e] = (__bf16)fmaxf(middle, x * 0x1p-24f);
+        of[2][e] = (__bf16)fmaxf(rest - middle, x * 0x1p-25f);
+    }
+    // x + V^T . P^T of 16 features, P one of the parts
+    static __device__ __forceinline__ f32x4 multiply(const bf16x4 (&v)[BLOCKS], const bf16xn& part, f32x4 x)
+    {
+        if constexpr (BLOCKS == 2)
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), part, x, 0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, part), x, 0, 0, 0);
+    }
+};
+
 __device__ __forceinline__ int divided(int x, int by)  // 0 <= x < 2^24, by > 0
 {
     const int q = (int)((float)x * __builtin_amdgcn_rcpf((float)by)), r = x - q * by;
