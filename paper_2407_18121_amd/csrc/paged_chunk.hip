@@ -461,7 +461,7 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
         }
 
         const bool masked = bad || row + TR - 1 > lowest;  // some row does not see some slot of the tile
-        float p[RB][BLOCKS][4];
+        float p[RB][BLOCKS][4], least = 0.f;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             if (masked) {
@@ -493,7 +493,9 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
             for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    p[rb][t][r] = __builtin_amdgcn_exp2f((s[rb][t][r] - m[rb]) * of_diff);
+                    const float x = (s[rb][t][r] - m[rb]) * of_diff;
+                    if constexpr (T::kHalf) least = fminf(least, x);
+                    p[rb][t][r] = __builtin_amdgcn_exp2f(x);
                     sum += p[rb][t][r];
                 }
             l[rb] += sum;
@@ -502,9 +504,19 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
         if constexpr (T::kHalf) {
             using Parts = WeightParts<BLOCKS>;
             constexpr int PV = Parts::N;
-            if (masked) {
-                // An infinite V must not reach the rows that do not see it, as 0 times infinity would: it leaves the product, and every row adds the
-                // kinds that it sees.
+            // Weights whose parts would leave bf16's range, which count where V is large enough, enter apart, times 2^64.
+            bool small = __any(least < kSmallExponent);
+            if (__builtin_expect(small, 0)) {
+                bool some = false;  // what is not seen, and scores of -inf, whose weight is 0 either way, are none of them
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int e = 0; e < PV; ++e) some |= p[rb][e / 4][e % 4] > 0.f && p[rb][e / 4][e % 4] < kSmall;
+                small = __any(some);
+            }
+            if (masked || small) {
+                // An infinite V must not reach the rows that do not see it, as 0 times infinity would, nor those whose weight for it is in the other product: it
+                // leaves the products, and every row adds the kinds that it sees.
                 bool some = false;
 #pragma unroll
                 for (int i = 0; i < OB; ++i)
@@ -550,6 +562,22 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 Parts parts;
+                if (__builtin_expect(small, 0)) {
+#pragma unroll
+                    for (int e = 0; e < PV; ++e) {
+                        float& x = p[rb][e / 4][e % 4];
+                        parts.set(e, x < kSmall ? x * 0x1p64f : 0.f);
+                        x = x < kSmall ? 0.f : x;
+                    }
+#pragma unroll
+                    for (int i = 0; i < OB; ++i) {
+                        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int part = 0; part < 3; ++part) x = Parts::multiply(vh[i], parts.of[part], x);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[rb][i][r] = fmaf(x[r], 0x1p-64f, o[rb][i][r]);
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < PV; ++e) parts.set(e, p[rb][e / 4][e % 4]);
 #pragma unroll

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import paged_ref
 import token_ref as ref
 from paper_2407_18121_amd import binding as ec
 from util import quantize, to_dev, to_host, torch_dtype
@@ -51,3 +52,55 @@ def test_large_scores(dtype, D, L, n, H, score, sign):
         tol = (m + 40) * ref.U * np.abs(rows).mean(0) + np.abs(want) * ref.STEP[dtype]
         assert (np.abs(out[i] - want) <= tol).all(), (i, np.abs(out[i] - want).max())
         assert (np.abs(lse[i] - (top + np.log(m))) <= 2 * ref.U * abs(top) + (m + 40) * ref.U).all()
+
+
+def definition(k, v, q, L, dtype, scale, page=16):
+    """ref.chunk of one sequence and key/value head whose pages lie in order."""
+    N = -(-len(k) // page)
+    pages = [np.concatenate([x, np.zeros((N * page - len(x), x.shape[1]), x.dtype)]).reshape(N, 1, page, -1) for x in (k, v)]
+    z = np.zeros((N, 1, page))
+    pool = paged_ref.Pool(pages[0], pages[1], z.astype(np.int32), z, np.arange(N, dtype=np.int32)[None])
+    return ref.chunk(pool, q, [L], [0, len(q)], scale, dtype)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,H", [(1, 1), (3, 1), (20, 1), (5, 16), (100, 1), (200, 1)])
+@pytest.mark.parametrize("below", [90, 105, 115, 124])
+def test_infinite_values_of_small_weights(dtype, D, n, H, below):
+    """Rows of weight 2^-below of the others', one that all tokens see and one that comes with the first of them: their infinities stay infinite, beside those of
+    ordinary rows too."""
+    rng = np.random.default_rng(n + below)
+    L = 130
+    q, k = np.zeros((n, H, D), np.float32), np.zeros((L + n, D), np.float32)
+    q[:, :, 0] = 1
+    v = quantize(rng.standard_normal((L + n, D)), dtype)
+    k[[37, L], 0] = -below
+    v[37, [2, 3, 4, 5]] = np.inf, -np.inf, np.inf, np.nan
+    v[L, [4, 6, 7, 8]] = -np.inf, np.inf, -np.inf, np.nan
+    v[36, [9, 4]] = np.inf, np.inf
+    v[L + n - 1, 10] = -np.inf
+    out, lse = run(k, v, q, L, dtype, float(np.log(2)))
+    want, tol, want_lse, lse_tol = definition(k, v, q, L, dtype, float(np.log(2)))
+    ok = ref.fits(out, want, tol)
+    assert ok.all(), (np.argwhere(~ok)[:6].tolist(), out[~ok][:6], want[~ok][:6])
+    assert (np.abs(lse - want_lse) <= lse_tol).all()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,H", [(1, 16), (2, 16), (16, 2)])
+@pytest.mark.parametrize("below", [60, 104, 118, 124])
+def test_small_weights_are_held_in_24_bits(dtype, D, n, H, below):
+    """Two rows of weights near 2^-below of the others', large enough in V to be all that comes out, nearly cancel in the features of a head or two: what their weights are off by shows."""
+    rng = np.random.default_rng(7)
+    L = 40
+    q, k, v = np.zeros((n, H, D), np.float32), np.zeros((L + n, D), np.float32), np.zeros((L + n, D), np.float32)
+    u = quantize(rng.uniform(0.1, 1.0, (n, H)), dtype)
+    q[:, :, 0], q[:, :, 1] = 1, u
+    k[[5, 30], 0], k[5, 1] = -below, -1
+    v[5] = 2.0 ** 100
+    w = np.resize(u, D)
+    v[30] = -quantize(2.0 ** 100 * np.exp2(-w.astype(np.float64)), dtype)
+    out, _ = run(k, v, q, L, dtype, float(np.log(2)))
+    want, tol, _, _ = definition(k, v, q, L, dtype, float(np.log(2)))
+    ok = np.abs(out - want) <= tol
+    assert ok.all(), (np.argwhere(~ok)[:6].tolist(), out[~ok][:6], want[~ok][:6], tol[~ok][:6])
