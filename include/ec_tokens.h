@@ -82,8 +82,8 @@ int ec_paged_rotary_store(const void* q, const void* k, const void* v, int64_t q
  *   ws              DEVICE scratch, ec_workspace_bytes(EC_FN_PAGED_CHUNK_STEP, B,H,T,D,dt), of one call at a time
  * Requires T <= 2^24, T * H <= 2^30.  Products are formed on the matrix cores with fp32 accumulation, sums and the softmax in fp32.  Where a sequence of bf16
  * brings more than 32 tokens times query heads of a key/value head, its weights enter the product with V rounded to bf16 (their sum does not); with
- * fewer, and in fp32, they enter with all 24 bits.  A weight below the range of normal fp32 numbers, 2^-126 of the largest, is 0.  An infinite or NaN row
- * of V reaches the tokens that see it, and no others.  ws needs no contents.  Results are deterministic: a row's sum is formed in an order that depends on
+ * fewer, and in fp32, they enter with all 24 bits.  A weight below the range of normal fp32 numbers, 2^-126 of the largest, may count as 0, and an infinite V
+ * with it gives NaN then.  An infinite or NaN row of V reaches the tokens that see it, and no others.  ws needs no contents.  Results are deterministic: a row's sum is formed in an order that depends on
  * the lengths of the whole batch and on T, not on time.
  */
 int ec_paged_chunk_step(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table, const int32_t* start_b,

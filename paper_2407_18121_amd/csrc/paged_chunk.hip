@@ -286,6 +286,23 @@ template <int DT, int D, int WAVES> __device__ __forceinline__ void chunk_nothin
     }
 }
 
+// Values that are no numbers, summed over up to 32 rows of V by kind: +inf counts 1, -inf 64 and NaN 4096 where the row has a weight, and 2^18 times that, which
+// is NaN whichever it is, where it is seen with a weight of 0.
+__device__ __forceinline__ float kind_of(float v) { return v == INFINITY ? 1.f : v == -INFINITY ? 64.f : v != v ? 4096.f : 0.f; }
+__device__ __forceinline__ bf16x4 kind_of(bf16x4 v_)
+{
+    const s16x4 v = __builtin_bit_cast(s16x4, v_), inf = (short)0x7f80 - (s16x4){0, 0, 0, 0};
+    return __builtin_bit_cast(bf16x4, ((v == inf) & (short)0x3f80) | ((v == (inf | (short)0x8000)) & (short)0x4280) | (((v & (short)0x7fff) > inf) & (short)0x4580));
+}
+__device__ __forceinline__ float kind_weight(float p, bool seen) { return p > 0.f ? 1.f : seen ? 0x1p18f : 0.f; }
+__device__ __forceinline__ float with_kinds(float x, float n)
+{
+    const int kinds = (int)fminf(n, 4096.f);
+    x += kinds & 0x3f ? INFINITY : 0.f;
+    x += kinds & 0xfc0 ? -INFINITY : 0.f;
+    return x + (kinds & 0x1000 ? NAN : 0.f);
+}
+
 // Up to 16 RB rows: the workgroup's waves share the slots, a wave takes every WAVES-th tile of TR of them and keeps a running (maximum, sum,
 // weighted V) for the rows.
 //   S^T = K . Q^T      matrix instructions, so that a lane owns one row in 16 and 4 consecutive slots of a block of 16
@@ -461,6 +478,7 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
         }
 
         const bool masked = bad || row + TR - 1 > lowest;  // some row does not see some slot of the tile
+        auto sees = [&](int upto, int t, int r) __attribute__((always_inline)) { return row + t * 16 + quarter * 4 + r <= upto && !(bad >> (t * 2 + quarter / 2) & 1); };
         float p[RB][BLOCKS][4], least = 0.f;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -468,10 +486,8 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
 #pragma unroll
                 for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = row + t * 16 + quarter * 4 + r;
-                        if (j > limit[rb] || (bad >> (t * 2 + quarter / 2) & 1)) s[rb][t][r] = -INFINITY;
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        if (!sees(limit[rb], t, r)) s[rb][t][r] = -INFINITY;
             }
             float top = s[rb][0][0];
 #pragma unroll
@@ -516,7 +532,7 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
             }
             if (masked || small) {
                 // An infinite V must not reach the rows that do not see it, as 0 times infinity would, nor those whose weight for it is in the other product: it
-                // leaves the products, and every row adds the kinds that it sees.
+                // leaves the products, and every row adds the kinds that it sees, NaN where it sees any kind with a weight of 0.
                 bool some = false;
 #pragma unroll
                 for (int i = 0; i < OB; ++i)
@@ -526,30 +542,26 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
                         some |= (is[0] | is[1] | is[2] | is[3]) != 0;
                     }
                 if (__builtin_expect(__any(some), 0)) {
-                    constexpr float kinds[3] = {INFINITY, -INFINITY, NAN};
-                    typename Parts::bf16xn ones[RB];
+                    typename Parts::bf16xn weights[RB];
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const int upto = anew(limit[rb]);  // (found out again, and not kept from above)
 #pragma unroll
-                        for (int e = 0; e < PV; ++e) ones[rb][e] = p[rb][e / 4][e % 4] > 0.f ? (__bf16)1.f : (__bf16)0.f;
+                        for (int e = 0; e < PV; ++e) weights[rb][e] = (__bf16)kind_weight(p[rb][e / 4][e % 4], sees(upto, e / 4, e % 4));
+                    }
 #pragma unroll
-                    for (int i = 0; i < OB; ++i)
+                    for (int i = 0; i < OB; ++i) {
+                        bf16x4 kinds[BLOCKS];
 #pragma unroll
-                        for (int kind = 0; kind < 3; ++kind) {
-                            bf16x4 of_kind[BLOCKS];
+                        for (int t = 0; t < BLOCKS; ++t) kinds[t] = kind_of(vh[i][t]);
 #pragma unroll
-                            for (int t = 0; t < BLOCKS; ++t) {
-                                const s16x4 v = __builtin_bit_cast(s16x4, vh[i][t]), inf = (short)0x7f80 - (s16x4){0, 0, 0, 0};
-                                const s16x4 is = kind == 0 ? v == inf : kind == 1 ? v == (inf | (short)0x8000) : (v & (short)0x7fff) > inf;
-                                of_kind[t] = __builtin_bit_cast(bf16x4, is & (short)0x3f80);  // 1
-                            }
+                        for (int rb = 0; rb < RB; ++rb) {
+                            const f32x4 n = Parts::multiply(kinds, weights[rb], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) {
-                                const f32x4 n = Parts::multiply(of_kind, ones[rb], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) o[rb][i][r] += n[r] > 0.f ? kinds[kind] : 0.f;
-                            }
+                            for (int r = 0; r < 4; ++r) o[rb][i][r] = with_kinds(o[rb][i][r], n[r]);
                         }
+                        __builtin_amdgcn_sched_barrier(0);  // (one after the other: few registers)
+                    }
 #pragma unroll
                     for (int i = 0; i < OB; ++i)
 #pragma unroll
@@ -593,27 +605,32 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
 #pragma unroll
                     for (int e = 0; e < 4; ++e) some |= !(fabsf(vw[i][e]) < INFINITY);
                 if (__builtin_expect(__any(some), 0)) {
-                    constexpr float kinds[3] = {INFINITY, -INFINITY, NAN};
+                    // (what follows from V and the limits is found out again here, and not kept from above)
 #pragma unroll
-                    for (int kind = 0; kind < 3; ++kind)
+                    for (int i = 0; i < OB; ++i) asm volatile("" : "+v"(vw[i]));
 #pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) {
-                            f32x4 n[OB];
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const int upto = anew(limit[rb]);
+                        f32x4 n[OB];
 #pragma unroll
-                            for (int i = 0; i < OB; ++i) n[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int i = 0; i < OB; ++i) n[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int i = 0; i < OB; ++i)
+                        for (int i = 0; i < OB; ++i) {
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float v = vw[i][e];
-                                    const bool is = kind == 0 ? v == INFINITY : kind == 1 ? v == -INFINITY : v != v;
-                                    n[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.f : 0.f, p[rb][0][i % 4] > 0.f ? 1.f : 0.f, n[i / 4 * 4 + e], 0, 0, 0);
-                                }
-#pragma unroll
-                            for (int i = 0; i < OB; ++i)
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) o[rb][i][r] += n[i][r] > 0.f ? kinds[kind] : 0.f;
+                            for (int e = 0; e < 4; ++e)
+                                n[i / 4 * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kind_of(vw[i][e]), kind_weight(p[rb][0][i % 4], sees(upto, 0, i % 4)),
+                                                                                       n[i / 4 * 4 + e], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);  // (one after the other: few registers)
                         }
+#pragma unroll
+                        for (int i = 0; i < OB; ++i) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) o[rb][i][r] = with_kinds(o[rb][i][r], n[i][r]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < OB; ++i) asm volatile("" : "+v"(vw[i]));
 #pragma unroll
                     for (int i = 0; i < OB; ++i)
 #pragma unroll
@@ -926,8 +943,8 @@ template <int DT, int D, int N> __device__ __forceinline__ void join_few(const C
             if (!(x[g].y == 0.f)) top = fmaxf(top, x[g].x);  // (NaN counts)
 #pragma unroll
         for (int g = 0; g < N; ++g) {
-            const float weight = g >= tile.count || x[g].y == 0.f ? 0.f : exp2f((x[g].x - top) * a.scale_log2e);
-            if (g < tile.count && !(x[g].y == 0.f)) {  // a segment of which the row sees nothing has sums of 0
+            const float weight = x[g].y == 0.f ? 0.f : exp2f((x[g].x - top) * a.scale_log2e);
+            if (g < tile.count) {  // (a segment of which the row sees nothing has sums of 0, one in which it sees scores of -inf only zeros or NaN)
                 sum = fmaf(x[g].y, weight, sum);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(v[g][e], weight, o[e]);

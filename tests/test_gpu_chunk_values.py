@@ -104,3 +104,26 @@ def test_small_weights_are_held_in_24_bits(dtype, D, n, H, below):
     want, tol, _, _ = definition(k, v, q, L, dtype, float(np.log(2)))
     ok = np.abs(out - want) <= tol
     assert ok.all(), (np.argwhere(~ok)[:6].tolist(), out[~ok][:6], want[~ok][:6], tol[~ok][:6])
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("L,n,H", [(0, 2, 1), (130, 1, 1), (130, 3, 1), (130, 20, 1), (100, 5, 16), (100, 100, 1), (130, 200, 1), (3000, 5, 2), (3000, 200, 2)])
+@pytest.mark.parametrize("scores", ["2^-200", "-inf"])
+def test_values_of_no_weight(dtype, D, L, n, H, scores):
+    """Rows that weigh 0: what is infinite or no number in their V gives NaN to every token that sees them, 0 times infinity, whichever tile they lie in, and to no other."""
+    rng = np.random.default_rng(n + L)
+    slots = L + n
+    q, k = np.zeros((n, H, D), np.float32), np.zeros((slots, D), np.float32)
+    q[:, :, 0] = 4 if scores == "-inf" else 1
+    v = quantize(rng.standard_normal((slots, D)), dtype)
+    rows = sorted({r for r in (1, L // 2 + 1, L + 1, L + n // 2, slots - 2, slots - 1) if 1 <= r < slots})  # (row 0 has a weight for everybody)
+    k[rows, 0] = quantize(np.float32(-2.9e38), dtype) if scores == "-inf" else -200
+    scale = 1.0 if scores == "-inf" else float(np.log(2))
+    want, tol, want_lse, lse_tol = definition(k, v, q, L, dtype, scale)
+    for i, r in enumerate(rows):
+        v[r, [3 * i, 3 * i + 1, 3 * i + 2]] = np.inf, -np.inf, np.nan
+        want[[t for t in range(n) if r <= L + t], :, 3 * i:3 * i + 3] = np.nan
+    out, lse = run(k, v, q, L, dtype, scale)
+    ok = ref.fits(out, want, tol)
+    assert ok.all(), (np.argwhere(~ok)[:6].tolist(), out[~ok][:6], want[~ok][:6])
+    assert ref.fits(lse, want_lse, lse_tol).all()
