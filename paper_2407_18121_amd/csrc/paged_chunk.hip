@@ -23,6 +23,7 @@ constexpr int kFewWaves = 4, kManyWaves = 8;
 // Workgroups that the chip holds at once
 template <int DT, int D, int WAVES> constexpr int kChunkPlaces = WAVES == kFewWaves ? PagedTile<DT, D>::kResident * kComputeUnits : kComputeUnits;
 constexpr int kMostPlaces = 2 * kComputeUnits, kChunkParts = 4 * kMostPlaces;  // kChunkParts: segments whose results the workspace holds, at most
+constexpr int kShortUnits = 4;                            // units, of four waves, up to which tiles are never cut
 constexpr int kChunkTiles = 128;                          // tiles from which on segments may take several rounds
 constexpr int kJoinWaves = 4, kJoinGroups = 8;            // waves of a joining workgroup, and workgroups that share a tile's rows
 
@@ -41,7 +42,7 @@ struct ChunkStep {
     int B, T, H, Hkv, group;
     uint32_t group_mul, group_shift;  // x / group = (4 x * group_mul >> 32) >> group_shift for x < 2^30
     uint32_t heads_mul, heads_shift;  // x / Hkv, as above
-    int rounds;
+    int rounds, rounds_64;  // that segments may take, and if tiles of many rows have 64
     bool small;       // the units of all tiles have 29 bits, whatever token_start holds
     bool cut;         // whether tiles may be cut and the second launch follows
     float scale, scale_log2e;
@@ -75,16 +76,12 @@ __device__ __forceinline__ int about(int x, float low) { return (int)(((float)x 
 
 __device__ __forceinline__ int token_of(const ChunkStep& a, int row) { return (int)(__umulhi((uint32_t)row << 2, a.group_mul) >> a.group_shift); }
 
-// Rows of a tile of a sequence with so many: as few as hold them where the bytes of K and V are the bound, so that few matrix instructions are spent on rows
-// that are not there; 128 share what comes in where they are many, in bf16 (32 rows of fp32 take four times as long in the matrix pipe as K and V
-// take to come in from the L2).
-template <int MANY> __device__ __forceinline__ int chunk_tile_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : MANY; }
-
 // What a sequence brings: `tiles` tiles of `tile_rows` rows, `units` units of UNIT slots that its last token sees.
 struct ChunkSeq {
     int L, t0, n, rows, tile_rows, tiles, units, first_units;  // first_units: that the first tile sees
     bool live;
-    template <int MANY, int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b)
+    // many: binary logarithm of the rows of a tile of a sequence with more than 32
+    template <int UNIT> __device__ __forceinline__ void read(const ChunkStep& a, int b, int many)
     {
         L = -1, t0 = n = 0;
         if (b < a.B) {
@@ -95,10 +92,18 @@ struct ChunkSeq {
         const int slots = a.pages.slots();
         live = L >= 0 && L < slots;
         rows = n * a.group;
-        tile_rows = chunk_tile_rows<MANY>(rows);
-        tiles = (rows + tile_rows - 1) >> (tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : MANY == 64 ? 6 : 7);
         units = !n ? 0 : live ? (min(L + n, slots) + UNIT - 1) / UNIT : 1;
-        first_units = !n ? 0 : live ? min(L + token_of(a, min(tile_rows, rows) - 1), slots - 1) / UNIT + 1 : 1;
+        tile<UNIT>(a, many);
+    }
+    // Tiles of as few rows as hold a sequence's where the bytes of K and V are the bound, so that few matrix instructions are spent on rows that are not there;
+    // many share what comes in where they are many, in bf16 (32 rows of fp32 take four times as long in the matrix pipe as K and V take to come in
+    // from the L2).
+    template <int UNIT> __device__ __forceinline__ void tile(const ChunkStep& a, int many)
+    {
+        const int shift = rows <= 16 ? 4 : rows <= 32 ? 5 : many;
+        tile_rows = 1 << shift;
+        tiles = (rows + tile_rows - 1) >> shift;
+        first_units = !n ? 0 : live ? min(L + token_of(a, min(tile_rows, rows) - 1), a.pages.slots() - 1) / UNIT + 1 : 1;
     }
 };
 // Sum over the wave, of numbers below 2^54.
@@ -112,15 +117,20 @@ struct ChunkCut {
     int whole, segments, each;
 };
 // What all of them are cut by: the units that are a place's share of the whole batch, and the rounds that segments may take.
-// ONE: whether a launch can have one round only, which four waves of bf16 never have.
-template <int UNIT, bool ONE> struct ChunkShare {
+// ONE: whether a launch can have one round only, which four waves of bf16 never have. SHORT: units up to which a sequence's tiles are never cut, as the host
+// leaves the second launch away in tables of no more slots.
+template <int UNIT, int SHORT, bool ONE> struct ChunkShare {
     int units, rounds;  // rounds 0: one, in which segments of at most `units` find places
+    int many;           // see ChunkSeq
     // Units of a segment, at least: as many as its results, written and read again, take the time of (with 4 instead of 8 slots a row 2048 first tokens of 32
     // heads 110 us instead of 64), or half as many where workgroups would have nothing to do (8 drafts of 32 tokens over 2900 rows 33.4 us instead of 41.3,
     // with 6 36.3)
     __device__ __forceinline__ int least(const ChunkSeq& s) const { return max(min(s.rows, s.tile_rows) * (rounds > 1 ? 8 : 4), 256) / UNIT; }
     // Segments of a tile of U units of at most `units` each, but no less than `floor`.
-    __device__ __forceinline__ int segments(int U, int floor) const { return max(min(about(U + units - 1, low_rcp(units)), about(U, low_rcp(floor))), 1); }
+    __device__ __forceinline__ int segments(int U, int floor) const
+    {
+        return U <= SHORT ? 1 : max(min(about(U + units - 1, low_rcp(units)), about(U, low_rcp(floor))), 1);
+    }
     // A tile of U units, against a share of A:
     //   U > A       S = r U / A segments, which take r rounds: the r for which r (U / S) is least
     //   U <= A < 4U as many tiles whole as fit into rounds that are full, the rest cut into what is left of the share
@@ -133,6 +143,7 @@ template <int UNIT, bool ONE> struct ChunkShare {
         int n = 1, whole = 0;
         if (ONE && !rounds) {
             n = segments(U, floor);
+        } else if (U <= SHORT) {
         } else if (U > A) {
             n = about(U, low);
             if (rounds > 1 && U < 4 * A) {
@@ -143,7 +154,7 @@ template <int UNIT, bool ONE> struct ChunkShare {
                     if (r <= rounds && t < time) time = t, n = m;
                 }
             }
-        } else if (rounds > 1 && U > 0 && A < 4 * U) {
+        } else if (rounds > 1 && A < 4 * U) {
             const int k = divided(A, U), rest = A - k * U;
             if (rest >= floor && rest * 8 >= A && (long long)s.tiles * rest >= A && (long long)s.tiles * k * U < 1 << 24) {
                 n = divided(U, rest);
@@ -154,44 +165,67 @@ template <int UNIT, bool ONE> struct ChunkShare {
         return {whole, n, divided(U + n - 1, n)};
     }
 };
-template <int UNIT, bool ONE, int PLACES, class N> __device__ __forceinline__ ChunkShare<UNIT, ONE> chunk_share_of(const ChunkStep& a, N all, N most)
+// Sums over the batch, in 32 bits where the units of all tiles fit.
+struct SmallSum {
+    typedef uint32_t type;
+    static __device__ __forceinline__ type of(long long x) { return last_lane(wave_scan((int)x)); }
+};
+struct LargeSum {
+    typedef unsigned long long type;
+    static __device__ __forceinline__ type of(long long x) { return wave_sum(x); }
+};
+// Rows of a tile of a sequence of bf16 with more than 32: 128, or 64 where neither tiles of 128 nor their segments (of `least` units each) give all compute units
+// something to do. 512 tokens behind 768 rows of 32 heads 25.2 us instead of 29.7, 100 tokens behind 3000 rows H32/8 24.9 instead of 27.6; where segments
+// do, 128 rows read K and V half as often: 32 tokens behind 65000 rows H40/8 83 us instead of 89, 8 sequences of 2900 rows 28.2 instead of 30.4.
+// s: of this lane's sequence, read for tiles of 128 rows, if there are no more than lanes
+template <int UNIT, class Sum> __device__ __forceinline__ int many_rows(const ChunkStep& a, ChunkSeq& s)
 {
+    typename Sum::type tiles = 0, items = 0;
+    bool many = false;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        if (a.B > kWave) s.read<UNIT>(a, b0 + threadIdx.x % kWave, 7);
+        many |= __any(s.rows > 32);
+        if (!many && a.B <= kWave) return 7;
+        tiles += Sum::of(s.tiles), items += Sum::of((long long)s.tiles * max(s.units * UNIT / (a.rounds > 1 ? 1024 : 512), 1));
+    }
+    return many && tiles * a.Hkv <= kComputeUnits / 2 && items * a.Hkv < kComputeUnits ? 6 : 7;
+}
+template <int UNIT, int SHORT, bool ONE, int PLACES, class Sum> __device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share_of(const ChunkStep& a, ChunkSeq& s, int many, int rounds)
+{
+    using N = typename Sum::type;
+    N all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        if (a.B > kWave) s.read<UNIT>(a, b0 + threadIdx.x % kWave, many);
+        most += Sum::of((long long)s.tiles * s.units), all += Sum::of((long long)s.tiles * (s.units + s.first_units));
+    }
+    all *= a.Hkv, most *= a.Hkv;
     // one round: most / share <= PLACES parts; several: rounds * most / share and 2 most / share <= 4 PLACES, as most <= all
-    const N share = a.rounds > 1 ? (all + (2 * PLACES - 1)) / (2 * PLACES) : (most + (PLACES - 1)) / PLACES;
+    const N share = rounds > 1 ? (all + (2 * PLACES - 1)) / (2 * PLACES) : (most + (PLACES - 1)) / PLACES;
     const int units = (int)min(max(share, (N)1), (N)((1 << 24) - 1));  // (from four times the units of the longest table on nothing is cut)
+    if (ONE && rounds == 1 && a.B <= kWave) {  // the least units by which all segments find places at once, if a few more than the share do
+        for (int more = 0; more < 4; ++more) {
+            const ChunkShare<UNIT, SHORT, ONE> finer = {units + more, 0, many};
+            if (Sum::of((long long)s.tiles * finer.segments(s.units, finer.least(s))) * a.Hkv <= PLACES) return finer;
+        }
+    }
     const N held = (N)4 * PLACES * units;
-    return {units, a.rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2};
+    return {units, rounds == 1 ? 1 : 4 * most <= held ? 4 : 3 * most <= held ? 3 : 2, many};
 }
 // s: of this lane's sequence afterwards, if there are no more than lanes
-template <int MANY, int UNIT, bool ONE, int PLACES> __device__ __forceinline__ ChunkShare<UNIT, ONE> chunk_share(const ChunkStep& a, ChunkSeq& s)
+// MANY: binary logarithm of the rows of a tile of a sequence with more than 32, 0 for 6 or 7
+template <int MANY, int UNIT, int SHORT, bool ONE, int PLACES> __device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
-    if (!a.cut) {  // a share that no tile exceeds
-        if (a.B <= kWave) s.read<MANY, UNIT>(a, threadIdx.x % kWave);
-        return {1 << 22, 1};
-    }
-    if (a.small) {
-        uint32_t all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
-        for (int b0 = 0; b0 < a.B; b0 += kWave) {
-            s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
-            const int units = wave_scan(s.tiles * s.units), both = wave_scan(s.tiles * (s.units + s.first_units));
-            most += last_lane(units), all += last_lane(both);
+    int many = MANY ? MANY : 7, rounds = a.rounds;
+    if (a.B <= kWave) s.read<UNIT>(a, threadIdx.x % kWave, many);
+    if (MANY == 0) {
+        many = a.small ? many_rows<UNIT, SmallSum>(a, s) : many_rows<UNIT, LargeSum>(a, s);
+        if (many == 6) {
+            rounds = a.rounds_64;
+            if (a.B <= kWave) s.tile<UNIT>(a, many);
         }
-        const auto share = chunk_share_of<UNIT, ONE, PLACES>(a, all * a.Hkv, most * a.Hkv);
-        if (ONE && a.rounds == 1 && a.B <= kWave) {  // the least units by which all segments find places at once, if a few more than the share do
-            for (int more = 0; more < 4; ++more) {
-                const ChunkShare<UNIT, ONE> finer = {share.units + more, 0};
-                if (last_lane(wave_scan(s.tiles * finer.segments(s.units, finer.least(s)))) * a.Hkv <= PLACES) return finer;
-            }
-        }
-        return share;
     }
-    unsigned long long all = 0, most = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
-        all += wave_sum((long long)s.tiles * (s.units + s.first_units));
-        most += wave_sum((long long)s.tiles * s.units);
-    }
-    return chunk_share_of<UNIT, ONE, PLACES>(a, all * a.Hkv, most * a.Hkv);
+    if (!a.cut) return {1 << 22, 1, many};  // a share that no tile exceeds
+    return a.small ? chunk_share_of<UNIT, SHORT, ONE, PLACES, SmallSum>(a, s, many, rounds) : chunk_share_of<UNIT, SHORT, ONE, PLACES, LargeSum>(a, s, many, rounds);
 }
 
 // Units that a tile's last row sees.
@@ -212,14 +246,15 @@ struct ChunkItem {
 };
 // The item of a workgroup: heads change fastest, so that the eight XCDs, which get workgroups in turn, keep to their heads, then tiles from the last one,
 // which sees most, then segments. s: as chunk_share leaves it.
-template <int MANY, int UNIT, bool ONE> __device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT, ONE>& share, ChunkSeq& s, int id, int wave)
+template <int UNIT, int SHORT, bool ONE>
+__device__ __forceinline__ ChunkItem chunk_item(const ChunkStep& a, const ChunkShare<UNIT, SHORT, ONE>& share, ChunkSeq& s, int id, int wave)
 {
     const int lane = lane_anew(), j = (int)(__umulhi((uint32_t)id << 2, a.heads_mul) >> a.heads_shift), hk = id - j * a.Hkv;
     int before = 0, parts_before = 0;  // parts: and cut tiles in the high half, both at most kChunkParts
     ChunkItem it;
     it.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        if (a.B > kWave) s.read<MANY, UNIT>(a, b0 + lane);
+        if (a.B > kWave) s.read<UNIT>(a, b0 + lane, share.many);
         const ChunkCut cut = share.of(s);
         const int cut_tiles = s.tiles - cut.whole, items = s.tiles + cut_tiles * (cut.segments - 1), parts = cut_tiles * cut.segments + (cut_tiles << 16);
         const int upto = wave_scan(items), parts_upto = wave_scan(parts);
@@ -254,11 +289,11 @@ template <int MANY, int UNIT, bool ONE> __device__ __forceinline__ ChunkItem chu
     }
     return it;
 }
-template <int MANY, int UNIT, bool ONE> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT, ONE>& share, ChunkSeq& s)
+template <int UNIT, int SHORT, bool ONE> __device__ __forceinline__ void count_cut_tiles(const ChunkStep& a, const ChunkShare<UNIT, SHORT, ONE>& share, ChunkSeq& s)
 {
     int n = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        if (a.B > kWave) s.read<MANY, UNIT>(a, b0 + threadIdx.x % kWave);
+        if (a.B > kWave) s.read<UNIT>(a, b0 + threadIdx.x % kWave, share.many);
         n += last_lane(wave_scan(s.tiles - share.of(s).whole));
     }
     if (threadIdx.x == 0) *a.cut_tiles = n * a.Hkv;
@@ -869,20 +904,20 @@ __device__ __forceinline__ bool chunk_few_rows(const ChunkStep& a, const ChunkIt
 #include "paged_chunk_many.h"
 namespace ec {
 
-// MANY: rows of a tile of a sequence with more than 32
+// MANY: see chunk_share
 template <int DT, int D, int WAVES, int MANY>
 __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void paged_chunk_kernel(ChunkStep first)
 {
     using T = PagedTile<DT, D>;
-    constexpr int UNIT = WAVES * T::TR;
+    constexpr int UNIT = WAVES * T::TR, SHORT = kShortUnits * kFewWaves / WAVES;
     __shared__ __align__(256) unsigned char tiles[WAVES * 4 * T::BYTES];  // of every wave: two tiles of K, two of V
-    constexpr int SUMS = MANY == 64 ? 6 * kWave : WAVES * 32;  // (64 rows: three parts of two waves)
+    constexpr int SUMS = MANY == 0 ? 6 * kWave : WAVES * 32;  // (64 rows: three parts of two waves)
     __shared__ float sh_m[SUMS], sh_l[SUMS];
     __shared__ int flags[WAVES];
     const int first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     ChunkSeq s;
-    const auto share = chunk_share<MANY, UNIT, (DT == EC_F32 || WAVES == kManyWaves), kChunkPlaces<DT, D, WAVES>>(first, s);
-    if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles<MANY, UNIT>(first, share, s);
+    const auto share = chunk_share<MANY, UNIT, SHORT, (DT == EC_F32 || WAVES == kManyWaves), kChunkPlaces<DT, D, WAVES>>(first, s);
+    if (blockIdx.x == 0 && first.cut && threadIdx.x < kWave) count_cut_tiles(first, share, s);
     auto take = [&](const ChunkStep& a, const ChunkItem& at, int wave) __attribute__((always_inline)) {
         if (!at.s.live) {
             chunk_nothing<DT, D, WAVES>(a, at, wave);
@@ -899,7 +934,17 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
         if constexpr (DT == EC_BF16) {
             static_assert(sizeof(tiles) >= WAVES * kManySlots * D * 2 && UNIT % kManySlots == 0);
             if (at.s.tile_rows > 32) {
-                if (chunk_many_rows<D, WAVES, MANY / 32>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT)) return;
+                bool done;
+                if (MANY == 0 && at.s.tile_rows == 64) {
+                    asm volatile("; tiles of 64 rows" ::: "memory");  // (nothing of one is shared with the other, which would take registers)
+                    done = chunk_many_rows<D, WAVES, MANY == 0 ? 2 : 4>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT);
+                    asm volatile("; end of tiles of 64 rows" ::: "memory");
+                } else {
+                    asm volatile("; tiles of 128 rows" ::: "memory");
+                    done = chunk_many_rows<D, WAVES, 4>(a, at, wave, tiles, sh_m, sh_l, flags, UNIT);
+                    asm volatile("; end of tiles of 128 rows" ::: "memory");
+                }
+                if (done) return;
                 by_16();
                 return;
             }
@@ -915,8 +960,8 @@ __global__ __launch_bounds__(WAVES* kWave, (PagedTile<DT, D>::kResident)) void p
         const ChunkStep a = chunk_args();
         int wave = first_wave;  // (what follows from it is not kept from item to item)
         asm volatile("" : "+s"(wave));
-        if (id != blockIdx.x && a.B <= kWave) s.read<MANY, UNIT>(a, lane_anew());
-        const ChunkItem at = chunk_item<MANY, UNIT>(a, share, s, id, wave);
+        if (id != blockIdx.x && a.B <= kWave) s.read<UNIT>(a, lane_anew(), share.many);
+        const ChunkItem at = chunk_item(a, share, s, id, wave);
         if (at.b < 0) return;
         take(a, at, wave);
         __syncthreads();  // the tiles have been read
@@ -1046,42 +1091,30 @@ struct ChunkPlaces {  // where things lie in a workspace
 };
 size_t paged_chunk_ws(int T, int H, int D) { return ChunkPlaces(T, H, D).end; }
 
-// Rows of a tile of a sequence of bf16 with more than 32: 128, or 64 where neither tiles of 128 nor their segments (`least` units each) give all compute units
-// something to do. 512 tokens behind 768 rows of 32 heads 26.7 us instead of 30.2, 100 tokens behind 3000 rows H32/8 24.9 instead of 27.4; where segments
-// do, 128 rows read K and V half as often: 32 tokens behind 65000 rows H40/8 83 us instead of 89, 8 sequences of 2900 rows 28.2 instead of 30.4.
-static int many_rows(long long tiles, int slots)
-{
-    const long long segments = std::max(1, slots / (128 * (tiles >= kChunkTiles ? 8 : 4)));
-    return tiles <= kComputeUnits / 2 && tiles * segments < kComputeUnits ? 64 : 128;
-}
-
 template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
 {
     constexpr int UNIT = kFewWaves * PagedTile<DT, D>::TR;
-    const int rows = DT == EC_F32 ? 32 : many_rows(most_tiles(a.T, a.group, a.Hkv, a.B, 128), a.pages.slots());
-    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, rows);
-    a.rounds = tiles >= kChunkTiles ? 4 : 1;
-    const long long seq_tiles = most_tiles(a.T, a.group, a.Hkv, 1, rows), units = (a.pages.slots() + UNIT - 1) / UNIT;
+    const long long tiles = most_tiles(a.T, a.group, a.Hkv, a.B, DT == EC_F32 ? 32 : 128);
+    const bool few = DT == EC_F32 || tiles > kComputeUnits;  // waves
+    const int least_rows = DT == EC_F32 ? 32 : few ? 128 : 64;
+    const long long least_tiles = most_tiles(a.T, a.group, a.Hkv, a.B, least_rows);
+    a.rounds = tiles >= kChunkTiles ? 4 : 1, a.rounds_64 = least_tiles >= kChunkTiles ? 4 : 1;
+    const long long seq_tiles = most_tiles(a.T, a.group, a.Hkv, 1, least_rows), units = (a.pages.slots() + UNIT - 1) / UNIT;
     a.small = a.B < 1 << 20 && seq_tiles < 1 << 20 && seq_tiles * a.B * 2 * units < 1 << 29;
-    a.cut = units > 4;  // (the second launch takes longer than shorter sequences)
+    a.cut = units > kShortUnits;  // (the second launch takes longer than shorter sequences)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
     auto go = [&](auto waves, auto many) {
         constexpr int W = decltype(waves)::value;
-        const long long groups = a.cut ? std::max<long long>(tiles, kChunkPlaces<DT, D, W>) : tiles;
+        const long long groups = a.cut ? std::max<long long>(tiles, kChunkPlaces<DT, D, W>) : least_tiles;
         hipLaunchKernelGGL((paged_chunk_kernel<DT, D, W, decltype(many)::value>), dim3((unsigned)groups), dim3(W * kWave), 0, stream, a);
     };
     using Few = std::integral_constant<int, kFewWaves>;
-    if constexpr (DT == EC_F32) {
-        go(Few{}, std::integral_constant<int, 32>{});
-    } else {
-        using Many = std::integral_constant<int, kManyWaves>;
-        if (rows == 64) go(Many{}, std::integral_constant<int, 64>{});
-        else if (tiles <= kComputeUnits) go(Many{}, std::integral_constant<int, 128>{});
-        else go(Few{}, std::integral_constant<int, 128>{});
-    }
+    if constexpr (DT == EC_F32) go(Few{}, std::integral_constant<int, 5>{});
+    else if (few) go(Few{}, std::integral_constant<int, 7>{});
+    else go(std::integral_constant<int, kManyWaves>{}, std::integral_constant<int, 0>{});
     if (const int rc = status_from_hip(hipGetLastError())) return rc;
     if (!a.cut) return EC_OK;
-    const long long joins = std::min<long long>(tiles, most_parts(a.T, a.H)) * kJoinGroups;
+    const long long joins = std::min<long long>(least_tiles, most_parts(a.T, a.H)) * kJoinGroups;
     hipLaunchKernelGGL((paged_chunk_join_kernel<DT, D>), dim3((unsigned)std::min<long long>(joins, 2048)), dim3(kJoinWaves * kWave), 0, stream, a);
     return status_from_hip(hipGetLastError());
 }
@@ -1099,7 +1132,7 @@ int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages
     const ChunkPlaces at(T, H, D);
     char* const w = static_cast<char*>(ws);
     const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul_of(group), shift_of(group),
-                      mul_of(Hkv), shift_of(Hkv), 1, false, false, scale, scale * kLog2e,
+                      mul_of(Hkv), shift_of(Hkv), 1, 1, false, false, scale, scale * kLog2e,
                       reinterpret_cast<int*>(w), reinterpret_cast<CutTile*>(w + at.records), part_rows(T, H), reinterpret_cast<float*>(w + at.partials),
                       reinterpret_cast<float2*>(w + at.stats)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);
