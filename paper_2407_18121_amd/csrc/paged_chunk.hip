@@ -23,6 +23,7 @@ constexpr int kFewWaves = 4, kManyWaves = 8;
 // Workgroups that the chip holds at once
 template <int DT, int D, int WAVES> constexpr int kChunkPlaces = WAVES == kFewWaves ? PagedTile<DT, D>::kResident * kComputeUnits : kComputeUnits;
 constexpr int kMostPlaces = 2 * kComputeUnits, kChunkParts = 4 * kMostPlaces;  // kChunkParts: segments whose results the workspace holds, at most
+constexpr int kMostGroups = 1 << 22;                      // of a launch, whose threads have to fit into 32 bits
 constexpr int kShortUnits = 4;                            // units, of four waves, up to which tiles are never cut
 constexpr int kChunkTiles = 128;                          // tiles from which on segments may take several rounds
 constexpr int kJoinWaves = 4, kJoinGroups = 8;            // waves of a joining workgroup, and workgroups that share a tile's rows
@@ -174,9 +175,10 @@ struct LargeSum {
     typedef unsigned long long type;
     static __device__ __forceinline__ type of(long long x) { return wave_sum(x); }
 };
-// Rows of a tile of a sequence of bf16 with more than 32: 128, or 64 where neither tiles of 128 nor their segments (of `least` units each) give all compute units
-// something to do. 512 tokens behind 768 rows of 32 heads 25.2 us instead of 29.7, 100 tokens behind 3000 rows H32/8 24.9 instead of 27.6; where segments
-// do, 128 rows read K and V half as often: 32 tokens behind 65000 rows H40/8 83 us instead of 89, 8 sequences of 2900 rows 28.2 instead of 30.4.
+// Rows of a tile of a sequence of bf16 with more than 32: 128, or 64 where neither tiles of 128 nor their segments (of ChunkShare::least units each) give all
+// compute units something to do. 512 tokens behind 768 rows of 32 heads 25.1 us instead of 28.8, 100 behind 3000 rows H32/8 24.8 instead of 26.7, 32 behind
+// 2900 18.8 instead of 22.4; where they do, 128 rows read K and V half as often: 8 sequences of 32 tokens behind 2900 rows 31.2 us instead of 43.3, 32
+// tokens behind 65000 rows H40/8 79 instead of 87, 1024 first tokens of 32 heads 27.1 instead of 33.9.
 // s: of this lane's sequence, read for tiles of 128 rows, if there are no more than lanes
 template <int UNIT, class Sum> __device__ __forceinline__ int many_rows(const ChunkStep& a, ChunkSeq& s)
 {
@@ -1105,7 +1107,7 @@ template <int DT, int D> static int launch(ChunkStep a, hipStream_t stream)
     // as many workgroups as there can be tiles, and as the chip holds if some may be cut: they go on to further segments where there are more
     auto go = [&](auto waves, auto many) {
         constexpr int W = decltype(waves)::value;
-        const long long groups = a.cut ? std::max<long long>(tiles, kChunkPlaces<DT, D, W>) : least_tiles;
+        const long long groups = std::min<long long>(a.cut ? std::max<long long>(tiles, kChunkPlaces<DT, D, W>) : least_tiles, kMostGroups);
         hipLaunchKernelGGL((paged_chunk_kernel<DT, D, W, decltype(many)::value>), dim3((unsigned)groups), dim3(W * kWave), 0, stream, a);
     };
     using Few = std::integral_constant<int, kFewWaves>;

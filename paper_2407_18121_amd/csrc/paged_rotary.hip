@@ -147,9 +147,10 @@ __global__ __launch_bounds__(kRotaryThreads) void paged_rotary_kernel(Rotary a, 
 
 template <int DT, int D> static void launch(const Rotary& a, bool neighbours, hipStream_t stream)
 {
-    // a token a workgroup, unless that leaves most of its threads without work, and the chip's compute units have four workgroups each all the same
+    // a token a workgroup, unless that leaves most of its threads without work, and the chip's compute units have four workgroups each all the same, or makes 2^32
+    // threads, more than a launch can have
     const int items = (a.H + 2 * a.Hkv) * (D / Elem<DT>::kPerChunk / 2);
-    const int each = std::max(1, std::min({kRotaryTokens, 2 * kRotaryThreads / items, a.T / (4 * kComputeUnits)}));
+    const int each = std::max(1 + (a.T >> 24), std::min({kRotaryTokens, 2 * kRotaryThreads / items, a.T / (4 * kComputeUnits)}));
     const dim3 grid((a.T + each - 1) / each), block(kRotaryThreads);
     auto go = [&](auto pairs, auto whole) {
         if (each == 1) hipLaunchKernelGGL((paged_rotary_kernel<DT, D, pairs.value, whole.value, true>), grid, block, 0, stream, a, 1);
