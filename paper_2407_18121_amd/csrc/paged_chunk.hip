@@ -1134,7 +1134,7 @@ int paged_chunk_dispatch(const void* q, const void* k_pages, const void* v_pages
     const ChunkPlaces at(T, H, D);
     char* const w = static_cast<char*>(ws);
     const ChunkStep a{q, k_pages, v_pages, out, lse, start_b, token_start, pages, B, T, H, Hkv, (int)group, mul_of(group), shift_of(group),
-                      mul_of(Hkv), shift_of(Hkv), 1, 1, false, false, scale, scale * kLog2e,
+                      mul_of(Hkv), shift_of(Hkv), 1, 1, false, false, scale, std::min(scale * kLog2e, -kLowest),
                       reinterpret_cast<int*>(w), reinterpret_cast<CutTile*>(w + at.records), part_rows(T, H), reinterpret_cast<float*>(w + at.partials),
                       reinterpret_cast<float2*>(w + at.stats)};
     if (dt == EC_BF16) return D == 128 ? launch<EC_BF16, 128>(a, stream) : launch<EC_BF16, 64>(a, stream);

@@ -127,3 +127,21 @@ def test_values_of_no_weight(dtype, D, L, n, H, scores):
     ok = ref.fits(out, want, tol)
     assert ok.all(), (np.argwhere(~ok)[:6].tolist(), out[~ok][:6], want[~ok][:6])
     assert ref.fits(lse, want_lse, lse_tol).all()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,H", [(1, 1), (20, 1), (100, 1), (300, 2)])
+def test_the_largest_scales(dtype, D, n, H):
+    """A scale beyond the range of fp32 in units of a power of two: rows of the largest score weigh the same, all others nothing."""
+    rng = np.random.default_rng(n)
+    L = 300
+    q, k = np.zeros((n, H, D), np.float32), np.zeros((L + n, D), np.float32)
+    q[:, :, 0] = 1
+    k[:, 0] = np.where(rng.random(L + n) < 0.5, 0.0, -1.0)
+    v = quantize(rng.standard_normal((L + n, D)), dtype)
+    out, lse = run(k, v, q, L, dtype, 3.3e38)
+    for i in range(n):
+        rows = v[:L + i + 1][k[:L + i + 1, 0] == 0].astype(np.float64)
+        tol = (len(rows) + 40) * ref.U * np.abs(rows).mean(0) + np.abs(rows.mean(0)) * ref.STEP[dtype]
+        assert (np.abs(out[i] - rows.mean(0)) <= tol).all()
+        assert (np.abs(lse[i] - np.log(len(rows))) <= (len(rows) + 40) * ref.U).all()
