@@ -277,8 +277,10 @@ def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, kin
       base    the base raised, so that the slowest pair is divided by the factor and the fastest stays: base * factor^(rot/(rot-2))
       parts   pairs that turn more than `high` times over the trained context stay, those that turn less than `low` times are divided by the factor, those
               between in proportion; mscale = 0.1 ln(factor) + 1"""
-    if rot < 2 or rot % 2 or factor < 1.0 or kind not in ("linear", "base", "parts"):
-        raise ValueError(f"rot {rot} must be even, the factor {factor} at least 1, the kind {kind!r} one of linear, base, parts")
+    if rot < 2 or rot % 2 or not 1.0 <= factor < math.inf or not 0.0 < base < math.inf or kind not in ("linear", "base", "parts"):
+        raise ValueError(f"rot {rot} must be even, the factor {factor} at least 1, the base {base} above 0, the kind {kind!r} one of linear, base, parts")
+    if kind == "parts" and not (low < high and trained > 0):
+        raise ValueError(f"the pairs between low {low} and high {high} need low < high and a trained context, not {trained}")
     if kind == "base" and factor > 1.0:
         if rot == 2:
             raise ValueError("a raised base needs more than one pair")
