@@ -62,7 +62,7 @@ int ec_paged_plan(const int32_t* len_b, const int32_t* new_b, const int32_t* see
  *   pos_pages       written: pos; may be NULL
  *   mass_pages      written: 0, what the frequency policy's rows start from; may be NULL
  * Requires rot even, 2 <= rot <= D, a finite mscale, steps of at least a token's elements, T <= 2^24, T * H <= 2^30.  q, k, v, q_out, the pools and the
- * steps lie on 16-byte boundaries (else EC_EUNSUPPORTED).  Two tokens of one row: either of them.  Arithmetic is in fp32, rounded once.
+ * steps lie on 16-byte boundaries (else EC_EUNSUPPORTED).  Two tokens of one row leave a mixture of them there.  Arithmetic is in fp32, rounded once.
  */
 typedef enum { EC_ROTARY_HALVES = 0, EC_ROTARY_NEIGHBOURS = 1 } ec_rotary_pairing;
 int ec_paged_rotary_store(const void* q, const void* k, const void* v, int64_t q_step, int64_t k_step, int64_t v_step, const int32_t* pos,
