@@ -61,3 +61,30 @@ def test_64_features(H, Hkv, rows, n):
 @pytest.mark.parametrize("D,L,news", [(128, [577, 100], [300, 7]), (64, [400], [5]), (64, [5000], [40]), (128, [0], [500]), (128, [3000, 20, 500], [1, 1, 2])])
 def test_fp32(D, L, news):
     check("f32", 8, 2, D, L, news)
+
+
+def test_replays_choose_anew():
+    """One captured call whose lengths ask for tiles of 64 rows in one replay, of 128 in the next, and for few rows: what an eager call gives, bit for bit."""
+    H, D, page, T, most = 32, 128, 64, 300, 3300
+    rng = np.random.default_rng(3)
+    pool = make(rng, "bf16", H, D, page, [most], spare=0)
+    q = quantize(rng.standard_normal((T, H, D)), "bf16")
+    dq, k, v = to_dev(q, "bf16"), to_dev(pool.k, "bf16"), to_dev(pool.v, "bf16")
+    i = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, start, starts = i(pool.table), i([0]), i([0, 0])
+    size = ec.new_workspace(ec.EC_FN_PAGED_CHUNK_STEP, 1, H, T, D, ec.EC_BF16)
+    out, ws = torch.zeros_like(dq), torch.full_like(size, 255)
+    call = lambda out, ws: ec.ec_paged_chunk_step(dq, k, v, table, start, starts, 0.1, out, ws)  # noqa: E731
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    for L, n in ((100, 300), (2900, 300), (0, 299), (3000, 20), (3000, 250), (100, 300), (700, 1)):
+        start.copy_(i([L])), starts.copy_(i([0, n]))
+        eager = torch.zeros_like(out)
+        call(eager, torch.full_like(size, 255))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:n], eager[:n]), (L, n)
+        want, tol, _, _ = ref.chunk(pool, q, [L], [0, n], 0.1, "bf16")
+        assert (np.abs(to_host(out)[:n] - want[:n]) <= tol[:n]).all(), (L, n)
