@@ -8,8 +8,8 @@
 // out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
 //
 // Few rows are bound by the bytes of K and V (8 sequences of up to 2900 rows H32/8 D128 bf16 with 5 tokens each: 58 MB, 21.9 us, of which 8 before the first
-// load, between the last and the output and in the second launch; 8 of 1000 rows H32 fp32 with one: 262 MB, 49 us, 5.4 TB/s), many rows by the matrix pipes (2048
-// tokens behind 65000 rows H40/8: 2.55 ms, 1.09 PFLOP/s; fp32, 1024 first tokens of 32 heads: 133 us, 65 TFLOP/s).
+// load, between the last and the output and in the second launch; 8 of 1000 rows H32 fp32 with one: 262 MB, 49 us, 5.3 TB/s), many rows by the matrix pipes (2048
+// tokens behind 65000 rows H40/8: 2.47 to 2.68 ms from card to card, 1.03 to 1.12 PFLOP/s; fp32, 1024 first tokens of 32 heads: 134 us, 64 TFLOP/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -192,7 +192,8 @@ template <int UNIT, class Sum> __device__ __forceinline__ int many_rows(const Ch
     }
     return many && tiles * a.Hkv <= kComputeUnits / 2 && items * a.Hkv < kComputeUnits ? 6 : 7;
 }
-template <int UNIT, int SHORT, bool ONE, int PLACES, class Sum> __device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share_of(const ChunkStep& a, ChunkSeq& s, int many, int rounds)
+template <int UNIT, int SHORT, bool ONE, int PLACES, class Sum>
+__device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share_of(const ChunkStep& a, ChunkSeq& s, int many, int rounds)
 {
     using N = typename Sum::type;
     N all = 0, most = 0;  // twice the units of all tiles, about; the units if every tile of a sequence saw as much as the last one: at most `all`
@@ -215,7 +216,8 @@ template <int UNIT, int SHORT, bool ONE, int PLACES, class Sum> __device__ __for
 }
 // s: of this lane's sequence afterwards, if there are no more than lanes
 // MANY: binary logarithm of the rows of a tile of a sequence with more than 32, 0 for 6 or 7
-template <int MANY, int UNIT, int SHORT, bool ONE, int PLACES> __device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share(const ChunkStep& a, ChunkSeq& s)
+template <int MANY, int UNIT, int SHORT, bool ONE, int PLACES>
+__device__ __forceinline__ ChunkShare<UNIT, SHORT, ONE> chunk_share(const ChunkStep& a, ChunkSeq& s)
 {
     int many = MANY ? MANY : 7, rounds = a.rounds;
     if (a.B <= kWave) s.read<UNIT>(a, threadIdx.x % kWave, many);

@@ -5,13 +5,15 @@
 // the second operand of O^T += V^T . P^T as they stand, V transposed on its way out of LDS. Two phases a tile, each with vector work beside matrix work:
 //   A  probabilities of tile i beside the scores of tile i + 1       B  O^T += V^T . P^T of tile i beside the row maximum of tile i + 1
 // The probabilities' sum is that of the fp32 numbers; rounding them to bf16, half a step off each, is what keeps the product at one matrix instruction where
-// few rows, which are bound by memory, take three: with many rows the matrix pipes are the bound.
+// few rows, which are bound by memory, take three: with many rows the matrix pipes are the bound. (In two parts, 16 bits: 2048 tokens behind 65000 rows H40/8 2680
+// -> 4076 us, 1024 first tokens of 32 heads 27.0 -> 37.0, 512 behind 768 rows 25.5 -> 29.7; the outputs, rounded to bf16 themselves, are off by 1.66e-3 rms
+// instead of 1.67e-3 to 1.70e-3.)
 //
-// A tile takes two workgroups of a compute unit 3300 cycles of 2048 in the matrix pipe (D128; the pipes of a busy unit work 61 % of the time in 2.55 ms over
-// 65000 rows, H40/8, 2048 tokens: 1.09 PFLOP/s), what remains being the exponentials and the instructions between; a lone workgroup takes 3100. Where a
+// A tile takes two workgroups of a compute unit 3300 cycles of 2048 in the matrix pipe (D128; the pipes of a busy unit work 61 % of the time over
+// 65000 rows, H40/8, 2048 tokens: 2.47 to 2.68 ms from card to card, 1.03 to 1.12 PFLOP/s), what remains being the exponentials and the instructions between; a lone workgroup takes 3100. Where a
 // batch has fewer tiles than the chip has compute units, a workgroup has eight waves, two groups of four that take turns at the tiles, each with tiles of
-// its own in LDS: 4100 cycles a pair (512 tokens behind 768 rows, H32: 41.2 -> 30.9 us); where it has less than half as many, and segments do not make up for
-// it, tiles of 64 rows (see many_rows). The sums of a row's parts meet in LDS at the end.
+// its own in LDS: 4100 cycles a pair (512 tokens behind 768 rows, H32: 41.2 -> 30.9 us); where it has at most half as many, and segments do not make up for
+// it, tiles of 64 rows (see many_rows; 30.9 -> 25.1). The sums of a row's parts meet in LDS at the end.
 //
 // Operands (lane l, half h = l / 32):  A (32 x 16): lane holds A[l % 32][8h .. 8h+7]    B (16 x 32): B[8h .. 8h+7][l % 32]
 //                                      C (32 x 32): C[8g + 4h + t][l % 32] in register 4g + t, g,t in 0..3
